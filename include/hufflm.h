@@ -124,7 +124,9 @@ typedef enum {
   HL_EHIP = 5           /* HIP runtime error */
 } hl_status;
 
-typedef enum { HL_F32 = 0, HL_BF16 = 1, HL_F16 = 2 } hl_dtype;
+/* HL_E4M3: 8 bits (4 of exponent, 3 of mantissa, no infinities), only where a
+ * function names it. */
+typedef enum { HL_F32 = 0, HL_BF16 = 1, HL_F16 = 2, HL_E4M3 = 3 } hl_dtype;
 
 #define HL_MAGIC 0x31464C48u
 #define HL_VERSION 2u
@@ -139,6 +141,8 @@ typedef enum { HL_F32 = 0, HL_BF16 = 1, HL_F16 = 2 } hl_dtype;
 #define HL_LMAX16_MIN 5u
 #define HL_LMAX16_MAX 12u
 #define HL_PAIR_MAX 11u       /* the fused kernel's table window: pairs of codes up to it take the fast form */
+#define HL_NORM_MAX_HIDDEN 32768u   /* columns of hl_rms_norm */
+#define HL_ATTENTION_MAX_DIM 256u   /* columns of a head in hl_prefix_attention */
 #define HL_NOALLOC_SCRATCH_BYTES (4u << 20)  /* scratch of hl_decode_gemv_noalloc, per GPU */
 
 typedef enum { HL_FORMAT_SPLIT = 0, HL_FORMAT_WHOLE_EXPONENT = 1, HL_FORMAT_FP16 = 2 } hl_format;
@@ -390,6 +394,110 @@ hl_status hl_decode_gemm(const hl_tensor* t, const void* x_dev, hl_dtype x_dtype
 hl_status hl_gemv_bf16(const uint16_t* w_dev, uint64_t rows, uint64_t cols,
                        const void* x_dev, hl_dtype x_dtype, uint32_t batch,
                        float* y_dev, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Between the products of a decoder layer: norm, attention and its cache.
+ * The paper's layers (Sec. 2.1) are their products; these operators are what a
+ * decode step over compressed weights needs besides. They take and give plain
+ * tensors, in the activation types of the products above.
+ * ------------------------------------------------------------------------- */
+
+/* RMS norm with the residual's addition, of `tokens` rows of `hidden` columns
+ * (row-major, contiguous):
+ *   t = x + residual,  sum = t,  out = t / sqrt(mean(t^2) + eps) * weight.
+ * x, residual, weight: float32, bf16 or float16, each its own type; t is held
+ * in float32, and `sum` (of residual's type) is its only rounding: the norm is
+ * of the unrounded sum. residual_dev NULL: t = x, and sum_dev is not written
+ * (r_dtype is ignored). sum_dev may be residual_dev, and x_dev or residual_dev
+ * may be out_dev where the two have one type.
+ * out_dtype: float32, bf16, float16, or HL_E4M3 with float32 scales: the
+ * columns of a group share scale = max|out| / 448 (1 where that is below the
+ * least normal float32, as for a group of zeros), and out holds out / scale
+ * rounded to nearest, ties to even. group: 32, 64 or 128 columns (dividing
+ * hidden; scale_dev [tokens][hidden/group]), or 0 for the whole row (scale_dev
+ * [tokens]). For other out types group must be 0 and scale_dev is ignored.
+ * A NaN in a row makes the row's out NaN.
+ * Rows that start at multiples of 16 bytes (every pointer 16-byte aligned and
+ * hidden a multiple of 8) are read in the widest pieces; others work, with
+ * narrower ones (a group then gives HL_EINVAL). Errors: HL_EINVAL (also for a
+ * pointer not aligned to its element), HL_EUNSUPPORTED for hidden above
+ * HL_NORM_MAX_HIDDEN. */
+hl_status hl_rms_norm(const void* x_dev, hl_dtype x_dtype, const void* residual_dev, hl_dtype r_dtype,
+                      const void* weight_dev, hl_dtype w_dtype, uint64_t tokens, uint64_t hidden, float eps,
+                      void* sum_dev, void* out_dev, hl_dtype out_dtype, uint32_t group, float* scale_dev,
+                      void* stream);
+
+/* Keys and values [sequence][token][key head][column] in device memory, by
+ * strides in elements (of 16 bits): any order of the first three, columns next
+ * to each other. Pointers 16-byte aligned, strides multiples of 8. */
+typedef struct {
+  const void* k_dev;
+  const void* v_dev;
+  uint64_t tokens;   /* capacity of a sequence (of a prefix: its length); 0: there is none */
+  uint64_t k_seq, k_token, k_head;
+  uint64_t v_seq, v_token, v_head;
+} hl_kv;
+
+/* An attention call's shape: `batch` sequences with `queries` new tokens each,
+ * `heads` query heads of `dim` columns, heads / kv_heads of which share a key
+ * head (heads % kv_heads == 0; dim a multiple of 8, at most
+ * HL_ATTENTION_MAX_DIM). */
+typedef struct {
+  hl_dtype dtype;    /* of q, keys, values and out: HL_BF16 or HL_F16 */
+  uint32_t batch, queries, heads, kv_heads, dim;
+  float scale;       /* of the scores (1/sqrt(dim) as a rule) */
+  hl_kv prefix;      /* shared by all sequences: its k_seq and v_seq are ignored */
+  hl_kv own;         /* each sequence's own, at the first lens[b] tokens of its capacity */
+} hl_attention;
+
+/* Bytes of device workspace hl_prefix_attention needs on the current GPU (0 on
+ * bad arguments). */
+size_t hl_attention_workspace_bytes(const hl_attention* attention, int with_weights);
+
+/* Attention of each sequence's new tokens over a prefix that all sequences
+ * share and over its own cache, which already holds the new tokens' keys and
+ * values at its end. The prefix is read once for the whole batch.
+ *   s_j = scale * q . k_j,  out = sum_j p_j v_j,  p = softmax(s)
+ * over all keys of the prefix and, for token i of `queries`, the own keys
+ * j < lens[b] - (queries - 1 - i). A token that sees no key (or only scores of
+ * minus infinity) has out = 0 and lse = minus infinity. Keys and values that a
+ * token does not see do not affect it, whatever they hold.
+ * q_dev, out_dev: [batch][queries][heads][dim]. lens_dev: int32 [batch], read
+ * on the device (a length above own.tokens counts as own.tokens, a negative
+ * one as 0); NULL only where own.tokens == 0. lse_dev (or NULL): float32
+ * [batch][queries][heads], log(sum_j exp(s_j)).
+ * weight_out_dev (or NULL): float32 [batch][kv_heads][own.tokens], what
+ * eviction goes by: weight_in_dev (NULL: zeros; may be the same buffer) plus,
+ * for every own key, the sum of its p over the call's tokens and the heads
+ * that share it. It holds a float32 score for each (row, own key) in the
+ * workspace, so it is meant for few new tokens.
+ * Scores, softmax statistics and sums are float32; p is rounded to the 16-bit
+ * type for the second product. Every sum has a fixed order.
+ * workspace_dev: hl_attention_workspace_bytes (16-byte aligned, no initial
+ * contents needed); calls that may run concurrently need separate ones.
+ * Errors: HL_EINVAL (also for a missing or short workspace), HL_EUNSUPPORTED
+ * for dim above HL_ATTENTION_MAX_DIM and sizes past the kernels' 32-bit
+ * counts. */
+hl_status hl_prefix_attention(const hl_attention* attention, const void* q_dev, const int32_t* lens_dev,
+                              void* out_dev, float* lse_dev, const float* weight_in_dev, float* weight_out_dev,
+                              void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* Eviction from a cache by accumulated attention weight: of every sequence and
+ * key head at most `keep` tokens stay, moved in their order to the first slots
+ * of another cache. With n = lens[b] (bounded as in hl_prefix_attention): all
+ * tokens where n <= keep; else the newest `recent` (recent <= keep) and, of
+ * the others, the keep - recent of greatest weight; of equal ones the lowest
+ * slot, NaN below every number.
+ * from, to: caches of `batch` sequences, kv_heads and dim (a multiple of 8),
+ * that do not overlap; to->tokens >= keep. weight_dev: float32
+ * [batch][kv_heads][from->tokens]. Written: the first `keep` tokens of `to`
+ * (zeros past the kept ones), weight_out_dev float32 and slots_dev int32
+ * [batch][kv_heads][keep] (the kept tokens' weights and their slots in `from`;
+ * 0 and -1 past them), lens_out_dev int32 [batch] (min(n, keep)). Any 16-bit
+ * type. Errors: HL_EINVAL, HL_EUNSUPPORTED for sizes past 32-bit counts. */
+hl_status hl_cache_evict(const hl_kv* from, const hl_kv* to, uint32_t batch, uint32_t kv_heads, uint32_t dim,
+                         const float* weight_dev, const int32_t* lens_dev, uint64_t keep, uint64_t recent,
+                         float* weight_out_dev, int32_t* slots_dev, int32_t* lens_out_dev, void* stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,249 @@
+// Eviction from a cache by accumulated attention weight (hl_cache_evict): of
+// each sequence and key head the newest tokens and the heaviest of the others
+// are kept and moved, in their order, to a smaller cache.
+//
+// Two kernels. select_kernel, one block a (sequence, key head), finds the
+// weight of the last token kept by its digits (11, 11 and 10 bits of the
+// weight as an ordered integer: a histogram in LDS each), then numbers the
+// kept tokens with one prefix sum over the block; ties go to the lowest slot.
+// It reads the weights, a hundredth of the cache. move_kernel copies the kept
+// rows in 16-byte pieces and is bound by HBM.
+#include <algorithm>
+
+#include "gpu_host.h"
+
+namespace hl {
+
+constexpr uint32_t kThreads = 1024;
+constexpr uint32_t kEach = 8;                      // weights of a thread in a tile
+constexpr uint32_t kTile = kThreads * kEach;
+constexpr uint32_t kBins = 2048;
+constexpr uint32_t kCopies = 4;                    // of the histogram: lanes of a wave often count in one bin
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+struct EvictArgs {
+  const float* weight;
+  const int32_t* lens;
+  float* weight_out;
+  int32_t *slots, *lens_out;
+  const uint16_t *k, *v;
+  uint16_t *k_out, *v_out;
+  uint64_t k_seq, k_token, k_head, v_seq, v_token, v_head;                          // of the cache
+  uint64_t ko_seq, ko_token, ko_head, vo_seq, vo_token, vo_head;                    // of the smaller one
+  uint32_t batch, kv_heads, dim, tokens, keep, recent;
+};
+
+// A weight as an integer of the same order; -0 equals 0, NaN is below all.
+__device__ inline uint32_t ordered(float w) {
+  if (w != w) return 0;
+  const uint32_t b = __builtin_bit_cast(uint32_t, w + 0.0f);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+
+// Sum of v over the threads before this one, and over all (`total`). s: LDS,
+// one word a wave; may be used again at once.
+__device__ inline uint64_t before(uint64_t v, uint64_t* s, uint64_t* total) {
+  const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  uint64_t sum = v;
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint64_t o = __shfl_up(sum, d);
+    if (lane >= (uint32_t)d) sum += o;
+  }
+  __syncthreads();
+  if (lane == 63) s[wave] = sum;
+  __syncthreads();
+  uint64_t ahead = 0, all = 0;
+  for (uint32_t i = 0; i < kThreads / 64; ++i) {
+    ahead += i < wave ? s[i] : 0;
+    all += s[i];
+  }
+  *total = all;
+  return ahead + sum - v;
+}
+
+__global__ void __launch_bounds__(1024) select_kernel(EvictArgs a) {
+  __shared__ uint32_t s_bin[kCopies][kBins];
+  __shared__ uint64_t s_wave[kThreads / 64];
+  __shared__ uint32_t s_digit, s_above, s_in;
+  const uint32_t head = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+  const uint64_t item = (uint64_t)b * a.kv_heads + head;
+  const float* w = a.weight + item * a.tokens;
+  float* w_out = a.weight_out + item * a.keep;
+  int32_t* slots = a.slots + item * a.keep;
+  const int32_t len = a.lens[b];
+  const uint32_t n = len <= 0 ? 0 : min((uint32_t)len, a.tokens);
+  if (head == 0 && tid == 0) a.lens_out[b] = (int32_t)min(n, a.keep);
+  if (n <= a.keep) {
+    for (uint32_t i = tid; i < a.keep; i += kThreads) {
+      slots[i] = i < n ? (int32_t)i : -1;
+      w_out[i] = i < n ? w[i] : 0.0f;
+    }
+    return;
+  }
+  const uint32_t old = n - a.recent, need = a.keep - a.recent;  // need < old
+  for (uint32_t i = tid; i < a.recent; i += kThreads) {
+    slots[need + i] = (int32_t)(old + i);
+    w_out[need + i] = w[old + i];
+  }
+  if (need == 0) return;
+  const bool held = old <= kTile;  // the weights stay in registers
+  uint32_t key[kEach];
+  auto load = [&](uint32_t tile) {
+#pragma unroll
+    for (uint32_t j = 0; j < kEach; ++j) {
+      const uint32_t i = tile + tid * kEach + j;
+      key[j] = i < old ? ordered(w[i]) : 0;
+    }
+  };
+  // The digits, from the highest, of the last weight kept: `prefix` has those
+  // found, `left` counts the tokens still to take among the weights that begin
+  // with it, `shift` is what of a weight is not compared yet.
+  uint32_t prefix = 0, left = need, shift = 32;
+  const uint32_t widths[3] = {11, 11, 10};
+  for (int pass = 0; pass < 3; ++pass) {
+    const uint32_t width = widths[pass], bins = 1u << width;
+    for (uint32_t i = tid; i < kCopies * kBins; i += kThreads) (&s_bin[0][0])[i] = 0;
+    __syncthreads();
+    for (uint32_t tile = 0; tile < old; tile += kTile) {
+      if (!held || pass == 0) load(tile);
+#pragma unroll
+      for (uint32_t j = 0; j < kEach; ++j)
+        if (tile + tid * kEach + j < old && (pass == 0 || key[j] >> shift == prefix))
+          atomicAdd(&s_bin[tid % kCopies][(key[j] >> (shift - width)) & (bins - 1)], 1u);
+    }
+    __syncthreads();
+    // thread t has bins 2t' and 2t'+1 counted from the highest; the counts
+    // above them say which bin the last token kept is in
+    uint32_t high = 0, low = 0;
+    const uint32_t at = bins - 2 - 2 * tid;
+    if (2 * tid < bins)
+      for (uint32_t c = 0; c < kCopies; ++c) high += s_bin[c][at + 1], low += s_bin[c][at];
+    uint64_t all;
+    const uint32_t above = (uint32_t)before(high + low, s_wave, &all);
+    if (above < left && left <= above + high) s_digit = at + 1, s_above = above, s_in = high;
+    if (above + high < left && left <= above + high + low) s_digit = at, s_above = above + high, s_in = low;
+    __syncthreads();
+    prefix = prefix << width | s_digit;
+    left -= s_above;
+    shift -= width;
+    const bool whole = s_in == left;  // all that begin so are kept: lower digits do not matter
+    __syncthreads();
+    if (whole) break;
+  }
+  // Kept: the first digits above `prefix`, and the first `left` tokens equal to it.
+  uint64_t base = 0;  // of earlier tiles: tokens above, and equal (high word)
+  for (uint32_t tile = 0; tile < old; tile += kTile) {
+    if (!held) load(tile);
+    uint64_t mine = 0;
+#pragma unroll
+    for (uint32_t j = 0; j < kEach; ++j) {
+      if (tile + tid * kEach + j >= old) continue;
+      const uint32_t d = key[j] >> shift;
+      mine += d > prefix ? 1u : d == prefix ? 1ull << 32 : 0u;
+    }
+    uint64_t all, at = base + before(mine, s_wave, &all);
+    base += all;
+#pragma unroll
+    for (uint32_t j = 0; j < kEach; ++j) {
+      const uint32_t i = tile + tid * kEach + j;
+      if (i >= old) continue;
+      const uint32_t d = key[j] >> shift, more = (uint32_t)at, same = (uint32_t)(at >> 32);
+      if (d > prefix || (d == prefix && same < left)) {
+        const uint32_t to = more + min(same, left);
+        slots[to] = (int32_t)i;
+        w_out[to] = w[i];
+      }
+      at += d > prefix ? 1u : d == prefix ? 1ull << 32 : 0u;
+    }
+  }
+}
+
+constexpr uint32_t kMoves = 4;  // 16-byte pieces of K, and of V, a thread moves
+
+// Piece x of a sequence's kept rows: x = (row * heads + head) * (dim/8) + 16-byte
+// piece. Slots that hold no token give zeros.
+__global__ void __launch_bounds__(256) move_kernel(EvictArgs a) {
+  const uint32_t b = blockIdx.y, pieces = a.dim / 8;
+  const uint64_t count = (uint64_t)a.keep * a.kv_heads * pieces;
+  const uint64_t x0 = (uint64_t)blockIdx.x * 256 * kMoves + threadIdx.x;
+  u32x4 k[kMoves], v[kMoves];
+  uint64_t ko[kMoves], vo[kMoves];
+  int32_t slot[kMoves];
+#pragma unroll
+  for (uint32_t m = 0; m < kMoves; ++m) {
+    const uint64_t x = x0 + m * 256;
+    if (x >= count) continue;
+    const uint32_t y = (uint32_t)(x / pieces), d = (uint32_t)(x % pieces) * 8, row = y / a.kv_heads,
+                   head = y % a.kv_heads;
+    slot[m] = a.slots[((uint64_t)b * a.kv_heads + head) * a.keep + row];
+    ko[m] = b * a.ko_seq + row * a.ko_token + head * a.ko_head + d;
+    vo[m] = b * a.vo_seq + row * a.vo_token + head * a.vo_head + d;
+  }
+#pragma unroll
+  for (uint32_t m = 0; m < kMoves; ++m) {
+    const uint64_t x = x0 + m * 256;
+    if (x >= count) continue;
+    k[m] = v[m] = u32x4{0, 0, 0, 0};
+    if (slot[m] < 0) continue;
+    const uint32_t y = (uint32_t)(x / pieces), d = (uint32_t)(x % pieces) * 8, head = y % a.kv_heads;
+    const uint64_t s = (uint32_t)slot[m];
+    k[m] = *reinterpret_cast<const u32x4*>(a.k + b * a.k_seq + s * a.k_token + head * a.k_head + d);
+    v[m] = *reinterpret_cast<const u32x4*>(a.v + b * a.v_seq + s * a.v_token + head * a.v_head + d);
+  }
+#pragma unroll
+  for (uint32_t m = 0; m < kMoves; ++m) {
+    if (x0 + m * 256 >= count) continue;
+    *reinterpret_cast<u32x4*>(a.k_out + ko[m]) = k[m];
+    *reinterpret_cast<u32x4*>(a.v_out + vo[m]) = v[m];
+  }
+}
+
+}  // namespace hl
+
+using namespace hl;
+
+static hl_status check_cache(const hl_kv* c) {
+  if (!c || c->tokens == 0 || !c->k_dev || !c->v_dev || !aligned(c->k_dev, 16) || !aligned(c->v_dev, 16))
+    return HL_EINVAL;
+  for (uint64_t x : {c->k_token, c->v_token, c->k_head, c->v_head, c->k_seq, c->v_seq}) {
+    if (x % 8) return HL_EINVAL;
+    if (x >= (1ull << 40)) return HL_EUNSUPPORTED;
+  }
+  return HL_OK;
+}
+
+extern "C" hl_status hl_cache_evict(const hl_kv* from, const hl_kv* to, uint32_t batch, uint32_t kv_heads,
+                                    uint32_t dim, const float* weight_dev, const int32_t* lens_dev, uint64_t keep,
+                                    uint64_t recent, float* weight_out_dev, int32_t* slots_dev, int32_t* lens_out_dev,
+                                    void* stream) {
+  hl_status st = check_cache(from);
+  if (st == HL_OK) st = check_cache(to);
+  if (st != HL_OK) return st;
+  if (!weight_dev || !lens_dev || !weight_out_dev || !slots_dev || !lens_out_dev || batch == 0 || kv_heads == 0 ||
+      dim == 0 || dim % 8 || keep == 0 || recent > keep || to->tokens < keep)
+    return HL_EINVAL;
+  if (!aligned(weight_dev, 4) || !aligned(lens_dev, 4) || !aligned(weight_out_dev, 4) || !aligned(slots_dev, 4) ||
+      !aligned(lens_out_dev, 4))
+    return HL_EINVAL;
+  if (from->tokens >= (1ull << 30) || keep >= (1ull << 30) || batch > 65535 || kv_heads > 65535 || dim > 65536)
+    return HL_EUNSUPPORTED;
+  const uint64_t blocks = (keep * kv_heads * (dim / 8) + 256 * kMoves - 1) / (256 * kMoves);
+  if (keep * kv_heads >= (1ull << 32) || blocks >= (1ull << 31)) return HL_EUNSUPPORTED;
+  EvictArgs a = {};
+  a.weight = weight_dev, a.lens = lens_dev, a.weight_out = weight_out_dev, a.slots = slots_dev;
+  a.lens_out = lens_out_dev;
+  a.k = static_cast<const uint16_t*>(from->k_dev), a.v = static_cast<const uint16_t*>(from->v_dev);
+  a.k_out = static_cast<uint16_t*>(const_cast<void*>(to->k_dev));
+  a.v_out = static_cast<uint16_t*>(const_cast<void*>(to->v_dev));
+  a.k_seq = from->k_seq, a.k_token = from->k_token, a.k_head = from->k_head;
+  a.v_seq = from->v_seq, a.v_token = from->v_token, a.v_head = from->v_head;
+  a.ko_seq = to->k_seq, a.ko_token = to->k_token, a.ko_head = to->k_head;
+  a.vo_seq = to->v_seq, a.vo_token = to->v_token, a.vo_head = to->v_head;
+  a.batch = batch, a.kv_heads = kv_heads, a.dim = dim, a.tokens = (uint32_t)from->tokens;
+  a.keep = (uint32_t)keep, a.recent = (uint32_t)recent;
+  const hipStream_t s = (hipStream_t)stream;
+  st = enqueue(select_kernel, dim3(kv_heads, batch), dim3(kThreads), s, a);
+  if (st != HL_OK) return st;
+  return enqueue(move_kernel, dim3((uint32_t)blocks, batch), dim3(256), s, a);
+}

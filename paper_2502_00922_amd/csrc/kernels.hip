@@ -32,6 +32,7 @@
 #include <type_traits>
 #include <unordered_map>
 
+#include "gpu_host.h"
 #include "hl_internal.h"
 #include "hufflm.h"
 
@@ -2312,22 +2313,6 @@ __global__ void __launch_bounds__(1024) gemv_bf16_kernel(const uint16_t* w, cons
 
 // ------------------------------------------------------------------ launch helpers
 
-constexpr int kMaxDevices = 64;
-
-// The current GPU's compute units; asked of the runtime once per GPU (a
-// launch's plan needs them several times).
-static int device_cus() {
-  static std::atomic<int> known[kMaxDevices];
-  int dev = 0, cus = 0;
-  if (hipGetDevice(&dev) != hipSuccess) return 256;
-  const bool keep = dev >= 0 && dev < kMaxDevices;
-  if (keep && (cus = known[dev].load(std::memory_order_relaxed)) > 0) return cus;
-  if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0)
-    return 256;
-  if (keep) known[dev].store(cus, std::memory_order_relaxed);
-  return cus;
-}
-
 constexpr uint32_t kMaxLds = 160 * 1024;
 
 // Raises a kernel's dynamic LDS limit on the current GPU to at least `lds`
@@ -2679,7 +2664,6 @@ using namespace hl;
 // Buffers the kernels read or write in 16-byte pieces (activations, decoded
 // weights, workspace, uncompressed weights) must be 16-byte aligned, fp32
 // outputs 4-byte aligned; a null workspace is allowed where it is optional.
-static bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 extern "C" hl_status hl_tensor_view(const void* blob_dev, const void* blob_host, size_t blob_bytes,
                                     uint32_t* lut_dev, hl_tensor* out) {

@@ -1,15 +1,17 @@
 """ctypes binding of libhufflm.so (argument marshalling only).
 
-Every step of the codec runs in the library: the host encoder in C++, decoding
-and the fused decode-GEMV in gfx950 kernels. PyTorch only provides device
+Every step of the codec runs in the library: the host encoder in C++, decoding,
+the fused decode-GEMV and the operators between the products (norm, attention,
+cache eviction) in gfx950 kernels. PyTorch only provides device
 memory and the current HIP stream. There is no fallback: if the library is
 missing, loading raises.
 """
 from __future__ import annotations
 
 import ctypes
+import math
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import numpy as np
 
@@ -17,7 +19,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libhufflm.so")
 
 HL_OK, HL_EINVAL, HL_ENOMEM, HL_ECORRUPT, HL_EUNSUPPORTED, HL_EHIP = range(6)
-HL_F32, HL_BF16, HL_F16 = 0, 1, 2
+HL_F32, HL_BF16, HL_F16, HL_E4M3 = 0, 1, 2, 3
 HL_FORMAT_SPLIT, HL_FORMAT_WHOLE_EXPONENT, HL_FORMAT_FP16 = 0, 1, 2
 HEADER_BYTES = 128
 LUT_BYTES = 49440
@@ -75,6 +77,20 @@ class TensorView(ctypes.Structure):
                 ("cb", Codebook), ("cb8", Codebook8), ("cb16", Codebook16)]
 
 
+class KeysValues(ctypes.Structure):
+    """hl_kv: keys and values by strides."""
+    _fields_ = [("k_dev", ctypes.c_void_p), ("v_dev", ctypes.c_void_p), ("tokens", ctypes.c_uint64),
+                ("k_seq", ctypes.c_uint64), ("k_token", ctypes.c_uint64), ("k_head", ctypes.c_uint64),
+                ("v_seq", ctypes.c_uint64), ("v_token", ctypes.c_uint64), ("v_head", ctypes.c_uint64)]
+
+
+class AttentionShape(ctypes.Structure):
+    """hl_attention."""
+    _fields_ = [("dtype", ctypes.c_int), ("batch", ctypes.c_uint32), ("queries", ctypes.c_uint32),
+                ("heads", ctypes.c_uint32), ("kv_heads", ctypes.c_uint32), ("dim", ctypes.c_uint32),
+                ("scale", ctypes.c_float), ("prefix", KeysValues), ("own", KeysValues)]
+
+
 _lib = None
 
 EXPORTS = ["hl_status_str", "hl_default_seg_len", "hl_default_grp_rows", "hl_build_codebook", "hl_encode",
@@ -82,7 +98,7 @@ EXPORTS = ["hl_status_str", "hl_default_seg_len", "hl_default_grp_rows", "hl_bui
            "hl_tensor_view", "hl_tensor_prepare", "hl_decode", "hl_gemv_workspace_bytes",
            "hl_decode_gemv", "hl_decode_gemv_noalloc", "hl_decode_gemv_multi", "hl_gemm_workspace_bytes",
            "hl_decode_gemm",
-           "hl_gemv_bf16"]
+           "hl_gemv_bf16", "hl_rms_norm", "hl_attention_workspace_bytes", "hl_prefix_attention", "hl_cache_evict"]
 
 
 def lib() -> ctypes.CDLL:
@@ -142,6 +158,18 @@ def lib() -> ctypes.CDLL:
     L.hl_gemv_bf16.restype = c.c_int
     L.hl_gemv_bf16.argtypes = [c.c_void_p, c.c_uint64, c.c_uint64, c.c_void_p, c.c_int, c.c_uint32,
                                c.c_void_p, c.c_void_p]
+    L.hl_rms_norm.restype = c.c_int
+    L.hl_rms_norm.argtypes = [c.c_void_p, c.c_int, c.c_void_p, c.c_int, c.c_void_p, c.c_int, c.c_uint64, c.c_uint64,
+                              c.c_float, c.c_void_p, c.c_void_p, c.c_int, c.c_uint32, c.c_void_p, c.c_void_p]
+    L.hl_attention_workspace_bytes.restype = c.c_size_t
+    L.hl_attention_workspace_bytes.argtypes = [c.POINTER(AttentionShape), c.c_int]
+    L.hl_prefix_attention.restype = c.c_int
+    L.hl_prefix_attention.argtypes = [c.POINTER(AttentionShape), c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p,
+                                      c.c_void_p, c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p]
+    L.hl_cache_evict.restype = c.c_int
+    L.hl_cache_evict.argtypes = [c.POINTER(KeysValues), c.POINTER(KeysValues), c.c_uint32, c.c_uint32, c.c_uint32,
+                                 c.c_void_p, c.c_void_p, c.c_uint64, c.c_uint64, c.c_void_p, c.c_void_p, c.c_void_p,
+                                 c.c_void_p]
     _lib = L
     return L
 
@@ -464,3 +492,223 @@ def gemv_bf16(w, x, y=None, stream=None):
     _check(lib().hl_gemv_bf16(w.data_ptr(), R, K, x.data_ptr(), dt,
                               x.shape[0], y.data_ptr(), _stream_ptr(stream)), "hl_gemv_bf16")
     return y
+
+
+class NormResult(NamedTuple):
+    out: object              # the normalised rows
+    sum: Optional[object]    # x + residual, in residual's type (None without one)
+    scale: Optional[object]  # of an 8-bit out
+
+
+class AttentionResult(NamedTuple):
+    out: object
+    weights: Optional[object]
+    lse: Optional[object]
+
+
+class EvictResult(NamedTuple):
+    k: object
+    v: object
+    weights: object
+    lens: object
+    slots: object
+
+
+_VALUE_TYPES = None
+
+
+def _value_types():
+    """Codes of the types that norms read and write, by torch type."""
+    global _VALUE_TYPES
+    if _VALUE_TYPES is None:
+        import torch
+        _VALUE_TYPES = {torch.float32: HL_F32, torch.bfloat16: HL_BF16, torch.float16: HL_F16,
+                        torch.float8_e4m3fn: HL_E4M3}
+    return _VALUE_TYPES
+
+
+def rms_norm(x, weight, residual=None, eps: float = 1e-5, out_dtype=None, group: int = 0, out=None, sum_out=None,
+             scale_out=None, stream=None) -> NormResult:
+    """t = x + residual; out = t / sqrt(mean(t^2) + eps) * weight over the last dimension.
+
+    x and residual: [..., hidden] float32, bfloat16 or float16, contiguous; weight: [hidden]. The sum is kept in
+    residual's type (``sum_out`` may be ``residual`` itself). ``out_dtype`` defaults to weight's type;
+    torch.float8_e4m3fn gives 8 bits and float32 scales, one for each ``group`` columns (32, 64 or 128) or, with 0,
+    for each row. Outputs that are not given are allocated."""
+    import torch
+    types = _value_types()
+    hidden = weight.shape[0] if weight.dim() == 1 else -1
+    if x.dim() < 1 or x.shape[-1] != hidden or hidden < 1 or x.numel() < 1:
+        raise ValueError(f"x must be [..., hidden] and weight [hidden], got {tuple(x.shape)} and {tuple(weight.shape)}")
+    e4m3 = torch.float8_e4m3fn
+    ot = out.dtype if out is not None and out_dtype is None else out_dtype or weight.dtype
+    xt, wt, oc = types.get(x.dtype), types.get(weight.dtype), types.get(ot)
+    if xt is None or wt is None or oc is None or xt == HL_E4M3 or wt == HL_E4M3:
+        raise ValueError("x and weight must be float32, bfloat16 or float16; out these or float8_e4m3fn")
+    shape, tokens, dev = x.shape, x.numel() // hidden, x.device
+    if out is None:
+        out = torch.empty(shape, dtype=ot, device=dev)
+    bufs = {"x": x, "weight": weight, "out": out}
+    rt = HL_F32
+    if residual is not None:
+        rt = types.get(residual.dtype)
+        if rt is None or rt == HL_E4M3 or residual.shape != shape:
+            raise ValueError(f"residual must have x's shape {tuple(shape)} and be float32, bfloat16 or float16")
+        if sum_out is None:
+            sum_out = torch.empty(shape, dtype=residual.dtype, device=dev)
+        elif sum_out.dtype != residual.dtype or sum_out.shape != shape:
+            raise ValueError("sum_out must have residual's shape and type")
+        bufs["residual"], bufs["sum_out"] = residual, sum_out
+    elif sum_out is not None:
+        raise ValueError("sum_out needs a residual")
+    if out.dtype != ot or out.shape != shape:
+        raise ValueError(f"out must be {tuple(shape)} of {ot}")
+    if oc == HL_E4M3:
+        if group not in (0, 32, 64, 128) or (group and hidden % group):
+            raise ValueError("group must be 0, or 32, 64 or 128 and divide hidden")
+        need = (*shape[:-1], hidden // group) if group else tuple(shape[:-1])
+        if scale_out is None:
+            scale_out = torch.empty(need, dtype=torch.float32, device=dev)
+        elif scale_out.dtype != torch.float32 or tuple(scale_out.shape) != tuple(need):
+            raise ValueError(f"scale_out must be float32 {tuple(need)}")
+        bufs["scale_out"] = scale_out
+    elif group or scale_out is not None:
+        raise ValueError("group and scale_out need an 8-bit out")
+    for name, t in bufs.items():
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        if t.device != dev or not t.is_cuda:
+            raise ValueError(f"{name} must be on {dev}, a GPU, not {t.device}")
+    has = residual is not None
+    _check(lib().hl_rms_norm(x.data_ptr(), xt, residual.data_ptr() if has else None, rt, weight.data_ptr(), wt,
+                             tokens, hidden, eps, sum_out.data_ptr() if has else None, out.data_ptr(), oc, group,
+                             scale_out.data_ptr() if oc == HL_E4M3 else None, _stream_ptr(stream)), "hl_rms_norm")
+    return NormResult(out, sum_out, scale_out)
+
+
+def _keys_values(k, v, name: str, dims: int, dtype, device):
+    """hl_kv of keys and values [(sequence,) token, key head, column] with any strides but columns in a row."""
+    if k is None or v is None or k.dim() != dims or v.shape != k.shape:
+        raise ValueError(f"{name}: keys and values of one shape, {dims} dimensions")
+    if k.dtype != dtype or v.dtype != dtype:
+        raise ValueError(f"{name}: dtype {k.dtype} and {v.dtype}, expected {dtype}")
+    if k.device != device or v.device != device or not k.is_cuda:
+        raise ValueError(f"{name} must be on {device}, a GPU, not {k.device} and {v.device}")
+    ks, vs = k.stride(), v.stride()
+    if (ks[-1] != 1 or vs[-1] != 1) and k.shape[-1] > 1:
+        raise ValueError(f"{name}: the columns of a head must lie next to each other")
+    return KeysValues(k.data_ptr(), v.data_ptr(), k.shape[-3], ks[0] if dims == 4 else 0, ks[-3], ks[-2],
+                      vs[0] if dims == 4 else 0, vs[-3], vs[-2])
+
+
+def _small(t, name: str, dtype, shape, device):
+    """A contiguous buffer of this type, shape and device (else ValueError)."""
+    _dev_arg(t, name, (dtype,), shape)
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}, not {t.device}")
+    return t
+
+
+def prefix_attention(q, k=None, v=None, lens=None, prefix_k=None, prefix_v=None, scale: Optional[float] = None,
+                     weights=None, out=None, weights_out=None, lse=None, stream=None,
+                     workspace=None) -> AttentionResult:
+    """Attention of new tokens over a prefix shared by the batch and over each sequence's own cache.
+
+    q: [batch, queries, heads, dim] bfloat16 or float16, contiguous. k, v: the own caches
+    [batch, capacity, kv_heads, dim] (any strides with columns in a row), of which sequence b's first ``lens[b]``
+    (int32) tokens are there, the new ones at their end. prefix_k, prefix_v: [length, kv_heads, dim]. Either set may
+    be left out. Token i sees the whole prefix and the own keys before lens[b] - (queries - 1 - i). ``scale`` defaults
+    to 1/sqrt(dim).
+
+    ``weights`` (float32 [batch, kv_heads, capacity]) or ``weights_out``: also gives the weights plus what each own
+    key was given by this call (``weights_out`` may be ``weights``; without ``weights``, plus zeros). ``lse``: a
+    float32 [batch, queries, heads] buffer for the logarithms of the softmax sums. ``workspace``: a uint8 buffer of
+    attention_workspace's size; allocated where it is not given."""
+    import torch
+    if q.dim() != 4 or q.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("q must be [batch, queries, heads, dim] bfloat16 or float16")
+    batch, queries, heads, dim = q.shape
+    dev = q.device
+    if not q.is_cuda or not q.is_contiguous():
+        raise ValueError("q must be contiguous and on the GPU")
+    a = AttentionShape(HL_BF16 if q.dtype == torch.bfloat16 else HL_F16, batch, queries, heads, 0, dim,
+                       1.0 / math.sqrt(dim) if scale is None else scale)
+    kv_heads = None
+    if k is not None or v is not None:
+        a.own = _keys_values(k, v, "k, v", 4, q.dtype, dev)
+        kv_heads = k.shape[2]
+        if k.shape[0] != batch or k.shape[3] != dim:
+            raise ValueError(f"k, v must be [{batch}, capacity, kv_heads, {dim}], got {tuple(k.shape)}")
+        _small(lens, "lens", torch.int32, (batch,), dev)
+    if prefix_k is not None or prefix_v is not None:
+        a.prefix = _keys_values(prefix_k, prefix_v, "prefix_k, prefix_v", 3, q.dtype, dev)
+        if prefix_k.shape[2] != dim or kv_heads not in (None, prefix_k.shape[1]):
+            raise ValueError(f"prefix_k, prefix_v must be [length, kv_heads, {dim}] with the own caches' kv_heads, "
+                             f"got {tuple(prefix_k.shape)}")
+        kv_heads = prefix_k.shape[1]
+    if not kv_heads or heads % kv_heads:
+        raise ValueError("a prefix or own caches are needed, with kv_heads that divide heads")
+    a.kv_heads = kv_heads
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _small(out, "out", q.dtype, q.shape, dev)
+    if weights is not None or weights_out is not None:
+        if k is None:
+            raise ValueError("weights are of the own caches' keys")
+        need = (batch, kv_heads, k.shape[1])
+        if weights is not None:
+            _small(weights, "weights", torch.float32, need, dev)
+        if weights_out is None:
+            weights_out = torch.empty(need, dtype=torch.float32, device=dev)
+        else:
+            _small(weights_out, "weights_out", torch.float32, need, dev)
+    if lse is not None:
+        _small(lse, "lse", torch.float32, (batch, queries, heads), dev)
+    L = lib()
+    if workspace is None:
+        workspace = torch.empty(L.hl_attention_workspace_bytes(ctypes.byref(a), weights_out is not None),
+                                dtype=torch.uint8, device=dev)
+    else:
+        _dev_arg(workspace, "workspace")
+        _on_device(dev, workspace=workspace)
+    _check(L.hl_prefix_attention(ctypes.byref(a), q.data_ptr(), lens.data_ptr() if k is not None else None,
+                                 out.data_ptr(), lse.data_ptr() if lse is not None else None,
+                                 weights.data_ptr() if weights is not None else None,
+                                 weights_out.data_ptr() if weights_out is not None else None, workspace.data_ptr(),
+                                 workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
+           "hl_prefix_attention")
+    return AttentionResult(out, weights_out, lse)
+
+
+def cache_evict(k, v, weights, lens, keep: int, recent: int = 0, k_out=None, v_out=None, stream=None) -> EvictResult:
+    """At most ``keep`` tokens of every sequence and key head, moved in their order to the first slots of another cache:
+    the newest ``recent`` and, of the others, those of greatest accumulated weight (ties: the lowest slot).
+
+    k, v: [batch, capacity, kv_heads, dim], 16-bit, any strides with columns in a row; weights: float32
+    [batch, kv_heads, capacity]; lens: int32 [batch]. k_out, v_out (default: new ones of capacity ``keep``): caches of
+    at least ``keep`` tokens that do not overlap k and v. Gives these, the kept tokens' weights (float32) and slots
+    (int32) [batch, kv_heads, keep] - 0 and -1 past the kept ones, whose rows are zeros - and the new lengths."""
+    import torch
+    if k.dim() != 4 or k.dtype not in (torch.bfloat16, torch.float16, torch.int16):
+        raise ValueError("k must be [batch, capacity, kv_heads, dim] bfloat16, float16 or int16")
+    batch, capacity, heads, dim = k.shape
+    dev = k.device
+    src = _keys_values(k, v, "k, v", 4, k.dtype, dev)
+    if keep < 1 or not 0 <= recent <= keep:
+        raise ValueError("keep must be at least 1 and recent between 0 and keep")
+    _small(weights, "weights", torch.float32, (batch, heads, capacity), dev)
+    _small(lens, "lens", torch.int32, (batch,), dev)
+    if k_out is None and v_out is None:
+        k_out = torch.empty((batch, keep, heads, dim), dtype=k.dtype, device=dev)
+        v_out = torch.empty_like(k_out)
+    dst = _keys_values(k_out, v_out, "k_out, v_out", 4, k.dtype, dev)
+    if (k_out.shape[0], *k_out.shape[2:]) != (batch, heads, dim) or k_out.shape[1] < keep:
+        raise ValueError(f"k_out must be [{batch}, at least {keep}, {heads}, {dim}], got {tuple(k_out.shape)}")
+    w_out = torch.empty((batch, heads, keep), dtype=torch.float32, device=dev)
+    slots = torch.empty((batch, heads, keep), dtype=torch.int32, device=dev)
+    lens_out = torch.empty_like(lens)
+    _check(lib().hl_cache_evict(ctypes.byref(src), ctypes.byref(dst), batch, heads, dim, weights.data_ptr(),
+                                lens.data_ptr(), keep, recent, w_out.data_ptr(), slots.data_ptr(),
+                                lens_out.data_ptr(), _stream_ptr(stream)), "hl_cache_evict")
+    return EvictResult(k_out, v_out, w_out, lens_out, slots)
