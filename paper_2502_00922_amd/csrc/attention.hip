@@ -15,16 +15,21 @@
 // parts of each row. Lengths are read on the device; nothing depends on the
 // order in which blocks run, and there are no atomics.
 //
-// Inside a block a wave works alone: it loads 32 keys and their values from
-// memory to registers, one step ahead, and no LDS or barrier stands in its
-// loop. The matrix instruction takes K as its left operand and Q as its right,
-// so a lane ends up with scores of one query (lane % 16), which is also what
-// the second product needs of P as its right operand: the keys are only
-// numbered differently in the two products, and P never leaves its lane. The
-// values are loaded as rows (lane % 16 owns 8 neighbouring columns of 8 keys)
-// and turned in registers, one byte permutation for two elements; the columns
-// of one lane go to 8 different instructions, so that turning needs no other
-// lane's data.
+// Items of up to 16 rows (a decode step's own caches) are "narrow": the four
+// waves of a block take different keys, 32 at a time, straight from memory to
+// registers and one step ahead; nothing in their loop waits for another wave,
+// and their four results are added in LDS at the end. Larger items are "wide":
+// the four waves have different rows and the same keys, which the block loads
+// from memory to LDS without registers between, 32 at a time and up to three
+// times ahead, so that memory is read once for up to 128 rows.
+//
+// The matrix instruction takes K as its left operand and Q as its right, so a
+// lane ends up with scores of one query (lane % 16), which is also what the
+// second product needs of P as its right operand: the keys are only numbered
+// differently in the two products, and P never leaves its lane. The values are
+// read as rows (lane % 16 owns 8 neighbouring columns of 8 keys) and turned in
+// registers, one byte permutation for two elements; the columns of one lane go
+// to 8 different instructions, so that turning needs no other lane's data.
 #include <algorithm>
 #include <type_traits>
 
@@ -35,6 +40,7 @@ namespace hl {
 constexpr uint32_t kUnit = 128;        // keys of a unit
 constexpr uint32_t kWaves = 4;         // of a block
 constexpr uint32_t kStep = 32;         // keys of a wave's step
+constexpr uint32_t kThreads = 64 * kWaves;
 constexpr float kSlack = 8.0f;         // powers of two that a score may pass the maximum kept for it by
 constexpr float kLog2e = 1.44269504088896341f;
 
@@ -52,11 +58,10 @@ struct Kv {
   uint32_t tokens;  // the prefix's length, or an own cache's capacity
 };
 
-// Rows of an item: `tile` = 16 * R * across, R 16-row tiles a wave, `across`
-// waves side by side (the other kWaves / across take other keys).
+// Rows of an item: 16 (narrow), or r 16-row tiles for each wave (wide).
 struct Tiling {
-  uint32_t r, across, tiles;  // tiles: items of one head (and sequence)
-  __host__ __device__ uint32_t rows() const { return 16 * r * across; }
+  uint32_t r, tiles;  // r: 0 narrow; tiles: items of one head (and sequence)
+  __host__ __device__ uint32_t rows() const { return r ? 16 * r * kWaves : 16; }
 };
 
 struct AttentionArgs {
@@ -81,41 +86,64 @@ __device__ inline uint32_t own_length(const AttentionArgs& a, uint32_t b) {
 
 __host__ __device__ inline uint32_t units_of(uint32_t keys) { return (keys + kUnit - 1) / kUnit; }
 
+// Sum over the lanes up to this one. Whole wave; by row shifts and row
+// broadcasts, which take a few cycles where a shuffle through LDS takes a
+// hundred.
+__device__ inline uint32_t scan_lanes(uint32_t v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);  // lane - 1 of a row of 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);  // lane - 2
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);  // lane - 4
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);  // lane - 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // row 0's last to row 1, row 2's to row 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // lane 31 to rows 2 and 3
+  return v;
+}
+
+// The own caches' part of the line: sequence after sequence, 64 at a time a
+// lane each. `each`: units of one of a sequence's items, `end`: where its units
+// end, from where the 64 sequences' begin.
+struct OwnLine {
+  uint32_t each, end, first;  // first: sequence of lane 0
+};
+
+__device__ inline OwnLine own_line(const AttentionArgs& a, uint32_t first) {
+  const uint32_t b = first + threadIdx.x % 64;
+  OwnLine o;
+  o.first = first;
+  o.each = b < a.batch ? units_of(own_length(a, b)) : 0;
+  o.end = scan_lanes(a.kv_heads * a.to.tiles * o.each);
+  return o;
+}
+
+// Units of sequences 0 .. b-1 (b = batch: of all). Whole wave.
+__device__ inline uint32_t own_units_before(const AttentionArgs& a, const OwnLine& o, uint32_t b) {
+  if (a.own.tokens == 0 || b == 0) return 0;
+  uint32_t sum = 0, b0 = 0;
+  for (; b0 + 64 < b; b0 += 64) sum += __builtin_amdgcn_readlane(own_line(a, b0).end, 63);
+  return sum + __builtin_amdgcn_readlane(b0 == o.first ? o.end : own_line(a, b0).end, b - 1 - b0);
+}
+
 // Where sequence b's units begin in the line, counted from the own caches'
 // first, and how many units one of its items has.
 struct OwnPlace {
   uint32_t b, begin, each;
 };
 
-// Sum of all sequences' units before b (b = batch: of all). Whole wave.
-__device__ inline uint32_t own_units_before(const AttentionArgs& a, uint32_t b) {
-  uint32_t sum = 0;
-  const uint32_t items = a.kv_heads * a.to.tiles;
-  for (uint32_t i = threadIdx.x % 64; i < b; i += 64) sum += items * units_of(own_length(a, i));
-  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-  return __builtin_amdgcn_readfirstlane(sum);
-}
-
 // The sequence that unit u (counted as above) belongs to. Whole wave.
-__device__ inline OwnPlace own_place(const AttentionArgs& a, uint32_t u) {
-  const uint32_t lane = threadIdx.x % 64, items = a.kv_heads * a.to.tiles;
+__device__ inline OwnPlace own_place(const AttentionArgs& a, const OwnLine& o, uint32_t u) {
+  const uint32_t items = a.kv_heads * a.to.tiles;
   uint32_t base = 0;
   for (uint32_t b0 = 0; b0 < a.batch; b0 += 64) {
-    const uint32_t each = b0 + lane < a.batch ? units_of(own_length(a, b0 + lane)) : 0;
-    uint32_t end = items * each;
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t o = __shfl_up(end, d);
-      if (lane >= (uint32_t)d) end += o;
-    }
-    const uint64_t past = __ballot(base + end > u);
+    const OwnLine l = b0 == o.first ? o : own_line(a, b0);
+    const uint64_t past = __ballot(base + l.end > u);
     if (past) {
-      const int l = __builtin_ctzll(past);
-      const uint32_t e = __builtin_amdgcn_readlane(each, l), f = __builtin_amdgcn_readlane(end, l);
-      return {b0 + (uint32_t)l, base + f - items * e, e};
+      const int i = __builtin_ctzll(past);
+      const uint32_t each = __builtin_amdgcn_readlane(l.each, i), end = __builtin_amdgcn_readlane(l.end, i);
+      return {b0 + (uint32_t)i, base + end - items * each, each};
     }
-    base += __builtin_amdgcn_readlane(end, 63);
+    base += __builtin_amdgcn_readlane(l.end, 63);
   }
-  return {a.batch, base, 1};  // past the line's end: no caller asks
+  return {a.batch - 1, base, 1};  // past the line's end: no caller asks
 }
 
 // The block that unit u of `total` is in when `blocks` share them, at most one
@@ -135,11 +163,10 @@ __device__ inline f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
                                                   0);
 }
 
-// Ends a row of matrix instructions: nothing is moved across it, and the
-// instructions after it may write the operands of those before. On gfx950 a
-// product has come out wrong now and then when the instruction right after it
-// wrote one of its operand registers; the compiler places no wait states
-// there, and five are enough.
+// Ends a row of matrix instructions: the instructions after it may write the
+// operands of those before. On gfx950 a product has come out wrong now and then
+// when the instruction right after it wrote one of its operand registers; the
+// compiler places no wait states there, and five are enough.
 __device__ inline void products_end() {
   __builtin_amdgcn_sched_barrier(0);
   asm volatile("s_nop 4");
@@ -154,20 +181,23 @@ __device__ inline uint32_t pack(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, p);
 }
 
+// All bits of each half that is an infinity or NaN (whose exponent is all
+// ones, so that one more carries into the sign's place).
 template <class T>
-__device__ inline float widen(uint32_t h) {
-  if constexpr (std::is_same<T, __bf16>::value)
-    return __builtin_bit_cast(float, h << 16);
-  else
-    return (float)__builtin_bit_cast(_Float16, (uint16_t)h);
+__device__ inline uint32_t beyond(uint32_t pair) {
+  constexpr uint32_t e = std::is_same<T, __bf16>::value ? 0x7F807F80u : 0x7C007C00u;
+  const uint32_t m = ((pair & e) + (std::is_same<T, __bf16>::value ? 0x00800080u : 0x04000400u)) & 0x80008000u;
+  return (m - (m >> 15)) | m;
 }
 
-// Whether a 16-bit value is an infinity or NaN.
-template <class T>
-__device__ inline bool beyond(uint32_t h) {
-  constexpr uint32_t e = std::is_same<T, __bf16>::value ? 0x7F80 : 0x7C00;
-  return (h & e) == e;
+// Keeps sums with v from being formed before the loop that needs them, where
+// they would take a register each.
+__device__ inline uint32_t here(uint32_t v) {
+  asm volatile("" : "+v"(v));
+  return v;
 }
+
+__device__ inline uint32_t lane_id() { return here(threadIdx.x % 64); }
 
 // What one wave needs of an item.
 struct Item {
@@ -200,46 +230,47 @@ struct Tile {
 // in which the first product leaves its scores in a lane.
 __device__ inline uint32_t key_of(uint32_t c, int e) { return (e < 4 ? 0 : 12) + 4 * c + e; }
 
-// Loads keys key .. key+31 of `it`; past its end, its last key again.
-template <int D, bool FULL>
-__device__ inline void load_tile(Tile<D>& t, const Item& it, uint32_t dim, uint32_t key) {
-  using S = Shape<D>;
-  const uint32_t lane = threadIdx.x % 64, n = lane % 16, c = lane / 16;
-  const uint16_t* kp = it.k + (uint64_t)key * it.k_token;
-  const uint16_t* vp = it.v + (uint64_t)key * it.v_token;
-  uint32_t ko[2], vo[8], left = it.keys - 1 - key;
-  if (left >= kStep - 1) {
-    ko[0] = n * it.k_token, ko[1] = ko[0] + 16 * it.k_token;
-    vo[0] = 4 * c * it.v_token;
+// Loads keys (values) key .. key+31 of `it`; where they may pass its end
+// (LAST), its last one again.
+template <int D, bool FULL, bool LAST>
+__device__ inline void load_k(Tile<D>& t, const Item& it, uint32_t dim, uint32_t key) {
+  const uint32_t lane = lane_id(), n = lane % 16, c = lane / 16;
+  const uint8_t* kp = reinterpret_cast<const uint8_t*>(it.k + (uint64_t)key * it.k_token);
+  const uint32_t left = it.keys - 1 - key, bytes = 2 * it.k_token, first = here(n * bytes);
 #pragma unroll
-    for (int e = 1; e < 8; ++e) vo[e] = vo[0] + (key_of(0, e)) * it.v_token;
-  } else {
-    ko[0] = min(n, left) * it.k_token, ko[1] = min(16 + n, left) * it.k_token;
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t at = LAST ? min(16 * h + n, left) * bytes : first + 16 * h * bytes;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) vo[e] = min(key_of(c, e), left) * it.v_token;
-  }
-#pragma unroll
-  for (int s = 0; s < S::KS; ++s) {
-    const uint32_t d = c * 8 + s * 32;
-    const bool in = FULL || d < dim;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(kp + (ko[h] + (in ? d : 0)));
+    for (int s = 0; s < Shape<D>::KS; ++s) {
+      const uint32_t d = c * 8 + s * 32;
+      const bool in = FULL || d < dim;
+      const u32x4 w = *reinterpret_cast<const u32x4*>(kp + (at + (in ? 2 * d : 0)));
       t.k[h][s] = in ? w : u32x4{0, 0, 0, 0};
     }
   }
+}
+
+template <int D, bool FULL, bool LAST>
+__device__ inline void load_v(Tile<D>& t, const Item& it, uint32_t dim, uint32_t key) {
+  using S = Shape<D>;
+  const uint32_t lane = lane_id(), n = lane % 16, c = lane / 16;
+  const uint8_t* vp = reinterpret_cast<const uint8_t*>(it.v + (uint64_t)key * it.v_token);
+  const uint32_t left = it.keys - 1 - key, bytes = 2 * it.v_token;
 #pragma unroll
   for (int h = 0; h < S::HALVES; ++h) {
     uint32_t d = n * S::VE + h * 128;
     if (!FULL && d >= dim) d = 0;  // columns that no output is stored from
+    const uint32_t first = here(4 * c * bytes + 2 * d);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
+      const uint32_t at = LAST ? min(key_of(c, e), left) * bytes + 2 * d : first + key_of(0, e) * bytes;
       if constexpr (S::VE == 8) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(vp + (vo[e] + d));
+        const u32x4 w = *reinterpret_cast<const u32x4*>(vp + at);
+#pragma unroll
         for (int j = 0; j < 4; ++j) t.v[e][h][j] = w[j];
       } else {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(vp + (vo[e] + d));
-        for (int j = 0; j < 2; ++j) t.v[e][h][j] = w[j];
+        const u32x2 w = *reinterpret_cast<const u32x2*>(vp + at);
+        t.v[e][h][0] = w[0], t.v[e][h][1] = w[1];
       }
     }
   }
@@ -253,50 +284,104 @@ struct State {
   float m[R], l[R];    // maximum (0 while there is none), this lane's part of the sum
   bool some[R];        // whether m is a score's
   uint32_t seen[R];    // keys that the query sees
+  uint32_t odd;        // whether a value of this lane was taken out of the product
 };
 
-// Contributions of values that are infinite or NaN, which the matrix product
-// has taken as 0: a query that does not see their key must not meet them.
-template <class T, int D, int R>
-__device__ inline void add_beyond(State<D, R>& st, const float (&p)[R][2][4], const Item& it,
-                                                     uint32_t dim, uint32_t key) {
+constexpr int kSet = 4;  // output tiles whose values are turned at a time: the operands take 16 registers
+
+// The left operands of output tiles i0 .. i0+kSet-1: values of 8 keys, for the
+// columns that the tiles give this lane. All are turned before a product may
+// follow.
+template <int D>
+__device__ inline void turn(u32x4 (&vt)[kSet], const Tile<D>& t, int i0) {
   using S = Shape<D>;
-  const uint32_t lane = threadIdx.x % 64, n = lane % 16, c = lane / 16;
-  for (uint32_t j = 0; j < kStep && key + j < it.keys; ++j) {
-    const uint16_t* row = it.v + (uint64_t)(key + j) * it.v_token;
 #pragma unroll
-    for (int rt = 0; rt < R; ++rt) {
-      float w = 0.0f;
+  for (int i = i0; i < i0 + kSet; ++i) {
+    const uint32_t sel = i % 2 ? 0x07060302u : 0x05040100u;
+    const int h = i / S::VE, j = i % S::VE / 2;
 #pragma unroll
-      for (uint32_t h = 0; h < 2; ++h)
+    for (int e = 0; e < 4; ++e) vt[i - i0][e] = __builtin_amdgcn_perm(t.v[2 * e + 1][h][j], t.v[2 * e][h][j], sel);
+  }
+  asm volatile("" : "+v"(vt[0]), "+v"(vt[1]), "+v"(vt[2]), "+v"(vt[3]));
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Ends the products of these operands, which keep their registers until then.
+__device__ inline void turned_end(const u32x4 (&vt)[kSet]) {
+  products_end();
+  asm volatile("" ::"v"(vt[0]), "v"(vt[1]), "v"(vt[2]), "v"(vt[3]));
+}
+
+// A pair of values to powers of two that say what each is: 1 for +infinity, 64
+// for -infinity, 4096 for a NaN, and 0 for the rest. Sums over a step's 32 keys
+// still tell them apart.
+template <class T>
+__device__ inline uint32_t kinds(uint32_t pair) {
+  constexpr bool bf = std::is_same<T, __bf16>::value;
+  constexpr uint32_t one = bf ? 0x3F803F80u : 0x3C003C00u, sixtyfour = bf ? 0x42804280u : 0x54005400u,
+                     big = bf ? 0x45804580u : 0x6C006C00u, mantissa = bf ? 0x007F007Fu : 0x03FF03FFu;
+  const uint32_t sign = pair & 0x80008000u, minus = (sign - (sign >> 15)) | sign;
+  const uint32_t some = (((pair & mantissa) + mantissa) << (bf ? 8 : 5)) & 0x80008000u, nan = (some - (some >> 15)) | some;
+  return beyond<T>(pair) & ((nan & big) | (~nan & ((minus & sixtyfour) | (~minus & one))));
+}
+
+// Adds to the outputs what the infinite and NaN values of keys key .. end
+// make of them, for the queries that see their keys alone: in the product with
+// the weights, where a hidden key has weight 0, they would make NaN of the
+// others too. A wave's steps are `stride` keys apart.
+template <class T, int D, bool FULL, int R>
+__device__ inline void add_beyond(State<D, R>& st, const Item& it, uint32_t dim, uint32_t key, uint32_t end,
+                                  uint32_t stride) {
+  const uint32_t c = lane_id() / 16;
+  constexpr uint32_t one = std::is_same<T, __bf16>::value ? 0x3F80u : 0x3C00u;
+#pragma unroll 1
+  for (; key < end; key += stride) {
+    Tile<D> t;
+    load_v<D, FULL, true>(t, it, dim, key);
+    u32x4 sees[R];
 #pragma unroll
-        for (uint32_t r = 0; r < 4; ++r) w = h == j / 16 && r == j % 4 ? p[rt][h][r] : w;
-      w = __shfl(w, (j % 16 / 4) * 16 + n);
-      if (key + j >= st.seen[rt]) continue;
+    for (int rt = 0; rt < R; ++rt)
 #pragma unroll
-      for (int t = 0; t < S::TILES; ++t)
+      for (int e = 0; e < 8; e += 2)
+        sees[rt][e / 2] =
+            (key + key_of(c, e) < st.seen[rt] ? one : 0) | (key + key_of(c, e + 1) < st.seen[rt] ? one << 16 : 0);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const uint32_t d = t / S::VE * 128 + (4 * c + r) * S::VE + t % S::VE;
-          if (d >= dim) continue;
-          const uint32_t b = row[d];
-          if (beyond<T>(b)) st.o[rt][t][r] += w * widen<T>(b);
+    for (int i0 = 0; i0 < Shape<D>::TILES; i0 += kSet) {
+      u32x4 vt[kSet];
+      turn<D>(vt, t, i0);
+#pragma unroll
+      for (int i = 0; i < kSet; ++i) {
+        u32x4 kind;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) kind[e] = kinds<T>(vt[i][e]);
+#pragma unroll
+        for (int rt = 0; rt < R; ++rt) {
+          const f32x4 sum = mfma<T>(kind, sees[rt], f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+          products_end();
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int n = (int)sum[r];
+            const float up = n & 63 ? INFINITY : 0.0f, down = n & 4032 ? -INFINITY : 0.0f;
+            st.o[rt][i0 + i][r] += n >= 4096 ? __builtin_nanf("") : up + down;
+          }
         }
+      }
     }
   }
 }
 
-// One step: scores of 32 keys, their weights, and the weighted values.
-// `all`: keys that every query of the wave sees; `most`: that some query sees.
-template <class T, int D, int R>
+// One step: scores of 32 keys, their weights, and the weighted values. EDGE:
+// some query may not see some of the keys; `most`: keys that some query sees.
+// get_k and get_v bring the step's keys and values into the tile.
+template <class T, int D, int R, bool EDGE, class GetK, class GetV>
 __device__ inline void step(State<D, R>& st, Tile<D>& t, const AttentionArgs& a, const Item& it, uint32_t key,
-                            uint32_t all, uint32_t most, uint32_t wave_row) {
+                            uint32_t most, uint32_t wave_row, GetK get_k, GetV get_v) {
   using S = Shape<D>;
-  const uint32_t lane = threadIdx.x % 64, n = lane % 16, c = lane / 16;
-  const bool edge = key + kStep > all;
+  const uint32_t lane = lane_id(), n = lane % 16, c = lane / 16;
   f32x4 s[R][2];
   float p[R][2][4];
   u32x4 w[R];
+  get_k(t, it, a.dim, key);
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int rt = 0; rt < R; ++rt)
@@ -309,6 +394,7 @@ __device__ inline void step(State<D, R>& st, Tile<D>& t, const AttentionArgs& a,
 #pragma unroll
       for (int h = 0; h < 2; ++h) s[rt][h] = mfma<T>(t.k[h][i], st.q[rt][i], s[rt][h]);
   products_end();
+  if constexpr (!EDGE) get_v(t, it, a.dim, key);  // on its way during the softmax
 #pragma unroll
   for (int rt = 0; rt < R; ++rt) {
     float top = -INFINITY;
@@ -316,7 +402,7 @@ __device__ inline void step(State<D, R>& st, Tile<D>& t, const AttentionArgs& a,
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int r = 0; r < 4; ++r) p[rt][h][r] = s[rt][h][r] * a.scale2;
-    if (edge) {
+    if constexpr (EDGE) {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -363,142 +449,156 @@ __device__ inline void step(State<D, R>& st, Tile<D>& t, const AttentionArgs& a,
     w[rt] = u32x4{pack<T>(p[rt][0][0], p[rt][0][1]), pack<T>(p[rt][0][2], p[rt][0][3]),
                   pack<T>(p[rt][1][0], p[rt][1][1]), pack<T>(p[rt][1][2], p[rt][1][3])};
   }
-  if (edge) {
+  if constexpr (EDGE) {
+    get_v(t, it, a.dim, key);
     // values that no query sees count 0, whatever they are; those that only
-    // some see must be finite in the product
-    bool odd = false;
+    // some see must be finite in the product (add_beyond has the others)
+    const uint32_t some = it.ordered ? ~0u : 0u;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const bool in = key + key_of(c, e) < most;
+      const uint32_t in = key + key_of(c, e) < most ? ~0u : 0u;
 #pragma unroll
       for (int h = 0; h < S::HALVES; ++h)
 #pragma unroll
         for (int j = 0; j < S::VE / 2; ++j) {
-          uint32_t& d = t.v[e][h][j];
-          if (!in) d = 0;
-          if (it.ordered) {
-            if (beyond<T>(d)) d &= 0xFFFF0000u, odd = true;
-            if (beyond<T>(d >> 16)) d &= 0xFFFFu, odd = true;
-          }
+          const uint32_t d = t.v[e][h][j] & in, off = beyond<T>(d) & some;
+          st.odd |= off;
+          t.v[e][h][j] = d & ~off;
         }
     }
-    if (it.ordered && __any(odd)) add_beyond<T, D, R>(st, p, it, a.dim, key);
   }
 #pragma unroll
-  for (int h = 0; h < S::HALVES; ++h) {
-    u32x4 vt[S::VE];
+  for (int i0 = 0; i0 < S::TILES; i0 += kSet) {
+    u32x4 vt[kSet];
+    turn<D>(vt, t, i0);
 #pragma unroll
-    for (int i = 0; i < S::VE; ++i) {
-      const uint32_t sel = i % 2 ? 0x07060302u : 0x05040100u;
+    for (int i = 0; i < kSet; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) vt[i][e] = __builtin_amdgcn_perm(t.v[2 * e + 1][h][i / 2], t.v[2 * e][h][i / 2], sel);
-    }
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int i = 0; i < S::VE; ++i)
-#pragma unroll
-      for (int rt = 0; rt < R; ++rt) st.o[rt][h * S::VE + i] = mfma<T>(vt[i], w[rt], st.o[rt][h * S::VE + i]);
-    products_end();
+      for (int rt = 0; rt < R; ++rt) st.o[rt][i0 + i] = mfma<T>(vt[i], w[rt], st.o[rt][i0 + i]);
+    turned_end(vt);
   }
 }
 
-// A block's LDS: each wave's output rows, padded by 4 so that rows start in
-// different banks, and their (maximum, sum).
-template <int D, int R>
+// LDS buffers of a wide item, a step's keys and values each.
+constexpr uint32_t buffers(int d) { return d == 256 ? 2 : 4; }
+constexpr uint32_t buffer_bytes(int d) { return kStep * d * 4; }
+
+// A block's LDS in floats: a narrow item's result of every wave (rows padded
+// by 4, so that they start in different banks) and their (maximum, sum), or a
+// wide item's buffers.
+template <int D, int RW>
 constexpr uint32_t lds_floats() {
-  return kWaves * 16 * R * (D + 4) + kWaves * 16 * R * 2;
+  constexpr uint32_t narrow = kWaves * 16 * (D + 4) + kWaves * 16 * 2;
+  constexpr uint32_t wide = RW ? buffers(D) * buffer_bytes(D) / 4 : 0;
+  return narrow > wide ? narrow : wide;
 }
 
-// Keys [k0, k1) of an item by one block; writes the part at `slot`.
-template <class T, int D, bool FULL, int R>
-__device__ inline void part(const AttentionArgs& a, const Item& it, const Tiling& tl, uint32_t k0, uint32_t k1,
-                            uint32_t slot, float* lds) {
-  using S = Shape<D>;
-  const uint32_t lane = threadIdx.x % 64, n = lane % 16, c = lane / 16;
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const uint32_t across = tl.across, along = kWaves / across;
-  const uint32_t wr = wave % across, kw = wave / across;
-  const uint32_t wave_row = it.row0 + wr * 16 * R;
-  State<D, R> st;
+// Starts a wave's state: its queries, from row `wave_row` of the item's head.
+template <int D, bool FULL, int R>
+__device__ inline void begin(State<D, R>& st, const AttentionArgs& a, const Item& it, uint32_t wave_row) {
+  const uint32_t lane = lane_id(), n = lane % 16, c = lane / 16;
+  st.odd = 0;
 #pragma unroll
   for (int rt = 0; rt < R; ++rt) {
     st.m[rt] = 0.0f, st.l[rt] = 0.0f, st.some[rt] = false;
 #pragma unroll
-    for (int i = 0; i < S::TILES; ++i) st.o[rt][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i = 0; i < Shape<D>::TILES; ++i) st.o[rt][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     const uint32_t row = min(wave_row + 16 * rt + n, it.rows - 1), tok = row / a.share;
     st.seen[rt] = it.ordered ? (it.keys + tok > it.back ? it.keys + tok - it.back : 0) : it.keys;
     const uint16_t* q = it.q + ((uint64_t)tok * a.heads + row % a.share) * a.dim;
 #pragma unroll
-    for (int s = 0; s < S::KS; ++s) {
+    for (int s = 0; s < Shape<D>::KS; ++s) {
       const uint32_t d = c * 8 + s * 32;
       const bool in = FULL || d < a.dim;
       const u32x4 w = *reinterpret_cast<const u32x4*>(q + (in ? d : 0));
       st.q[rt][s] = in ? w : u32x4{0, 0, 0, 0};
     }
   }
-  // keys seen by the wave's first and last row
-  uint32_t all = it.keys, most = it.keys;
-  if (it.ordered) {
-    const uint32_t first = min(wave_row, it.rows - 1) / a.share, last = min(wave_row + 16 * R, it.rows) - 1;
-    all = it.keys + first > it.back ? it.keys + first - it.back : 0;
-    most = it.keys + last / a.share > it.back ? it.keys + last / a.share - it.back : 0;
-  }
-  const uint32_t end = wave_row < it.rows ? min(k1, most) : 0;
-  uint32_t key = k0 + kStep * kw;
-  const uint32_t stride = kStep * along;
-  if (key < end) {
+}
+
+// Keys that the token of a head's row sees.
+__device__ inline uint32_t seen_by(const AttentionArgs& a, const Item& it, uint32_t row) {
+  const uint32_t n = it.keys + min(row, it.rows - 1) / a.share;
+  return !it.ordered ? it.keys : n > it.back ? n - it.back : 0;
+}
+
+// The sum of a query's weights, of which each of its four lanes has a part.
+__device__ inline float over_lanes(float l) {
+  l += __shfl_xor(l, 16);
+  return l + __shfl_xor(l, 32);
+}
+
+// Keys [k0, k1) of a narrow item by one block; writes the part at `slot`.
+template <class T, int D, bool FULL>
+__device__ inline void narrow_part(const AttentionArgs& a, const Item& it, uint32_t k0, uint32_t k1, uint32_t slot,
+                                   float* lds) {
+  using S = Shape<D>;
+  const uint32_t lane = lane_id(), n = lane % 16, c = lane / 16;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  State<D, 1> st;
+  begin<D, FULL, 1>(st, a, it, it.row0);
+  const uint32_t all = seen_by(a, it, it.row0), most = seen_by(a, it, it.row0 + 15), end = min(k1, most);
+  uint32_t key = k0 + kStep * wave;
+  const uint32_t whole = min(end, all);  // steps that end here or before hide no key
+  if constexpr (D == 256) {  // two steps' keys do not fit the registers
+    for (; key + kStep <= whole; key += kUnit) {
+      Tile<D> t;
+      step<T, D, 1, false>(st, t, a, it, key, most, it.row0, load_k<D, FULL, false>, load_v<D, FULL, false>);
+    }
+  } else if (key + kStep <= whole) {
+    const auto load = [&](Tile<D>& t, uint32_t at) {
+      load_k<D, FULL, false>(t, it, a.dim, at);
+      load_v<D, FULL, false>(t, it, a.dim, at);
+    };
+    const auto there = [](Tile<D>&, const Item&, uint32_t, uint32_t) {};
     Tile<D> t0, t1;
-    load_tile<D, FULL>(t0, it, a.dim, key);
+    load(t0, key);
     while (true) {
-      if constexpr (D == 256) {  // two steps' keys do not fit the registers
-        step<T, D, R>(st, t0, a, it, key, all, most, wave_row);
-        if ((key += stride) >= end) break;
-        load_tile<D, FULL>(t0, it, a.dim, key);
-        continue;
-      }
-      uint32_t next = key + stride;
-      if (next < end) load_tile<D, FULL>(t1, it, a.dim, next);
-      step<T, D, R>(st, t0, a, it, key, all, most, wave_row);
-      if (next >= end) break;
-      key = next, next += stride;
-      if (next < end) load_tile<D, FULL>(t0, it, a.dim, next);
-      step<T, D, R>(st, t1, a, it, key, all, most, wave_row);
-      if (next >= end) break;
-      key = next;
+      bool more = key + kUnit + kStep <= whole;
+      if (more) load(t1, key + kUnit);
+      step<T, D, 1, false>(st, t0, a, it, key, most, it.row0, there, there);
+      key += kUnit;
+      if (!more) break;
+      more = key + kUnit + kStep <= whole;
+      if (more) load(t0, key + kUnit);
+      step<T, D, 1, false>(st, t1, a, it, key, most, it.row0, there, there);
+      key += kUnit;
+      if (!more) break;
     }
   }
-  // join the waves that had other keys of the same rows
-  float* lds_ml = lds + kWaves * 16 * R * (D + 4);
-#pragma unroll
-  for (int rt = 0; rt < R; ++rt) {
-    float l = st.l[rt];
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    const uint32_t row = wave * 16 * R + 16 * rt + n;
-    if (c == 0) lds_ml[2 * row] = st.some[rt] || l != l ? st.m[rt] : -INFINITY, lds_ml[2 * row + 1] = l;
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-#pragma unroll
-      for (int h = 0; h < S::HALVES; ++h)
-#pragma unroll
-        for (int q = 0; q < S::VE; q += 4) {
-          const int i = h * S::VE + q;
-          *reinterpret_cast<float4*>(lds + (uint64_t)row * (D + 4) + h * 128 + (4 * c + r) * S::VE + q) =
-              make_float4(st.o[rt][i][r], st.o[rt][i + 1][r], st.o[rt][i + 2][r], st.o[rt][i + 3][r]);
-        }
+  const uint32_t edge = key;
+#pragma unroll 1
+  for (; key < end; key += kUnit) {
+    Tile<D> t;
+    step<T, D, 1, true>(st, t, a, it, key, most, it.row0, load_k<D, FULL, true>, load_v<D, FULL, true>);
   }
+  if (__any(st.odd != 0)) add_beyond<T, D, FULL, 1>(st, it, a.dim, edge, end, kUnit);
+  // add the four waves' results
+  float* lds_ml = lds + kWaves * 16 * (D + 4);
+  const float sum = over_lanes(st.l[0]);
+  const uint32_t at = here(wave * 16 + n);  // formed here: no register holds it through the loops
+  if (c == 0) lds_ml[2 * at] = st.some[0] || sum != sum ? st.m[0] : -INFINITY, lds_ml[2 * at + 1] = sum;
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int h = 0; h < S::HALVES; ++h)
+#pragma unroll
+      for (int q = 0; q < S::VE; q += 4) {
+        const int i = h * S::VE + q;
+        *reinterpret_cast<float4*>(lds + (uint64_t)at * (D + 4) + h * 128 + (4 * c + r) * S::VE + q) =
+            make_float4(st.o[0][i][r], st.o[0][i + 1][r], st.o[0][i + 2][r], st.o[0][i + 3][r]);
+      }
   __syncthreads();
-  const uint32_t rows = min(tl.rows(), it.rows - it.row0);
+  const uint32_t rows = min(16u, it.rows - it.row0);
   float* po = a.part_o + (uint64_t)slot * a.part_rows * D;
   float* pml = a.part_ml + (uint64_t)slot * a.part_rows * 2;
-  for (uint32_t x = threadIdx.x; x < rows * (D / 4); x += kWaves * 64) {
+  for (uint32_t x = here(threadIdx.x); x < rows * (D / 4); x += kThreads) {
     const uint32_t row = x / (D / 4), d = x % (D / 4) * 4;
-    const uint32_t at = row / (16 * R) * 16 * R + row % (16 * R);  // of key wave 0
     float m = -INFINITY, l = 0.0f;
-    for (uint32_t k = 0; k < along; ++k) m = fmaxf(m, lds_ml[2 * (at + k * across * 16 * R)]);
+    for (uint32_t k = 0; k < kWaves; ++k) m = fmaxf(m, lds_ml[2 * (row + 16 * k)]);
     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (uint32_t k = 0; k < along; ++k) {
-      const uint32_t from = at + k * across * 16 * R;
+    for (uint32_t k = 0; k < kWaves; ++k) {
+      const uint32_t from = row + 16 * k;
       const float mk = lds_ml[2 * from];
       const float f = mk == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mk - m);
       const float4 v = *reinterpret_cast<const float4*>(lds + (uint64_t)from * (D + 4) + d);
@@ -511,6 +611,170 @@ __device__ inline void part(const AttentionArgs& a, const Item& it, const Tiling
   __syncthreads();
 }
 
+// Which place of its row in an LDS buffer 16-byte piece j has, and which piece
+// has place j: the pieces of a row change places with the row's number, so that
+// the 16 lanes that read one piece of 16 rows together use all banks.
+template <int D>
+__device__ inline uint32_t place(uint32_t row, uint32_t j) {
+  return j ^ (D == 64 ? row / 2 % 8 : row % 16);
+}
+
+// 64 lanes' 16 bytes at base + offset (each lane's own) to LDS, one lane's after
+// the other's from `lds` on. Counted by vmcnt alone: the compiler, which would
+// wait for all such loads before any read of LDS, does not see it.
+__device__ inline void load_to_lds(const void* base, uint32_t offset, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 1\n\tglobal_load_lds_dwordx4 %1, %2"
+               :
+               : "s"(lds), "v"(offset), "s"(base)
+               : "memory", "m0");
+}
+
+// Loads of one wave for a buffer, of keys and of values.
+template <int D>
+constexpr uint32_t loads_each() {
+  return kStep * D * 2 / 1024 / kWaves;
+}
+
+// This wave's quarter of keys key .. key+31 of `it` to the buffer at `lds`;
+// past its end, its last key again, and past the head's columns, its first
+// columns again.
+template <int D, bool FULL>
+__device__ inline void load_buffer(const Item& it, uint32_t dim, uint32_t key, uint32_t lds) {
+  constexpr uint32_t pieces = D / 8, rows = 64 / pieces;  // rows of a load
+  const uint32_t lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const uint8_t* kp = reinterpret_cast<const uint8_t*>(it.k + (uint64_t)key * it.k_token);
+  const uint8_t* vp = reinterpret_cast<const uint8_t*>(it.v + (uint64_t)key * it.v_token);
+  const uint32_t left = it.keys - 1 - key;
+#pragma unroll
+  for (uint32_t i = 0; i < loads_each<D>(); ++i) {
+    const uint32_t x = wave * loads_each<D>() + i, row = x * rows + lane / pieces, from = min(row, left);
+    uint32_t d = place<D>(row, lane % pieces) * 16;
+    if (!FULL && d >= 2 * dim) d = 0;
+    load_to_lds(kp, from * 2 * it.k_token + d, lds + x * 1024);
+    load_to_lds(vp, from * 2 * it.v_token + d, lds + buffer_bytes(D) / 2 + x * 1024);
+  }
+}
+
+// Waits until all but the latest n buffers' loads of this wave are done, and
+// for the other waves.
+template <int D>
+__device__ inline void buffers_ready(uint32_t n) {
+  static_assert(loads_each<D>() * 2 <= 8, "vmcnt");
+  constexpr uint32_t each = loads_each<D>() * 2;
+  __builtin_amdgcn_sched_barrier(0);
+  if (n >= 2)
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * each) : "memory");
+  else if (n == 1)
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(each) : "memory");
+  else
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Keys [k0, k1) of a wide item by one block; each wave writes its rows of the
+// part at `slot`.
+template <class T, int D, bool FULL, int R>
+__device__ inline void wide_part(const AttentionArgs& a, const Item& it, uint32_t k0, uint32_t k1, uint32_t slot,
+                                 float* lds) {
+  using S = Shape<D>;
+  constexpr uint32_t bytes = buffer_bytes(D), ring = buffers(D);
+  const uint32_t lane = lane_id(), n = lane % 16, c = lane / 16;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const uint32_t wave_row = it.row0 + wave * 16 * R;
+  const uint32_t most = seen_by(a, it, wave_row + 16 * R - 1), all = seen_by(a, it, it.row0);
+  const uint32_t end = min(k1, seen_by(a, it, it.row0 + 16 * R * kWaves - 1));
+  const uint32_t mine = wave_row < it.rows ? min(end, most) : 0;
+  const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+  const uint32_t steps = k0 < end ? (end - k0 + kStep - 1) / kStep : 0;
+#pragma unroll
+  for (uint32_t i = 0; i + 1 < ring; ++i)
+    if (i < steps) load_buffer<D, FULL>(it, a.dim, k0 + i * kStep, at + i * bytes);
+  State<D, R> st;
+  begin<D, FULL, R>(st, a, it, wave_row);
+  // Steps begin at multiples of 16 rows, so which banks a lane's pieces are in
+  // does not depend on the step.
+  uint32_t kofs[S::KS], vofs[4];
+#pragma unroll
+  for (int s = 0; s < S::KS; ++s) kofs[s] = n * D * 2 + place<D>(n, c + 4 * s) * 16;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    vofs[e] = bytes / 2 + (4 * c + e) * D * 2 + place<D>(4 * c + e, n * S::VE / 8) * 16 + (S::VE == 4 ? n % 2 * 8 : 0);
+  const uint8_t* from;  // the step's buffer
+  const auto get_k = [&](Tile<D>& t, const Item&, uint32_t dim, uint32_t) {
+#pragma unroll
+    for (int s = 0; s < S::KS; ++s)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(from + kofs[s] + h * 16 * D * 2);
+        t.k[h][s] = FULL || c * 8 + s * 32 < dim ? w : u32x4{0, 0, 0, 0};
+      }
+  };
+  const auto get_v = [&](Tile<D>& t, const Item&, uint32_t, uint32_t) {
+#pragma unroll
+    for (int h = 0; h < S::HALVES; ++h)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        // 16 pieces on, the other half of a row of 256 columns
+        const uint8_t* v = from + vofs[e % 4] + h * 256 + (e < 4 ? 0 : 16 * D * 2);
+        if constexpr (S::VE == 8) {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(v);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) t.v[e][h][j] = w[j];
+        } else {
+          const u32x2 w = *reinterpret_cast<const u32x2*>(v);
+          t.v[e][h][0] = w[0], t.v[e][h][1] = w[1];
+        }
+      }
+  };
+  const auto ready = [&](uint32_t i) {
+    // All waves have left the buffer of step i - 1, which is loaded next.
+    buffers_ready<D>(min(steps - 1 - i, ring - 2));
+    if (i + ring - 1 < steps)
+      load_buffer<D, FULL>(it, a.dim, k0 + (i + ring - 1) * kStep, at + (i + ring - 1) % ring * bytes);
+    from = reinterpret_cast<const uint8_t*>(lds) + i % ring * bytes;
+  };
+  // the steps that hide no key of any wave, then the rest
+  const uint32_t whole = k0 < min(end, all) ? (min(end, all) - k0) / kStep : 0;
+  uint32_t i = 0;
+#pragma unroll 1
+  for (; i < whole; ++i) {
+    ready(i);
+    if (mine == 0) continue;
+    Tile<D> t;
+    step<T, D, R, false>(st, t, a, it, k0 + i * kStep, most, wave_row, get_k, get_v);
+  }
+#pragma unroll 1
+  for (; i < steps; ++i) {
+    ready(i);
+    if (k0 + i * kStep >= mine) continue;
+    Tile<D> t;
+    step<T, D, R, true>(st, t, a, it, k0 + i * kStep, most, wave_row, get_k, get_v);
+  }
+  if (__any(st.odd != 0)) add_beyond<T, D, FULL, R>(st, it, a.dim, k0 + whole * kStep, mine, kStep);
+  __syncthreads();  // the buffers are free
+  float* po = a.part_o + (uint64_t)slot * a.part_rows * D;
+  float* pml = a.part_ml + (uint64_t)slot * a.part_rows * 2;
+#pragma unroll
+  for (int rt = 0; rt < R; ++rt) {
+    const float sum = over_lanes(st.l[rt]);
+    const uint32_t row = here(wave * 16 * R + 16 * rt + n);
+    if (it.row0 + row >= it.rows) continue;
+    if (c == 0) pml[2 * row] = st.some[rt] || sum != sum ? st.m[rt] : -INFINITY, pml[2 * row + 1] = sum;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int h = 0; h < S::HALVES; ++h)
+#pragma unroll
+        for (int q = 0; q < S::VE; q += 4) {
+          const int i = h * S::VE + q;
+          *reinterpret_cast<float4*>(po + (uint64_t)row * D + h * 128 + (4 * c + r) * S::VE + q) =
+              make_float4(st.o[rt][i][r], st.o[rt][i + 1][r], st.o[rt][i + 2][r], st.o[rt][i + 3][r]);
+        }
+  }
+}
+
 // Blocks that stand next to each other in the line go to the same XCD, where
 // the row tiles of one head find its keys in the L2 (blocks are dealt to the 8
 // XCDs in turn).
@@ -518,11 +782,13 @@ __device__ inline uint32_t line_block(uint32_t blocks) {
   return blocks % 8 ? blockIdx.x : blockIdx.x % 8 * (blocks / 8) + blockIdx.x / 8;
 }
 
-template <class T, int D, bool FULL, int RMAX>
-__global__ void __launch_bounds__(256, 1) parts_kernel(AttentionArgs a) {
-  __shared__ __attribute__((aligned(16))) float lds[lds_floats<D, RMAX>()];
+// RW: 16-row tiles of a wave in wide items (0: the call has none).
+template <class T, int D, bool FULL, int RW>
+__global__ void __launch_bounds__(kThreads, 2) parts_kernel(AttentionArgs a) {
+  __shared__ __attribute__((aligned(16))) float lds[lds_floats<D, RW>()];
   const uint32_t up = units_of(a.prefix.tokens), prefix_units = a.kv_heads * a.tp.tiles * up;
-  const uint32_t total = prefix_units + own_units_before(a, a.own.tokens ? a.batch : 0);
+  const OwnLine line = a.own.tokens ? own_line(a, 0) : OwnLine{0, 0, 0};
+  const uint32_t total = prefix_units + own_units_before(a, line, a.batch);
   const uint32_t blk = line_block(a.blocks), blocks = min(a.blocks, total);
   if (blk >= blocks) return;
   uint32_t u = (uint32_t)((uint64_t)blk * total / blocks);
@@ -540,7 +806,7 @@ __global__ void __launch_bounds__(256, 1) parts_kernel(AttentionArgs a) {
       it.row0 = item % a.tp.tiles * a.tp.rows(), it.rows = a.batch * a.queries * a.share;
       it.scores = nullptr;
     } else {
-      const OwnPlace pl = own_place(a, u - prefix_units);
+      const OwnPlace pl = own_place(a, line, u - prefix_units);
       const uint32_t x = u - prefix_units - pl.begin, y = x / pl.each;
       in = x % pl.each, each = pl.each, head = y / a.to.tiles;
       item = a.kv_heads * a.tp.tiles + pl.b * a.kv_heads * a.to.tiles + y;
@@ -555,29 +821,34 @@ __global__ void __launch_bounds__(256, 1) parts_kernel(AttentionArgs a) {
                       : nullptr;
     }
     const uint32_t take = min(each - in, end - u);
-    const Tiling& tl = shared ? a.tp : a.to;
-    if (RMAX == 1 || tl.r == 1)
-      part<T, D, FULL, 1>(a, it, tl, in * kUnit, (in + take) * kUnit, blk + item, lds);
+    if (RW == 0 || !(shared ? a.tp.r : a.to.r))
+      narrow_part<T, D, FULL>(a, it, in * kUnit, (in + take) * kUnit, blk + item, lds);
     else
-      part<T, D, FULL, RMAX>(a, it, tl, in * kUnit, (in + take) * kUnit, blk + item, lds);
+      wide_part<T, D, FULL, RW ? RW : 1>(a, it, in * kUnit, (in + take) * kUnit, blk + item, lds);
     u += take;
   }
 }
 
-// Adds a row's parts, one wave a row: lane's columns are lane*D/64 ..
-template <class T, int D>
+constexpr uint32_t kSplitRows = 4096;  // rows up to which a block joins a row
+constexpr uint32_t kAhead = 8;  // parts whose loads a joining wave has in flight
+
+// Adds a row's parts; lane's columns are lane*D/64 .. A row is a wave's, or
+// (SPLIT, for few rows) a block's, whose waves take every fourth part each.
+template <class T, int D, bool SPLIT>
 __global__ void __launch_bounds__(256) join_kernel(AttentionArgs a) {
   constexpr int E = D / 64;
-  const uint32_t lane = threadIdx.x % 64;
-  const uint32_t row = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / 64);
+  constexpr uint32_t WAVES = SPLIT ? 4 : 1;
+  const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const uint32_t row = SPLIT ? blockIdx.x : blockIdx.x * 4 + wave, w0 = SPLIT ? wave : 0;
   if (row >= a.batch * a.queries * a.heads) return;
   const uint32_t tok = row / a.heads, hq = row % a.heads, b = tok / a.queries, head = hq / a.share, g = hq % a.share;
   const uint32_t up = units_of(a.prefix.tokens), prefix_units = a.kv_heads * a.tp.tiles * up;
   uint32_t own_each = 0, own_begin = 0, total = prefix_units;
   if (a.own.tokens) {
     own_each = units_of(own_length(a, b));
-    own_begin = prefix_units + own_units_before(a, b);
-    total += own_units_before(a, a.batch);
+    const OwnLine line = own_line(a, 0);
+    own_begin = prefix_units + own_units_before(a, line, b);
+    total += own_units_before(a, line, a.batch);
   }
   const uint32_t blocks = min(a.blocks, total);
   // the row's parts: over the prefix, then over its own keys
@@ -595,8 +866,9 @@ __global__ void __launch_bounds__(256) join_kernel(AttentionArgs a) {
     slot[1] = first + a.kv_heads * a.tp.tiles + b * a.kv_heads * a.to.tiles + y;
     count[1] = block_of(u + own_each - 1, total, blocks) - first + 1;
   }
-  const uint32_t parts = count[0] + count[1];
-  auto place = [&](uint32_t i) {
+  const uint32_t parts = (count[0] + count[1] + WAVES - 1 - w0) / WAVES;  // of this wave
+  auto place = [&](uint32_t x) {
+    const uint32_t i = x * WAVES + w0;
     return i < count[0] ? (uint64_t)(slot[0] + i) * a.part_rows + at[0]
                         : (uint64_t)(slot[1] + i - count[0]) * a.part_rows + at[1];
   };
@@ -618,11 +890,36 @@ __global__ void __launch_bounds__(256) join_kernel(AttentionArgs a) {
     for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
     l = l * f0 + sum, m = now;
     for (int e = 0; e < E; ++e) o[e] *= f0;
-#pragma unroll 8
-    for (uint32_t i = 0; i < some; ++i) {
-      const float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(uint32_t, fi), i));
-      const float* p = a.part_o + place(i0 + i) * D + lane * E;
-      for (int e = 0; e < E; ++e) o[e] += f * p[e];
+    for (uint32_t i = 0; i < some; i += kAhead) {
+      float p[kAhead][E];  // their loads in flight together; past the last part, it again with weight 0
+#pragma unroll
+      for (uint32_t j = 0; j < kAhead; ++j) {
+        const float* q = a.part_o + place(i0 + min(i + j, some - 1)) * D + lane * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e) p[j][e] = q[e];
+      }
+#pragma unroll
+      for (uint32_t j = 0; j < kAhead; ++j) {
+        const float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(uint32_t, fi), (i + j) % 64));
+        // a part without a key has no output either (it may hold anything's product with 0)
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] += i + j < some && f != 0.0f ? f * p[j][e] : 0.0f;
+      }
+    }
+  }
+  if constexpr (SPLIT) {
+    __shared__ float s_m[4], s_l[4], s_o[4][D];
+    if (lane == 0) s_m[wave] = m, s_l[wave] = l;
+    for (int e = 0; e < E; ++e) s_o[wave][lane * E + e] = o[e];
+    __syncthreads();
+    if (wave != 0) return;
+    m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+    l = 0.0f;
+    for (int e = 0; e < E; ++e) o[e] = 0.0f;
+    for (int w = 0; w < 4; ++w) {
+      const float f = s_m[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(s_m[w] - m);
+      l += f * s_l[w];
+      for (int e = 0; e < E; ++e) o[e] += f != 0.0f ? f * s_o[w][lane * E + e] : 0.0f;
     }
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -664,11 +961,10 @@ __global__ void __launch_bounds__(256) weights_kernel(AttentionArgs a) {
 
 // ------------------------------------------------------------------- host
 
-// Rows a wave and waves side by side for items of `rows` rows.
-static Tiling tiling(uint64_t rows, uint32_t dim) {
+// Items of `rows` rows: narrow up to 16; wide ones take r 16-row tiles a wave.
+static Tiling tiling(uint64_t rows, uint32_t r) {
   Tiling t;
-  t.r = rows > 16 && dim <= 128 ? 2 : 1;
-  t.across = rows <= 16 * t.r ? 1 : rows <= 32 * t.r ? 2 : 4;
+  t.r = rows <= 16 ? 0 : r;
   t.tiles = (uint32_t)((rows + t.rows() - 1) / t.rows());
   return t;
 }
@@ -686,8 +982,8 @@ static hl_status check_kv(const hl_kv& s, uint64_t tokens, uint32_t dim, bool se
     if (x % 8) return HL_EINVAL;
     if (x >= (1ull << 40)) return HL_EUNSUPPORTED;
   }
-  // a step's offsets (32 tokens and a row) stay within 32 bits
-  if (s.k_token >= (1ull << 26) || s.v_token >= (1ull << 26)) return HL_EUNSUPPORTED;
+  // the offsets in bytes within 64 tokens stay within 32 bits
+  if (s.k_token >= (1ull << 25) || s.v_token >= (1ull << 25)) return HL_EUNSUPPORTED;
   (void)dim;
   return HL_OK;
 }
@@ -720,13 +1016,14 @@ static hl_status attention_plan(const hl_attention* h, bool weights, AttentionPl
   a.batch = h->batch, a.queries = h->queries, a.heads = h->heads, a.kv_heads = h->kv_heads, a.dim = h->dim;
   a.share = h->heads / h->kv_heads;
   a.scale2 = h->scale * kLog2e;
-  a.tp = tiling((uint64_t)h->batch * h->queries * a.share, h->dim);
-  a.to = tiling((uint64_t)h->queries * a.share, h->dim);
+  const uint64_t shared_rows = (uint64_t)h->batch * h->queries * a.share, own_rows = (uint64_t)h->queries * a.share;
+  const uint32_t r = std::max(shared_rows, own_rows) > 64 && h->dim <= 128 ? 2 : 1;
+  a.tp = tiling(shared_rows, r), a.to = tiling(own_rows, r);
   const uint64_t items = (uint64_t)h->kv_heads * (a.tp.tiles + (uint64_t)h->batch * a.to.tiles);
   const uint64_t units = (uint64_t)h->kv_heads * ((uint64_t)a.tp.tiles * units_of(a.prefix.tokens) +
                                                   (uint64_t)h->batch * a.to.tiles * units_of(a.own.tokens));
   if (units >= (1ull << 31)) return HL_EUNSUPPORTED;
-  a.blocks = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>((uint64_t)device_cus(), units));
+  a.blocks = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>((uint64_t)device_cus() * 2, units));
   a.part_rows = std::max(a.tp.rows(), a.to.rows());
   const uint32_t held = h->dim <= 64 ? 64 : h->dim <= 128 ? 128 : 256;
   const uint64_t slots = a.blocks + items;
@@ -745,20 +1042,25 @@ static hl_status attention_plan(const hl_attention* h, bool weights, AttentionPl
   return HL_OK;
 }
 
-template <class T, int D, bool FULL, int RMAX>
+template <class T, int D, bool FULL, int RW>
 static hl_status run(const AttentionArgs& a, hipStream_t s) {
-  hl_status st = enqueue(parts_kernel<T, D, FULL, RMAX>, dim3(a.blocks), dim3(kWaves * 64), s, a);
+  hl_status st = enqueue(parts_kernel<T, D, FULL, RW>, dim3(a.blocks), dim3(kThreads), s, a);
   if (st != HL_OK) return st;
   const uint32_t rows = a.batch * a.queries * a.heads;
-  st = enqueue(join_kernel<T, D>, dim3((rows + 3) / 4), dim3(256), s, a);
+  // A block a row while that fills the card: each of the row's parts is a trip
+  // to memory, and few rows have many.
+  st = rows <= kSplitRows ? enqueue(join_kernel<T, D, true>, dim3(rows), dim3(256), s, a)
+                          : enqueue(join_kernel<T, D, false>, dim3((rows + 3) / 4), dim3(256), s, a);
   if (st != HL_OK || !a.scores) return st;
   return enqueue(weights_kernel, dim3((a.own.tokens + 255) / 256, a.kv_heads, a.batch), dim3(256), s, a);
 }
 
 template <class T, int D, bool FULL>
 static hl_status run_rows(const AttentionArgs& a, hipStream_t s) {
+  const uint32_t r = std::max(a.tp.r, a.to.r);
+  if (r == 0) return run<T, D, FULL, 0>(a, s);
   if constexpr (D <= 128) {
-    if (a.tp.r > 1 || a.to.r > 1) return run<T, D, FULL, 2>(a, s);
+    if (r == 2) return run<T, D, FULL, 2>(a, s);
   }
   return run<T, D, FULL, 1>(a, s);
 }

@@ -155,7 +155,7 @@ def test_strides():
 
 
 def test_offsets_past_32_bits():
-    rows, stride = 70, (1 << 26) - 8
+    rows, stride = 70, (1 << 25) - 8
     big = torch.empty(rows * stride + 64, dtype=torch.bfloat16, device="cuda")
     k = big.as_strided((1, rows, 1, 64), (0, stride, 64, 1))
     base = make(torch.bfloat16, 1, 1, 4, 1, 64, 0, rows)

@@ -51,7 +51,7 @@ def attention(**bad):
     (dict(dim=0), hl.HL_EINVAL), (dict(dim=100), hl.HL_EINVAL), (dict(scale=float("nan")), hl.HL_EINVAL),
     (dict(dim=264), hl.HL_EUNSUPPORTED), (dict(own__k_dev=None), hl.HL_EINVAL), (dict(prefix__v_dev=A + 8), hl.HL_EINVAL),
     (dict(own__k_token=132), hl.HL_EINVAL), (dict(own__v_seq=4), hl.HL_EINVAL),
-    (dict(prefix__k_token=1 << 26), hl.HL_EUNSUPPORTED), (dict(prefix__tokens=1 << 30), hl.HL_EUNSUPPORTED),
+    (dict(prefix__k_token=1 << 25), hl.HL_EUNSUPPORTED), (dict(prefix__tokens=1 << 30), hl.HL_EUNSUPPORTED),
     (dict(batch=70000), hl.HL_EUNSUPPORTED), (dict(queries=1 << 25), hl.HL_EUNSUPPORTED)])
 def test_attention_shape(L, bad, status):
     a = attention(**bad)
