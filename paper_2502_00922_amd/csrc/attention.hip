@@ -287,29 +287,33 @@ struct State {
   uint32_t odd;        // whether a value of this lane was taken out of the product
 };
 
-constexpr int kSet = 4;  // output tiles whose values are turned at a time: the operands take 16 registers
+// Output tiles whose values are turned at a time: an operand takes 4 registers.
+constexpr int set_of(int d) { return d == 256 ? 2 : 4; }
 
-// The left operands of output tiles i0 .. i0+kSet-1: values of 8 keys, for the
+// The left operands of output tiles i0 .. i0+SET-1: values of 8 keys, for the
 // columns that the tiles give this lane. All are turned before a product may
 // follow.
-template <int D>
-__device__ inline void turn(u32x4 (&vt)[kSet], const Tile<D>& t, int i0) {
+template <int D, int SET>
+__device__ inline void turn(u32x4 (&vt)[SET], const Tile<D>& t, int i0) {
   using S = Shape<D>;
 #pragma unroll
-  for (int i = i0; i < i0 + kSet; ++i) {
+  for (int i = i0; i < i0 + SET; ++i) {
     const uint32_t sel = i % 2 ? 0x07060302u : 0x05040100u;
     const int h = i / S::VE, j = i % S::VE / 2;
 #pragma unroll
     for (int e = 0; e < 4; ++e) vt[i - i0][e] = __builtin_amdgcn_perm(t.v[2 * e + 1][h][j], t.v[2 * e][h][j], sel);
   }
-  asm volatile("" : "+v"(vt[0]), "+v"(vt[1]), "+v"(vt[2]), "+v"(vt[3]));
+#pragma unroll
+  for (int i = 0; i < SET; ++i) asm volatile("" : "+v"(vt[i]));
   __builtin_amdgcn_sched_barrier(0);
 }
 
 // Ends the products of these operands, which keep their registers until then.
-__device__ inline void turned_end(const u32x4 (&vt)[kSet]) {
+template <int SET>
+__device__ inline void turned_end(const u32x4 (&vt)[SET]) {
   products_end();
-  asm volatile("" ::"v"(vt[0]), "v"(vt[1]), "v"(vt[2]), "v"(vt[3]));
+#pragma unroll
+  for (int i = 0; i < SET; ++i) asm volatile("" ::"v"(vt[i]));
 }
 
 // A pair of values to powers of two that say what each is: 1 for +infinity, 64
@@ -346,11 +350,11 @@ __device__ inline void add_beyond(State<D, R>& st, const Item& it, uint32_t dim,
         sees[rt][e / 2] =
             (key + key_of(c, e) < st.seen[rt] ? one : 0) | (key + key_of(c, e + 1) < st.seen[rt] ? one << 16 : 0);
 #pragma unroll
-    for (int i0 = 0; i0 < Shape<D>::TILES; i0 += kSet) {
-      u32x4 vt[kSet];
-      turn<D>(vt, t, i0);
+    for (int i0 = 0; i0 < Shape<D>::TILES; i0 += set_of(D)) {
+      u32x4 vt[set_of(D)];
+      turn<D, set_of(D)>(vt, t, i0);
 #pragma unroll
-      for (int i = 0; i < kSet; ++i) {
+      for (int i = 0; i < set_of(D); ++i) {
         u32x4 kind;
 #pragma unroll
         for (int e = 0; e < 4; ++e) kind[e] = kinds<T>(vt[i][e]);
@@ -468,14 +472,14 @@ __device__ inline void step(State<D, R>& st, Tile<D>& t, const AttentionArgs& a,
     }
   }
 #pragma unroll
-  for (int i0 = 0; i0 < S::TILES; i0 += kSet) {
-    u32x4 vt[kSet];
-    turn<D>(vt, t, i0);
+  for (int i0 = 0; i0 < S::TILES; i0 += set_of(D)) {
+    u32x4 vt[set_of(D)];
+    turn<D, set_of(D)>(vt, t, i0);
 #pragma unroll
-    for (int i = 0; i < kSet; ++i)
+    for (int i = 0; i < set_of(D); ++i)
 #pragma unroll
       for (int rt = 0; rt < R; ++rt) st.o[rt][i0 + i] = mfma<T>(vt[i], w[rt], st.o[rt][i0 + i]);
-    turned_end(vt);
+    turned_end<set_of(D)>(vt);
   }
 }
 
@@ -621,12 +625,13 @@ __device__ inline uint32_t place(uint32_t row, uint32_t j) {
 
 // 64 lanes' 16 bytes at base + offset (each lane's own) to LDS, one lane's after
 // the other's from `lds` on. Counted by vmcnt alone: the compiler, which would
-// wait for all such loads before any read of LDS, does not see it.
+// wait for all such loads before any read of LDS, does not see it. (M0 holds the
+// LDS address; nothing else here uses it.)
 __device__ inline void load_to_lds(const void* base, uint32_t offset, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 1\n\tglobal_load_lds_dwordx4 %1, %2"
                :
                : "s"(lds), "v"(offset), "s"(base)
-               : "memory", "m0");
+               : "memory");
 }
 
 // Loads of one wave for a buffer, of keys and of values.

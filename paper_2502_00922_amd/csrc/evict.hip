@@ -14,11 +14,11 @@
 
 namespace hl {
 
-constexpr uint32_t kThreads = 1024;
-constexpr uint32_t kEach = 8;                      // weights of a thread in a tile
-constexpr uint32_t kTile = kThreads * kEach;
+constexpr uint32_t kThreads = 1024, kWaves = kThreads / 64;
+constexpr uint32_t kRow = 4 * kThreads;  // weights of a row: four a thread, next to each other
 constexpr uint32_t kBins = 2048;
-constexpr uint32_t kCopies = 4;                    // of the histogram: lanes of a wave often count in one bin
+constexpr uint32_t kCopies = 4;          // of the histogram: lanes of a wave often count in one bin
+constexpr uint32_t kCopy = kBins + 16;   // their distance: a bin's copies are in different banks
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -41,32 +41,60 @@ __device__ inline uint32_t ordered(float w) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// Sum of v over the threads before this one, and over all (`total`). s: LDS,
-// one word a wave; may be used again at once.
-__device__ inline uint64_t before(uint64_t v, uint64_t* s, uint64_t* total) {
-  const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  uint64_t sum = v;
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint64_t o = __shfl_up(sum, d);
-    if (lane >= (uint32_t)d) sum += o;
-  }
-  __syncthreads();
-  if (lane == 63) s[wave] = sum;
-  __syncthreads();
-  uint64_t ahead = 0, all = 0;
-  for (uint32_t i = 0; i < kThreads / 64; ++i) {
-    ahead += i < wave ? s[i] : 0;
-    all += s[i];
-  }
-  *total = all;
-  return ahead + sum - v;
+// The weight that an ordered integer stands for; w[i] itself where two weights
+// have one integer.
+__device__ inline float weight_of(uint32_t key, const float* w, uint32_t i) {
+  if (key == 0 || key == 0x80000000u) return w[i];
+  return __builtin_bit_cast(float, key & 0x80000000u ? key ^ 0x80000000u : ~key);
 }
 
+// Sum over the lanes up to this one. Whole wave; by row shifts and row
+// broadcasts, which take a few cycles where a shuffle through LDS takes a
+// hundred.
+__device__ inline uint32_t scan_lanes(uint32_t v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);  // lane - 1 of a row of 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);  // lane - 2
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);  // lane - 4
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);  // lane - 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // row 0's last to row 1, row 2's to row 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // lane 31 to rows 2 and 3
+  return v;
+}
+
+// A thread's rows of weights as ordered integers: weight x of row r is token
+// base + r*kRow + 4*thread + x. Places from `old` on get 0, the least of all, and
+// stand after every token: as fewer than `old` tokens are to be found, none of
+// these is, and nothing below tells them from tokens.
+template <uint32_t ROWS>
+__device__ inline void load_keys(uint32_t (&key)[ROWS][4], const float* w, uint32_t base, uint32_t old) {
+  const bool wide = (reinterpret_cast<uintptr_t>(w) & 15) == 0;
+  float f[ROWS][4];  // all loads first, so that they are in flight together
+#pragma unroll
+  for (uint32_t r = 0; r < ROWS; ++r) {
+    const uint32_t at = base + r * kRow + 4 * threadIdx.x;
+    if (wide && base + (r + 1) * kRow <= old) {
+      const float4 v = *reinterpret_cast<const float4*>(w + at);
+      f[r][0] = v.x, f[r][1] = v.y, f[r][2] = v.z, f[r][3] = v.w;
+    } else {
+#pragma unroll
+      for (uint32_t x = 0; x < 4; ++x) f[r][x] = at + x < old ? w[at + x] : __builtin_nanf("");
+    }
+  }
+#pragma unroll
+  for (uint32_t r = 0; r < ROWS; ++r)
+#pragma unroll
+    for (uint32_t x = 0; x < 4; ++x) key[r][x] = ordered(f[r][x]);
+}
+
+// ROWS: rows of weights that stay in registers. Longer caches are read again
+// for each digit, ROWS rows at a time.
+template <uint32_t ROWS>
 __global__ void __launch_bounds__(1024) select_kernel(EvictArgs a) {
-  __shared__ uint32_t s_bin[kCopies][kBins];
-  __shared__ uint64_t s_wave[kThreads / 64];
-  __shared__ uint32_t s_digit, s_above, s_in;
-  const uint32_t head = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+  __shared__ uint32_t s_bin[kCopies][kCopy];
+  __shared__ uint32_t s_wave[kWaves], s_digit, s_above, s_in;
+  __shared__ uint32_t s_more[ROWS * kWaves], s_same[ROWS * kWaves];
+  const uint32_t head = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid % 64;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const uint64_t item = (uint64_t)b * a.kv_heads + head;
   const float* w = a.weight + item * a.tokens;
   float* w_out = a.weight_out + item * a.keep;
@@ -82,79 +110,99 @@ __global__ void __launch_bounds__(1024) select_kernel(EvictArgs a) {
     return;
   }
   const uint32_t old = n - a.recent, need = a.keep - a.recent;  // need < old
+  uint32_t key[ROWS][4];
+  const bool held = old <= ROWS * kRow;
+  if (need) load_keys<ROWS>(key, w, 0, old);
   for (uint32_t i = tid; i < a.recent; i += kThreads) {
     slots[need + i] = (int32_t)(old + i);
     w_out[need + i] = w[old + i];
   }
   if (need == 0) return;
-  const bool held = old <= kTile;  // the weights stay in registers
-  uint32_t key[kEach];
-  auto load = [&](uint32_t tile) {
-#pragma unroll
-    for (uint32_t j = 0; j < kEach; ++j) {
-      const uint32_t i = tile + tid * kEach + j;
-      key[j] = i < old ? ordered(w[i]) : 0;
-    }
-  };
   // The digits, from the highest, of the last weight kept: `prefix` has those
   // found, `left` counts the tokens still to take among the weights that begin
   // with it, `shift` is what of a weight is not compared yet.
   uint32_t prefix = 0, left = need, shift = 32;
-  const uint32_t widths[3] = {11, 11, 10};
   for (int pass = 0; pass < 3; ++pass) {
-    const uint32_t width = widths[pass], bins = 1u << width;
-    for (uint32_t i = tid; i < kCopies * kBins; i += kThreads) (&s_bin[0][0])[i] = 0;
+    const uint32_t width = pass < 2 ? 11 : 10, bins = 1u << width;
+    for (uint32_t i = tid; i < kCopies * kCopy; i += kThreads) (&s_bin[0][0])[i] = 0;
     __syncthreads();
-    for (uint32_t tile = 0; tile < old; tile += kTile) {
-      if (!held || pass == 0) load(tile);
+    for (uint32_t base = 0; base < old; base += ROWS * kRow) {
+      if (!held) load_keys<ROWS>(key, w, base, old);
 #pragma unroll
-      for (uint32_t j = 0; j < kEach; ++j)
-        if (tile + tid * kEach + j < old && (pass == 0 || key[j] >> shift == prefix))
-          atomicAdd(&s_bin[tid % kCopies][(key[j] >> (shift - width)) & (bins - 1)], 1u);
+      for (uint32_t r = 0; r < ROWS; ++r) {
+        if (base + r * kRow >= old) break;
+#pragma unroll
+        for (uint32_t x = 0; x < 4; ++x)
+          if (pass == 0 || key[r][x] >> shift == prefix)
+            atomicAdd(&s_bin[tid % kCopies][(key[r][x] >> (shift - width)) & (bins - 1)], 1u);
+      }
     }
     __syncthreads();
-    // thread t has bins 2t' and 2t'+1 counted from the highest; the counts
-    // above them say which bin the last token kept is in
+    // thread t has bins 2t and 2t+1 counted from the highest; the counts above
+    // them say which bin the last token kept is in
     uint32_t high = 0, low = 0;
     const uint32_t at = bins - 2 - 2 * tid;
     if (2 * tid < bins)
       for (uint32_t c = 0; c < kCopies; ++c) high += s_bin[c][at + 1], low += s_bin[c][at];
-    uint64_t all;
-    const uint32_t above = (uint32_t)before(high + low, s_wave, &all);
+    const uint32_t sum = scan_lanes(high + low);
+    if (lane == 63) s_wave[wave] = sum;
+    __syncthreads();
+    const uint32_t waves = scan_lanes(lane < kWaves ? s_wave[lane] : 0);
+    const uint32_t above = sum - high - low + (wave ? __builtin_amdgcn_readlane(waves, wave - 1) : 0);
     if (above < left && left <= above + high) s_digit = at + 1, s_above = above, s_in = high;
     if (above + high < left && left <= above + high + low) s_digit = at, s_above = above + high, s_in = low;
     __syncthreads();
     prefix = prefix << width | s_digit;
     left -= s_above;
     shift -= width;
-    const bool whole = s_in == left;  // all that begin so are kept: lower digits do not matter
-    __syncthreads();
-    if (whole) break;
+    if (s_in == left) break;  // all that begin so are kept: lower digits do not matter
   }
-  // Kept: the first digits above `prefix`, and the first `left` tokens equal to it.
-  uint64_t base = 0;  // of earlier tiles: tokens above, and equal (high word)
-  for (uint32_t tile = 0; tile < old; tile += kTile) {
-    if (!held) load(tile);
-    uint64_t mine = 0;
+  // Kept: the first digits above `prefix`, and the first `left` tokens equal to
+  // it. Each token's place is the number of kept ones before it.
+  uint32_t more0 = 0, same0 = 0;  // of earlier rows
+  for (uint32_t base = 0; base < old; base += ROWS * kRow) {
+    if (!held) load_keys<ROWS>(key, w, base, old);
+    uint32_t ahead[ROWS];  // above and equal (high half) in this row and wave before this thread
+    __syncthreads();
 #pragma unroll
-    for (uint32_t j = 0; j < kEach; ++j) {
-      if (tile + tid * kEach + j >= old) continue;
-      const uint32_t d = key[j] >> shift;
-      mine += d > prefix ? 1u : d == prefix ? 1ull << 32 : 0u;
-    }
-    uint64_t all, at = base + before(mine, s_wave, &all);
-    base += all;
+    for (uint32_t r = 0; r < ROWS; ++r) {
+      uint32_t mine = 0;
 #pragma unroll
-    for (uint32_t j = 0; j < kEach; ++j) {
-      const uint32_t i = tile + tid * kEach + j;
-      if (i >= old) continue;
-      const uint32_t d = key[j] >> shift, more = (uint32_t)at, same = (uint32_t)(at >> 32);
-      if (d > prefix || (d == prefix && same < left)) {
-        const uint32_t to = more + min(same, left);
-        slots[to] = (int32_t)i;
-        w_out[to] = w[i];
+      for (uint32_t x = 0; x < 4; ++x) {
+        const uint32_t d = key[r][x] >> shift;
+        mine += d > prefix ? 1u : d == prefix ? 1u << 16 : 0u;
       }
-      at += d > prefix ? 1u : d == prefix ? 1ull << 32 : 0u;
+      const uint32_t sum = scan_lanes(mine);
+      ahead[r] = sum - mine;
+      if (lane == 63) s_more[r * kWaves + wave] = sum & 0xFFFF, s_same[r * kWaves + wave] = sum >> 16;
+    }
+    __syncthreads();
+    if (wave == 0) {
+      uint32_t more = more0, same = same0;
+      for (uint32_t i = 0; i < ROWS * kWaves; i += 64) {
+        const bool in = i + lane < ROWS * kWaves;
+        const uint32_t m = in ? s_more[i + lane] : 0, e = in ? s_same[i + lane] : 0;
+        const uint32_t ms = scan_lanes(m), es = scan_lanes(e);
+        if (in) s_more[i + lane] = more + ms - m, s_same[i + lane] = same + es - e;
+        more += __builtin_amdgcn_readlane(ms, 63), same += __builtin_amdgcn_readlane(es, 63);
+      }
+      if (lane == 0) s_above = more, s_in = same;
+    }
+    __syncthreads();
+    more0 = s_above, same0 = s_in;
+#pragma unroll
+    for (uint32_t r = 0; r < ROWS; ++r) {
+      uint32_t more = s_more[r * kWaves + wave] + (ahead[r] & 0xFFFF), same = s_same[r * kWaves + wave] + (ahead[r] >> 16);
+#pragma unroll
+      for (uint32_t x = 0; x < 4; ++x) {
+        const uint32_t i = base + r * kRow + 4 * tid + x, d = key[r][x] >> shift;
+        if (d > prefix || (d == prefix && same < left)) {
+          const uint32_t to = more + min(same, left);
+          slots[to] = (int32_t)i;
+          w_out[to] = weight_of(key[r][x], w, i);
+        }
+        more += d > prefix, same += d == prefix;
+      }
     }
   }
 }
@@ -243,7 +291,10 @@ extern "C" hl_status hl_cache_evict(const hl_kv* from, const hl_kv* to, uint32_t
   a.batch = batch, a.kv_heads = kv_heads, a.dim = dim, a.tokens = (uint32_t)from->tokens;
   a.keep = (uint32_t)keep, a.recent = (uint32_t)recent;
   const hipStream_t s = (hipStream_t)stream;
-  st = enqueue(select_kernel, dim3(kv_heads, batch), dim3(kThreads), s, a);
+  const dim3 items(kv_heads, batch), threads(kThreads);
+  st = from->tokens <= kRow ? enqueue(select_kernel<1>, items, threads, s, a)
+       : from->tokens <= 4 * kRow ? enqueue(select_kernel<4>, items, threads, s, a)
+                                  : enqueue(select_kernel<16>, items, threads, s, a);
   if (st != HL_OK) return st;
   return enqueue(move_kernel, dim3((uint32_t)blocks, batch), dim3(256), s, a);
 }

@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import struct
 from typing import NamedTuple, Optional
 
 import numpy as np
@@ -162,12 +163,12 @@ def lib() -> ctypes.CDLL:
     L.hl_rms_norm.argtypes = [c.c_void_p, c.c_int, c.c_void_p, c.c_int, c.c_void_p, c.c_int, c.c_uint64, c.c_uint64,
                               c.c_float, c.c_void_p, c.c_void_p, c.c_int, c.c_uint32, c.c_void_p, c.c_void_p]
     L.hl_attention_workspace_bytes.restype = c.c_size_t
-    L.hl_attention_workspace_bytes.argtypes = [c.POINTER(AttentionShape), c.c_int]
+    L.hl_attention_workspace_bytes.argtypes = [c.c_void_p, c.c_int]
     L.hl_prefix_attention.restype = c.c_int
-    L.hl_prefix_attention.argtypes = [c.POINTER(AttentionShape), c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p,
+    L.hl_prefix_attention.argtypes = [c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p,
                                       c.c_void_p, c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p]
     L.hl_cache_evict.restype = c.c_int
-    L.hl_cache_evict.argtypes = [c.POINTER(KeysValues), c.POINTER(KeysValues), c.c_uint32, c.c_uint32, c.c_uint32,
+    L.hl_cache_evict.argtypes = [c.c_void_p, c.c_void_p, c.c_uint32, c.c_uint32, c.c_uint32,
                                  c.c_void_p, c.c_void_p, c.c_uint64, c.c_uint64, c.c_void_p, c.c_void_p, c.c_void_p,
                                  c.c_void_p]
     _lib = L
@@ -527,6 +528,18 @@ def _value_types():
     return _VALUE_TYPES
 
 
+def _plain(device: int, bufs) -> None:
+    """Every given buffer is contiguous and on this GPU (get_device's number), else ValueError. A call's checks go
+    through here only to say what is wrong: the call itself asks the same in one expression."""
+    for name, t in bufs.items():
+        if t is None:
+            continue
+        if t.get_device() != device or not t.is_cuda:
+            raise ValueError(f"{name} must be on GPU {device}, not {t.device}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+
+
 def rms_norm(x, weight, residual=None, eps: float = 1e-5, out_dtype=None, group: int = 0, out=None, sum_out=None,
              scale_out=None, stream=None) -> NormResult:
     """t = x + residual; out = t / sqrt(mean(t^2) + eps) * weight over the last dimension.
@@ -537,76 +550,87 @@ def rms_norm(x, weight, residual=None, eps: float = 1e-5, out_dtype=None, group:
     for each row. Outputs that are not given are allocated."""
     import torch
     types = _value_types()
-    hidden = weight.shape[0] if weight.dim() == 1 else -1
-    if x.dim() < 1 or x.shape[-1] != hidden or hidden < 1 or x.numel() < 1:
-        raise ValueError(f"x must be [..., hidden] and weight [hidden], got {tuple(x.shape)} and {tuple(weight.shape)}")
-    e4m3 = torch.float8_e4m3fn
-    ot = out.dtype if out is not None and out_dtype is None else out_dtype or weight.dtype
+    shape, dev = x.shape, x.get_device()
+    if weight.dim() != 1 or not shape or shape[-1] != weight.shape[0] or x.numel() == 0:
+        raise ValueError(f"x must be [..., hidden] and weight [hidden], got {tuple(shape)} and {tuple(weight.shape)}")
+    hidden = shape[-1]
+    ot = out_dtype if out_dtype is not None else weight.dtype if out is None else out.dtype
     xt, wt, oc = types.get(x.dtype), types.get(weight.dtype), types.get(ot)
     if xt is None or wt is None or oc is None or xt == HL_E4M3 or wt == HL_E4M3:
         raise ValueError("x and weight must be float32, bfloat16 or float16; out these or float8_e4m3fn")
-    shape, tokens, dev = x.shape, x.numel() // hidden, x.device
     if out is None:
-        out = torch.empty(shape, dtype=ot, device=dev)
-    bufs = {"x": x, "weight": weight, "out": out}
-    rt = HL_F32
+        out = torch.empty_like(x, dtype=ot) if x.dtype != ot else torch.empty_like(x)
+    elif out.dtype != ot or out.shape != shape:
+        raise ValueError(f"out must be {tuple(shape)} of {ot}")
+    good = dev >= 0 and x.is_contiguous() and weight.is_contiguous() and weight.get_device() == dev \
+        and out.is_contiguous() and out.get_device() == dev
+    rt, r_ptr, s_ptr, scale_ptr = HL_F32, None, None, None
     if residual is not None:
         rt = types.get(residual.dtype)
         if rt is None or rt == HL_E4M3 or residual.shape != shape:
             raise ValueError(f"residual must have x's shape {tuple(shape)} and be float32, bfloat16 or float16")
         if sum_out is None:
-            sum_out = torch.empty(shape, dtype=residual.dtype, device=dev)
+            sum_out = torch.empty_like(residual)
         elif sum_out.dtype != residual.dtype or sum_out.shape != shape:
             raise ValueError("sum_out must have residual's shape and type")
-        bufs["residual"], bufs["sum_out"] = residual, sum_out
+        good = good and residual.is_contiguous() and residual.get_device() == dev and sum_out.is_contiguous() \
+            and sum_out.get_device() == dev
+        r_ptr, s_ptr = residual.data_ptr(), sum_out.data_ptr()
     elif sum_out is not None:
         raise ValueError("sum_out needs a residual")
-    if out.dtype != ot or out.shape != shape:
-        raise ValueError(f"out must be {tuple(shape)} of {ot}")
     if oc == HL_E4M3:
         if group not in (0, 32, 64, 128) or (group and hidden % group):
             raise ValueError("group must be 0, or 32, 64 or 128 and divide hidden")
         need = (*shape[:-1], hidden // group) if group else tuple(shape[:-1])
         if scale_out is None:
-            scale_out = torch.empty(need, dtype=torch.float32, device=dev)
+            scale_out = torch.empty(need, dtype=torch.float32, device=x.device)
         elif scale_out.dtype != torch.float32 or tuple(scale_out.shape) != tuple(need):
             raise ValueError(f"scale_out must be float32 {tuple(need)}")
-        bufs["scale_out"] = scale_out
+        good = good and scale_out.is_contiguous() and scale_out.get_device() == dev
+        scale_ptr = scale_out.data_ptr()
     elif group or scale_out is not None:
         raise ValueError("group and scale_out need an 8-bit out")
-    for name, t in bufs.items():
-        if not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
-        if t.device != dev or not t.is_cuda:
-            raise ValueError(f"{name} must be on {dev}, a GPU, not {t.device}")
-    has = residual is not None
-    _check(lib().hl_rms_norm(x.data_ptr(), xt, residual.data_ptr() if has else None, rt, weight.data_ptr(), wt,
-                             tokens, hidden, eps, sum_out.data_ptr() if has else None, out.data_ptr(), oc, group,
-                             scale_out.data_ptr() if oc == HL_E4M3 else None, _stream_ptr(stream)), "hl_rms_norm")
+    if not good:
+        _plain(dev, {"x": x, "weight": weight, "out": out, "residual": residual, "sum_out": sum_out,
+                     "scale_out": scale_out})
+    s = lib().hl_rms_norm(x.data_ptr(), xt, r_ptr, rt, weight.data_ptr(), wt, x.numel() // hidden, hidden, eps, s_ptr,
+                          out.data_ptr(), oc, group, scale_ptr, _stream_ptr(stream))
+    if s:
+        _check(s, "hl_rms_norm")
     return NormResult(out, sum_out, scale_out)
 
 
-def _keys_values(k, v, name: str, dims: int, dtype, device):
-    """hl_kv of keys and values [(sequence,) token, key head, column] with any strides but columns in a row."""
+def _keys_values(k, v, name: str, dims: int, dtype, device: int):
+    """The fields of hl_kv for keys and values [(sequence,) token, key head, column] with any strides but columns in a
+    row."""
     if k is None or v is None or k.dim() != dims or v.shape != k.shape:
         raise ValueError(f"{name}: keys and values of one shape, {dims} dimensions")
     if k.dtype != dtype or v.dtype != dtype:
         raise ValueError(f"{name}: dtype {k.dtype} and {v.dtype}, expected {dtype}")
-    if k.device != device or v.device != device or not k.is_cuda:
-        raise ValueError(f"{name} must be on {device}, a GPU, not {k.device} and {v.device}")
+    if k.get_device() != device or v.get_device() != device or device < 0:
+        raise ValueError(f"{name} must be on GPU {device}, not {k.device} and {v.device}")
     ks, vs = k.stride(), v.stride()
     if (ks[-1] != 1 or vs[-1] != 1) and k.shape[-1] > 1:
         raise ValueError(f"{name}: the columns of a head must lie next to each other")
-    return KeysValues(k.data_ptr(), v.data_ptr(), k.shape[-3], ks[0] if dims == 4 else 0, ks[-3], ks[-2],
-                      vs[0] if dims == 4 else 0, vs[-3], vs[-2])
+    if dims == 3:
+        return (k.data_ptr(), v.data_ptr(), k.shape[0], 0, ks[0], ks[1], 0, vs[0], vs[1])
+    return (k.data_ptr(), v.data_ptr(), k.shape[1], *ks[:3], *vs[:3])
 
 
-def _small(t, name: str, dtype, shape, device):
+def _small(t, name: str, dtype, shape, device: int):
     """A contiguous buffer of this type, shape and device (else ValueError)."""
-    _dev_arg(t, name, (dtype,), shape)
-    if t.device != device:
-        raise ValueError(f"{name} must be on {device}, not {t.device}")
+    import torch
+    if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.shape == shape and t.is_contiguous()
+            and t.get_device() == device):
+        _dev_arg(t, name, (dtype,), shape)
+        raise ValueError(f"{name} must be on GPU {device}, not {t.device}")
     return t
+
+
+_NO_KV = (0,) * 9
+# hl_attention and hl_kv as bytes: filling them field by field takes longer than a small call's kernels
+_ATTENTION = struct.Struct("=i5If4x18Q")
+_KV = struct.Struct("=9Q")
 
 
 def prefix_attention(q, k=None, v=None, lens=None, prefix_k=None, prefix_v=None, scale: Optional[float] = None,
@@ -622,33 +646,31 @@ def prefix_attention(q, k=None, v=None, lens=None, prefix_k=None, prefix_v=None,
 
     ``weights`` (float32 [batch, kv_heads, capacity]) or ``weights_out``: also gives the weights plus what each own
     key was given by this call (``weights_out`` may be ``weights``; without ``weights``, plus zeros). ``lse``: a
-    float32 [batch, queries, heads] buffer for the logarithms of the softmax sums. ``workspace``: a uint8 buffer of
-    attention_workspace's size; allocated where it is not given."""
+    float32 [batch, queries, heads] buffer for the logarithms of the softmax sums. ``workspace``: a device buffer of
+    hl_attention_workspace_bytes; allocated where it is not given."""
     import torch
     if q.dim() != 4 or q.dtype not in (torch.bfloat16, torch.float16):
         raise ValueError("q must be [batch, queries, heads, dim] bfloat16 or float16")
     batch, queries, heads, dim = q.shape
-    dev = q.device
-    if not q.is_cuda or not q.is_contiguous():
+    dev = q.get_device()
+    if dev < 0 or not q.is_contiguous():
         raise ValueError("q must be contiguous and on the GPU")
-    a = AttentionShape(HL_BF16 if q.dtype == torch.bfloat16 else HL_F16, batch, queries, heads, 0, dim,
-                       1.0 / math.sqrt(dim) if scale is None else scale)
-    kv_heads = None
+    own = prefix = _NO_KV
+    kv_heads = lens_ptr = w_ptr = w_out_ptr = lse_ptr = None
     if k is not None or v is not None:
-        a.own = _keys_values(k, v, "k, v", 4, q.dtype, dev)
+        own = _keys_values(k, v, "k, v", 4, q.dtype, dev)
         kv_heads = k.shape[2]
         if k.shape[0] != batch or k.shape[3] != dim:
             raise ValueError(f"k, v must be [{batch}, capacity, kv_heads, {dim}], got {tuple(k.shape)}")
-        _small(lens, "lens", torch.int32, (batch,), dev)
+        lens_ptr = _small(lens, "lens", torch.int32, (batch,), dev).data_ptr()
     if prefix_k is not None or prefix_v is not None:
-        a.prefix = _keys_values(prefix_k, prefix_v, "prefix_k, prefix_v", 3, q.dtype, dev)
-        if prefix_k.shape[2] != dim or kv_heads not in (None, prefix_k.shape[1]):
+        prefix = _keys_values(prefix_k, prefix_v, "prefix_k, prefix_v", 3, q.dtype, dev)
+        if prefix_k.shape[2] != dim or (kv_heads is not None and kv_heads != prefix_k.shape[1]):
             raise ValueError(f"prefix_k, prefix_v must be [length, kv_heads, {dim}] with the own caches' kv_heads, "
                              f"got {tuple(prefix_k.shape)}")
         kv_heads = prefix_k.shape[1]
     if not kv_heads or heads % kv_heads:
         raise ValueError("a prefix or own caches are needed, with kv_heads that divide heads")
-    a.kv_heads = kv_heads
     if out is None:
         out = torch.empty_like(q)
     else:
@@ -658,26 +680,27 @@ def prefix_attention(q, k=None, v=None, lens=None, prefix_k=None, prefix_v=None,
             raise ValueError("weights are of the own caches' keys")
         need = (batch, kv_heads, k.shape[1])
         if weights is not None:
-            _small(weights, "weights", torch.float32, need, dev)
+            w_ptr = _small(weights, "weights", torch.float32, need, dev).data_ptr()
         if weights_out is None:
-            weights_out = torch.empty(need, dtype=torch.float32, device=dev)
+            weights_out = torch.empty(need, dtype=torch.float32, device=q.device)
         else:
             _small(weights_out, "weights_out", torch.float32, need, dev)
+        w_out_ptr = weights_out.data_ptr()
     if lse is not None:
-        _small(lse, "lse", torch.float32, (batch, queries, heads), dev)
+        lse_ptr = _small(lse, "lse", torch.float32, (batch, queries, heads), dev).data_ptr()
+    a = _ATTENTION.pack(HL_BF16 if q.dtype == torch.bfloat16 else HL_F16, batch, queries, heads, kv_heads, dim,
+                        1.0 / math.sqrt(dim) if scale is None else scale, *prefix, *own)
     L = lib()
     if workspace is None:
-        workspace = torch.empty(L.hl_attention_workspace_bytes(ctypes.byref(a), weights_out is not None),
-                                dtype=torch.uint8, device=dev)
+        workspace = torch.empty(L.hl_attention_workspace_bytes(a, w_out_ptr is not None), dtype=torch.uint8,
+                                device=q.device)
     else:
         _dev_arg(workspace, "workspace")
-        _on_device(dev, workspace=workspace)
-    _check(L.hl_prefix_attention(ctypes.byref(a), q.data_ptr(), lens.data_ptr() if k is not None else None,
-                                 out.data_ptr(), lse.data_ptr() if lse is not None else None,
-                                 weights.data_ptr() if weights is not None else None,
-                                 weights_out.data_ptr() if weights_out is not None else None, workspace.data_ptr(),
-                                 workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
-           "hl_prefix_attention")
+        _on_device(q.device, workspace=workspace)
+    s = L.hl_prefix_attention(a, q.data_ptr(), lens_ptr, out.data_ptr(), lse_ptr, w_ptr, w_out_ptr,
+                              workspace.data_ptr(), workspace.nbytes, _stream_ptr(stream))
+    if s:
+        _check(s, "hl_prefix_attention")
     return AttentionResult(out, weights_out, lse)
 
 
@@ -693,22 +716,23 @@ def cache_evict(k, v, weights, lens, keep: int, recent: int = 0, k_out=None, v_o
     if k.dim() != 4 or k.dtype not in (torch.bfloat16, torch.float16, torch.int16):
         raise ValueError("k must be [batch, capacity, kv_heads, dim] bfloat16, float16 or int16")
     batch, capacity, heads, dim = k.shape
-    dev = k.device
+    dev = k.get_device()
     src = _keys_values(k, v, "k, v", 4, k.dtype, dev)
     if keep < 1 or not 0 <= recent <= keep:
         raise ValueError("keep must be at least 1 and recent between 0 and keep")
     _small(weights, "weights", torch.float32, (batch, heads, capacity), dev)
     _small(lens, "lens", torch.int32, (batch,), dev)
     if k_out is None and v_out is None:
-        k_out = torch.empty((batch, keep, heads, dim), dtype=k.dtype, device=dev)
+        k_out = k.new_empty((batch, keep, heads, dim))
         v_out = torch.empty_like(k_out)
     dst = _keys_values(k_out, v_out, "k_out, v_out", 4, k.dtype, dev)
-    if (k_out.shape[0], *k_out.shape[2:]) != (batch, heads, dim) or k_out.shape[1] < keep:
+    if k_out.shape[0] != batch or k_out.shape[2] != heads or k_out.shape[3] != dim or k_out.shape[1] < keep:
         raise ValueError(f"k_out must be [{batch}, at least {keep}, {heads}, {dim}], got {tuple(k_out.shape)}")
-    w_out = torch.empty((batch, heads, keep), dtype=torch.float32, device=dev)
-    slots = torch.empty((batch, heads, keep), dtype=torch.int32, device=dev)
+    w_out = weights.new_empty((batch, heads, keep))
+    slots = lens.new_empty((batch, heads, keep))
     lens_out = torch.empty_like(lens)
-    _check(lib().hl_cache_evict(ctypes.byref(src), ctypes.byref(dst), batch, heads, dim, weights.data_ptr(),
-                                lens.data_ptr(), keep, recent, w_out.data_ptr(), slots.data_ptr(),
-                                lens_out.data_ptr(), _stream_ptr(stream)), "hl_cache_evict")
+    s = lib().hl_cache_evict(_KV.pack(*src), _KV.pack(*dst), batch, heads, dim, weights.data_ptr(), lens.data_ptr(), keep,
+                             recent, w_out.data_ptr(), slots.data_ptr(), lens_out.data_ptr(), _stream_ptr(stream))
+    if s:
+        _check(s, "hl_cache_evict")
     return EvictResult(k_out, v_out, w_out, lens_out, slots)

@@ -93,6 +93,14 @@ def test_evict(L, bad, status):
         assert L.hl_cache_evict(*{**good, "src": None}.values(), None) == hl.HL_EINVAL
 
 
+def test_packed_structures():
+    # the bytes that the binding packs are the structures' own
+    kv = hl.KeysValues(*range(1, 10))
+    assert hl._KV.pack(*range(1, 10)) == bytes(kv)
+    a = hl.AttentionShape(hl.HL_F16, 2, 3, 4, 5, 6, 0.25, kv, hl.KeysValues(*range(11, 20)))
+    assert hl._ATTENTION.pack(hl.HL_F16, 2, 3, 4, 5, 6, 0.25, *range(1, 10), *range(11, 20)) == bytes(a)
+
+
 def test_registers(tmp_path):
     # every code object of the library, not the first alone
     fat = str(tmp_path / "fat")
