@@ -532,20 +532,15 @@ __device__ inline float over_lanes(float l) {
   return l + __shfl_xor(l, 32);
 }
 
-// Keys [k0, k1) of a narrow item by one block; writes the part at `slot`.
+// A wave's share of a narrow item's keys [.., k1): 32 from `key` on, and again
+// every `stride`.
 template <class T, int D, bool FULL>
-__device__ inline void narrow_part(const AttentionArgs& a, const Item& it, uint32_t k0, uint32_t k1, uint32_t slot,
-                                   float* lds) {
-  using S = Shape<D>;
-  const uint32_t lane = lane_id(), n = lane % 16, c = lane / 16;
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  State<D, 1> st;
-  begin<D, FULL, 1>(st, a, it, it.row0);
+__device__ inline void narrow_keys(State<D, 1>& st, const AttentionArgs& a, const Item& it, uint32_t key, uint32_t k1,
+                                   uint32_t stride) {
   const uint32_t all = seen_by(a, it, it.row0), most = seen_by(a, it, it.row0 + 15), end = min(k1, most);
-  uint32_t key = k0 + kStep * wave;
   const uint32_t whole = min(end, all);  // steps that end here or before hide no key
   if constexpr (D == 256) {  // two steps' keys do not fit the registers
-    for (; key + kStep <= whole; key += kUnit) {
+    for (; key + kStep <= whole; key += stride) {
       Tile<D> t;
       step<T, D, 1, false>(st, t, a, it, key, most, it.row0, load_k<D, FULL, false>, load_v<D, FULL, false>);
     }
@@ -558,27 +553,36 @@ __device__ inline void narrow_part(const AttentionArgs& a, const Item& it, uint3
     Tile<D> t0, t1;
     load(t0, key);
     while (true) {
-      bool more = key + kUnit + kStep <= whole;
-      if (more) load(t1, key + kUnit);
+      bool more = key + stride + kStep <= whole;
+      if (more) load(t1, key + stride);
       step<T, D, 1, false>(st, t0, a, it, key, most, it.row0, there, there);
-      key += kUnit;
+      key += stride;
       if (!more) break;
-      more = key + kUnit + kStep <= whole;
-      if (more) load(t0, key + kUnit);
+      more = key + stride + kStep <= whole;
+      if (more) load(t0, key + stride);
       step<T, D, 1, false>(st, t1, a, it, key, most, it.row0, there, there);
-      key += kUnit;
+      key += stride;
       if (!more) break;
     }
   }
   const uint32_t edge = key;
 #pragma unroll 1
-  for (; key < end; key += kUnit) {
+  for (; key < end; key += stride) {
     Tile<D> t;
     step<T, D, 1, true>(st, t, a, it, key, most, it.row0, load_k<D, FULL, true>, load_v<D, FULL, true>);
   }
-  if (__any(st.odd != 0)) add_beyond<T, D, FULL, 1>(st, it, a.dim, edge, end, kUnit);
-  // add the four waves' results
-  float* lds_ml = lds + kWaves * 16 * (D + 4);
+  if (__any(st.odd != 0)) add_beyond<T, D, FULL, 1>(st, it, a.dim, edge, end, stride);
+  st.odd = 0;
+}
+
+// Adds the results that WAVES waves have of the same 16 rows and calls
+// out(row, d, o, m, l) for four columns from d on of each of the first `rows`.
+template <int D, int WAVES, class Out>
+__device__ inline void add_waves(const State<D, 1>& st, uint32_t rows, float* lds, Out out) {
+  using S = Shape<D>;
+  const uint32_t lane = lane_id(), n = lane % 16, c = lane / 16;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  float* lds_ml = lds + WAVES * 16 * (D + 4);
   const float sum = over_lanes(st.l[0]);
   const uint32_t at = here(wave * 16 + n);  // formed here: no register holds it through the loops
   if (c == 0) lds_ml[2 * at] = st.some[0] || sum != sum ? st.m[0] : -INFINITY, lds_ml[2 * at + 1] = sum;
@@ -593,15 +597,12 @@ __device__ inline void narrow_part(const AttentionArgs& a, const Item& it, uint3
             make_float4(st.o[0][i][r], st.o[0][i + 1][r], st.o[0][i + 2][r], st.o[0][i + 3][r]);
       }
   __syncthreads();
-  const uint32_t rows = min(16u, it.rows - it.row0);
-  float* po = a.part_o + (uint64_t)slot * a.part_rows * D;
-  float* pml = a.part_ml + (uint64_t)slot * a.part_rows * 2;
-  for (uint32_t x = here(threadIdx.x); x < rows * (D / 4); x += kThreads) {
+  for (uint32_t x = here(threadIdx.x); x < rows * (D / 4); x += WAVES * 64) {
     const uint32_t row = x / (D / 4), d = x % (D / 4) * 4;
     float m = -INFINITY, l = 0.0f;
-    for (uint32_t k = 0; k < kWaves; ++k) m = fmaxf(m, lds_ml[2 * (row + 16 * k)]);
+    for (uint32_t k = 0; k < WAVES; ++k) m = fmaxf(m, lds_ml[2 * (row + 16 * k)]);
     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (uint32_t k = 0; k < kWaves; ++k) {
+    for (uint32_t k = 0; k < WAVES; ++k) {
       const uint32_t from = row + 16 * k;
       const float mk = lds_ml[2 * from];
       const float f = mk == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mk - m);
@@ -609,9 +610,25 @@ __device__ inline void narrow_part(const AttentionArgs& a, const Item& it, uint3
       o.x += f * v.x, o.y += f * v.y, o.z += f * v.z, o.w += f * v.w;
       l += f * lds_ml[2 * from + 1];
     }
-    *reinterpret_cast<float4*>(po + (uint64_t)row * D + d) = o;
-    if (d == 0) pml[2 * row] = m, pml[2 * row + 1] = l;
+    out(row, d, o, m, l);
   }
+}
+
+// Keys [k0, k1) of a narrow item by one block; writes the part at `slot`.
+template <class T, int D, bool FULL>
+__device__ inline void narrow_part(const AttentionArgs& a, const Item& it, uint32_t k0, uint32_t k1, uint32_t slot,
+                                   float* lds) {
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  State<D, 1> st;
+  begin<D, FULL, 1>(st, a, it, it.row0);
+  narrow_keys<T, D, FULL>(st, a, it, k0 + kStep * wave, k1, kUnit);
+  float* po = a.part_o + (uint64_t)slot * a.part_rows * D;
+  float* pml = a.part_ml + (uint64_t)slot * a.part_rows * 2;
+  add_waves<D, kWaves>(st, min(16u, it.rows - it.row0), lds,
+                       [&](uint32_t row, uint32_t d, float4 o, float m, float l) {
+                         *reinterpret_cast<float4*>(po + (uint64_t)row * D + d) = o;
+                         if (d == 0) pml[2 * row] = m, pml[2 * row + 1] = l;
+                       });
   __syncthreads();
 }
 
@@ -700,9 +717,10 @@ __device__ inline void wide_part(const AttentionArgs& a, const Item& it, uint32_
   begin<D, FULL, R>(st, a, it, wave_row);
   // Steps begin at multiples of 16 rows, so which banks a lane's pieces are in
   // does not depend on the step.
-  uint32_t kofs[S::KS], vofs[4];
+  constexpr int KD = S::KS < 4 ? S::KS : 4;  // of 256 columns, the second half is 16 pieces on
+  uint32_t kofs[KD], vofs[4];
 #pragma unroll
-  for (int s = 0; s < S::KS; ++s) kofs[s] = n * D * 2 + place<D>(n, c + 4 * s) * 16;
+  for (int s = 0; s < KD; ++s) kofs[s] = n * D * 2 + place<D>(n, c + 4 * s) * 16;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
     vofs[e] = bytes / 2 + (4 * c + e) * D * 2 + place<D>(4 * c + e, n * S::VE / 8) * 16 + (S::VE == 4 ? n % 2 * 8 : 0);
@@ -712,7 +730,7 @@ __device__ inline void wide_part(const AttentionArgs& a, const Item& it, uint32_
     for (int s = 0; s < S::KS; ++s)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(from + kofs[s] + h * 16 * D * 2);
+        const u32x4 w = *reinterpret_cast<const u32x4*>(from + kofs[s % KD] + s / KD * 256 + h * 16 * D * 2);
         t.k[h][s] = FULL || c * 8 + s * 32 < dim ? w : u32x4{0, 0, 0, 0};
       }
   };
@@ -787,6 +805,30 @@ __device__ inline uint32_t line_block(uint32_t blocks) {
   return blocks % 8 ? blockIdx.x : blockIdx.x % 8 * (blocks / 8) + blockIdx.x / 8;
 }
 
+// A head's rows of the whole batch over the prefix, from row0 on.
+__device__ inline Item prefix_item(const AttentionArgs& a, uint32_t head, uint32_t row0) {
+  Item it;
+  it.k = a.prefix.k + head * a.prefix.k_head, it.v = a.prefix.v + head * a.prefix.v_head;
+  it.k_token = a.prefix.k_token, it.v_token = a.prefix.v_token;
+  it.q = a.q + (uint64_t)head * a.share * a.dim;
+  it.keys = a.prefix.tokens, it.back = 0, it.ordered = false;
+  it.row0 = row0, it.rows = a.batch * a.queries * a.share;
+  it.scores = nullptr;
+  return it;
+}
+
+// A head's rows of sequence b over its own cache, from row0 on.
+__device__ inline Item own_item(const AttentionArgs& a, uint32_t b, uint32_t head, uint32_t row0) {
+  Item it;
+  it.k = a.own.k + b * a.own.k_seq + head * a.own.k_head, it.v = a.own.v + b * a.own.v_seq + head * a.own.v_head;
+  it.k_token = a.own.k_token, it.v_token = a.own.v_token;
+  it.q = a.q + ((uint64_t)b * a.queries * a.heads + (uint64_t)head * a.share) * a.dim;
+  it.keys = own_length(a, b), it.back = a.queries - 1, it.ordered = a.queries > 1;
+  it.row0 = row0, it.rows = a.queries * a.share;
+  it.scores = a.scores ? a.scores + ((uint64_t)b * a.kv_heads + head) * it.rows * a.score_stride : nullptr;
+  return it;
+}
+
 // RW: 16-row tiles of a wave in wide items (0: the call has none).
 template <class T, int D, bool FULL, int RW>
 __global__ void __launch_bounds__(kThreads, 2) parts_kernel(AttentionArgs a) {
@@ -800,30 +842,17 @@ __global__ void __launch_bounds__(kThreads, 2) parts_kernel(AttentionArgs a) {
   const uint32_t end = (uint32_t)(((uint64_t)blk + 1) * total / blocks);
   while (u < end) {
     Item it;
-    uint32_t item, in, each, head;
+    uint32_t item, in, each;
     const bool shared = u < prefix_units;
     if (shared) {
-      item = u / up, in = u % up, each = up, head = item / a.tp.tiles;
-      it.k = a.prefix.k + head * a.prefix.k_head, it.v = a.prefix.v + head * a.prefix.v_head;
-      it.k_token = a.prefix.k_token, it.v_token = a.prefix.v_token;
-      it.q = a.q + (uint64_t)head * a.share * a.dim;
-      it.keys = a.prefix.tokens, it.back = 0, it.ordered = false;
-      it.row0 = item % a.tp.tiles * a.tp.rows(), it.rows = a.batch * a.queries * a.share;
-      it.scores = nullptr;
+      item = u / up, in = u % up, each = up;
+      it = prefix_item(a, item / a.tp.tiles, item % a.tp.tiles * a.tp.rows());
     } else {
       const OwnPlace pl = own_place(a, line, u - prefix_units);
       const uint32_t x = u - prefix_units - pl.begin, y = x / pl.each;
-      in = x % pl.each, each = pl.each, head = y / a.to.tiles;
+      in = x % pl.each, each = pl.each;
       item = a.kv_heads * a.tp.tiles + pl.b * a.kv_heads * a.to.tiles + y;
-      it.k = a.own.k + pl.b * a.own.k_seq + head * a.own.k_head;
-      it.v = a.own.v + pl.b * a.own.v_seq + head * a.own.v_head;
-      it.k_token = a.own.k_token, it.v_token = a.own.v_token;
-      it.q = a.q + ((uint64_t)pl.b * a.queries * a.heads + (uint64_t)head * a.share) * a.dim;
-      it.keys = own_length(a, pl.b), it.back = a.queries - 1, it.ordered = a.queries > 1;
-      it.row0 = y % a.to.tiles * a.to.rows(), it.rows = a.queries * a.share;
-      it.scores = a.scores
-                      ? a.scores + ((uint64_t)pl.b * a.kv_heads + head) * it.rows * a.score_stride
-                      : nullptr;
+      it = own_item(a, pl.b, y / a.to.tiles, y % a.to.tiles * a.to.rows());
     }
     const uint32_t take = min(each - in, end - u);
     if (RW == 0 || !(shared ? a.tp.r : a.to.r))
@@ -831,6 +860,67 @@ __global__ void __launch_bounds__(kThreads, 2) parts_kernel(AttentionArgs a) {
     else
       wide_part<T, D, FULL, RW ? RW : 1>(a, it, in * kUnit, (in + take) * kUnit, blk + item, lds);
     u += take;
+  }
+}
+
+// What weight a key gets from a sequence's rows of one key head: the sum of
+// exp2(score - m) * inv, with (m, inv) of row r at ml[2 * (r / share * step +
+// r % share)]. Scores that the mask hides (of the earlier of several tokens)
+// are not there.
+__device__ inline float key_weight(const AttentionArgs& a, const float* scores, const float* ml, uint32_t step,
+                                   uint32_t key, uint32_t keys) {
+  const uint32_t newer = keys - 1 - key;
+  float w = 0.0f;
+  for (uint32_t i = newer < a.queries ? a.queries - 1 - newer : 0; i < a.queries; ++i)
+    for (uint32_t g = 0; g < a.share; ++g) {
+      const float* r = ml + 2 * ((uint64_t)i * step + g);
+      w += __builtin_amdgcn_exp2f(scores[(uint64_t)(i * a.share + g) * a.score_stride + key] - r[0]) * r[1];
+    }
+  return w;
+}
+
+constexpr uint32_t kSoloWaves = 8;
+
+// A whole sequence and key head by one block, over the prefix and its own keys:
+// no parts, no second kernel. Rows of a head: at most 16.
+template <class T, int D, bool FULL>
+__global__ void __launch_bounds__(kSoloWaves * 64, 2) solo_kernel(AttentionArgs a) {
+  __shared__ __attribute__((aligned(16))) float lds[kSoloWaves * 16 * (D + 4) + kSoloWaves * 16 * 2];
+  __shared__ float s_ml[32];
+  const uint32_t head = blockIdx.x, b = blockIdx.y, rows = a.queries * a.share;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  constexpr uint32_t stride = kSoloWaves * kStep;
+  Item own = {};
+  if (a.own.tokens) own = own_item(a, b, head, 0);
+  Item pre = prefix_item(a, head, 0);
+  pre.q += (uint64_t)b * a.queries * a.heads * a.dim, pre.rows = rows;
+  State<D, 1> st;
+  begin<D, FULL, 1>(st, a, pre, 0);  // every row sees the whole prefix
+  if (pre.keys) narrow_keys<T, D, FULL>(st, a, pre, kStep * wave, pre.keys, stride);
+  if (a.own.tokens) {
+    const uint32_t n = lane_id() % 16;
+    st.seen[0] = seen_by(a, own, n);
+    // the waves that had a step of the prefix less than the others begin
+    narrow_keys<T, D, FULL>(st, a, own, kStep * ((wave - (pre.keys + kStep - 1) / kStep) % kSoloWaves), own.keys, stride);
+  }
+  const uint64_t first = (uint64_t)b * a.queries * a.heads + (uint64_t)head * a.share;
+  add_waves<D, kSoloWaves>(st, rows, lds, [&](uint32_t row, uint32_t d, float4 o, float m, float l) {
+    const uint64_t at = first + (uint64_t)(row / a.share) * a.heads + row % a.share;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    if (d < a.dim)
+      *reinterpret_cast<u32x2*>(a.out + at * a.dim + d) =
+          u32x2{pack<T>(o.x * inv, o.y * inv), pack<T>(o.z * inv, o.w * inv)};
+    if (d == 0) {
+      if (a.lse) a.lse[at] = l == 0.0f ? -INFINITY : m / kLog2e + logf(l);
+      s_ml[2 * row] = l == 0.0f ? 0.0f : m, s_ml[2 * row + 1] = inv;
+    }
+  });
+  if (!a.weight_out) return;
+  __syncthreads();  // the block's scores are written
+  const uint64_t at = ((uint64_t)b * a.kv_heads + head) * a.own.tokens;
+  for (uint32_t key = threadIdx.x; key < a.own.tokens; key += kSoloWaves * 64) {
+    const float w = key < own.keys ? key_weight(a, own.scores, s_ml, a.share, key, own.keys) : 0.0f;
+    a.weight_out[at + key] = a.weight_in ? a.weight_in[at + key] + w : w;
   }
 }
 
@@ -947,20 +1037,12 @@ __global__ void __launch_bounds__(256) join_kernel(AttentionArgs a) {
 __global__ void __launch_bounds__(256) weights_kernel(AttentionArgs a) {
   const uint32_t head = blockIdx.y, b = blockIdx.z, key = blockIdx.x * 256 + threadIdx.x;
   if (key >= a.own.tokens) return;
-  const uint64_t at = ((uint64_t)b * a.kv_heads + head) * a.own.tokens + key;
+  const uint64_t item = (uint64_t)b * a.kv_heads + head, at = item * a.own.tokens + key;
+  const uint32_t keys = own_length(a, b);
   float w = 0.0f;
-  if (key < own_length(a, b)) {
-    const uint32_t rows = a.queries * a.share;
-    const float* s = a.scores + ((uint64_t)b * a.kv_heads + head) * rows * a.score_stride + key;
-    const float* ml = a.row_ml + 2 * ((uint64_t)b * a.queries * a.heads + (uint64_t)head * a.share);
-    // the scores that the mask hides (of the earlier of several tokens) are not there
-    const uint32_t newer = own_length(a, b) - 1 - key;
-    for (uint32_t i = newer < a.queries ? a.queries - 1 - newer : 0; i < a.queries; ++i)
-      for (uint32_t g = 0; g < a.share; ++g) {
-        const float* r = ml + 2 * ((uint64_t)i * a.heads + g);
-        w += __builtin_amdgcn_exp2f(s[(uint64_t)(i * a.share + g) * a.score_stride] - r[0]) * r[1];
-      }
-  }
+  if (key < keys)
+    w = key_weight(a, a.scores + item * a.queries * a.share * a.score_stride,
+                   a.row_ml + 2 * ((uint64_t)b * a.queries * a.heads + (uint64_t)head * a.share), a.heads, key, keys);
   a.weight_out[at] = a.weight_in ? a.weight_in[at] + w : w;
 }
 
@@ -974,9 +1056,12 @@ static Tiling tiling(uint64_t rows, uint32_t r) {
   return t;
 }
 
+constexpr uint64_t kSoloKeys = 2048;
+
 struct AttentionPlan {
   AttentionArgs a;
   uint64_t bytes, part_o, part_ml, row_ml, scores;  // of the workspace: its size and its parts' places
+  bool solo;
 };
 
 static hl_status check_kv(const hl_kv& s, uint64_t tokens, uint32_t dim, bool sequences) {
@@ -1038,6 +1123,10 @@ static hl_status attention_plan(const hl_attention* h, bool weights, AttentionPl
     n += (floats * 4 + 255) / 256 * 256;
     return at;
   };
+  // A block a sequence and key head where that is short: it reads the prefix
+  // again for each sequence (from the L2s, as far as it is the same), and saves
+  // the second kernel.
+  pl->solo = own_rows <= 16 && a.prefix.tokens + a.own.tokens <= kSoloKeys;
   pl->part_o = take(slots * a.part_rows * held);
   pl->part_ml = take(slots * a.part_rows * 2);
   a.score_stride = (a.own.tokens + kStep - 1) / kStep * kStep;
@@ -1061,7 +1150,8 @@ static hl_status run(const AttentionArgs& a, hipStream_t s) {
 }
 
 template <class T, int D, bool FULL>
-static hl_status run_rows(const AttentionArgs& a, hipStream_t s) {
+static hl_status run_rows(const AttentionArgs& a, bool solo, hipStream_t s) {
+  if (solo) return enqueue(solo_kernel<T, D, FULL>, dim3(a.kv_heads, a.batch), dim3(kSoloWaves * 64), s, a);
   const uint32_t r = std::max(a.tp.r, a.to.r);
   if (r == 0) return run<T, D, FULL, 0>(a, s);
   if constexpr (D <= 128) {
@@ -1071,13 +1161,13 @@ static hl_status run_rows(const AttentionArgs& a, hipStream_t s) {
 }
 
 template <class T>
-static hl_status run_type(const AttentionArgs& a, hipStream_t s) {
-  if (a.dim == 64) return run_rows<T, 64, true>(a, s);
-  if (a.dim < 64) return run_rows<T, 64, false>(a, s);
-  if (a.dim == 128) return run_rows<T, 128, true>(a, s);
-  if (a.dim < 128) return run_rows<T, 128, false>(a, s);
-  if (a.dim == 256) return run_rows<T, 256, true>(a, s);
-  return run_rows<T, 256, false>(a, s);
+static hl_status run_type(const AttentionArgs& a, bool solo, hipStream_t s) {
+  if (a.dim == 64) return run_rows<T, 64, true>(a, solo, s);
+  if (a.dim < 64) return run_rows<T, 64, false>(a, solo, s);
+  if (a.dim == 128) return run_rows<T, 128, true>(a, solo, s);
+  if (a.dim < 128) return run_rows<T, 128, false>(a, solo, s);
+  if (a.dim == 256) return run_rows<T, 256, true>(a, solo, s);
+  return run_rows<T, 256, false>(a, solo, s);
 }
 
 }  // namespace hl
@@ -1111,6 +1201,6 @@ extern "C" hl_status hl_prefix_attention(const hl_attention* attention, const vo
     a.row_ml = reinterpret_cast<float*>(ws + pl.row_ml);
     a.scores = reinterpret_cast<float*>(ws + pl.scores);
   }
-  return attention->dtype == HL_BF16 ? run_type<__bf16>(a, (hipStream_t)stream)
-                                     : run_type<_Float16>(a, (hipStream_t)stream);
+  return attention->dtype == HL_BF16 ? run_type<__bf16>(a, pl.solo, (hipStream_t)stream)
+                                     : run_type<_Float16>(a, pl.solo, (hipStream_t)stream);
 }

@@ -515,17 +515,30 @@ class EvictResult(NamedTuple):
     slots: object
 
 
-_VALUE_TYPES = None
+class _Torch:
+    """What a call of the operators needs of torch and of the library, looked up once: an import statement and the
+    attributes' chains cost a small call a tenth of its time."""
 
-
-def _value_types():
-    """Codes of the types that norms read and write, by torch type."""
-    global _VALUE_TYPES
-    if _VALUE_TYPES is None:
+    def __init__(self):
         import torch
-        _VALUE_TYPES = {torch.float32: HL_F32, torch.bfloat16: HL_BF16, torch.float16: HL_F16,
-                        torch.float8_e4m3fn: HL_E4M3}
-    return _VALUE_TYPES
+        self.codes = {torch.float32: HL_F32, torch.bfloat16: HL_BF16, torch.float16: HL_F16,
+                      torch.float8_e4m3fn: HL_E4M3}
+        self.float32, self.int32, self.uint8 = torch.float32, torch.int32, torch.uint8
+        self.half = {torch.bfloat16: HL_BF16, torch.float16: HL_F16}
+        self.two_bytes = (torch.bfloat16, torch.float16, torch.int16)
+        self.empty, self.empty_like, self.Tensor = torch.empty, torch.empty_like, torch.Tensor
+        self.raw_stream = torch._C._cuda_getCurrentRawStream
+        self.lib = lib()
+
+
+_torch = None
+
+
+def _lookups() -> _Torch:
+    global _torch
+    if _torch is None:
+        _torch = _Torch()
+    return _torch
 
 
 def _plain(device: int, bufs) -> None:
@@ -548,8 +561,8 @@ def rms_norm(x, weight, residual=None, eps: float = 1e-5, out_dtype=None, group:
     residual's type (``sum_out`` may be ``residual`` itself). ``out_dtype`` defaults to weight's type;
     torch.float8_e4m3fn gives 8 bits and float32 scales, one for each ``group`` columns (32, 64 or 128) or, with 0,
     for each row. Outputs that are not given are allocated."""
-    import torch
-    types = _value_types()
+    T = _torch or _lookups()
+    types = T.codes
     shape, dev = x.shape, x.get_device()
     if weight.dim() != 1 or not shape or shape[-1] != weight.shape[0] or x.numel() == 0:
         raise ValueError(f"x must be [..., hidden] and weight [hidden], got {tuple(shape)} and {tuple(weight.shape)}")
@@ -559,7 +572,7 @@ def rms_norm(x, weight, residual=None, eps: float = 1e-5, out_dtype=None, group:
     if xt is None or wt is None or oc is None or xt == HL_E4M3 or wt == HL_E4M3:
         raise ValueError("x and weight must be float32, bfloat16 or float16; out these or float8_e4m3fn")
     if out is None:
-        out = torch.empty_like(x, dtype=ot) if x.dtype != ot else torch.empty_like(x)
+        out = T.empty_like(x, dtype=ot)
     elif out.dtype != ot or out.shape != shape:
         raise ValueError(f"out must be {tuple(shape)} of {ot}")
     good = dev >= 0 and x.is_contiguous() and weight.is_contiguous() and weight.get_device() == dev \
@@ -570,7 +583,7 @@ def rms_norm(x, weight, residual=None, eps: float = 1e-5, out_dtype=None, group:
         if rt is None or rt == HL_E4M3 or residual.shape != shape:
             raise ValueError(f"residual must have x's shape {tuple(shape)} and be float32, bfloat16 or float16")
         if sum_out is None:
-            sum_out = torch.empty_like(residual)
+            sum_out = T.empty_like(residual)
         elif sum_out.dtype != residual.dtype or sum_out.shape != shape:
             raise ValueError("sum_out must have residual's shape and type")
         good = good and residual.is_contiguous() and residual.get_device() == dev and sum_out.is_contiguous() \
@@ -583,8 +596,8 @@ def rms_norm(x, weight, residual=None, eps: float = 1e-5, out_dtype=None, group:
             raise ValueError("group must be 0, or 32, 64 or 128 and divide hidden")
         need = (*shape[:-1], hidden // group) if group else tuple(shape[:-1])
         if scale_out is None:
-            scale_out = torch.empty(need, dtype=torch.float32, device=x.device)
-        elif scale_out.dtype != torch.float32 or tuple(scale_out.shape) != tuple(need):
+            scale_out = T.empty(need, dtype=T.float32, device=x.device)
+        elif scale_out.dtype != T.float32 or tuple(scale_out.shape) != tuple(need):
             raise ValueError(f"scale_out must be float32 {tuple(need)}")
         good = good and scale_out.is_contiguous() and scale_out.get_device() == dev
         scale_ptr = scale_out.data_ptr()
@@ -593,8 +606,9 @@ def rms_norm(x, weight, residual=None, eps: float = 1e-5, out_dtype=None, group:
     if not good:
         _plain(dev, {"x": x, "weight": weight, "out": out, "residual": residual, "sum_out": sum_out,
                      "scale_out": scale_out})
-    s = lib().hl_rms_norm(x.data_ptr(), xt, r_ptr, rt, weight.data_ptr(), wt, x.numel() // hidden, hidden, eps, s_ptr,
-                          out.data_ptr(), oc, group, scale_ptr, _stream_ptr(stream))
+    s = T.lib.hl_rms_norm(x.data_ptr(), xt, r_ptr, rt, weight.data_ptr(), wt, x.numel() // hidden, hidden, eps, s_ptr,
+                          out.data_ptr(), oc, group, scale_ptr,
+                          T.raw_stream(dev) if stream is None else stream.cuda_stream)
     if s:
         _check(s, "hl_rms_norm")
     return NormResult(out, sum_out, scale_out)
@@ -619,8 +633,7 @@ def _keys_values(k, v, name: str, dims: int, dtype, device: int):
 
 def _small(t, name: str, dtype, shape, device: int):
     """A contiguous buffer of this type, shape and device (else ValueError)."""
-    import torch
-    if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.shape == shape and t.is_contiguous()
+    if not (isinstance(t, _torch.Tensor) and t.dtype == dtype and t.shape == shape and t.is_contiguous()
             and t.get_device() == device):
         _dev_arg(t, name, (dtype,), shape)
         raise ValueError(f"{name} must be on GPU {device}, not {t.device}")
@@ -648,8 +661,10 @@ def prefix_attention(q, k=None, v=None, lens=None, prefix_k=None, prefix_v=None,
     key was given by this call (``weights_out`` may be ``weights``; without ``weights``, plus zeros). ``lse``: a
     float32 [batch, queries, heads] buffer for the logarithms of the softmax sums. ``workspace``: a device buffer of
     hl_attention_workspace_bytes; allocated where it is not given."""
-    import torch
-    if q.dim() != 4 or q.dtype not in (torch.bfloat16, torch.float16):
+    T = _torch or _lookups()
+    dtype = q.dtype
+    code = T.half.get(dtype)
+    if code is None or q.dim() != 4:
         raise ValueError("q must be [batch, queries, heads, dim] bfloat16 or float16")
     batch, queries, heads, dim = q.shape
     dev = q.get_device()
@@ -658,13 +673,13 @@ def prefix_attention(q, k=None, v=None, lens=None, prefix_k=None, prefix_v=None,
     own = prefix = _NO_KV
     kv_heads = lens_ptr = w_ptr = w_out_ptr = lse_ptr = None
     if k is not None or v is not None:
-        own = _keys_values(k, v, "k, v", 4, q.dtype, dev)
+        own = _keys_values(k, v, "k, v", 4, dtype, dev)
         kv_heads = k.shape[2]
         if k.shape[0] != batch or k.shape[3] != dim:
             raise ValueError(f"k, v must be [{batch}, capacity, kv_heads, {dim}], got {tuple(k.shape)}")
-        lens_ptr = _small(lens, "lens", torch.int32, (batch,), dev).data_ptr()
+        lens_ptr = _small(lens, "lens", T.int32, (batch,), dev).data_ptr()
     if prefix_k is not None or prefix_v is not None:
-        prefix = _keys_values(prefix_k, prefix_v, "prefix_k, prefix_v", 3, q.dtype, dev)
+        prefix = _keys_values(prefix_k, prefix_v, "prefix_k, prefix_v", 3, dtype, dev)
         if prefix_k.shape[2] != dim or (kv_heads is not None and kv_heads != prefix_k.shape[1]):
             raise ValueError(f"prefix_k, prefix_v must be [length, kv_heads, {dim}] with the own caches' kv_heads, "
                              f"got {tuple(prefix_k.shape)}")
@@ -672,33 +687,33 @@ def prefix_attention(q, k=None, v=None, lens=None, prefix_k=None, prefix_v=None,
     if not kv_heads or heads % kv_heads:
         raise ValueError("a prefix or own caches are needed, with kv_heads that divide heads")
     if out is None:
-        out = torch.empty_like(q)
+        out = T.empty_like(q)
     else:
-        _small(out, "out", q.dtype, q.shape, dev)
+        _small(out, "out", dtype, q.shape, dev)
     if weights is not None or weights_out is not None:
         if k is None:
             raise ValueError("weights are of the own caches' keys")
         need = (batch, kv_heads, k.shape[1])
         if weights is not None:
-            w_ptr = _small(weights, "weights", torch.float32, need, dev).data_ptr()
+            w_ptr = _small(weights, "weights", T.float32, need, dev).data_ptr()
         if weights_out is None:
-            weights_out = torch.empty(need, dtype=torch.float32, device=q.device)
+            weights_out = T.empty(need, dtype=T.float32, device=q.device)
         else:
-            _small(weights_out, "weights_out", torch.float32, need, dev)
+            _small(weights_out, "weights_out", T.float32, need, dev)
         w_out_ptr = weights_out.data_ptr()
     if lse is not None:
-        lse_ptr = _small(lse, "lse", torch.float32, (batch, queries, heads), dev).data_ptr()
-    a = _ATTENTION.pack(HL_BF16 if q.dtype == torch.bfloat16 else HL_F16, batch, queries, heads, kv_heads, dim,
+        lse_ptr = _small(lse, "lse", T.float32, (batch, queries, heads), dev).data_ptr()
+    a = _ATTENTION.pack(code, batch, queries, heads, kv_heads, dim,
                         1.0 / math.sqrt(dim) if scale is None else scale, *prefix, *own)
-    L = lib()
+    L = T.lib
     if workspace is None:
-        workspace = torch.empty(L.hl_attention_workspace_bytes(a, w_out_ptr is not None), dtype=torch.uint8,
+        workspace = T.empty(L.hl_attention_workspace_bytes(a, w_out_ptr is not None), dtype=T.uint8,
                                 device=q.device)
     else:
         _dev_arg(workspace, "workspace")
         _on_device(q.device, workspace=workspace)
     s = L.hl_prefix_attention(a, q.data_ptr(), lens_ptr, out.data_ptr(), lse_ptr, w_ptr, w_out_ptr,
-                              workspace.data_ptr(), workspace.nbytes, _stream_ptr(stream))
+                              workspace.data_ptr(), workspace.nbytes, T.raw_stream(dev) if stream is None else stream.cuda_stream)
     if s:
         _check(s, "hl_prefix_attention")
     return AttentionResult(out, weights_out, lse)
@@ -712,27 +727,27 @@ def cache_evict(k, v, weights, lens, keep: int, recent: int = 0, k_out=None, v_o
     [batch, kv_heads, capacity]; lens: int32 [batch]. k_out, v_out (default: new ones of capacity ``keep``): caches of
     at least ``keep`` tokens that do not overlap k and v. Gives these, the kept tokens' weights (float32) and slots
     (int32) [batch, kv_heads, keep] - 0 and -1 past the kept ones, whose rows are zeros - and the new lengths."""
-    import torch
-    if k.dim() != 4 or k.dtype not in (torch.bfloat16, torch.float16, torch.int16):
+    T = _torch or _lookups()
+    if k.dim() != 4 or k.dtype not in T.two_bytes:
         raise ValueError("k must be [batch, capacity, kv_heads, dim] bfloat16, float16 or int16")
     batch, capacity, heads, dim = k.shape
     dev = k.get_device()
     src = _keys_values(k, v, "k, v", 4, k.dtype, dev)
     if keep < 1 or not 0 <= recent <= keep:
         raise ValueError("keep must be at least 1 and recent between 0 and keep")
-    _small(weights, "weights", torch.float32, (batch, heads, capacity), dev)
-    _small(lens, "lens", torch.int32, (batch,), dev)
+    _small(weights, "weights", T.float32, (batch, heads, capacity), dev)
+    _small(lens, "lens", T.int32, (batch,), dev)
     if k_out is None and v_out is None:
         k_out = k.new_empty((batch, keep, heads, dim))
-        v_out = torch.empty_like(k_out)
+        v_out = T.empty_like(k_out)
     dst = _keys_values(k_out, v_out, "k_out, v_out", 4, k.dtype, dev)
     if k_out.shape[0] != batch or k_out.shape[2] != heads or k_out.shape[3] != dim or k_out.shape[1] < keep:
         raise ValueError(f"k_out must be [{batch}, at least {keep}, {heads}, {dim}], got {tuple(k_out.shape)}")
     w_out = weights.new_empty((batch, heads, keep))
     slots = lens.new_empty((batch, heads, keep))
-    lens_out = torch.empty_like(lens)
-    s = lib().hl_cache_evict(_KV.pack(*src), _KV.pack(*dst), batch, heads, dim, weights.data_ptr(), lens.data_ptr(), keep,
-                             recent, w_out.data_ptr(), slots.data_ptr(), lens_out.data_ptr(), _stream_ptr(stream))
+    lens_out = T.empty_like(lens)
+    s = T.lib.hl_cache_evict(_KV.pack(*src), _KV.pack(*dst), batch, heads, dim, weights.data_ptr(), lens.data_ptr(), keep,
+                             recent, w_out.data_ptr(), slots.data_ptr(), lens_out.data_ptr(), T.raw_stream(dev) if stream is None else stream.cuda_stream)
     if s:
         _check(s, "hl_cache_evict")
     return EvictResult(k_out, v_out, w_out, lens_out, slots)
