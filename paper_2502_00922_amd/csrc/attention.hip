@@ -26,11 +26,14 @@
 // The matrix instruction takes K as its left operand and Q as its right, so a
 // lane ends up with scores of one query (lane % 16), which is also what the
 // second product needs of P as its right operand: the keys are only numbered
-// differently in the two products, and P never leaves its lane. The values are
-// read as rows (lane % 16 owns 8 neighbouring columns of 8 keys) and turned in
-// registers, one byte permutation for two elements; the columns of one lane go
-// to 8 different instructions, so that turning needs no other lane's data.
+// differently in the two products, and P never leaves its lane. The values'
+// operand has 8 keys of one column in a lane. Narrow items read rows (lane % 16
+// owns 8 neighbouring columns of 8 keys) and turn them in registers, one byte
+// permutation for two elements; the columns of one lane go to 8 different
+// instructions, so that turning needs no other lane's data. Wide items let the
+// transposing LDS read do it, whose 16 lanes exchange 4 keys of 16 columns.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "gpu_host.h"
@@ -47,6 +50,7 @@ constexpr float kLog2e = 1.44269504088896341f;
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
@@ -76,7 +80,8 @@ struct AttentionArgs {
   uint32_t batch, queries, heads, kv_heads, dim, share;  // share: query heads of a key head
   uint32_t blocks, part_rows, score_stride;
   Tiling tp, to;
-  float scale2;  // scale * log2(e): scores are kept in powers of two
+  float scale2;  // |scale| * log2(e), or 1: scores are kept in powers of two
+  uint32_t q_and, q_xor;  // on pairs of q: its sign is the scale's, and it is 0 where the scale is
 };
 
 __device__ inline uint32_t own_length(const AttentionArgs& a, uint32_t b) {
@@ -220,10 +225,21 @@ struct Shape {
   static constexpr int TILES = D / 16;      // of the second product's output
 };
 
+// A narrow step's keys and values, as rows.
 template <int D>
 struct Tile {
+  static constexpr bool TURNED = false;
   u32x4 k[2][Shape<D>::KS];
   uint32_t v[8][Shape<D>::HALVES][Shape<D>::VE / 2];
+};
+
+// A wide step's: the values as the second product's left operands, output tile
+// i having columns 16*i ...
+template <int D>
+struct TurnedTile {
+  static constexpr bool TURNED = true;
+  u32x4 k[2][Shape<D>::KS];
+  u32x4 v[Shape<D>::TILES];
 };
 
 // Key of value row e in lane group c, counted from the step's first: the order
@@ -316,6 +332,22 @@ __device__ inline void turned_end(const u32x4 (&vt)[SET]) {
   for (int i = 0; i < SET; ++i) asm volatile("" ::"v"(vt[i]));
 }
 
+// The left operands of a wide item's output tiles i0 .. i0+SET-1, two bytes at
+// a time from memory: for the few steps that add_beyond looks at again.
+template <int SET>
+__device__ inline void gather_v(u32x4 (&vt)[SET], const Item& it, uint32_t dim, uint32_t key, int i0) {
+  const uint32_t lane = lane_id(), n = lane % 16, c = lane / 16, left = it.keys - 1 - key;
+#pragma unroll
+  for (int i = 0; i < SET; ++i) {
+    const uint16_t* column = it.v + min((i0 + i) * 16 + n, dim - 1);  // past the head's, its last one
+    const auto value = [&](int e) {
+      return (uint32_t)column[(uint64_t)(key + min(key_of(c, e), left)) * it.v_token];
+    };
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) vt[i][e / 2] = value(e) | value(e + 1) << 16;
+  }
+}
+
 // A pair of values to powers of two that say what each is: 1 for +infinity, 64
 // for -infinity, 4096 for a NaN, and 0 for the rest. Sums over a step's 32 keys
 // still tell them apart.
@@ -333,7 +365,7 @@ __device__ inline uint32_t kinds(uint32_t pair) {
 // make of them, for the queries that see their keys alone: in the product with
 // the weights, where a hidden key has weight 0, they would make NaN of the
 // others too. A wave's steps are `stride` keys apart.
-template <class T, int D, bool FULL, int R>
+template <class T, int D, bool FULL, int R, bool TURNED>
 __device__ inline void add_beyond(State<D, R>& st, const Item& it, uint32_t dim, uint32_t key, uint32_t end,
                                   uint32_t stride) {
   const uint32_t c = lane_id() / 16;
@@ -341,7 +373,7 @@ __device__ inline void add_beyond(State<D, R>& st, const Item& it, uint32_t dim,
 #pragma unroll 1
   for (; key < end; key += stride) {
     Tile<D> t;
-    load_v<D, FULL, true>(t, it, dim, key);
+    if constexpr (!TURNED) load_v<D, FULL, true>(t, it, dim, key);
     u32x4 sees[R];
 #pragma unroll
     for (int rt = 0; rt < R; ++rt)
@@ -352,7 +384,10 @@ __device__ inline void add_beyond(State<D, R>& st, const Item& it, uint32_t dim,
 #pragma unroll
     for (int i0 = 0; i0 < Shape<D>::TILES; i0 += set_of(D)) {
       u32x4 vt[set_of(D)];
-      turn<D, set_of(D)>(vt, t, i0);
+      if constexpr (TURNED)
+        gather_v<set_of(D)>(vt, it, dim, key, i0);
+      else
+        turn<D, set_of(D)>(vt, t, i0);
 #pragma unroll
       for (int i = 0; i < set_of(D); ++i) {
         u32x4 kind;
@@ -377,13 +412,12 @@ __device__ inline void add_beyond(State<D, R>& st, const Item& it, uint32_t dim,
 // One step: scores of 32 keys, their weights, and the weighted values. EDGE:
 // some query may not see some of the keys; `most`: keys that some query sees.
 // get_k and get_v bring the step's keys and values into the tile.
-template <class T, int D, int R, bool EDGE, class GetK, class GetV>
-__device__ inline void step(State<D, R>& st, Tile<D>& t, const AttentionArgs& a, const Item& it, uint32_t key,
+template <class T, int D, int R, bool EDGE, class Keys, class GetK, class GetV>
+__device__ inline void step(State<D, R>& st, Keys& t, const AttentionArgs& a, const Item& it, uint32_t key,
                             uint32_t most, uint32_t wave_row, GetK get_k, GetV get_v) {
   using S = Shape<D>;
   const uint32_t lane = lane_id(), n = lane % 16, c = lane / 16;
   f32x4 s[R][2];
-  float p[R][2][4];
   u32x4 w[R];
   get_k(t, it, a.dim, key);
   __builtin_amdgcn_sched_barrier(0);
@@ -401,31 +435,28 @@ __device__ inline void step(State<D, R>& st, Tile<D>& t, const AttentionArgs& a,
   if constexpr (!EDGE) get_v(t, it, a.dim, key);  // on its way during the softmax
 #pragma unroll
   for (int rt = 0; rt < R; ++rt) {
-    float top = -INFINITY;
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) p[rt][h][r] = s[rt][h][r] * a.scale2;
     if constexpr (EDGE) {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          if (key + 16 * h + 4 * c + r >= st.seen[rt]) p[rt][h][r] = -INFINITY;
+          if (key + 16 * h + 4 * c + r >= st.seen[rt]) s[rt][h][r] = -INFINITY;
     }
     if (it.scores) {
       const uint32_t row = wave_row + 16 * rt + n;
       if (row < it.rows) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-          *reinterpret_cast<float4*>(it.scores + (uint64_t)row * a.score_stride + key + 16 * h + 4 * c) =
-              make_float4(p[rt][h][0], p[rt][h][1], p[rt][h][2], p[rt][h][3]);
+          *reinterpret_cast<f32x4*>(it.scores + (uint64_t)row * a.score_stride + key + 16 * h + 4 * c) =
+              s[rt][h] * a.scale2;
       }
     }
+    float top = -INFINITY;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) top = fmaxf(top, p[rt][h][r]);
+      for (int r = 0; r < 4; ++r) top = fmaxf(top, s[rt][h][r]);
+    top *= a.scale2;
     // The maximum need not be the true one, only near it: the output is
     // scaled again when a score passes it by more than 2^8, so the weights
     // stay in the 16-bit types' range and most steps scale nothing.
@@ -444,42 +475,62 @@ __device__ inline void step(State<D, R>& st, Tile<D>& t, const AttentionArgs& a,
       }
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < 2; ++h) {
+      float p[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        p[rt][h][r] = __builtin_amdgcn_exp2f(p[rt][h][r] - st.m[rt]);
-        st.l[rt] += p[rt][h][r];
+        p[r] = __builtin_amdgcn_exp2f(fmaf(s[rt][h][r], a.scale2, -st.m[rt]));
+        st.l[rt] += p[r];
       }
-    w[rt] = u32x4{pack<T>(p[rt][0][0], p[rt][0][1]), pack<T>(p[rt][0][2], p[rt][0][3]),
-                  pack<T>(p[rt][1][0], p[rt][1][1]), pack<T>(p[rt][1][2], p[rt][1][3])};
+      w[rt][2 * h] = pack<T>(p[0], p[1]), w[rt][2 * h + 1] = pack<T>(p[2], p[3]);
+    }
   }
   if constexpr (EDGE) {
     get_v(t, it, a.dim, key);
     // values that no query sees count 0, whatever they are; those that only
     // some see must be finite in the product (add_beyond has the others)
     const uint32_t some = it.ordered ? ~0u : 0u;
+    const auto clean = [&](uint32_t v, uint32_t in) {
+      const uint32_t d = v & in, off = beyond<T>(d) & some;
+      st.odd |= off;
+      return d & ~off;
+    };
+    uint32_t in[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t in = key + key_of(c, e) < most ? ~0u : 0u;
+    for (int e = 0; e < 8; ++e) in[e] = key + key_of(c, e) < most ? ~0u : 0u;
+    if constexpr (Keys::TURNED) {
 #pragma unroll
-      for (int h = 0; h < S::HALVES; ++h)
+      for (int i = 0; i < S::TILES; ++i)
 #pragma unroll
-        for (int j = 0; j < S::VE / 2; ++j) {
-          const uint32_t d = t.v[e][h][j] & in, off = beyond<T>(d) & some;
-          st.odd |= off;
-          t.v[e][h][j] = d & ~off;
-        }
+        for (int e = 0; e < 8; e += 2)
+          t.v[i][e / 2] = clean(t.v[i][e / 2], (in[e] & 0xFFFFu) | (in[e + 1] & 0xFFFF0000u));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int h = 0; h < S::HALVES; ++h)
+#pragma unroll
+          for (int j = 0; j < S::VE / 2; ++j) t.v[e][h][j] = clean(t.v[e][h][j], in[e]);
     }
   }
+  if constexpr (Keys::TURNED) {
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-  for (int i0 = 0; i0 < S::TILES; i0 += set_of(D)) {
-    u32x4 vt[set_of(D)];
-    turn<D, set_of(D)>(vt, t, i0);
+    for (int i = 0; i < S::TILES; ++i)
 #pragma unroll
-    for (int i = 0; i < set_of(D); ++i)
+      for (int rt = 0; rt < R; ++rt) st.o[rt][i] = mfma<T>(t.v[i], w[rt], st.o[rt][i]);
+    products_end();
+  } else {
 #pragma unroll
-      for (int rt = 0; rt < R; ++rt) st.o[rt][i0 + i] = mfma<T>(vt[i], w[rt], st.o[rt][i0 + i]);
-    turned_end<set_of(D)>(vt);
+    for (int i0 = 0; i0 < S::TILES; i0 += set_of(D)) {
+      u32x4 vt[set_of(D)];
+      turn<D, set_of(D)>(vt, t, i0);
+#pragma unroll
+      for (int i = 0; i < set_of(D); ++i)
+#pragma unroll
+        for (int rt = 0; rt < R; ++rt) st.o[rt][i0 + i] = mfma<T>(vt[i], w[rt], st.o[rt][i0 + i]);
+      turned_end<set_of(D)>(vt);
+    }
   }
 }
 
@@ -515,7 +566,7 @@ __device__ inline void begin(State<D, R>& st, const AttentionArgs& a, const Item
       const uint32_t d = c * 8 + s * 32;
       const bool in = FULL || d < a.dim;
       const u32x4 w = *reinterpret_cast<const u32x4*>(q + (in ? d : 0));
-      st.q[rt][s] = in ? w : u32x4{0, 0, 0, 0};
+      st.q[rt][s] = in ? (w & a.q_and) ^ a.q_xor : u32x4{0, 0, 0, 0};
     }
   }
 }
@@ -571,7 +622,7 @@ __device__ inline void narrow_keys(State<D, 1>& st, const AttentionArgs& a, cons
     Tile<D> t;
     step<T, D, 1, true>(st, t, a, it, key, most, it.row0, load_k<D, FULL, true>, load_v<D, FULL, true>);
   }
-  if (__any(st.odd != 0)) add_beyond<T, D, FULL, 1>(st, it, a.dim, edge, end, stride);
+  if (__any(st.odd != 0)) add_beyond<T, D, FULL, 1, false>(st, it, a.dim, edge, end, stride);
   st.odd = 0;
 }
 
@@ -718,37 +769,33 @@ __device__ inline void wide_part(const AttentionArgs& a, const Item& it, uint32_
   // Steps begin at multiples of 16 rows, so which banks a lane's pieces are in
   // does not depend on the step.
   constexpr int KD = S::KS < 4 ? S::KS : 4;  // of 256 columns, the second half is 16 pieces on
-  uint32_t kofs[KD], vofs[4];
+  uint32_t kofs[KD];
 #pragma unroll
   for (int s = 0; s < KD; ++s) kofs[s] = n * D * 2 + place<D>(n, c + 4 * s) * 16;
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    vofs[e] = bytes / 2 + (4 * c + e) * D * 2 + place<D>(4 * c + e, n * S::VE / 8) * 16 + (S::VE == 4 ? n % 2 * 8 : 0);
-  const uint8_t* from;  // the step's buffer
-  const auto get_k = [&](Tile<D>& t, const Item&, uint32_t dim, uint32_t) {
+  // Columns 16*i .. of keys 4*c .. 4*c+3: of each key 4 lanes read 4 columns.
+  // Tile i's pieces are tile 0's with 2*i changed in their number.
+  const uint32_t vrow = 4 * c + n / 4;
+  const uint32_t vofs = bytes / 2 + vrow * D * 2 + place<D>(vrow, n % 4 / 2) * 16 + n % 2 * 8;
+  uint32_t from;  // the step's buffer
+  const auto get_k = [&](TurnedTile<D>& t, const Item&, uint32_t dim, uint32_t) {
 #pragma unroll
     for (int s = 0; s < S::KS; ++s)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(from + kofs[s % KD] + s / KD * 256 + h * 16 * D * 2);
+        const u32x4 w = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(lds) + from + kofs[s % KD] +
+                                                        s / KD * 256 + h * 16 * D * 2);
         t.k[h][s] = FULL || c * 8 + s * 32 < dim ? w : u32x4{0, 0, 0, 0};
       }
   };
-  const auto get_v = [&](Tile<D>& t, const Item&, uint32_t, uint32_t) {
+  const auto get_v = [&](TurnedTile<D>& t, const Item&, uint32_t, uint32_t) {
 #pragma unroll
-    for (int h = 0; h < S::HALVES; ++h)
+    for (int i = 0; i < S::TILES; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        // 16 pieces on, the other half of a row of 256 columns
-        const uint8_t* v = from + vofs[e % 4] + h * 256 + (e < 4 ? 0 : 16 * D * 2);
-        if constexpr (S::VE == 8) {
-          const u32x4 w = *reinterpret_cast<const u32x4*>(v);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) t.v[e][h][j] = w[j];
-        } else {
-          const u32x2 w = *reinterpret_cast<const u32x2*>(v);
-          t.v[e][h][0] = w[0], t.v[e][h][1] = w[1];
-        }
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t v = at + ((from + vofs) ^ (i % 8 * 32)) + i / 8 * 256 + h * 16 * D * 2;
+        const s16x4 w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)v);
+        const u32x2 d = __builtin_bit_cast(u32x2, w);
+        t.v[i][2 * h] = d[0], t.v[i][2 * h + 1] = d[1];
       }
   };
   const auto ready = [&](uint32_t i) {
@@ -756,7 +803,7 @@ __device__ inline void wide_part(const AttentionArgs& a, const Item& it, uint32_
     buffers_ready<D>(min(steps - 1 - i, ring - 2));
     if (i + ring - 1 < steps)
       load_buffer<D, FULL>(it, a.dim, k0 + (i + ring - 1) * kStep, at + (i + ring - 1) % ring * bytes);
-    from = reinterpret_cast<const uint8_t*>(lds) + i % ring * bytes;
+    from = i % ring * bytes;
   };
   // the steps that hide no key of any wave, then the rest
   const uint32_t whole = k0 < min(end, all) ? (min(end, all) - k0) / kStep : 0;
@@ -765,17 +812,17 @@ __device__ inline void wide_part(const AttentionArgs& a, const Item& it, uint32_
   for (; i < whole; ++i) {
     ready(i);
     if (mine == 0) continue;
-    Tile<D> t;
+    TurnedTile<D> t;
     step<T, D, R, false>(st, t, a, it, k0 + i * kStep, most, wave_row, get_k, get_v);
   }
 #pragma unroll 1
   for (; i < steps; ++i) {
     ready(i);
     if (k0 + i * kStep >= mine) continue;
-    Tile<D> t;
+    TurnedTile<D> t;
     step<T, D, R, true>(st, t, a, it, k0 + i * kStep, most, wave_row, get_k, get_v);
   }
-  if (__any(st.odd != 0)) add_beyond<T, D, FULL, R>(st, it, a.dim, k0 + whole * kStep, mine, kStep);
+  if (__any(st.odd != 0)) add_beyond<T, D, FULL, R, true>(st, it, a.dim, k0 + whole * kStep, mine, kStep);
   __syncthreads();  // the buffers are free
   float* po = a.part_o + (uint64_t)slot * a.part_rows * D;
   float* pml = a.part_ml + (uint64_t)slot * a.part_rows * 2;
@@ -786,15 +833,8 @@ __device__ inline void wide_part(const AttentionArgs& a, const Item& it, uint32_
     if (it.row0 + row >= it.rows) continue;
     if (c == 0) pml[2 * row] = st.some[rt] || sum != sum ? st.m[rt] : -INFINITY, pml[2 * row + 1] = sum;
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-#pragma unroll
-      for (int h = 0; h < S::HALVES; ++h)
-#pragma unroll
-        for (int q = 0; q < S::VE; q += 4) {
-          const int i = h * S::VE + q;
-          *reinterpret_cast<float4*>(po + (uint64_t)row * D + h * 128 + (4 * c + r) * S::VE + q) =
-              make_float4(st.o[rt][i][r], st.o[rt][i + 1][r], st.o[rt][i + 2][r], st.o[rt][i + 3][r]);
-        }
+    for (int i = 0; i < S::TILES; ++i)
+      *reinterpret_cast<f32x4*>(po + (uint64_t)row * D + 16 * i + 4 * c) = st.o[rt][i];
   }
 }
 
@@ -925,25 +965,30 @@ __global__ void __launch_bounds__(kSoloWaves * 64, 2) solo_kernel(AttentionArgs 
 }
 
 constexpr uint32_t kSplitRows = 4096;  // rows up to which a block joins a row
-constexpr uint32_t kAhead = 8;  // parts whose loads a joining wave has in flight
+constexpr uint32_t kAhead = 8;         // parts whose loads a joining thread has in flight
 
-// Adds a row's parts; lane's columns are lane*D/64 .. A row is a wave's, or
-// (SPLIT, for few rows) a block's, whose waves take every fourth part each.
+// Adds a row's parts. D/4 lanes have four columns of a row each; they are all
+// that a row has, or (SPLIT, for few rows) a block has one row, whose parts its
+// 1024/D groups of lanes take in turn.
 template <class T, int D, bool SPLIT>
 __global__ void __launch_bounds__(256) join_kernel(AttentionArgs a) {
-  constexpr int E = D / 64;
-  constexpr uint32_t WAVES = SPLIT ? 4 : 1;
-  const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const uint32_t row = SPLIT ? blockIdx.x : blockIdx.x * 4 + wave, w0 = SPLIT ? wave : 0;
-  if (row >= a.batch * a.queries * a.heads) return;
+  constexpr uint32_t L = D / 4, GROUPS = 256 / L, STREAMS = SPLIT ? GROUPS : 1;
+  const uint32_t ln = threadIdx.x % L, group = threadIdx.x / L, rows = a.batch * a.queries * a.heads;
+  const uint32_t stream = SPLIT ? group : 0;
+  const uint32_t own_row = SPLIT ? blockIdx.x : blockIdx.x * GROUPS + group;
+  const uint32_t row = min(own_row, rows - 1);  // lanes past the last row repeat it and store nothing
   const uint32_t tok = row / a.heads, hq = row % a.heads, b = tok / a.queries, head = hq / a.share, g = hq % a.share;
   const uint32_t up = units_of(a.prefix.tokens), prefix_units = a.kv_heads * a.tp.tiles * up;
-  uint32_t own_each = 0, own_begin = 0, total = prefix_units;
+  uint32_t own_each = 0, own_begin = prefix_units, total = prefix_units;
   if (a.own.tokens) {
     own_each = units_of(own_length(a, b));
-    const OwnLine line = own_line(a, 0);
-    own_begin = prefix_units + own_units_before(a, line, b);
-    total += own_units_before(a, line, a.batch);
+    for (uint32_t b0 = 0; b0 < a.batch; b0 += 64) {
+      const OwnLine line = own_line(a, b0);
+      const uint32_t at = b - b0 - 1, end = __shfl(line.end, at % 64);
+      if (b == b0) own_begin = total;
+      if (at < 63) own_begin = total + end;
+      total += __builtin_amdgcn_readlane(line.end, 63);
+    }
   }
   const uint32_t blocks = min(a.blocks, total);
   // the row's parts: over the prefix, then over its own keys
@@ -961,72 +1006,68 @@ __global__ void __launch_bounds__(256) join_kernel(AttentionArgs a) {
     slot[1] = first + a.kv_heads * a.tp.tiles + b * a.kv_heads * a.to.tiles + y;
     count[1] = block_of(u + own_each - 1, total, blocks) - first + 1;
   }
-  const uint32_t parts = (count[0] + count[1] + WAVES - 1 - w0) / WAVES;  // of this wave
-  auto place = [&](uint32_t x) {
-    const uint32_t i = x * WAVES + w0;
+  const uint32_t parts = (count[0] + count[1] + STREAMS - 1 - stream) / STREAMS;  // of this group
+  const auto place = [&](uint32_t x) {
+    const uint32_t i = x * STREAMS + stream;
     return i < count[0] ? (uint64_t)(slot[0] + i) * a.part_rows + at[0]
                         : (uint64_t)(slot[1] + i - count[0]) * a.part_rows + at[1];
   };
-  float m = -INFINITY, l = 0.0f, o[E];
-  for (int e = 0; e < E; ++e) o[e] = 0.0f;
-  for (uint32_t i0 = 0; i0 < parts; i0 += 64) {
-    const uint32_t some = min(64u, parts - i0);
+  const auto add = [](float4& o, float f, float4 p) {
+    // a part without a key has no output either (it may hold anything's product with 0)
+    if (f != 0.0f) o.x += f * p.x, o.y += f * p.y, o.z += f * p.z, o.w += f * p.w;
+  };
+  float m = -INFINITY, l = 0.0f;
+  float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (uint32_t i0 = 0; i0 < parts; i0 += L) {
+    const uint32_t some = min(L, parts - i0);
     float mi = -INFINITY, li = 0.0f;
-    if (lane < some) {
-      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * place(i0 + lane));
+    if (ln < some) {
+      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * place(i0 + ln));
       mi = ml.x, li = ml.y;
     }
     float top = mi;
-    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    for (uint32_t d = L / 2; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
     const float now = fmaxf(m, top);
     const float f0 = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - now);
     const float fi = mi == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mi - now);
     float sum = fi * li;
-    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+    for (uint32_t d = L / 2; d; d >>= 1) sum += __shfl_xor(sum, d);
     l = l * f0 + sum, m = now;
-    for (int e = 0; e < E; ++e) o[e] *= f0;
+    o.x *= f0, o.y *= f0, o.z *= f0, o.w *= f0;
     for (uint32_t i = 0; i < some; i += kAhead) {
-      float p[kAhead][E];  // their loads in flight together; past the last part, it again with weight 0
+      float4 p[kAhead];  // their loads in flight together; past the last part, it again with weight 0
+#pragma unroll
+      for (uint32_t j = 0; j < kAhead; ++j)
+        p[j] = *reinterpret_cast<const float4*>(a.part_o + place(i0 + min(i + j, some - 1)) * D + ln * 4);
 #pragma unroll
       for (uint32_t j = 0; j < kAhead; ++j) {
-        const float* q = a.part_o + place(i0 + min(i + j, some - 1)) * D + lane * E;
-#pragma unroll
-        for (int e = 0; e < E; ++e) p[j][e] = q[e];
-      }
-#pragma unroll
-      for (uint32_t j = 0; j < kAhead; ++j) {
-        const float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(uint32_t, fi), (i + j) % 64));
-        // a part without a key has no output either (it may hold anything's product with 0)
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] += i + j < some && f != 0.0f ? f * p[j][e] : 0.0f;
+        const float f = __shfl(fi, (i + j) % L, L);
+        add(o, i + j < some ? f : 0.0f, p[j]);
       }
     }
   }
   if constexpr (SPLIT) {
-    __shared__ float s_m[4], s_l[4], s_o[4][D];
-    if (lane == 0) s_m[wave] = m, s_l[wave] = l;
-    for (int e = 0; e < E; ++e) s_o[wave][lane * E + e] = o[e];
+    __shared__ float s_m[GROUPS], s_l[GROUPS];
+    __shared__ float4 s_o[GROUPS][L];
+    if (ln == 0) s_m[group] = m, s_l[group] = l;
+    s_o[group][ln] = o;
     __syncthreads();
-    if (wave != 0) return;
-    m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-    l = 0.0f;
-    for (int e = 0; e < E; ++e) o[e] = 0.0f;
-    for (int w = 0; w < 4; ++w) {
+    if (group != 0) return;
+    m = -INFINITY, l = 0.0f;
+    for (uint32_t w = 0; w < GROUPS; ++w) m = fmaxf(m, s_m[w]);
+    o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (uint32_t w = 0; w < GROUPS; ++w) {
       const float f = s_m[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(s_m[w] - m);
       l += f * s_l[w];
-      for (int e = 0; e < E; ++e) o[e] += f != 0.0f ? f * s_o[w][lane * E + e] : 0.0f;
+      add(o, f, s_o[w][ln]);
     }
   }
+  if (own_row >= rows) return;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  if (lane * E < a.dim) {
-    uint16_t* q = a.out + (uint64_t)row * a.dim + lane * E;
-    if constexpr (E == 1) {
-      q[0] = (uint16_t)pack<T>(o[0] * inv, 0.0f);
-    } else {
-      for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t*>(q + e) = pack<T>(o[e] * inv, o[e + 1] * inv);
-    }
-  }
-  if (lane == 0) {
+  if (ln * 4 < a.dim)
+    *reinterpret_cast<u32x2*>(a.out + (uint64_t)row * a.dim + ln * 4) =
+        u32x2{pack<T>(o.x * inv, o.y * inv), pack<T>(o.z * inv, o.w * inv)};
+  if (ln == 0) {
     if (a.lse) a.lse[row] = l == 0.0f ? -INFINITY : m / kLog2e + logf(l);
     if (a.row_ml) a.row_ml[2 * row] = l == 0.0f ? 0.0f : m, a.row_ml[2 * row + 1] = inv;
   }
@@ -1056,7 +1097,8 @@ static Tiling tiling(uint64_t rows, uint32_t r) {
   return t;
 }
 
-constexpr uint64_t kSoloKeys = 2048;
+constexpr uint64_t kSoloKeys = 768, kSoloKeysMany = 1024;  // keys up to which a block takes a sequence and head
+constexpr uint64_t kFewUnits = 10;                         // of a compute unit
 
 struct AttentionPlan {
   AttentionArgs a;
@@ -1105,7 +1147,8 @@ static hl_status attention_plan(const hl_attention* h, bool weights, AttentionPl
   a.prefix = kv_of(h->prefix), a.own = kv_of(h->own);
   a.batch = h->batch, a.queries = h->queries, a.heads = h->heads, a.kv_heads = h->kv_heads, a.dim = h->dim;
   a.share = h->heads / h->kv_heads;
-  a.scale2 = h->scale * kLog2e;
+  a.scale2 = h->scale == 0.0f ? 1.0f : fabsf(h->scale) * kLog2e;
+  a.q_and = h->scale == 0.0f ? 0 : ~0u, a.q_xor = h->scale < 0.0f ? 0x80008000u : 0;
   const uint64_t shared_rows = (uint64_t)h->batch * h->queries * a.share, own_rows = (uint64_t)h->queries * a.share;
   const uint32_t r = std::max(shared_rows, own_rows) > 64 && h->dim <= 128 ? 2 : 1;
   a.tp = tiling(shared_rows, r), a.to = tiling(own_rows, r);
@@ -1113,7 +1156,12 @@ static hl_status attention_plan(const hl_attention* h, bool weights, AttentionPl
   const uint64_t units = (uint64_t)h->kv_heads * ((uint64_t)a.tp.tiles * units_of(a.prefix.tokens) +
                                                   (uint64_t)h->batch * a.to.tiles * units_of(a.own.tokens));
   if (units >= (1ull << 31)) return HL_EUNSUPPORTED;
-  a.blocks = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>((uint64_t)device_cus() * 2, units));
+  // A unit a block while that fills no more than two blocks a compute unit.
+  // Beyond, two hide each other's waits; but each block leaves a part, and where
+  // there is little to read and to compute, one a compute unit writes less.
+  const uint64_t cus = (uint64_t)device_cus();
+  const uint64_t few = r < 2 && units > 2 * cus && units <= kFewUnits * cus ? 1 : 2;
+  a.blocks = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(cus * few, units));
   a.part_rows = std::max(a.tp.rows(), a.to.rows());
   const uint32_t held = h->dim <= 64 ? 64 : h->dim <= 128 ? 128 : 256;
   const uint64_t slots = a.blocks + items;
@@ -1126,7 +1174,8 @@ static hl_status attention_plan(const hl_attention* h, bool weights, AttentionPl
   // A block a sequence and key head where that is short: it reads the prefix
   // again for each sequence (from the L2s, as far as it is the same), and saves
   // the second kernel.
-  pl->solo = own_rows <= 16 && a.prefix.tokens + a.own.tokens <= kSoloKeys;
+  pl->solo = own_rows <= 16 && a.prefix.tokens + a.own.tokens <=
+                                   ((uint64_t)h->batch * h->kv_heads * 2 >= cus ? kSoloKeysMany : kSoloKeys);
   pl->part_o = take(slots * a.part_rows * held);
   pl->part_ml = take(slots * a.part_rows * 2);
   a.score_stride = (a.own.tokens + kStep - 1) / kStep * kStep;
@@ -1144,7 +1193,7 @@ static hl_status run(const AttentionArgs& a, hipStream_t s) {
   // A block a row while that fills the card: each of the row's parts is a trip
   // to memory, and few rows have many.
   st = rows <= kSplitRows ? enqueue(join_kernel<T, D, true>, dim3(rows), dim3(256), s, a)
-                          : enqueue(join_kernel<T, D, false>, dim3((rows + 3) / 4), dim3(256), s, a);
+                          : enqueue(join_kernel<T, D, false>, dim3((rows + 1024 / D - 1) / (1024 / D)), dim3(256), s, a);
   if (st != HL_OK || !a.scores) return st;
   return enqueue(weights_kernel, dim3((a.own.tokens + 255) / 256, a.kv_heads, a.batch), dim3(256), s, a);
 }
