@@ -1098,7 +1098,6 @@ static Tiling tiling(uint64_t rows, uint32_t r) {
 }
 
 constexpr uint64_t kSoloKeys = 768, kSoloKeysMany = 1024;  // keys up to which a block takes a sequence and head
-constexpr uint64_t kFewUnits = 10;                         // of a compute unit
 
 struct AttentionPlan {
   AttentionArgs a;
@@ -1156,12 +1155,9 @@ static hl_status attention_plan(const hl_attention* h, bool weights, AttentionPl
   const uint64_t units = (uint64_t)h->kv_heads * ((uint64_t)a.tp.tiles * units_of(a.prefix.tokens) +
                                                   (uint64_t)h->batch * a.to.tiles * units_of(a.own.tokens));
   if (units >= (1ull << 31)) return HL_EUNSUPPORTED;
-  // A unit a block while that fills no more than two blocks a compute unit.
-  // Beyond, two hide each other's waits; but each block leaves a part, and where
-  // there is little to read and to compute, one a compute unit writes less.
+  // two blocks a compute unit: what their registers allow, and they hide each other's waits
   const uint64_t cus = (uint64_t)device_cus();
-  const uint64_t few = r < 2 && units > 2 * cus && units <= kFewUnits * cus ? 1 : 2;
-  a.blocks = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(cus * few, units));
+  a.blocks = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(cus * 2, units));
   a.part_rows = std::max(a.tp.rows(), a.to.rows());
   const uint32_t held = h->dim <= 64 ? 64 : h->dim <= 128 ? 128 : 256;
   const uint64_t slots = a.blocks + items;
