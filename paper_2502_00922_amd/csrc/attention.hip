@@ -7,13 +7,12 @@
 // one key head that see the same keys form an item: over the prefix, the rows
 // of the whole batch (so the prefix is read once for all of them), over an own
 // cache, the rows of its sequence; up to 128 rows an item, more items beyond.
-// Every item's keys are cut into units of 128, all units stand in one line
-// (the prefix's items, then the sequences'), and each block takes an equal
-// stretch of the line, whatever the lengths are. It walks an item's keys with
-// the running maximum and sum of the softmax and leaves (maximum, sum,
-// unnormalised output) of its part in the workspace; the join kernel adds the
-// parts of each row. Lengths are read on the device; nothing depends on the
-// order in which blocks run, and there are no atomics.
+// Every item's keys are cut into units of 128, and each block takes an equal
+// stretch of units, whatever the lengths are. It walks an item's keys with the
+// running maximum and sum of the softmax and leaves (maximum, sum, unnormalised
+// output) of its part in the workspace; the join kernel adds the parts of each
+// row. Lengths are read on the device; nothing depends on the order in which
+// blocks run, and there are no atomics.
 //
 // Items of up to 16 rows (a decode step's own caches) are "narrow": the four
 // waves of a block take different keys, 32 at a time, straight from memory to
@@ -21,7 +20,9 @@
 // and their four results are added in LDS at the end. Larger items are "wide":
 // the four waves have different rows and the same keys, which the block loads
 // from memory to LDS without registers between, 32 at a time and up to three
-// times ahead, so that memory is read once for up to 128 rows.
+// times ahead, so that memory is read once for up to 128 rows. The narrow
+// items' units stand in one line and the wide items' in another, and the blocks
+// are divided between the two by their units.
 //
 // The matrix instruction takes K as its left operand and Q as its right, so a
 // lane ends up with scores of one query (lane % 16), which is also what the
@@ -41,8 +42,12 @@
 namespace hl {
 
 constexpr uint32_t kUnit = 128;        // keys of a unit
-constexpr uint32_t kWaves = 4;         // of a block
 constexpr uint32_t kStep = 32;         // keys of a wave's step
+constexpr uint32_t kWaves = 4;         // of a block
+// Units of a wide stretch, at least, where there are enough, for one and two
+// 16-row tiles a wave: it leaves 64 rows, as many bytes as a unit has, or 128,
+// which take long enough to compute that more blocks pay.
+constexpr uint32_t kLeastWide[3] = {1, 2, 1};
 constexpr uint32_t kThreads = 64 * kWaves;
 constexpr float kSlack = 8.0f;         // powers of two that a score may pass the maximum kept for it by
 constexpr float kLog2e = 1.44269504088896341f;
@@ -76,9 +81,9 @@ struct AttentionArgs {
   float* lse;
   const float* weight_in;
   float* weight_out;
-  float *part_o, *part_ml, *row_ml, *scores;  // workspace
+  float *wide_o, *wide_ml, *narrow_o, *narrow_ml, *row_ml, *scores;  // workspace
   uint32_t batch, queries, heads, kv_heads, dim, share;  // share: query heads of a key head
-  uint32_t blocks, part_rows, score_stride;
+  uint32_t blocks, wide_rows, narrow_rows, score_stride;  // rows: of a part's place in the workspace
   Tiling tp, to;
   float scale2;  // |scale| * log2(e), or 1: scores are kept in powers of two
   uint32_t q_and, q_xor;  // on pairs of q: its sign is the scale's, and it is 0 where the scale is
@@ -104,7 +109,7 @@ __device__ inline uint32_t scan_lanes(uint32_t v) {
   return v;
 }
 
-// The own caches' part of the line: sequence after sequence, 64 at a time a
+// The own caches' part of their line: sequence after sequence, 64 at a time a
 // lane each. `each`: units of one of a sequence's items, `end`: where its units
 // end, from where the 64 sequences' begin.
 struct OwnLine {
@@ -151,11 +156,38 @@ __device__ inline OwnPlace own_place(const AttentionArgs& a, const OwnLine& o, u
   return {a.batch - 1, base, 1};  // past the line's end: no caller asks
 }
 
-// The block that unit u of `total` is in when `blocks` share them, at most one
-// block a unit: block k has floor(k*total/blocks) up to
-// floor((k+1)*total/blocks), never none.
-__device__ inline uint32_t block_of(uint32_t u, uint32_t total, uint32_t blocks) {
-  return (uint32_t)((((uint64_t)u + 1) * blocks - 1) / total);
+// A line of units and those that share it, `takers` at most one a unit: taker k
+// has units floor(k*total/takers) up to floor((k+1)*total/takers), never none.
+struct Line {
+  uint32_t total, takers;
+  __device__ uint32_t first(uint32_t k) const { return (uint32_t)((uint64_t)k * total / takers); }
+  __device__ uint32_t taker(uint32_t u) const { return (uint32_t)((((uint64_t)u + 1) * takers - 1) / total); }
+};
+
+// Both lines; `wide_blocks` of the blocks, a multiple of 8, take the wide one.
+struct Lines {
+  Line wide, narrow;
+  uint32_t prefix_units, wide_blocks;
+};
+
+__device__ inline Lines lines_of(const AttentionArgs& a, uint32_t own_units) {
+  Lines l;
+  l.prefix_units = a.kv_heads * a.tp.tiles * units_of(a.prefix.tokens);
+  l.wide.total = (a.tp.r ? l.prefix_units : 0) + (a.to.r ? own_units : 0);
+  l.narrow.total = l.prefix_units + own_units - l.wide.total;
+  uint32_t w = 0;
+  if (l.wide.total) {
+    w = a.blocks;
+    if (l.narrow.total) w = (uint32_t)((uint64_t)a.blocks * l.wide.total / (l.wide.total + l.narrow.total));
+    const uint32_t least = max(a.tp.r, a.to.r) == 2 ? kLeastWide[2] : kLeastWide[1];
+    w = min(w, (l.wide.total + least - 1) / least);
+    w = min((w + 7) / 8 * 8, a.blocks - (l.narrow.total ? 8 : 0));
+    w = max(w, 8u);
+  }
+  l.wide_blocks = w;
+  l.wide.takers = min(w, l.wide.total);
+  l.narrow.takers = min(a.blocks - w, l.narrow.total);
+  return l;
 }
 
 template <class T>
@@ -671,11 +703,11 @@ __device__ inline void narrow_part(const AttentionArgs& a, const Item& it, uint3
                                    float* lds) {
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   State<D, 1> st;
-  begin<D, FULL, 1>(st, a, it, it.row0);
+  begin<D, FULL, 1>(st, a, it, 0);
   narrow_keys<T, D, FULL>(st, a, it, k0 + kStep * wave, k1, kUnit);
-  float* po = a.part_o + (uint64_t)slot * a.part_rows * D;
-  float* pml = a.part_ml + (uint64_t)slot * a.part_rows * 2;
-  add_waves<D, kWaves>(st, min(16u, it.rows - it.row0), lds,
+  float* po = a.narrow_o + (uint64_t)slot * a.narrow_rows * D;
+  float* pml = a.narrow_ml + (uint64_t)slot * a.narrow_rows * 2;
+  add_waves<D, kWaves>(st, it.rows, lds,
                        [&](uint32_t row, uint32_t d, float4 o, float m, float l) {
                          *reinterpret_cast<float4*>(po + (uint64_t)row * D + d) = o;
                          if (d == 0) pml[2 * row] = m, pml[2 * row + 1] = l;
@@ -824,8 +856,8 @@ __device__ inline void wide_part(const AttentionArgs& a, const Item& it, uint32_
   }
   if (__any(st.odd != 0)) add_beyond<T, D, FULL, R, true>(st, it, a.dim, k0 + whole * kStep, mine, kStep);
   __syncthreads();  // the buffers are free
-  float* po = a.part_o + (uint64_t)slot * a.part_rows * D;
-  float* pml = a.part_ml + (uint64_t)slot * a.part_rows * 2;
+  float* po = a.wide_o + (uint64_t)slot * a.wide_rows * D;
+  float* pml = a.wide_ml + (uint64_t)slot * a.wide_rows * 2;
 #pragma unroll
   for (int rt = 0; rt < R; ++rt) {
     const float sum = over_lanes(st.l[rt]);
@@ -836,13 +868,6 @@ __device__ inline void wide_part(const AttentionArgs& a, const Item& it, uint32_
     for (int i = 0; i < S::TILES; ++i)
       *reinterpret_cast<f32x4*>(po + (uint64_t)row * D + 16 * i + 4 * c) = st.o[rt][i];
   }
-}
-
-// Blocks that stand next to each other in the line go to the same XCD, where
-// the row tiles of one head find its keys in the L2 (blocks are dealt to the 8
-// XCDs in turn).
-__device__ inline uint32_t line_block(uint32_t blocks) {
-  return blocks % 8 ? blockIdx.x : blockIdx.x % 8 * (blocks / 8) + blockIdx.x / 8;
 }
 
 // A head's rows of the whole batch over the prefix, from row0 on.
@@ -869,36 +894,61 @@ __device__ inline Item own_item(const AttentionArgs& a, uint32_t b, uint32_t hea
   return it;
 }
 
+// Unit u of a line: its item, the unit's number in it, and the item's units.
+struct Place {
+  Item it;
+  uint32_t item, in, each;
+};
+
+// WIDE: of the wide line. Its items are numbered the prefix's first, then the
+// sequences'. Whole wave.
+template <bool WIDE>
+__device__ inline Place place_of(const AttentionArgs& a, const OwnLine& line, const Lines& l, uint32_t u) {
+  Place p;
+  const bool has_prefix = WIDE == (a.tp.r != 0);
+  const uint32_t before = has_prefix ? l.prefix_units : 0;
+  if (u < before) {
+    p.each = units_of(a.prefix.tokens), p.item = u / p.each, p.in = u % p.each;
+    p.it = prefix_item(a, p.item / a.tp.tiles, p.item % a.tp.tiles * a.tp.rows());
+  } else {
+    const OwnPlace own = own_place(a, line, u - before);
+    const uint32_t x = u - before - own.begin, y = x / own.each;
+    p.each = own.each, p.in = x % own.each;
+    p.item = (has_prefix ? a.kv_heads * a.tp.tiles : 0) + own.b * a.kv_heads * a.to.tiles + y;
+    p.it = own_item(a, own.b, y / a.to.tiles, y % a.to.tiles * a.to.rows());
+  }
+  return p;
+}
+
 // RW: 16-row tiles of a wave in wide items (0: the call has none).
 template <class T, int D, bool FULL, int RW>
 __global__ void __launch_bounds__(kThreads, 2) parts_kernel(AttentionArgs a) {
   __shared__ __attribute__((aligned(16))) float lds[lds_floats<D, RW>()];
-  const uint32_t up = units_of(a.prefix.tokens), prefix_units = a.kv_heads * a.tp.tiles * up;
   const OwnLine line = a.own.tokens ? own_line(a, 0) : OwnLine{0, 0, 0};
-  const uint32_t total = prefix_units + own_units_before(a, line, a.batch);
-  const uint32_t blk = line_block(a.blocks), blocks = min(a.blocks, total);
-  if (blk >= blocks) return;
-  uint32_t u = (uint32_t)((uint64_t)blk * total / blocks);
-  const uint32_t end = (uint32_t)(((uint64_t)blk + 1) * total / blocks);
-  while (u < end) {
-    Item it;
-    uint32_t item, in, each;
-    const bool shared = u < prefix_units;
-    if (shared) {
-      item = u / up, in = u % up, each = up;
-      it = prefix_item(a, item / a.tp.tiles, item % a.tp.tiles * a.tp.rows());
-    } else {
-      const OwnPlace pl = own_place(a, line, u - prefix_units);
-      const uint32_t x = u - prefix_units - pl.begin, y = x / pl.each;
-      in = x % pl.each, each = pl.each;
-      item = a.kv_heads * a.tp.tiles + pl.b * a.kv_heads * a.to.tiles + y;
-      it = own_item(a, pl.b, y / a.to.tiles, y % a.to.tiles * a.to.rows());
+  const Lines l = lines_of(a, own_units_before(a, line, a.batch));
+  // Blocks are dealt to the 8 XCDs in turn. Each XCD has its share of both
+  // lines, and takers that stand next to each other, so that the row tiles of a
+  // head find its keys in the L2.
+  const uint32_t xcd = blockIdx.x % 8, nth = blockIdx.x / 8, wide = l.wide_blocks / 8;
+  if (RW && nth < wide) {
+    const uint32_t taker = xcd * wide + nth;
+    if (taker >= l.wide.takers) return;
+    const uint32_t end = l.wide.first(taker + 1);
+    for (uint32_t u = l.wide.first(taker); u < end;) {
+      const Place p = place_of<true>(a, line, l, u);
+      const uint32_t take = min(p.each - p.in, end - u);
+      wide_part<T, D, FULL, RW ? RW : 1>(a, p.it, p.in * kUnit, (p.in + take) * kUnit, taker + p.item, lds);
+      u += take;
     }
-    const uint32_t take = min(each - in, end - u);
-    if (RW == 0 || !(shared ? a.tp.r : a.to.r))
-      narrow_part<T, D, FULL>(a, it, in * kUnit, (in + take) * kUnit, blk + item, lds);
-    else
-      wide_part<T, D, FULL, RW ? RW : 1>(a, it, in * kUnit, (in + take) * kUnit, blk + item, lds);
+    return;
+  }
+  const uint32_t taker = xcd * (a.blocks / 8 - wide) + nth - wide;
+  if (taker >= l.narrow.takers) return;
+  const uint32_t end = l.narrow.first(taker + 1);
+  for (uint32_t u = l.narrow.first(taker); u < end;) {
+    const Place p = place_of<false>(a, line, l, u);
+    const uint32_t take = min(p.each - p.in, end - u);
+    narrow_part<T, D, FULL>(a, p.it, p.in * kUnit, (p.in + take) * kUnit, taker + p.item, lds);
     u += take;
   }
 }
@@ -978,40 +1028,43 @@ __global__ void __launch_bounds__(256) join_kernel(AttentionArgs a) {
   const uint32_t own_row = SPLIT ? blockIdx.x : blockIdx.x * GROUPS + group;
   const uint32_t row = min(own_row, rows - 1);  // lanes past the last row repeat it and store nothing
   const uint32_t tok = row / a.heads, hq = row % a.heads, b = tok / a.queries, head = hq / a.share, g = hq % a.share;
-  const uint32_t up = units_of(a.prefix.tokens), prefix_units = a.kv_heads * a.tp.tiles * up;
-  uint32_t own_each = 0, own_begin = prefix_units, total = prefix_units;
+  const uint32_t up = units_of(a.prefix.tokens);
+  uint32_t own_each = 0, own_begin = 0, own_units = 0;
   if (a.own.tokens) {
     own_each = units_of(own_length(a, b));
     for (uint32_t b0 = 0; b0 < a.batch; b0 += 64) {
       const OwnLine line = own_line(a, b0);
       const uint32_t at = b - b0 - 1, end = __shfl(line.end, at % 64);
-      if (b == b0) own_begin = total;
-      if (at < 63) own_begin = total + end;
-      total += __builtin_amdgcn_readlane(line.end, 63);
+      if (b == b0) own_begin = own_units;
+      if (at < 63) own_begin = own_units + end;
+      own_units += __builtin_amdgcn_readlane(line.end, 63);
     }
   }
-  const uint32_t blocks = min(a.blocks, total);
+  const Lines lines = lines_of(a, own_units);
   // the row's parts: over the prefix, then over its own keys
-  uint32_t slot[2] = {0, 0}, at[2], count[2] = {0, 0};
-  const uint32_t rp = tok * a.share + g, ro = tok % a.queries * a.share + g;
-  at[0] = rp % a.tp.rows(), at[1] = ro % a.to.rows();
+  const float2* part_ml[2];
+  const float* part_o[2];
+  uint32_t part_step[2], count[2] = {0, 0};
+  const auto find = [&](int x, const Tiling& tl, uint32_t r, uint32_t item, uint32_t u, uint32_t each) {
+    const Line line = tl.r ? lines.wide : lines.narrow;
+    const uint32_t first = line.taker(u), rows = tl.r ? a.wide_rows : a.narrow_rows;
+    const uint64_t at = (uint64_t)(first + item) * rows + r % tl.rows();
+    count[x] = line.taker(u + each - 1) - first + 1, part_step[x] = rows;
+    part_ml[x] = reinterpret_cast<const float2*>(tl.r ? a.wide_ml : a.narrow_ml) + at;
+    part_o[x] = (tl.r ? a.wide_o : a.narrow_o) + at * D + ln * 4;
+  };
+  part_ml[0] = part_ml[1] = nullptr, part_o[0] = part_o[1] = nullptr, part_step[0] = part_step[1] = 0;
+  const bool mixed = (a.tp.r != 0) == (a.to.r != 0);  // one line has both
   if (up) {
-    const uint32_t item = head * a.tp.tiles + rp / a.tp.rows(), u = item * up;
-    const uint32_t first = block_of(u, total, blocks);
-    slot[0] = first + item, count[0] = block_of(u + up - 1, total, blocks) - first + 1;
+    const uint32_t r = tok * a.share + g, item = head * a.tp.tiles + r / a.tp.rows();
+    find(0, a.tp, r, item, item * up, up);
   }
   if (own_each) {
-    const uint32_t y = head * a.to.tiles + ro / a.to.rows(), u = own_begin + y * own_each;
-    const uint32_t first = block_of(u, total, blocks);
-    slot[1] = first + a.kv_heads * a.tp.tiles + b * a.kv_heads * a.to.tiles + y;
-    count[1] = block_of(u + own_each - 1, total, blocks) - first + 1;
+    const uint32_t r = tok % a.queries * a.share + g, y = head * a.to.tiles + r / a.to.rows();
+    find(1, a.to, r, (mixed ? a.kv_heads * a.tp.tiles : 0) + b * a.kv_heads * a.to.tiles + y,
+         (mixed ? lines.prefix_units : 0) + own_begin + y * own_each, own_each);
   }
   const uint32_t parts = (count[0] + count[1] + STREAMS - 1 - stream) / STREAMS;  // of this group
-  const auto place = [&](uint32_t x) {
-    const uint32_t i = x * STREAMS + stream;
-    return i < count[0] ? (uint64_t)(slot[0] + i) * a.part_rows + at[0]
-                        : (uint64_t)(slot[1] + i - count[0]) * a.part_rows + at[1];
-  };
   const auto add = [](float4& o, float f, float4 p) {
     // a part without a key has no output either (it may hold anything's product with 0)
     if (f != 0.0f) o.x += f * p.x, o.y += f * p.y, o.z += f * p.z, o.w += f * p.w;
@@ -1022,7 +1075,9 @@ __global__ void __launch_bounds__(256) join_kernel(AttentionArgs a) {
     const uint32_t some = min(L, parts - i0);
     float mi = -INFINITY, li = 0.0f;
     if (ln < some) {
-      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * place(i0 + ln));
+      const uint32_t i = (i0 + ln) * STREAMS + stream;
+      const float2 ml = i < count[0] ? part_ml[0][(uint64_t)i * part_step[0]]
+                                     : part_ml[1][(uint64_t)(i - count[0]) * part_step[1]];
       mi = ml.x, li = ml.y;
     }
     float top = mi;
@@ -1037,8 +1092,12 @@ __global__ void __launch_bounds__(256) join_kernel(AttentionArgs a) {
     for (uint32_t i = 0; i < some; i += kAhead) {
       float4 p[kAhead];  // their loads in flight together; past the last part, it again with weight 0
 #pragma unroll
-      for (uint32_t j = 0; j < kAhead; ++j)
-        p[j] = *reinterpret_cast<const float4*>(a.part_o + place(i0 + min(i + j, some - 1)) * D + ln * 4);
+      for (uint32_t j = 0; j < kAhead; ++j) {
+        const uint32_t x = (i0 + min(i + j, some - 1)) * STREAMS + stream;
+        p[j] = *reinterpret_cast<const float4*>(
+            x < count[0] ? part_o[0] + (uint64_t)x * part_step[0] * D
+                         : part_o[1] + (uint64_t)(x - count[0]) * part_step[1] * D);
+      }
 #pragma unroll
       for (uint32_t j = 0; j < kAhead; ++j) {
         const float f = __shfl(fi, (i + j) % L, L);
@@ -1101,8 +1160,8 @@ constexpr uint64_t kSoloKeys = 768, kSoloKeysMany = 1024;  // keys up to which a
 
 struct AttentionPlan {
   AttentionArgs a;
-  uint64_t bytes, part_o, part_ml, row_ml, scores;  // of the workspace: its size and its parts' places
-  bool solo;
+  uint64_t bytes, wide_o, wide_ml, narrow_o, narrow_ml, row_ml, scores;  // of the workspace: its size and its parts' places
+  bool solo, wide;  // wide: whether the call has wide items
 };
 
 static hl_status check_kv(const hl_kv& s, uint64_t tokens, uint32_t dim, bool sequences) {
@@ -1151,16 +1210,22 @@ static hl_status attention_plan(const hl_attention* h, bool weights, AttentionPl
   const uint64_t shared_rows = (uint64_t)h->batch * h->queries * a.share, own_rows = (uint64_t)h->queries * a.share;
   const uint32_t r = std::max(shared_rows, own_rows) > 64 && h->dim <= 128 ? 2 : 1;
   a.tp = tiling(shared_rows, r), a.to = tiling(own_rows, r);
-  const uint64_t items = (uint64_t)h->kv_heads * (a.tp.tiles + (uint64_t)h->batch * a.to.tiles);
-  const uint64_t units = (uint64_t)h->kv_heads * ((uint64_t)a.tp.tiles * units_of(a.prefix.tokens) +
-                                                  (uint64_t)h->batch * a.to.tiles * units_of(a.own.tokens));
-  if (units >= (1ull << 31)) return HL_EUNSUPPORTED;
-  // two blocks a compute unit: what their registers allow, and they hide each other's waits
-  const uint64_t cus = (uint64_t)device_cus();
-  a.blocks = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(cus * 2, units));
-  a.part_rows = std::max(a.tp.rows(), a.to.rows());
+  // most that the lengths can come to, of each line
+  const uint64_t prefix_items = (uint64_t)h->kv_heads * a.tp.tiles, own_items = (uint64_t)h->batch * h->kv_heads * a.to.tiles;
+  const uint64_t prefix_units = prefix_items * units_of(a.prefix.tokens), own_units = own_items * units_of(a.own.tokens);
+  const uint64_t wide_units = (a.tp.r ? prefix_units : 0) + (a.to.r ? own_units : 0);
+  const uint64_t narrow_units = prefix_units + own_units - wide_units;
+  if (prefix_units + own_units >= (1ull << 31)) return HL_EUNSUPPORTED;
+  // two blocks a compute unit: what their registers allow, and they hide each
+  // other's waits; a multiple of 8, for the XCDs
+  const uint64_t cus = (uint64_t)device_cus(), most = std::max<uint64_t>(16, cus * 2 / 8 * 8);
+  const uint64_t asked = wide_units / kLeastWide[r] + narrow_units + 15;
+  a.blocks = (uint32_t)std::min<uint64_t>(most, std::max<uint64_t>(16, asked / 8 * 8));
+  a.wide_rows = std::max(a.tp.r ? a.tp.rows() : 0, a.to.r ? a.to.rows() : 0);
+  a.narrow_rows = (uint32_t)std::min<uint64_t>(16, std::max(a.tp.r ? 0 : shared_rows, a.to.r ? 0 : own_rows));
   const uint32_t held = h->dim <= 64 ? 64 : h->dim <= 128 ? 128 : 256;
-  const uint64_t slots = a.blocks + items;
+  const uint64_t wide_slots = wide_units ? a.blocks + prefix_items + own_items : 0;
+  const uint64_t narrow_slots = narrow_units ? a.blocks + prefix_items + own_items : 0;
   uint64_t n = 0;
   auto take = [&](uint64_t floats) {
     const uint64_t at = n;
@@ -1172,8 +1237,9 @@ static hl_status attention_plan(const hl_attention* h, bool weights, AttentionPl
   // the second kernel.
   pl->solo = own_rows <= 16 && a.prefix.tokens + a.own.tokens <=
                                    ((uint64_t)h->batch * h->kv_heads * 2 >= cus ? kSoloKeysMany : kSoloKeys);
-  pl->part_o = take(slots * a.part_rows * held);
-  pl->part_ml = take(slots * a.part_rows * 2);
+  pl->wide = wide_units != 0;
+  pl->wide_o = take(wide_slots * a.wide_rows * held), pl->wide_ml = take(wide_slots * a.wide_rows * 2);
+  pl->narrow_o = take(narrow_slots * a.narrow_rows * held), pl->narrow_ml = take(narrow_slots * a.narrow_rows * 2);
   a.score_stride = (a.own.tokens + kStep - 1) / kStep * kStep;
   pl->row_ml = weights ? take(rows * 2) : 0;
   pl->scores = weights ? take((uint64_t)h->batch * h->heads * h->queries * a.score_stride) : 0;
@@ -1195,10 +1261,11 @@ static hl_status run(const AttentionArgs& a, hipStream_t s) {
 }
 
 template <class T, int D, bool FULL>
-static hl_status run_rows(const AttentionArgs& a, bool solo, hipStream_t s) {
-  if (solo) return enqueue(solo_kernel<T, D, FULL>, dim3(a.kv_heads, a.batch), dim3(kSoloWaves * 64), s, a);
+static hl_status run_rows(const AttentionPlan& pl, hipStream_t s) {
+  const AttentionArgs& a = pl.a;
+  if (pl.solo) return enqueue(solo_kernel<T, D, FULL>, dim3(a.kv_heads, a.batch), dim3(kSoloWaves * 64), s, a);
   const uint32_t r = std::max(a.tp.r, a.to.r);
-  if (r == 0) return run<T, D, FULL, 0>(a, s);
+  if (!pl.wide) return run<T, D, FULL, 0>(a, s);
   if constexpr (D <= 128) {
     if (r == 2) return run<T, D, FULL, 2>(a, s);
   }
@@ -1206,13 +1273,14 @@ static hl_status run_rows(const AttentionArgs& a, bool solo, hipStream_t s) {
 }
 
 template <class T>
-static hl_status run_type(const AttentionArgs& a, bool solo, hipStream_t s) {
-  if (a.dim == 64) return run_rows<T, 64, true>(a, solo, s);
-  if (a.dim < 64) return run_rows<T, 64, false>(a, solo, s);
-  if (a.dim == 128) return run_rows<T, 128, true>(a, solo, s);
-  if (a.dim < 128) return run_rows<T, 128, false>(a, solo, s);
-  if (a.dim == 256) return run_rows<T, 256, true>(a, solo, s);
-  return run_rows<T, 256, false>(a, solo, s);
+static hl_status run_type(const AttentionPlan& pl, hipStream_t s) {
+  const AttentionArgs& a = pl.a;
+  if (a.dim == 64) return run_rows<T, 64, true>(pl, s);
+  if (a.dim < 64) return run_rows<T, 64, false>(pl, s);
+  if (a.dim == 128) return run_rows<T, 128, true>(pl, s);
+  if (a.dim < 128) return run_rows<T, 128, false>(pl, s);
+  if (a.dim == 256) return run_rows<T, 256, true>(pl, s);
+  return run_rows<T, 256, false>(pl, s);
 }
 
 }  // namespace hl
@@ -1241,11 +1309,12 @@ extern "C" hl_status hl_prefix_attention(const hl_attention* attention, const vo
   uint8_t* ws = static_cast<uint8_t*>(workspace_dev);
   a.q = static_cast<const uint16_t*>(q_dev), a.out = static_cast<uint16_t*>(out_dev);
   a.lens = lens_dev, a.lse = lse_dev, a.weight_in = weight_in_dev, a.weight_out = weight_out_dev;
-  a.part_o = reinterpret_cast<float*>(ws + pl.part_o), a.part_ml = reinterpret_cast<float*>(ws + pl.part_ml);
+  a.wide_o = reinterpret_cast<float*>(ws + pl.wide_o), a.wide_ml = reinterpret_cast<float*>(ws + pl.wide_ml);
+  a.narrow_o = reinterpret_cast<float*>(ws + pl.narrow_o), a.narrow_ml = reinterpret_cast<float*>(ws + pl.narrow_ml);
   if (weight_out_dev) {
     a.row_ml = reinterpret_cast<float*>(ws + pl.row_ml);
     a.scores = reinterpret_cast<float*>(ws + pl.scores);
   }
-  return attention->dtype == HL_BF16 ? run_type<__bf16>(a, pl.solo, (hipStream_t)stream)
-                                     : run_type<_Float16>(a, pl.solo, (hipStream_t)stream);
+  return attention->dtype == HL_BF16 ? run_type<__bf16>(pl, (hipStream_t)stream)
+                                     : run_type<_Float16>(pl, (hipStream_t)stream);
 }
