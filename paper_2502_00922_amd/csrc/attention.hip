@@ -1017,16 +1017,16 @@ __global__ void __launch_bounds__(kSoloWaves * 64, 2) solo_kernel(AttentionArgs 
 constexpr uint32_t kSplitRows = 4096;  // rows up to which a block joins a row
 constexpr uint32_t kAhead = 8;         // parts whose loads a joining thread has in flight
 
-// Adds a row's parts. D/4 lanes have four columns of a row each; they are all
-// that a row has, or (SPLIT, for few rows) a block has one row, whose parts its
-// 1024/D groups of lanes take in turn.
-template <class T, int D, bool SPLIT>
-__global__ void __launch_bounds__(256) join_kernel(AttentionArgs a) {
-  constexpr uint32_t L = D / 4, GROUPS = 256 / L, STREAMS = SPLIT ? GROUPS : 1;
-  const uint32_t ln = threadIdx.x % L, group = threadIdx.x / L, rows = a.batch * a.queries * a.heads;
-  const uint32_t stream = SPLIT ? group : 0;
-  const uint32_t own_row = SPLIT ? blockIdx.x : blockIdx.x * GROUPS + group;
-  const uint32_t row = min(own_row, rows - 1);  // lanes past the last row repeat it and store nothing
+// Where a row's parts are: over the prefix, then over its own keys.
+struct RowParts {
+  const float2* ml[2];
+  const float* o[2];
+  uint32_t step[2], count[2];  // step: rows from one part to the next
+};
+
+// Whole wave; the row may be another in each lane.
+template <int D>
+__device__ inline RowParts parts_of(const AttentionArgs& a, uint32_t row) {
   const uint32_t tok = row / a.heads, hq = row % a.heads, b = tok / a.queries, head = hq / a.share, g = hq % a.share;
   const uint32_t up = units_of(a.prefix.tokens);
   uint32_t own_each = 0, own_begin = 0, own_units = 0;
@@ -1041,33 +1041,58 @@ __global__ void __launch_bounds__(256) join_kernel(AttentionArgs a) {
     }
   }
   const Lines lines = lines_of(a, own_units);
-  // the row's parts: over the prefix, then over its own keys
-  const float2* part_ml[2];
-  const float* part_o[2];
-  uint32_t part_step[2], count[2] = {0, 0};
+  RowParts p = {};
   const auto find = [&](int x, const Tiling& tl, uint32_t r, uint32_t item, uint32_t u, uint32_t each) {
     const Line line = tl.r ? lines.wide : lines.narrow;
     const uint32_t first = line.taker(u), rows = tl.r ? a.wide_rows : a.narrow_rows;
     const uint64_t at = (uint64_t)(first + item) * rows + r % tl.rows();
-    count[x] = line.taker(u + each - 1) - first + 1, part_step[x] = rows;
-    part_ml[x] = reinterpret_cast<const float2*>(tl.r ? a.wide_ml : a.narrow_ml) + at;
-    part_o[x] = (tl.r ? a.wide_o : a.narrow_o) + at * D + ln * 4;
+    p.count[x] = line.taker(u + each - 1) - first + 1, p.step[x] = rows;
+    p.ml[x] = reinterpret_cast<const float2*>(tl.r ? a.wide_ml : a.narrow_ml) + at;
+    p.o[x] = (tl.r ? a.wide_o : a.narrow_o) + at * D;
   };
-  part_ml[0] = part_ml[1] = nullptr, part_o[0] = part_o[1] = nullptr, part_step[0] = part_step[1] = 0;
-  const bool mixed = (a.tp.r != 0) == (a.to.r != 0);  // one line has both
+  const bool both = (a.tp.r != 0) == (a.to.r != 0);  // one line has both
   if (up) {
     const uint32_t r = tok * a.share + g, item = head * a.tp.tiles + r / a.tp.rows();
     find(0, a.tp, r, item, item * up, up);
   }
   if (own_each) {
     const uint32_t r = tok % a.queries * a.share + g, y = head * a.to.tiles + r / a.to.rows();
-    find(1, a.to, r, (mixed ? a.kv_heads * a.tp.tiles : 0) + b * a.kv_heads * a.to.tiles + y,
-         (mixed ? lines.prefix_units : 0) + own_begin + y * own_each, own_each);
+    find(1, a.to, r, (both ? a.kv_heads * a.tp.tiles : 0) + b * a.kv_heads * a.to.tiles + y,
+         (both ? lines.prefix_units : 0) + own_begin + y * own_each, own_each);
   }
-  const uint32_t parts = (count[0] + count[1] + STREAMS - 1 - stream) / STREAMS;  // of this group
+  return p;
+}
+
+__device__ inline float2 part_ml(const RowParts& p, uint32_t i) {
+  return i < p.count[0] ? p.ml[0][(uint64_t)i * p.step[0]] : p.ml[1][(uint64_t)(i - p.count[0]) * p.step[1]];
+}
+
+// Adds a row's parts. D/4 lanes have four columns of a row each; they are all
+// that a row has, or (SPLIT, for few rows) a block has one row, whose parts its
+// 1024/D groups of lanes take in turn.
+template <class T, int D, bool SPLIT>
+__global__ void __launch_bounds__(256) join_kernel(AttentionArgs a) {
+  constexpr uint32_t L = D / 4, GROUPS = 256 / L, STREAMS = SPLIT ? GROUPS : 1;
+  const uint32_t rows = a.batch * a.queries * a.heads;
+  const uint32_t ln = threadIdx.x % L, group = threadIdx.x / L, stream = SPLIT ? group : 0;
+  const uint32_t own_row = SPLIT ? blockIdx.x : blockIdx.x * GROUPS + group;
+  const uint32_t row = min(own_row, rows - 1);  // lanes past the last row repeat it and store nothing
+  const RowParts rp = parts_of<D>(a, row);
+  const uint32_t parts = (rp.count[0] + rp.count[1] + STREAMS - 1 - stream) / STREAMS;  // of this group
   const auto add = [](float4& o, float f, float4 p) {
     // a part without a key has no output either (it may hold anything's product with 0)
     if (f != 0.0f) o.x += f * p.x, o.y += f * p.y, o.z += f * p.z, o.w += f * p.w;
+  };
+  // outputs of parts x .. x+kAhead-1, their loads in flight together; past the last part, it again
+  float4 p[kAhead];
+  const auto load = [&](uint32_t x) {
+#pragma unroll
+    for (uint32_t j = 0; j < kAhead; ++j) {
+      const uint32_t i = min(x + j, parts - 1) * STREAMS + stream;
+      p[j] = *reinterpret_cast<const float4*>(i < rp.count[0]
+                                                  ? rp.o[0] + (uint64_t)i * rp.step[0] * D + ln * 4
+                                                  : rp.o[1] + (uint64_t)(i - rp.count[0]) * rp.step[1] * D + ln * 4);
+    }
   };
   float m = -INFINITY, l = 0.0f;
   float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -1075,11 +1100,10 @@ __global__ void __launch_bounds__(256) join_kernel(AttentionArgs a) {
     const uint32_t some = min(L, parts - i0);
     float mi = -INFINITY, li = 0.0f;
     if (ln < some) {
-      const uint32_t i = (i0 + ln) * STREAMS + stream;
-      const float2 ml = i < count[0] ? part_ml[0][(uint64_t)i * part_step[0]]
-                                     : part_ml[1][(uint64_t)(i - count[0]) * part_step[1]];
+      const float2 ml = part_ml(rp, (i0 + ln) * STREAMS + stream);
       mi = ml.x, li = ml.y;
     }
+    load(i0);
     float top = mi;
     for (uint32_t d = L / 2; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
     const float now = fmaxf(m, top);
@@ -1090,14 +1114,7 @@ __global__ void __launch_bounds__(256) join_kernel(AttentionArgs a) {
     l = l * f0 + sum, m = now;
     o.x *= f0, o.y *= f0, o.z *= f0, o.w *= f0;
     for (uint32_t i = 0; i < some; i += kAhead) {
-      float4 p[kAhead];  // their loads in flight together; past the last part, it again with weight 0
-#pragma unroll
-      for (uint32_t j = 0; j < kAhead; ++j) {
-        const uint32_t x = (i0 + min(i + j, some - 1)) * STREAMS + stream;
-        p[j] = *reinterpret_cast<const float4*>(
-            x < count[0] ? part_o[0] + (uint64_t)x * part_step[0] * D
-                         : part_o[1] + (uint64_t)(x - count[0]) * part_step[1] * D);
-      }
+      if (i) load(i0 + i);
 #pragma unroll
       for (uint32_t j = 0; j < kAhead; ++j) {
         const float f = __shfl(fi, (i + j) % L, L);
@@ -1145,6 +1162,7 @@ __global__ void __launch_bounds__(256) weights_kernel(AttentionArgs a) {
                    a.row_ml + 2 * ((uint64_t)b * a.queries * a.heads + (uint64_t)head * a.share), a.heads, key, keys);
   a.weight_out[at] = a.weight_in ? a.weight_in[at] + w : w;
 }
+
 
 // ------------------------------------------------------------------- host
 
@@ -1254,8 +1272,9 @@ static hl_status run(const AttentionArgs& a, hipStream_t s) {
   const uint32_t rows = a.batch * a.queries * a.heads;
   // A block a row while that fills the card: each of the row's parts is a trip
   // to memory, and few rows have many.
-  st = rows <= kSplitRows ? enqueue(join_kernel<T, D, true>, dim3(rows), dim3(256), s, a)
-                          : enqueue(join_kernel<T, D, false>, dim3((rows + 1024 / D - 1) / (1024 / D)), dim3(256), s, a);
+  st = rows <= kSplitRows
+           ? enqueue(join_kernel<T, D, true>, dim3(rows), dim3(256), s, a)
+           : enqueue(join_kernel<T, D, false>, dim3((rows + 1024 / D - 1) / (1024 / D)), dim3(256), s, a);
   if (st != HL_OK || !a.scores) return st;
   return enqueue(weights_kernel, dim3((a.own.tokens + 255) / 256, a.kv_heads, a.batch), dim3(256), s, a);
 }
