@@ -17,6 +17,7 @@ namespace hl {
 constexpr uint32_t kThreads = 1024, kWaves = kThreads / 64;
 constexpr uint32_t kRow = 4 * kThreads;  // weights of a row: four a thread, next to each other
 constexpr uint32_t kBins = 2048;
+constexpr uint64_t kFewMoved = 65536;    // columns of K (and of V) that a selecting block moves itself, at most
 constexpr uint32_t kCopies = 4;          // of the histogram: lanes of a wave often count in one bin
 constexpr uint32_t kCopy = kBins + 16;   // their distance: a bin's copies are in different banks
 
@@ -86,10 +87,43 @@ __device__ inline void load_keys(uint32_t (&key)[ROWS][4], const float* w, uint3
     for (uint32_t x = 0; x < 4; ++x) key[r][x] = ordered(f[r][x]);
 }
 
+constexpr uint32_t kMoves = 4;  // 16-byte pieces of K, and of V, a thread has in flight
+
+// Moves pieces x0, x0 + step, .. (kMoves of them) of a sequence's kept rows:
+// piece(x) = (row, key head, first column), none from `count` on. Slots that
+// hold no token give zeros.
+template <class Piece>
+__device__ inline void move(const EvictArgs& a, uint32_t b, uint64_t x0, uint32_t step, uint64_t count, Piece piece) {
+  u32x4 k[kMoves], v[kMoves];
+  int32_t slot[kMoves];
+  uint32_t row[kMoves], head[kMoves], d[kMoves];
+#pragma unroll
+  for (uint32_t m = 0; m < kMoves; ++m) {
+    if (x0 + m * step >= count) continue;
+    piece(x0 + m * step, row[m], head[m], d[m]);
+    slot[m] = a.slots[((uint64_t)b * a.kv_heads + head[m]) * a.keep + row[m]];
+  }
+#pragma unroll
+  for (uint32_t m = 0; m < kMoves; ++m) {
+    if (x0 + m * step >= count) continue;
+    k[m] = v[m] = u32x4{0, 0, 0, 0};
+    if (slot[m] < 0) continue;
+    const uint64_t s = (uint32_t)slot[m];
+    k[m] = *reinterpret_cast<const u32x4*>(a.k + b * a.k_seq + s * a.k_token + head[m] * a.k_head + d[m]);
+    v[m] = *reinterpret_cast<const u32x4*>(a.v + b * a.v_seq + s * a.v_token + head[m] * a.v_head + d[m]);
+  }
+#pragma unroll
+  for (uint32_t m = 0; m < kMoves; ++m) {
+    if (x0 + m * step >= count) continue;
+    *reinterpret_cast<u32x4*>(a.k_out + b * a.ko_seq + row[m] * a.ko_token + head[m] * a.ko_head + d[m]) = k[m];
+    *reinterpret_cast<u32x4*>(a.v_out + b * a.vo_seq + row[m] * a.vo_token + head[m] * a.vo_head + d[m]) = v[m];
+  }
+}
+
 // ROWS: rows of weights that stay in registers. Longer caches are read again
 // for each digit, ROWS rows at a time.
 template <uint32_t ROWS>
-__global__ void __launch_bounds__(1024) select_kernel(EvictArgs a) {
+__device__ inline void select(const EvictArgs& a) {
   __shared__ uint32_t s_bin[kCopies][kCopy];
   __shared__ uint32_t s_wave[kWaves], s_digit, s_above, s_in;
   __shared__ uint32_t s_more[ROWS * kWaves], s_same[ROWS * kWaves];
@@ -207,44 +241,28 @@ __global__ void __launch_bounds__(1024) select_kernel(EvictArgs a) {
   }
 }
 
-constexpr uint32_t kMoves = 4;  // 16-byte pieces of K, and of V, a thread moves
+// MOVE: each block moves the rows that it has found, too.
+template <uint32_t ROWS, bool MOVE>
+__global__ void __launch_bounds__(1024) select_kernel(EvictArgs a) {
+  select<ROWS>(a);
+  if constexpr (MOVE) {
+    __syncthreads();  // the block's slots are written
+    const uint32_t pieces = a.dim / 8, count = a.keep * pieces, own = blockIdx.x;
+    for (uint32_t x0 = threadIdx.x; x0 < count; x0 += kThreads * kMoves)
+      move(a, blockIdx.y, x0, kThreads, count, [&](uint64_t x, uint32_t& row, uint32_t& head, uint32_t& d) {
+        row = (uint32_t)x / pieces, head = own, d = (uint32_t)x % pieces * 8;
+      });
+  }
+}
 
-// Piece x of a sequence's kept rows: x = (row * heads + head) * (dim/8) + 16-byte
-// piece. Slots that hold no token give zeros.
+// A sequence's kept rows by many blocks, all key heads of a row together.
 __global__ void __launch_bounds__(256) move_kernel(EvictArgs a) {
-  const uint32_t b = blockIdx.y, pieces = a.dim / 8;
-  const uint64_t count = (uint64_t)a.keep * a.kv_heads * pieces;
-  const uint64_t x0 = (uint64_t)blockIdx.x * 256 * kMoves + threadIdx.x;
-  u32x4 k[kMoves], v[kMoves];
-  uint64_t ko[kMoves], vo[kMoves];
-  int32_t slot[kMoves];
-#pragma unroll
-  for (uint32_t m = 0; m < kMoves; ++m) {
-    const uint64_t x = x0 + m * 256;
-    if (x >= count) continue;
-    const uint32_t y = (uint32_t)(x / pieces), d = (uint32_t)(x % pieces) * 8, row = y / a.kv_heads,
-                   head = y % a.kv_heads;
-    slot[m] = a.slots[((uint64_t)b * a.kv_heads + head) * a.keep + row];
-    ko[m] = b * a.ko_seq + row * a.ko_token + head * a.ko_head + d;
-    vo[m] = b * a.vo_seq + row * a.vo_token + head * a.vo_head + d;
-  }
-#pragma unroll
-  for (uint32_t m = 0; m < kMoves; ++m) {
-    const uint64_t x = x0 + m * 256;
-    if (x >= count) continue;
-    k[m] = v[m] = u32x4{0, 0, 0, 0};
-    if (slot[m] < 0) continue;
-    const uint32_t y = (uint32_t)(x / pieces), d = (uint32_t)(x % pieces) * 8, head = y % a.kv_heads;
-    const uint64_t s = (uint32_t)slot[m];
-    k[m] = *reinterpret_cast<const u32x4*>(a.k + b * a.k_seq + s * a.k_token + head * a.k_head + d);
-    v[m] = *reinterpret_cast<const u32x4*>(a.v + b * a.v_seq + s * a.v_token + head * a.v_head + d);
-  }
-#pragma unroll
-  for (uint32_t m = 0; m < kMoves; ++m) {
-    if (x0 + m * 256 >= count) continue;
-    *reinterpret_cast<u32x4*>(a.k_out + ko[m]) = k[m];
-    *reinterpret_cast<u32x4*>(a.v_out + vo[m]) = v[m];
-  }
+  const uint32_t pieces = a.dim / 8;
+  move(a, blockIdx.y, (uint64_t)blockIdx.x * 256 * kMoves + threadIdx.x, 256, (uint64_t)a.keep * a.kv_heads * pieces,
+       [&](uint64_t x, uint32_t& row, uint32_t& head, uint32_t& d) {
+         const uint32_t y = (uint32_t)(x / pieces);
+         row = y / a.kv_heads, head = y % a.kv_heads, d = (uint32_t)(x % pieces) * 8;
+       });
 }
 
 }  // namespace hl
@@ -292,9 +310,11 @@ extern "C" hl_status hl_cache_evict(const hl_kv* from, const hl_kv* to, uint32_t
   a.keep = (uint32_t)keep, a.recent = (uint32_t)recent;
   const hipStream_t s = (hipStream_t)stream;
   const dim3 items(kv_heads, batch), threads(kThreads);
-  st = from->tokens <= kRow ? enqueue(select_kernel<1>, items, threads, s, a)
-       : from->tokens <= 4 * kRow ? enqueue(select_kernel<4>, items, threads, s, a)
-                                  : enqueue(select_kernel<16>, items, threads, s, a);
+  // A block that finds few rows moves them itself, which saves a kernel.
+  if (from->tokens <= kRow && keep * dim <= kFewMoved) return enqueue(select_kernel<1, true>, items, threads, s, a);
+  st = from->tokens <= kRow ? enqueue(select_kernel<1, false>, items, threads, s, a)
+       : from->tokens <= 4 * kRow ? enqueue(select_kernel<4, false>, items, threads, s, a)
+                                  : enqueue(select_kernel<16, false>, items, threads, s, a);
   if (st != HL_OK) return st;
   return enqueue(move_kernel, dim3((uint32_t)blocks, batch), dim3(256), s, a);
 }
