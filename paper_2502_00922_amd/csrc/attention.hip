@@ -716,11 +716,12 @@ __device__ inline void narrow_part(const AttentionArgs& a, const Item& it, uint3
 }
 
 // Which place of its row in an LDS buffer 16-byte piece j has, and which piece
-// has place j: the pieces of a row change places with the row's number, so that
-// the 16 lanes that read one piece of 16 rows together use all banks.
+// has place j: pairs of pieces change places with the row's number. The 8 lanes
+// that read one piece of 8 rows in one cycle, and the 16 that read a pair of
+// pieces of 4 rows, then use different banks.
 template <int D>
 __device__ inline uint32_t place(uint32_t row, uint32_t j) {
-  return j ^ (D == 64 ? row / 2 % 8 : row % 16);
+  return j ^ 2 * (D == 64 ? row / 2 % 4 : row % 8);
 }
 
 // 64 lanes' 16 bytes at base + offset (each lane's own) to LDS, one lane's after
@@ -798,7 +799,7 @@ __device__ inline void wide_part(const AttentionArgs& a, const Item& it, uint32_
     if (i < steps) load_buffer<D, FULL>(it, a.dim, k0 + i * kStep, at + i * bytes);
   State<D, R> st;
   begin<D, FULL, R>(st, a, it, wave_row);
-  // Steps begin at multiples of 16 rows, so which banks a lane's pieces are in
+  // Steps begin at multiples of 8 rows, so which banks a lane's pieces are in
   // does not depend on the step.
   constexpr int KD = S::KS < 4 ? S::KS : 4;  // of 256 columns, the second half is 16 pieces on
   uint32_t kofs[KD];
