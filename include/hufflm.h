@@ -417,10 +417,9 @@ hl_status hl_gemv_bf16(const uint16_t* w_dev, uint64_t rows, uint64_t cols,
  * hidden; scale_dev [tokens][hidden/group]), or 0 for the whole row (scale_dev
  * [tokens]). For other out types group must be 0 and scale_dev is ignored.
  * A NaN in a row makes the row's out NaN.
- * Rows that start at multiples of 16 bytes (every pointer 16-byte aligned and
- * hidden a multiple of 8) are read in the widest pieces; others work, with
- * narrower ones (a group then gives HL_EINVAL). Errors: HL_EINVAL (also for a
- * pointer not aligned to its element), HL_EUNSUPPORTED for hidden above
+ * Pointers are aligned to their elements, with a group to 16 bytes; hidden may
+ * be any number. Errors: HL_EINVAL (also for a misaligned pointer),
+ * HL_EUNSUPPORTED for hidden above
  * HL_NORM_MAX_HIDDEN. */
 hl_status hl_rms_norm(const void* x_dev, hl_dtype x_dtype, const void* residual_dev, hl_dtype r_dtype,
                       const void* weight_dev, hl_dtype w_dtype, uint64_t tokens, uint64_t hidden, float eps,

@@ -49,6 +49,7 @@ constexpr uint32_t kWaves = 4;         // of a block
 // which take long enough to compute that more blocks pay.
 constexpr uint32_t kLeastWide[3] = {1, 2, 1};
 constexpr uint32_t kThreads = 64 * kWaves;
+constexpr uint64_t kManyUnits = 4;     // wide units of 128 rows that a block has, at least
 constexpr float kSlack = 8.0f;         // powers of two that a score may pass the maximum kept for it by
 constexpr float kLog2e = 1.44269504088896341f;
 
@@ -161,6 +162,8 @@ __device__ inline OwnPlace own_place(const AttentionArgs& a, const OwnLine& o, u
 struct Line {
   uint32_t total, takers;
   __device__ uint32_t first(uint32_t k) const { return (uint32_t)((uint64_t)k * total / takers); }
+  // takers, about, of `units` units that follow each other
+  uint32_t parts(uint32_t units) const { return total ? (uint32_t)((uint64_t)units * takers / total) + 1 : 0; }
   __device__ uint32_t taker(uint32_t u) const { return (uint32_t)((((uint64_t)u + 1) * takers - 1) / total); }
 };
 
@@ -170,7 +173,7 @@ struct Lines {
   uint32_t prefix_units, wide_blocks;
 };
 
-__device__ inline Lines lines_of(const AttentionArgs& a, uint32_t own_units) {
+__host__ __device__ inline Lines lines_of(const AttentionArgs& a, uint32_t own_units) {
   Lines l;
   l.prefix_units = a.kv_heads * a.tp.tiles * units_of(a.prefix.tokens);
   l.wide.total = (a.tp.r ? l.prefix_units : 0) + (a.to.r ? own_units : 0);
@@ -179,14 +182,14 @@ __device__ inline Lines lines_of(const AttentionArgs& a, uint32_t own_units) {
   if (l.wide.total) {
     w = a.blocks;
     if (l.narrow.total) w = (uint32_t)((uint64_t)a.blocks * l.wide.total / (l.wide.total + l.narrow.total));
-    const uint32_t least = max(a.tp.r, a.to.r) == 2 ? kLeastWide[2] : kLeastWide[1];
-    w = min(w, (l.wide.total + least - 1) / least);
-    w = min((w + 7) / 8 * 8, a.blocks - (l.narrow.total ? 8 : 0));
-    w = max(w, 8u);
+    const uint32_t least = a.tp.r == 2 || a.to.r == 2 ? kLeastWide[2] : kLeastWide[1];
+    w = std::min(w, (l.wide.total + least - 1) / least);
+    w = std::min((w + 7) / 8 * 8, a.blocks - (l.narrow.total ? 8 : 0));
+    w = std::max(w, 8u);
   }
   l.wide_blocks = w;
-  l.wide.takers = min(w, l.wide.total);
-  l.narrow.takers = min(a.blocks - w, l.narrow.total);
+  l.wide.takers = std::min(w, l.wide.total);
+  l.narrow.takers = std::min(a.blocks - w, l.narrow.total);
   return l;
 }
 
@@ -1015,7 +1018,7 @@ __global__ void __launch_bounds__(kSoloWaves * 64, 2) solo_kernel(AttentionArgs 
   }
 }
 
-constexpr uint32_t kSplitRows = 4096;  // rows up to which a block joins a row
+constexpr uint32_t kManyParts = 16;    // of a row that a block joins, at least
 constexpr uint32_t kAhead = 8;         // parts whose loads a joining thread has in flight
 
 // Where a row's parts are: over the prefix, then over its own keys.
@@ -1180,7 +1183,7 @@ constexpr uint64_t kSoloKeys = 768, kSoloKeysMany = 1024;  // keys up to which a
 struct AttentionPlan {
   AttentionArgs a;
   uint64_t bytes, wide_o, wide_ml, narrow_o, narrow_ml, row_ml, scores;  // of the workspace: its size and its parts' places
-  bool solo, wide;  // wide: whether the call has wide items
+  bool solo, wide, split;  // wide: whether the call has wide items; split: whether a block joins a row
 };
 
 static hl_status check_kv(const hl_kv& s, uint64_t tokens, uint32_t dim, bool sequences) {
@@ -1227,17 +1230,21 @@ static hl_status attention_plan(const hl_attention* h, bool weights, AttentionPl
   a.scale2 = h->scale == 0.0f ? 1.0f : fabsf(h->scale) * kLog2e;
   a.q_and = h->scale == 0.0f ? 0 : ~0u, a.q_xor = h->scale < 0.0f ? 0x80008000u : 0;
   const uint64_t shared_rows = (uint64_t)h->batch * h->queries * a.share, own_rows = (uint64_t)h->queries * a.share;
-  const uint32_t r = std::max(shared_rows, own_rows) > 64 && h->dim <= 128 ? 2 : 1;
-  a.tp = tiling(shared_rows, r), a.to = tiling(own_rows, r);
-  // most that the lengths can come to, of each line
-  const uint64_t prefix_items = (uint64_t)h->kv_heads * a.tp.tiles, own_items = (uint64_t)h->batch * h->kv_heads * a.to.tiles;
-  const uint64_t prefix_units = prefix_items * units_of(a.prefix.tokens), own_units = own_items * units_of(a.own.tokens);
-  const uint64_t wide_units = (a.tp.r ? prefix_units : 0) + (a.to.r ? own_units : 0);
-  const uint64_t narrow_units = prefix_units + own_units - wide_units;
-  if (prefix_units + own_units >= (1ull << 31)) return HL_EUNSUPPORTED;
   // two blocks a compute unit: what their registers allow, and they hide each
   // other's waits; a multiple of 8, for the XCDs
   const uint64_t cus = (uint64_t)device_cus(), most = std::max<uint64_t>(16, cus * 2 / 8 * 8);
+  // most that the lengths can come to, of each line
+  uint64_t prefix_items, own_items, prefix_units, own_units, wide_units;
+  uint32_t r = std::max(shared_rows, own_rows) > 64 && h->dim <= 128 ? 2 : 1;
+  for (;; r = 1) {
+    a.tp = tiling(shared_rows, r), a.to = tiling(own_rows, r);
+    prefix_items = (uint64_t)h->kv_heads * a.tp.tiles, own_items = (uint64_t)h->batch * h->kv_heads * a.to.tiles;
+    prefix_units = prefix_items * units_of(a.prefix.tokens), own_units = own_items * units_of(a.own.tokens);
+    wide_units = (a.tp.r ? prefix_units : 0) + (a.to.r ? own_units : 0);
+    if (r == 1 || wide_units >= kManyUnits * most) break;
+  }
+  const uint64_t narrow_units = prefix_units + own_units - wide_units;
+  if (prefix_units + own_units >= (1ull << 31)) return HL_EUNSUPPORTED;
   const uint64_t asked = wide_units / kLeastWide[r] + narrow_units + 15;
   a.blocks = (uint32_t)std::min<uint64_t>(most, std::max<uint64_t>(16, asked / 8 * 8));
   a.wide_rows = std::max(a.tp.r ? a.tp.rows() : 0, a.to.r ? a.to.rows() : 0);
@@ -1257,6 +1264,9 @@ static hl_status attention_plan(const hl_attention* h, bool weights, AttentionPl
   pl->solo = own_rows <= 16 && a.prefix.tokens + a.own.tokens <=
                                    ((uint64_t)h->batch * h->kv_heads * 2 >= cus ? kSoloKeysMany : kSoloKeys);
   pl->wide = wide_units != 0;
+  const Lines lines = lines_of(a, (uint32_t)own_units);
+  pl->split = (a.tp.r ? lines.wide : lines.narrow).parts(units_of(a.prefix.tokens)) +
+                  (a.to.r ? lines.wide : lines.narrow).parts(units_of(a.own.tokens)) > kManyParts;
   pl->wide_o = take(wide_slots * a.wide_rows * held), pl->wide_ml = take(wide_slots * a.wide_rows * 2);
   pl->narrow_o = take(narrow_slots * a.narrow_rows * held), pl->narrow_ml = take(narrow_slots * a.narrow_rows * 2);
   a.score_stride = (a.own.tokens + kStep - 1) / kStep * kStep;
@@ -1267,13 +1277,13 @@ static hl_status attention_plan(const hl_attention* h, bool weights, AttentionPl
 }
 
 template <class T, int D, bool FULL, int RW>
-static hl_status run(const AttentionArgs& a, hipStream_t s) {
+static hl_status run(const AttentionPlan& pl, hipStream_t s) {
+  const AttentionArgs& a = pl.a;
   hl_status st = enqueue(parts_kernel<T, D, FULL, RW>, dim3(a.blocks), dim3(kThreads), s, a);
   if (st != HL_OK) return st;
   const uint32_t rows = a.batch * a.queries * a.heads;
-  // A block a row while that fills the card: each of the row's parts is a trip
-  // to memory, and few rows have many.
-  st = rows <= kSplitRows
+  // A block a row where it has many parts: each is a trip to memory.
+  st = pl.split
            ? enqueue(join_kernel<T, D, true>, dim3(rows), dim3(256), s, a)
            : enqueue(join_kernel<T, D, false>, dim3((rows + 1024 / D - 1) / (1024 / D)), dim3(256), s, a);
   if (st != HL_OK || !a.scores) return st;
@@ -1285,11 +1295,11 @@ static hl_status run_rows(const AttentionPlan& pl, hipStream_t s) {
   const AttentionArgs& a = pl.a;
   if (pl.solo) return enqueue(solo_kernel<T, D, FULL>, dim3(a.kv_heads, a.batch), dim3(kSoloWaves * 64), s, a);
   const uint32_t r = std::max(a.tp.r, a.to.r);
-  if (!pl.wide) return run<T, D, FULL, 0>(a, s);
+  if (!pl.wide) return run<T, D, FULL, 0>(pl, s);
   if constexpr (D <= 128) {
-    if (r == 2) return run<T, D, FULL, 2>(a, s);
+    if (r == 2) return run<T, D, FULL, 2>(pl, s);
   }
-  return run<T, D, FULL, 1>(a, s);
+  return run<T, D, FULL, 1>(pl, s);
 }
 
 template <class T>
