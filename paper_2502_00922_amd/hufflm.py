@@ -553,6 +553,16 @@ def _plain(device: int, bufs) -> None:
             raise ValueError(f"{name} must be contiguous")
 
 
+def _on_stream(stream, device: int, f, *args):
+    """f(*args) with `stream` as the current one, so that what the call allocates belongs to it as well: memory that
+    another stream's work may still use, or get again before this stream has used it, is not touched."""
+    if stream.device_index != device:
+        raise ValueError(f"stream is on GPU {stream.device_index}, the tensors on {device}")
+    import torch
+    with torch.cuda.stream(stream):
+        return f(*args)
+
+
 def rms_norm(x, weight, residual=None, eps: float = 1e-5, out_dtype=None, group: int = 0, out=None, sum_out=None,
              scale_out=None, stream=None) -> NormResult:
     """t = x + residual; out = t / sqrt(mean(t^2) + eps) * weight over the last dimension.
@@ -560,7 +570,10 @@ def rms_norm(x, weight, residual=None, eps: float = 1e-5, out_dtype=None, group:
     x and residual: [..., hidden] float32, bfloat16 or float16, contiguous; weight: [hidden]. The sum is kept in
     residual's type (``sum_out`` may be ``residual`` itself). ``out_dtype`` defaults to weight's type;
     torch.float8_e4m3fn gives 8 bits and float32 scales, one for each ``group`` columns (32, 64 or 128) or, with 0,
-    for each row. Outputs that are not given are allocated."""
+    for each row. Outputs that are not given are allocated (on ``stream``, where one is given)."""
+    if stream is not None:
+        return _on_stream(stream, x.get_device(), rms_norm, x, weight, residual, eps, out_dtype, group, out, sum_out,
+                          scale_out)
     T = _torch or _lookups()
     types = T.codes
     shape, dev = x.shape, x.get_device()
@@ -607,8 +620,7 @@ def rms_norm(x, weight, residual=None, eps: float = 1e-5, out_dtype=None, group:
         _plain(dev, {"x": x, "weight": weight, "out": out, "residual": residual, "sum_out": sum_out,
                      "scale_out": scale_out})
     s = T.lib.hl_rms_norm(x.data_ptr(), xt, r_ptr, rt, weight.data_ptr(), wt, x.numel() // hidden, hidden, eps, s_ptr,
-                          out.data_ptr(), oc, group, scale_ptr,
-                          T.raw_stream(dev) if stream is None else stream.cuda_stream)
+                          out.data_ptr(), oc, group, scale_ptr, T.raw_stream(dev))
     if s:
         _check(s, "hl_rms_norm")
     return NormResult(out, sum_out, scale_out)
@@ -660,7 +672,10 @@ def prefix_attention(q, k=None, v=None, lens=None, prefix_k=None, prefix_v=None,
     ``weights`` (float32 [batch, kv_heads, capacity]) or ``weights_out``: also gives the weights plus what each own
     key was given by this call (``weights_out`` may be ``weights``; without ``weights``, plus zeros). ``lse``: a
     float32 [batch, queries, heads] buffer for the logarithms of the softmax sums. ``workspace``: a device buffer of
-    hl_attention_workspace_bytes; allocated where it is not given."""
+    hl_attention_workspace_bytes. Buffers that are not given are allocated (on ``stream``, where one is given)."""
+    if stream is not None:
+        return _on_stream(stream, q.get_device(), prefix_attention, q, k, v, lens, prefix_k, prefix_v, scale, weights,
+                          out, weights_out, lse, None, workspace)
     T = _torch or _lookups()
     dtype = q.dtype
     code = T.half.get(dtype)
@@ -707,13 +722,12 @@ def prefix_attention(q, k=None, v=None, lens=None, prefix_k=None, prefix_v=None,
                         1.0 / math.sqrt(dim) if scale is None else scale, *prefix, *own)
     L = T.lib
     if workspace is None:
-        workspace = T.empty(L.hl_attention_workspace_bytes(a, w_out_ptr is not None), dtype=T.uint8,
-                                device=q.device)
+        workspace = T.empty(L.hl_attention_workspace_bytes(a, w_out_ptr is not None), dtype=T.uint8, device=q.device)
     else:
         _dev_arg(workspace, "workspace")
         _on_device(q.device, workspace=workspace)
     s = L.hl_prefix_attention(a, q.data_ptr(), lens_ptr, out.data_ptr(), lse_ptr, w_ptr, w_out_ptr,
-                              workspace.data_ptr(), workspace.nbytes, T.raw_stream(dev) if stream is None else stream.cuda_stream)
+                              workspace.data_ptr(), workspace.nbytes, T.raw_stream(dev))
     if s:
         _check(s, "hl_prefix_attention")
     return AttentionResult(out, weights_out, lse)
@@ -726,7 +740,10 @@ def cache_evict(k, v, weights, lens, keep: int, recent: int = 0, k_out=None, v_o
     k, v: [batch, capacity, kv_heads, dim], 16-bit, any strides with columns in a row; weights: float32
     [batch, kv_heads, capacity]; lens: int32 [batch]. k_out, v_out (default: new ones of capacity ``keep``): caches of
     at least ``keep`` tokens that do not overlap k and v. Gives these, the kept tokens' weights (float32) and slots
-    (int32) [batch, kv_heads, keep] - 0 and -1 past the kept ones, whose rows are zeros - and the new lengths."""
+    (int32) [batch, kv_heads, keep] - 0 and -1 past the kept ones, whose rows are zeros - and the new lengths, allocated
+    (on ``stream``, where one is given)."""
+    if stream is not None:
+        return _on_stream(stream, k.get_device(), cache_evict, k, v, weights, lens, keep, recent, k_out, v_out)
     T = _torch or _lookups()
     if k.dim() != 4 or k.dtype not in T.two_bytes:
         raise ValueError("k must be [batch, capacity, kv_heads, dim] bfloat16, float16 or int16")
@@ -746,8 +763,8 @@ def cache_evict(k, v, weights, lens, keep: int, recent: int = 0, k_out=None, v_o
     w_out = weights.new_empty((batch, heads, keep))
     slots = lens.new_empty((batch, heads, keep))
     lens_out = T.empty_like(lens)
-    s = T.lib.hl_cache_evict(_KV.pack(*src), _KV.pack(*dst), batch, heads, dim, weights.data_ptr(), lens.data_ptr(), keep,
-                             recent, w_out.data_ptr(), slots.data_ptr(), lens_out.data_ptr(), T.raw_stream(dev) if stream is None else stream.cuda_stream)
+    s = T.lib.hl_cache_evict(_KV.pack(*src), _KV.pack(*dst), batch, heads, dim, weights.data_ptr(), lens.data_ptr(),
+                             keep, recent, w_out.data_ptr(), slots.data_ptr(), lens_out.data_ptr(), T.raw_stream(dev))
     if s:
         _check(s, "hl_cache_evict")
     return EvictResult(k_out, v_out, w_out, lens_out, slots)
