@@ -33,6 +33,15 @@
 // permutation for two elements; the columns of one lane go to 8 different
 // instructions, so that turning needs no other lane's data. Wide items let the
 // transposing LDS read do it, whose 16 lanes exchange 4 keys of 16 columns.
+//
+// Bounds and times (16 bits, 128 columns, 8 key heads, both kernels). Memory
+// bounds a decode step: 16 sequences of 32 heads on 4096 own keys each take 60
+// us (268 MB, 4.5 TB/s), on 131072 shared keys 112 us (537 MB, 4.8 TB/s), of 64
+// heads 122. The softmax bounds many new tokens: 4 x 256 of them on 4096 shared
+// and 512 own keys take 127 us (75 GFLOP, 590 TFLOP/s), and the matrix units are
+// busy a third of that time, the vector units about half of it. Short calls are
+// bound by their launches and by a few waits for memory in a row: 16 sequences
+// on 8192 shared keys take 19 us, three times what reading the keys takes.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -45,11 +54,18 @@ constexpr uint32_t kUnit = 128;        // keys of a unit
 constexpr uint32_t kStep = 32;         // keys of a wave's step
 constexpr uint32_t kWaves = 4;         // of a block
 // Units of a wide stretch, at least, where there are enough, for one and two
-// 16-row tiles a wave: it leaves 64 rows, as many bytes as a unit has, or 128,
-// which take long enough to compute that more blocks pay.
+// 16-row tiles a wave: a stretch leaves a part of 64 rows, as many bytes as a
+// unit has (16 sequences on 8192 shared keys: 19.4 us, with one unit 21.1; but
+// 32 sequences 25.3 and 24.1), or of 128, which take long enough to compute that
+// more blocks pay.
 constexpr uint32_t kLeastWide[3] = {1, 2, 1};
 constexpr uint32_t kThreads = 64 * kWaves;
-constexpr uint64_t kManyUnits = 4;     // wide units of 128 rows that a block has, at least
+// Units of 128 rows that a block has, at least, where items have so many: two
+// tiles a wave halve the reads of LDS for a product, and double what a part
+// writes and the join reads. 128 rows a key head on 8192 shared keys (one unit a
+// block): 28.5 us with two tiles, 24.6 with one; on 16384 35.1 and 31.0; on 32768
+// (four units) 48 both; on 131072 122 and 163.
+constexpr uint64_t kManyUnits = 4;
 constexpr float kSlack = 8.0f;         // powers of two that a score may pass the maximum kept for it by
 constexpr float kLog2e = 1.44269504088896341f;
 
@@ -976,7 +992,9 @@ __device__ inline float key_weight(const AttentionArgs& a, const float* scores, 
 constexpr uint32_t kSoloWaves = 8;
 
 // A whole sequence and key head by one block, over the prefix and its own keys:
-// no parts, no second kernel. Rows of a head: at most 16.
+// no parts, no second kernel. Rows of a head: at most 16. Bound by the waits for
+// memory, one for every 256 keys: 16 sequences on 512 own keys of 8 key heads
+// take 11 us (33 MB, 3 TB/s).
 template <class T, int D, bool FULL>
 __global__ void __launch_bounds__(kSoloWaves * 64, 2) solo_kernel(AttentionArgs a) {
   __shared__ __attribute__((aligned(16))) float lds[kSoloWaves * 16 * (D + 4) + kSoloWaves * 16 * 2];
@@ -1018,8 +1036,13 @@ __global__ void __launch_bounds__(kSoloWaves * 64, 2) solo_kernel(AttentionArgs 
   }
 }
 
-constexpr uint32_t kManyParts = 16;    // of a row that a block joins, at least
-constexpr uint32_t kAhead = 8;         // parts whose loads a joining thread has in flight
+// Parts of a row from which on a block joins it, about: fewer do not hide what
+// adding its groups' results in LDS takes. 4 sequences on 8192 shared keys (64
+// parts) take 15.8 us so and 22.2 with D/4 lanes a row, 16 sequences (32 parts)
+// 19.4 and 20.6; 16 on 4096 own keys (5 parts) 65.3 and 62.4, 8 x 8 new tokens on
+// 2000 shared and 777 own (up to 9) 37 and 22.
+constexpr uint32_t kManyParts = 16;
+constexpr uint32_t kAhead = 8;  // parts whose loads a joining thread has in flight
 
 // Where a row's parts are: over the prefix, then over its own keys.
 struct RowParts {
@@ -1071,7 +1094,10 @@ __device__ inline float2 part_ml(const RowParts& p, uint32_t i) {
   return i < p.count[0] ? p.ml[0][(uint64_t)i * p.step[0]] : p.ml[1][(uint64_t)(i - p.count[0]) * p.step[1]];
 }
 
-// Adds a row's parts. D/4 lanes have four columns of a row each; they are all
+// Adds a row's parts, each a maximum, a sum and D columns in float32: bound by
+// two waits for memory, one for the maxima (and as many columns as the registers
+// hold) and one for the rest, 6 us for 512 rows of up to 20 parts; many rows are
+// bound by its bandwidth, 18 us for 32768 rows. D/4 lanes have four columns of a row each; they are all
 // that a row has, or (SPLIT, for few rows) a block has one row, whose parts its
 // 1024/D groups of lanes take in turn.
 template <class T, int D, bool SPLIT>
@@ -1154,7 +1180,9 @@ __global__ void __launch_bounds__(256) join_kernel(AttentionArgs a) {
 }
 
 // weight_out = weight_in + the weight that the call's rows gave each own key;
-// a thread adds its key's rows in their order.
+// a thread adds its key's rows in their order, so that the sum is the same in
+// every run. The scores come from the parts kernel through the workspace: 8
+// sequences of 64 heads and 4096 keys, 8 MB, 5.4 us, most of it launch and wait.
 __global__ void __launch_bounds__(256) weights_kernel(AttentionArgs a) {
   const uint32_t head = blockIdx.y, b = blockIdx.z, key = blockIdx.x * 256 + threadIdx.x;
   if (key >= a.own.tokens) return;
@@ -1171,6 +1199,9 @@ __global__ void __launch_bounds__(256) weights_kernel(AttentionArgs a) {
 // ------------------------------------------------------------------- host
 
 // Items of `rows` rows: narrow up to 16; wide ones take r 16-row tiles a wave.
+// Of 16 rows or fewer, all but one of a wide item's waves would have none: one
+// sequence (4 rows a key head) on 2048 own keys takes 11.6 us, wide 14.8; on 8192
+// shared keys 14.8 and 15.5.
 static Tiling tiling(uint64_t rows, uint32_t r) {
   Tiling t;
   t.r = rows <= 16 ? 0 : r;
@@ -1178,7 +1209,12 @@ static Tiling tiling(uint64_t rows, uint32_t r) {
   return t;
 }
 
-constexpr uint64_t kSoloKeys = 768, kSoloKeysMany = 1024;  // keys up to which a block takes a sequence and head
+// Keys up to which a block takes a sequence and key head alone, and the same
+// where there is a block for every second compute unit. One sequence on 256 own
+// keys takes 5.6 us so and 9.0 in parts, on 512 8.0 and 9.4, on 768 9.8 and 9.5
+// (but one launch for two), on 1024 13.2 and 10.1; 16 sequences on 768 17.6 and
+// 19.9, on 1024 22 and 23, on 1536 30 and 28.
+constexpr uint64_t kSoloKeys = 768, kSoloKeysMany = 1024;
 
 struct AttentionPlan {
   AttentionArgs a;
@@ -1282,7 +1318,7 @@ static hl_status run(const AttentionPlan& pl, hipStream_t s) {
   hl_status st = enqueue(parts_kernel<T, D, FULL, RW>, dim3(a.blocks), dim3(kThreads), s, a);
   if (st != HL_OK) return st;
   const uint32_t rows = a.batch * a.queries * a.heads;
-  // A block a row where it has many parts: each is a trip to memory.
+  // A block a row where it has many parts, each of which is a trip to memory.
   st = pl.split
            ? enqueue(join_kernel<T, D, true>, dim3(rows), dim3(256), s, a)
            : enqueue(join_kernel<T, D, false>, dim3((rows + 1024 / D - 1) / (1024 / D)), dim3(256), s, a);
