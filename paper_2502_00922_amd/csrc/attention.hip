@@ -349,7 +349,7 @@ struct State {
   u32x4 q[R][Shape<D>::KS];
   f32x4 o[R][Shape<D>::TILES];
   float m[R], l[R];    // maximum (0 while there is none), this lane's part of the sum
-  bool some[R];        // whether m is a score's
+  float limit[R];      // m + kSlack; -infinity while m is no score
   uint32_t seen[R];    // keys that the query sees
   uint32_t odd;        // whether a value of this lane was taken out of the product
 };
@@ -494,7 +494,7 @@ __device__ inline void step(State<D, R>& st, Keys& t, const AttentionArgs& a, co
           if (key + 16 * h + 4 * c + r >= st.seen[rt]) s[rt][h][r] = -INFINITY;
     }
     if (it.scores) {
-      const uint32_t row = wave_row + 16 * rt + n;
+      const uint32_t row = here(wave_row + 16 * rt + n);  // nothing of this is formed in a call without weights
       if (row < it.rows) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -511,15 +511,15 @@ __device__ inline void step(State<D, R>& st, Keys& t, const AttentionArgs& a, co
     // The maximum need not be the true one, only near it: the output is
     // scaled again when a score passes it by more than 2^8, so the weights
     // stay in the 16-bit types' range and most steps scale nothing.
-    if (__any(top > (st.some[rt] ? st.m[rt] + kSlack : -INFINITY))) {
+    if (__any(top > st.limit[rt])) {
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
-      const bool had = st.some[rt];
+      const bool had = st.limit[rt] != -INFINITY;
       const float was = st.m[rt];
       const float now = had ? fmaxf(was, top) : top;
       if (now != -INFINITY) {
         const float f = had ? __builtin_amdgcn_exp2f(was - now) : 0.0f;
-        st.m[rt] = now, st.some[rt] = true;
+        st.m[rt] = now, st.limit[rt] = now + kSlack;
         st.l[rt] *= f;
 #pragma unroll
         for (int i = 0; i < S::TILES; ++i) st.o[rt][i] *= f;
@@ -606,7 +606,7 @@ __device__ inline void begin(State<D, R>& st, const AttentionArgs& a, const Item
   st.odd = 0;
 #pragma unroll
   for (int rt = 0; rt < R; ++rt) {
-    st.m[rt] = 0.0f, st.l[rt] = 0.0f, st.some[rt] = false;
+    st.m[rt] = 0.0f, st.l[rt] = 0.0f, st.limit[rt] = -INFINITY;
 #pragma unroll
     for (int i = 0; i < Shape<D>::TILES; ++i) st.o[rt][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     const uint32_t row = min(wave_row + 16 * rt + n, it.rows - 1), tok = row / a.share;
@@ -687,7 +687,7 @@ __device__ inline void add_waves(const State<D, 1>& st, uint32_t rows, float* ld
   float* lds_ml = lds + WAVES * 16 * (D + 4);
   const float sum = over_lanes(st.l[0]);
   const uint32_t at = here(wave * 16 + n);  // formed here: no register holds it through the loops
-  if (c == 0) lds_ml[2 * at] = st.some[0] || sum != sum ? st.m[0] : -INFINITY, lds_ml[2 * at + 1] = sum;
+  if (c == 0) lds_ml[2 * at] = st.limit[0] != -INFINITY || sum != sum ? st.m[0] : -INFINITY, lds_ml[2 * at + 1] = sum;
 #pragma unroll
   for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -760,16 +760,47 @@ constexpr uint32_t loads_each() {
   return kStep * D * 2 / 1024 / kWaves;
 }
 
+// This lane's pieces' places in memory, in bytes from a step's first key and
+// value, where the step's keys are all there.
+template <int D>
+struct Offsets {
+  uint32_t k[loads_each<D>()], v[loads_each<D>()];
+};
+
+template <int D, bool FULL>
+__device__ inline Offsets<D> offsets(const Item& it, uint32_t dim) {
+  constexpr uint32_t pieces = D / 8, rows = 64 / pieces;
+  const uint32_t lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  Offsets<D> o;
+#pragma unroll
+  for (uint32_t i = 0; i < loads_each<D>(); ++i) {
+    const uint32_t row = (wave * loads_each<D>() + i) * rows + lane / pieces;
+    uint32_t d = place<D>(row, lane % pieces) * 16;
+    if (!FULL && d >= 2 * dim) d = 0;
+    o.k[i] = row * 2 * it.k_token + d, o.v[i] = row * 2 * it.v_token + d;
+  }
+  return o;
+}
+
 // This wave's quarter of keys key .. key+31 of `it` to the buffer at `lds`;
 // past its end, its last key again, and past the head's columns, its first
 // columns again.
 template <int D, bool FULL>
-__device__ inline void load_buffer(const Item& it, uint32_t dim, uint32_t key, uint32_t lds) {
+__device__ inline void load_buffer(const Item& it, uint32_t dim, uint32_t key, uint32_t lds, const Offsets<D>& o) {
   constexpr uint32_t pieces = D / 8, rows = 64 / pieces;  // rows of a load
   const uint32_t lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const uint8_t* kp = reinterpret_cast<const uint8_t*>(it.k + (uint64_t)key * it.k_token);
   const uint8_t* vp = reinterpret_cast<const uint8_t*>(it.v + (uint64_t)key * it.v_token);
   const uint32_t left = it.keys - 1 - key;
+  if (left >= kStep - 1) {
+#pragma unroll
+    for (uint32_t i = 0; i < loads_each<D>(); ++i) {
+      const uint32_t x = wave * loads_each<D>() + i;
+      load_to_lds(kp, o.k[i], lds + x * 1024);
+      load_to_lds(vp, o.v[i], lds + buffer_bytes(D) / 2 + x * 1024);
+    }
+    return;
+  }
 #pragma unroll
   for (uint32_t i = 0; i < loads_each<D>(); ++i) {
     const uint32_t x = wave * loads_each<D>() + i, row = x * rows + lane / pieces, from = min(row, left);
@@ -813,9 +844,10 @@ __device__ inline void wide_part(const AttentionArgs& a, const Item& it, uint32_
   const uint32_t mine = wave_row < it.rows ? min(end, most) : 0;
   const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
   const uint32_t steps = k0 < end ? (end - k0 + kStep - 1) / kStep : 0;
+  const Offsets<D> places = offsets<D, FULL>(it, a.dim);
 #pragma unroll
   for (uint32_t i = 0; i + 1 < ring; ++i)
-    if (i < steps) load_buffer<D, FULL>(it, a.dim, k0 + i * kStep, at + i * bytes);
+    if (i < steps) load_buffer<D, FULL>(it, a.dim, k0 + i * kStep, at + i * bytes, places);
   State<D, R> st;
   begin<D, FULL, R>(st, a, it, wave_row);
   // Steps begin at multiples of 8 rows, so which banks a lane's pieces are in
@@ -854,7 +886,7 @@ __device__ inline void wide_part(const AttentionArgs& a, const Item& it, uint32_
     // All waves have left the buffer of step i - 1, which is loaded next.
     buffers_ready<D>(min(steps - 1 - i, ring - 2));
     if (i + ring - 1 < steps)
-      load_buffer<D, FULL>(it, a.dim, k0 + (i + ring - 1) * kStep, at + (i + ring - 1) % ring * bytes);
+      load_buffer<D, FULL>(it, a.dim, k0 + (i + ring - 1) * kStep, at + (i + ring - 1) % ring * bytes, places);
     from = i % ring * bytes;
   };
   // the steps that hide no key of any wave, then the rest
@@ -883,7 +915,7 @@ __device__ inline void wide_part(const AttentionArgs& a, const Item& it, uint32_
     const float sum = over_lanes(st.l[rt]);
     const uint32_t row = here(wave * 16 * R + 16 * rt + n);
     if (it.row0 + row >= it.rows) continue;
-    if (c == 0) pml[2 * row] = st.some[rt] || sum != sum ? st.m[rt] : -INFINITY, pml[2 * row + 1] = sum;
+    if (c == 0) pml[2 * row] = st.limit[rt] != -INFINITY || sum != sum ? st.m[rt] : -INFINITY, pml[2 * row + 1] = sum;
 #pragma unroll
     for (int i = 0; i < S::TILES; ++i)
       *reinterpret_cast<f32x4*>(po + (uint64_t)row * D + 16 * i + 4 * c) = st.o[rt][i];
