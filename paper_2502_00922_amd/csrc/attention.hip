@@ -19,8 +19,8 @@
 // registers and one step ahead; nothing in their loop waits for another wave,
 // and their four results are added in LDS at the end. Larger items are "wide":
 // the four waves have different rows and the same keys, which the block loads
-// from memory to LDS without registers between, 32 at a time and up to three
-// times ahead, so that memory is read once for up to 128 rows. The narrow
+// from memory to LDS without registers between, up to 64 at a time while those
+// before them are computed, so that memory is read once for up to 128 rows. The narrow
 // items' units stand in one line and the wide items' in another, and the blocks
 // are divided between the two by their units.
 //
@@ -585,7 +585,10 @@ __device__ inline void step(State<D, R>& st, Keys& t, const AttentionArgs& a, co
   }
 }
 
-// LDS buffers of a wide item, a step's keys and values each.
+// LDS buffers of a wide item, a step's keys and values each. Half of them are
+// computed while the other half is loaded, and the waves meet once a half: 4 x
+// 256 new tokens on 4096 shared keys take 118.7 us so, and 122.9 with a meeting
+// and a load each step.
 constexpr uint32_t buffers(int d) { return d == 256 ? 2 : 4; }
 constexpr uint32_t buffer_bytes(int d) { return kStep * d * 4; }
 
@@ -811,19 +814,10 @@ __device__ inline void load_buffer(const Item& it, uint32_t dim, uint32_t key, u
   }
 }
 
-// Waits until all but the latest n buffers' loads of this wave are done, and
-// for the other waves.
-template <int D>
-__device__ inline void buffers_ready(uint32_t n) {
-  static_assert(loads_each<D>() * 2 <= 8, "vmcnt");
-  constexpr uint32_t each = loads_each<D>() * 2;
+// Waits until this wave's loads are done, and for the other waves.
+__device__ inline void buffers_ready() {
   __builtin_amdgcn_sched_barrier(0);
-  if (n >= 2)
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * each) : "memory");
-  else if (n == 1)
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(each) : "memory");
-  else
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
@@ -835,7 +829,7 @@ template <class T, int D, bool FULL, int R>
 __device__ inline void wide_part(const AttentionArgs& a, const Item& it, uint32_t k0, uint32_t k1, uint32_t slot,
                                  float* lds) {
   using S = Shape<D>;
-  constexpr uint32_t bytes = buffer_bytes(D), ring = buffers(D);
+  constexpr uint32_t bytes = buffer_bytes(D), ring = buffers(D), half = ring / 2;
   const uint32_t lane = lane_id(), n = lane % 16, c = lane / 16;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const uint32_t wave_row = it.row0 + wave * 16 * R;
@@ -846,7 +840,7 @@ __device__ inline void wide_part(const AttentionArgs& a, const Item& it, uint32_
   const uint32_t steps = k0 < end ? (end - k0 + kStep - 1) / kStep : 0;
   const Offsets<D> places = offsets<D, FULL>(it, a.dim);
 #pragma unroll
-  for (uint32_t i = 0; i + 1 < ring; ++i)
+  for (uint32_t i = 0; i < half; ++i)
     if (i < steps) load_buffer<D, FULL>(it, a.dim, k0 + i * kStep, at + i * bytes, places);
   State<D, R> st;
   begin<D, FULL, R>(st, a, it, wave_row);
@@ -883,10 +877,13 @@ __device__ inline void wide_part(const AttentionArgs& a, const Item& it, uint32_
       }
   };
   const auto ready = [&](uint32_t i) {
-    // All waves have left the buffer of step i - 1, which is loaded next.
-    buffers_ready<D>(min(steps - 1 - i, ring - 2));
-    if (i + ring - 1 < steps)
-      load_buffer<D, FULL>(it, a.dim, k0 + (i + ring - 1) * kStep, at + (i + ring - 1) % ring * bytes, places);
+    if (i % half == 0) {
+      // Half of the buffers are loaded, and all waves have left the others.
+      buffers_ready();
+#pragma unroll
+      for (uint32_t j = i + half; j < i + ring; ++j)
+        if (j < steps) load_buffer<D, FULL>(it, a.dim, k0 + j * kStep, at + j % ring * bytes, places);
+    }
     from = i % ring * bytes;
   };
   // the steps that hide no key of any wave, then the rest
