@@ -35,13 +35,13 @@
 // transposing LDS read do it, whose 16 lanes exchange 4 keys of 16 columns.
 //
 // Bounds and times (16 bits, 128 columns, 8 key heads, both kernels). Memory
-// bounds a decode step: 16 sequences of 32 heads on 4096 own keys each take 60
-// us (268 MB, 4.5 TB/s), on 131072 shared keys 112 us (537 MB, 4.8 TB/s), of 64
+// bounds a decode step: 16 sequences of 32 heads on 4096 own keys each take 58
+// us (268 MB, 4.6 TB/s), on 131072 shared keys 111 us (537 MB, 4.8 TB/s), of 64
 // heads 122. The softmax bounds many new tokens: 4 x 256 of them on 4096 shared
-// and 512 own keys take 127 us (75 GFLOP, 590 TFLOP/s), and the matrix units are
-// busy a third of that time, the vector units about half of it. Short calls are
+// and 512 own keys take 119 us (75 GFLOP, 630 TFLOP/s), and the matrix units are
+// busy 38 % of the first kernel's time, the vector units 45 %. Short calls are
 // bound by their launches and by a few waits for memory in a row: 16 sequences
-// on 8192 shared keys take 19 us, three times what reading the keys takes.
+// on 8192 shared keys take 18 us, three times what reading the keys takes.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -63,9 +63,10 @@ constexpr uint32_t kThreads = 64 * kWaves;
 // Units of 128 rows that a block has, at least, where items have so many: two
 // tiles a wave halve the reads of LDS for a product, and double what a part
 // writes and the join reads. 128 rows a key head on 8192 shared keys (one unit a
-// block): 28.5 us with two tiles, 24.6 with one; on 16384 35.1 and 31.0; on 32768
-// (four units) 48 both; on 131072 122 and 163.
-constexpr uint64_t kManyUnits = 4;
+// block): 27.2 us with two tiles, 23.3 with one; on 32768 (four) 49.3 and 41.8; on
+// 65536 (eight) 72.3 and 73.8; on 131072 123 and 129; 4 x 128 new tokens on 4096
+// (eight) 72 and 83.
+constexpr uint64_t kManyUnits = 8;
 constexpr float kSlack = 8.0f;         // powers of two that a score may pass the maximum kept for it by
 constexpr float kLog2e = 1.44269504088896341f;
 

@@ -1,4 +1,4 @@
-"""prefix_attention where its rules take the forms that small calls do not: items of 128 rows (which need 2048 units of
+"""prefix_attention where its rules take the forms that small calls do not: items of 128 rows (which need 4096 units of
 128 keys on 256 compute units) and rows of many parts (MI355X). The bounds are those of test_gpu_prefix_attention; the
 definition is computed in 64 bits on the GPU here."""
 import math
@@ -49,18 +49,18 @@ def quick(monkeypatch):
 
 
 @pytest.mark.parametrize("dtype,batch,queries,heads,kv_heads,dim,prefix,own,lens", [
-    (torch.bfloat16, 65, 1, 64, 64, 64, 4096, 33, None),       # shared rows alone are wide
-    (torch.float16, 130, 1, 32, 32, 128, 4070, 20, None),      # two items a head, of 128 rows and 2
-    (torch.bfloat16, 2, 65, 64, 64, 128, 0, 2065, [2065, 64]),  # own rows; the second sequence's first token sees none
-    (torch.float16, 1, 100, 64, 32, 80, 4096, 150, [150]),     # both, columns that are not a power of two
-    (torch.bfloat16, 3, 33, 128, 32, 40, 1500, 333, [333, 0, 200])])
+    (torch.bfloat16, 65, 1, 64, 64, 64, 8192, 33, None),       # shared rows alone are wide
+    (torch.float16, 130, 1, 32, 32, 128, 8160, 20, None),      # two items a head, of 128 rows and 2
+    (torch.bfloat16, 2, 65, 64, 64, 128, 0, 4113, [4113, 64]),  # own rows; the second sequence's first token sees none
+    (torch.float16, 1, 100, 64, 32, 80, 8192, 150, [150]),     # both, columns that are not a power of two
+    (torch.bfloat16, 3, 33, 128, 32, 40, 3600, 333, [333, 0, 200])])
 def test_128_rows(dtype, batch, queries, heads, kv_heads, dim, prefix, own, lens):
     small.check(small.make(dtype, batch, queries, heads, kv_heads, dim, prefix, own, lens))
 
 
 @pytest.mark.parametrize("bad", [math.inf, math.nan])
 def test_128_rows_later_tokens_do_not_reach_earlier_ones(bad):
-    c = small.make(torch.bfloat16, 1, 65, 32, 32, 128, 8192, 130, [130])
+    c = small.make(torch.bfloat16, 1, 65, 32, 32, 128, 16384, 130, [130])
     want = hl.prefix_attention(**c)
     c["v"][0, 100:] = bad  # tokens 35 and later see these
     got = hl.prefix_attention(**c)
