@@ -53,13 +53,11 @@ namespace hl {
 constexpr uint32_t kUnit = 128;        // keys of a unit
 constexpr uint32_t kStep = 32;         // keys of a wave's step
 constexpr uint32_t kWaves = 4;         // of a block
-// Units of a wide stretch, at least, where there are enough, for one and two
-// 16-row tiles a wave: a stretch leaves a part of 64 rows, as many bytes as a
-// unit has (16 sequences on 8192 shared keys: 19.4 us, with one unit 21.1; but
-// 32 sequences 25.3 and 24.1), or of 128, which take long enough to compute that
-// more blocks pay.
-constexpr uint32_t kLeastWide[3] = {1, 2, 1};
 constexpr uint32_t kThreads = 64 * kWaves;
+// Units of a wide stretch, at least, where there are so many: a stretch leaves a
+// part of 64 rows or more, as many bytes as a unit has. 16 sequences on 8192
+// shared keys take 18.3 us so, with one unit 20.4.
+constexpr uint32_t kLeastWide = 2;
 // Units of 128 rows that a block has, at least, where items have so many: two
 // tiles a wave halve the reads of LDS for a product, and double what a part
 // writes and the join reads. 128 rows a key head on 8192 shared keys (one unit a
@@ -199,8 +197,7 @@ __host__ __device__ inline Lines lines_of(const AttentionArgs& a, uint32_t own_u
   if (l.wide.total) {
     w = a.blocks;
     if (l.narrow.total) w = (uint32_t)((uint64_t)a.blocks * l.wide.total / (l.wide.total + l.narrow.total));
-    const uint32_t least = a.tp.r == 2 || a.to.r == 2 ? kLeastWide[2] : kLeastWide[1];
-    w = std::min(w, (l.wide.total + least - 1) / least);
+    w = std::min(w, (l.wide.total + kLeastWide - 1) / kLeastWide);
     w = std::min((w + 7) / 8 * 8, a.blocks - (l.narrow.total ? 8 : 0));
     w = std::max(w, 8u);
   }
@@ -1311,7 +1308,7 @@ static hl_status attention_plan(const hl_attention* h, bool weights, AttentionPl
   }
   const uint64_t narrow_units = prefix_units + own_units - wide_units;
   if (prefix_units + own_units >= (1ull << 31)) return HL_EUNSUPPORTED;
-  const uint64_t asked = wide_units / kLeastWide[r] + narrow_units + 15;
+  const uint64_t asked = wide_units / kLeastWide + narrow_units + 15;
   a.blocks = (uint32_t)std::min<uint64_t>(most, std::max<uint64_t>(16, asked / 8 * 8));
   a.wide_rows = std::max(a.tp.r ? a.tp.rows() : 0, a.to.r ? a.to.rows() : 0);
   a.narrow_rows = (uint32_t)std::min<uint64_t>(16, std::max(a.tp.r ? 0 : shared_rows, a.to.r ? 0 : own_rows));
