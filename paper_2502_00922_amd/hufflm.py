@@ -498,7 +498,7 @@ def gemv_bf16(w, x, y=None, stream=None):
 class NormResult(NamedTuple):
     out: object              # the normalised rows
     sum: Optional[object]    # x + residual, in residual's type (None without one)
-    scale: Optional[object]  # of an 8-bit out
+    scale: Optional[object]  # of an 8-bit out: [..., hidden / group], or [..., 1] for whole rows
 
 
 class AttentionResult(NamedTuple):
@@ -569,8 +569,10 @@ def rms_norm(x, weight, residual=None, eps: float = 1e-5, out_dtype=None, group:
 
     x and residual: [..., hidden] float32, bfloat16 or float16, contiguous; weight: [hidden]. The sum is kept in
     residual's type (``sum_out`` may be ``residual`` itself). ``out_dtype`` defaults to weight's type;
-    torch.float8_e4m3fn gives 8 bits and float32 scales, one for each ``group`` columns (32, 64 or 128) or, with 0,
-    for each row. Outputs that are not given are allocated (on ``stream``, where one is given)."""
+    torch.float8_e4m3fn gives 8 bits and float32 scales [..., hidden / group], one for each ``group`` columns (32, 64
+    or 128), or, with 0, [..., 1], one for each row: ``out.float() * scale`` are the row's values. (``scale_out`` may
+    leave that last 1 out; the result's ``scale`` has it.) Outputs that are not given are allocated (on ``stream``,
+    where one is given)."""
     if stream is not None:
         return _on_stream(stream, x.get_device(), rms_norm, x, weight, residual, eps, out_dtype, group, out, sum_out,
                           scale_out)
@@ -607,11 +609,13 @@ def rms_norm(x, weight, residual=None, eps: float = 1e-5, out_dtype=None, group:
     if oc == HL_E4M3:
         if group not in (0, 32, 64, 128) or (group and hidden % group):
             raise ValueError("group must be 0, or 32, 64 or 128 and divide hidden")
-        need = (*shape[:-1], hidden // group) if group else tuple(shape[:-1])
+        need = (*shape[:-1], hidden // group if group else 1)
         if scale_out is None:
             scale_out = T.empty(need, dtype=T.float32, device=x.device)
-        elif scale_out.dtype != T.float32 or tuple(scale_out.shape) != tuple(need):
-            raise ValueError(f"scale_out must be float32 {tuple(need)}")
+        elif scale_out.dtype == T.float32 and not group and scale_out.shape == shape[:-1]:
+            scale_out = scale_out.unsqueeze(-1)
+        elif scale_out.dtype != T.float32 or tuple(scale_out.shape) != need:
+            raise ValueError(f"scale_out must be float32 {need}")
         good = good and scale_out.is_contiguous() and scale_out.get_device() == dev
         scale_ptr = scale_out.data_ptr()
     elif group or scale_out is not None:
