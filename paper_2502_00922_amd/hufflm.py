@@ -528,6 +528,7 @@ class _Torch:
         self.two_bytes = (torch.bfloat16, torch.float16, torch.int16)
         self.empty, self.empty_like, self.Tensor = torch.empty, torch.empty_like, torch.Tensor
         self.raw_stream = torch._C._cuda_getCurrentRawStream
+        self.current_device = torch._C._cuda_getDevice
         self.lib = lib()
 
 
@@ -563,6 +564,14 @@ def _on_stream(stream, device: int, f, *args):
         return f(*args)
 
 
+def _on_gpu(device: int, f, *args):
+    """f(*args) with this GPU as the current one: a kernel runs on the current GPU, also where its stream is another's
+    default stream (whose handle is 0 on each), and a launch is planned for that GPU."""
+    import torch
+    with torch.cuda.device(device):
+        return f(*args)
+
+
 def rms_norm(x, weight, residual=None, eps: float = 1e-5, out_dtype=None, group: int = 0, out=None, sum_out=None,
              scale_out=None, stream=None) -> NormResult:
     """t = x + residual; out = t / sqrt(mean(t^2) + eps) * weight over the last dimension.
@@ -579,6 +588,8 @@ def rms_norm(x, weight, residual=None, eps: float = 1e-5, out_dtype=None, group:
     T = _torch or _lookups()
     types = T.codes
     shape, dev = x.shape, x.get_device()
+    if dev >= 0 and dev != T.current_device():
+        return _on_gpu(dev, rms_norm, x, weight, residual, eps, out_dtype, group, out, sum_out, scale_out)
     if weight.dim() != 1 or not shape or shape[-1] != weight.shape[0] or x.numel() == 0:
         raise ValueError(f"x must be [..., hidden] and weight [hidden], got {tuple(shape)} and {tuple(weight.shape)}")
     hidden = shape[-1]
@@ -689,6 +700,9 @@ def prefix_attention(q, k=None, v=None, lens=None, prefix_k=None, prefix_v=None,
     dev = q.get_device()
     if dev < 0 or not q.is_contiguous():
         raise ValueError("q must be contiguous and on the GPU")
+    if dev != T.current_device():
+        return _on_gpu(dev, prefix_attention, q, k, v, lens, prefix_k, prefix_v, scale, weights, out, weights_out, lse,
+                       None, workspace)
     own = prefix = _NO_KV
     kv_heads = lens_ptr = w_ptr = w_out_ptr = lse_ptr = None
     if k is not None or v is not None:
@@ -753,6 +767,8 @@ def cache_evict(k, v, weights, lens, keep: int, recent: int = 0, k_out=None, v_o
         raise ValueError("k must be [batch, capacity, kv_heads, dim] bfloat16, float16 or int16")
     batch, capacity, heads, dim = k.shape
     dev = k.get_device()
+    if dev >= 0 and dev != T.current_device():
+        return _on_gpu(dev, cache_evict, k, v, weights, lens, keep, recent, k_out, v_out)
     src = _keys_values(k, v, "k, v", 4, k.dtype, dev)
     if keep < 1 or not 0 <= recent <= keep:
         raise ValueError("keep must be at least 1 and recent between 0 and keep")
