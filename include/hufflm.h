@@ -419,8 +419,8 @@ hl_status hl_gemv_bf16(const uint16_t* w_dev, uint64_t rows, uint64_t cols,
  * A NaN in a row makes the row's out NaN.
  * Pointers are aligned to their elements, with a group to 16 bytes; hidden may
  * be any number. Errors: HL_EINVAL (also for a misaligned pointer),
- * HL_EUNSUPPORTED for hidden above
- * HL_NORM_MAX_HIDDEN. */
+ * HL_EUNSUPPORTED for hidden above HL_NORM_MAX_HIDDEN and for more rows than a
+ * launch takes (2^23 of 4096 columns). */
 hl_status hl_rms_norm(const void* x_dev, hl_dtype x_dtype, const void* residual_dev, hl_dtype r_dtype,
                       const void* weight_dev, hl_dtype w_dtype, uint64_t tokens, uint64_t hidden, float eps,
                       void* sum_dev, void* out_dev, hl_dtype out_dtype, uint32_t group, float* scale_dev,

@@ -1247,6 +1247,7 @@ struct AttentionPlan {
   AttentionArgs a;
   uint64_t bytes, wide_o, wide_ml, narrow_o, narrow_ml, row_ml, scores;  // of the workspace: its size and its parts' places
   bool solo, wide, split;  // wide: whether the call has wide items; split: whether a block joins a row
+  uint64_t join_blocks;
 };
 
 static hl_status check_kv(const hl_kv& s, uint64_t tokens, uint32_t dim, bool sequences) {
@@ -1330,6 +1331,9 @@ static hl_status attention_plan(const hl_attention* h, bool weights, AttentionPl
   const Lines lines = lines_of(a, (uint32_t)own_units);
   pl->split = (a.tp.r ? lines.wide : lines.narrow).parts(units_of(a.prefix.tokens)) +
                   (a.to.r ? lines.wide : lines.narrow).parts(units_of(a.own.tokens)) > kManyParts;
+  const uint64_t each = pl->split ? 1 : 1024 / held;  // rows of a joining block
+  pl->join_blocks = (rows + each - 1) / each;
+  if (!pl->solo && !grid_fits(pl->join_blocks, 256)) return HL_EUNSUPPORTED;
   pl->wide_o = take(wide_slots * a.wide_rows * held), pl->wide_ml = take(wide_slots * a.wide_rows * 2);
   pl->narrow_o = take(narrow_slots * a.narrow_rows * held), pl->narrow_ml = take(narrow_slots * a.narrow_rows * 2);
   a.score_stride = (a.own.tokens + kStep - 1) / kStep * kStep;
@@ -1344,11 +1348,10 @@ static hl_status run(const AttentionPlan& pl, hipStream_t s) {
   const AttentionArgs& a = pl.a;
   hl_status st = enqueue(parts_kernel<T, D, FULL, RW>, dim3(a.blocks), dim3(kThreads), s, a);
   if (st != HL_OK) return st;
-  const uint32_t rows = a.batch * a.queries * a.heads;
   // A block a row where it has many parts, each of which is a trip to memory.
-  st = pl.split
-           ? enqueue(join_kernel<T, D, true>, dim3(rows), dim3(256), s, a)
-           : enqueue(join_kernel<T, D, false>, dim3((rows + 1024 / D - 1) / (1024 / D)), dim3(256), s, a);
+  const dim3 blocks((uint32_t)pl.join_blocks);
+  st = pl.split ? enqueue(join_kernel<T, D, true>, blocks, dim3(256), s, a)
+                : enqueue(join_kernel<T, D, false>, blocks, dim3(256), s, a);
   if (st != HL_OK || !a.scores) return st;
   return enqueue(weights_kernel, dim3((a.own.tokens + 255) / 256, a.kv_heads, a.batch), dim3(256), s, a);
 }

@@ -300,7 +300,7 @@ extern "C" hl_status hl_cache_evict(const hl_kv* from, const hl_kv* to, uint32_t
   if (from->tokens >= (1ull << 30) || keep >= (1ull << 30) || batch > 65535 || kv_heads > 65535 || dim > 65536)
     return HL_EUNSUPPORTED;
   const uint64_t blocks = (keep * kv_heads * (dim / 8) + 256 * kMoves - 1) / (256 * kMoves);
-  if (keep * kv_heads >= (1ull << 32) || blocks >= (1ull << 31)) return HL_EUNSUPPORTED;
+  if (keep * kv_heads >= (1ull << 32) || !grid_fits(blocks, 256)) return HL_EUNSUPPORTED;
   EvictArgs a = {};
   a.weight = weight_dev, a.lens = lens_dev, a.weight_out = weight_out_dev, a.slots = slots_dev;
   a.lens_out = lens_out_dev;

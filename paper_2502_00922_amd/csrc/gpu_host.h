@@ -27,6 +27,10 @@ inline int device_cus() {
 
 inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
+// Whether a launch of this many blocks along x can be: its threads along x must
+// be fewer than 2^32.
+inline bool grid_fits(uint64_t blocks, uint64_t threads) { return blocks < (1ull << 32) / threads; }
+
 // Enqueues a kernel that uses only static LDS.
 template <class K, class... A>
 hl_status enqueue(K kernel, dim3 grid, dim3 block, hipStream_t s, A... args) {

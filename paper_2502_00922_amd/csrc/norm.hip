@@ -250,8 +250,10 @@ __global__ void __launch_bounds__(1024) norm_kernel(NormArgs a) {
 
 template <int V>
 static hl_status launch_norm(const NormArgs& a, hipStream_t s) {
-  const uint32_t rows = a.waves == 1 ? 4 : 1;
-  return enqueue(norm_kernel<V>, dim3((a.tokens + rows - 1) / rows), dim3(a.waves == 1 ? 256 : a.waves * 64), s, a);
+  const uint32_t rows = a.waves == 1 ? 4 : 1, threads = a.waves == 1 ? 256 : a.waves * 64;
+  const uint64_t blocks = ((uint64_t)a.tokens + rows - 1) / rows;
+  if (!grid_fits(blocks, threads)) return HL_EUNSUPPORTED;
+  return enqueue(norm_kernel<V>, dim3((uint32_t)blocks), dim3(threads), s, a);
 }
 
 static uint32_t dtype_bytes(hl_dtype t) { return t == HL_F32 ? 4 : t == HL_E4M3 ? 1 : 2; }
