@@ -449,8 +449,8 @@ typedef struct {
   hl_kv own;         /* each sequence's own, at the first lens[b] tokens of its capacity */
 } hl_attention;
 
-/* Bytes of device workspace hl_prefix_attention needs on the current GPU (0 on
- * bad arguments). */
+/* Bytes of device workspace hl_prefix_attention needs on the current GPU, never
+ * 0 but on bad arguments. */
 size_t hl_attention_workspace_bytes(const hl_attention* attention, int with_weights);
 
 /* Attention of each sequence's new tokens over a prefix that all sequences
@@ -466,7 +466,8 @@ size_t hl_attention_workspace_bytes(const hl_attention* attention, int with_weig
  * one as 0); NULL only where own.tokens == 0. lse_dev (or NULL): float32
  * [batch][queries][heads], log(sum_j exp(s_j)).
  * weight_out_dev (or NULL): float32 [batch][kv_heads][own.tokens], what
- * eviction goes by: weight_in_dev (NULL: zeros; may be the same buffer) plus,
+ * eviction goes by (own.tokens is not 0 then): weight_in_dev (NULL: zeros; may
+ * be the same buffer) plus,
  * for every own key, the sum of its p over the call's tokens and the heads
  * that share it. It holds a float32 score for each (row, own key) in the
  * workspace, so it is meant for few new tokens.

@@ -1243,6 +1243,10 @@ static Tiling tiling(uint64_t rows, uint32_t r) {
 // 19.9, on 1024 22 and 23, on 1536 30 and 28.
 constexpr uint64_t kSoloKeys = 768, kSoloKeysMany = 1024;
 
+// A workspace's size, at least: 0 says that the arguments are bad, and
+// allocations of 0 bytes have no address.
+constexpr uint64_t kLeastWorkspace = 512;
+
 struct AttentionPlan {
   AttentionArgs a;
   uint64_t bytes, wide_o, wide_ml, narrow_o, narrow_ml, row_ml, scores;  // of the workspace: its size and its parts' places
@@ -1339,7 +1343,7 @@ static hl_status attention_plan(const hl_attention* h, bool weights, AttentionPl
   a.score_stride = (a.own.tokens + kStep - 1) / kStep * kStep;
   pl->row_ml = weights ? take(rows * 2) : 0;
   pl->scores = weights ? take((uint64_t)h->batch * h->heads * h->queries * a.score_stride) : 0;
-  pl->bytes = n;
+  pl->bytes = std::max(n, kLeastWorkspace);
   return HL_OK;
 }
 

@@ -733,7 +733,7 @@ def prefix_attention(q, k=None, v=None, lens=None, prefix_k=None, prefix_v=None,
             weights_out = T.empty(need, dtype=T.float32, device=q.device)
         else:
             _small(weights_out, "weights_out", T.float32, need, dev)
-        w_out_ptr = weights_out.data_ptr()
+        w_out_ptr = weights_out.data_ptr() if k.shape[1] else None
     if lse is not None:
         lse_ptr = _small(lse, "lse", T.float32, (batch, queries, heads), dev).data_ptr()
     a = _ATTENTION.pack(code, batch, queries, heads, kv_heads, dim,
