@@ -1306,6 +1306,10 @@ static hl_status attention_plan(const hl_attention* h, bool weights, AttentionPl
   uint32_t r = std::max(shared_rows, own_rows) > 64 && h->dim <= 128 ? 2 : 1;
   for (;; r = 1) {
     a.tp = tiling(shared_rows, r), a.to = tiling(own_rows, r);
+    // A set without keys has no items: those of a line are numbered on from the
+    // prefix's, and each has a part.
+    if (a.prefix.tokens == 0) a.tp.tiles = 0;
+    if (a.own.tokens == 0) a.to.tiles = 0;
     prefix_items = (uint64_t)h->kv_heads * a.tp.tiles, own_items = (uint64_t)h->batch * h->kv_heads * a.to.tiles;
     prefix_units = prefix_items * units_of(a.prefix.tokens), own_units = own_items * units_of(a.own.tokens);
     wide_units = (a.tp.r ? prefix_units : 0) + (a.to.r ? own_units : 0);
@@ -1318,8 +1322,10 @@ static hl_status attention_plan(const hl_attention* h, bool weights, AttentionPl
   a.wide_rows = std::max(a.tp.r ? a.tp.rows() : 0, a.to.r ? a.to.rows() : 0);
   a.narrow_rows = (uint32_t)std::min<uint64_t>(16, std::max(a.tp.r ? 0 : shared_rows, a.to.r ? 0 : own_rows));
   const uint32_t held = h->dim <= 64 ? 64 : h->dim <= 128 ? 128 : 256;
-  const uint64_t wide_slots = wide_units ? a.blocks + prefix_items + own_items : 0;
-  const uint64_t narrow_slots = narrow_units ? a.blocks + prefix_items + own_items : 0;
+  // A line's parts: a block (its taker) has one of each item that it takes units
+  // of, at taker + item, and both only grow along the line.
+  const uint64_t wide_slots = wide_units ? a.blocks + (a.tp.r ? prefix_items : 0) + (a.to.r ? own_items : 0) : 0;
+  const uint64_t narrow_slots = narrow_units ? a.blocks + (a.tp.r ? 0 : prefix_items) + (a.to.r ? 0 : own_items) : 0;
   uint64_t n = 0;
   auto take = [&](uint64_t floats) {
     const uint64_t at = n;
@@ -1338,10 +1344,11 @@ static hl_status attention_plan(const hl_attention* h, bool weights, AttentionPl
   const uint64_t each = pl->split ? 1 : 1024 / held;  // rows of a joining block
   pl->join_blocks = (rows + each - 1) / each;
   if (!pl->solo && !grid_fits(pl->join_blocks, 256)) return HL_EUNSUPPORTED;
-  pl->wide_o = take(wide_slots * a.wide_rows * held), pl->wide_ml = take(wide_slots * a.wide_rows * 2);
-  pl->narrow_o = take(narrow_slots * a.narrow_rows * held), pl->narrow_ml = take(narrow_slots * a.narrow_rows * 2);
+  const uint64_t wide = pl->solo ? 0 : wide_slots * a.wide_rows, narrow = pl->solo ? 0 : narrow_slots * a.narrow_rows;
+  pl->wide_o = take(wide * held), pl->wide_ml = take(wide * 2);
+  pl->narrow_o = take(narrow * held), pl->narrow_ml = take(narrow * 2);
   a.score_stride = (a.own.tokens + kStep - 1) / kStep * kStep;
-  pl->row_ml = weights ? take(rows * 2) : 0;
+  pl->row_ml = weights && !pl->solo ? take(rows * 2) : 0;
   pl->scores = weights ? take((uint64_t)h->batch * h->heads * h->queries * a.score_stride) : 0;
   pl->bytes = std::max(n, kLeastWorkspace);
   return HL_OK;
