@@ -460,7 +460,9 @@ size_t hl_attention_workspace_bytes(const hl_attention* attention, int with_weig
  * over all keys of the prefix and, for token i of `queries`, the own keys
  * j < lens[b] - (queries - 1 - i). A token that sees no key (or only scores of
  * minus infinity) has out = 0 and lse = minus infinity. Keys and values that a
- * token does not see do not affect it, whatever they hold.
+ * token does not see do not affect it, whatever they hold; an infinite or NaN
+ * value that it sees leaves its column of out infinite or NaN, however small the
+ * weight.
  * q_dev, out_dev: [batch][queries][heads][dim]. lens_dev: int32 [batch], read
  * on the device (a length above own.tokens counts as own.tokens, a negative
  * one as 0); NULL only where own.tokens == 0. lse_dev (or NULL): float32

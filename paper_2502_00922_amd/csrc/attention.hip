@@ -1136,10 +1136,10 @@ __global__ void __launch_bounds__(256) join_kernel(AttentionArgs a) {
   const uint32_t row = min(own_row, rows - 1);  // lanes past the last row repeat it and store nothing
   const RowParts rp = parts_of<D>(a, row);
   const uint32_t parts = (rp.count[0] + rp.count[1] + STREAMS - 1 - stream) / STREAMS;  // of this group
-  const auto add = [](float4& o, float f, float4 p) {
-    // a part without a key has no output either (it may hold anything's product with 0)
-    if (f != 0.0f) o.x += f * p.x, o.y += f * p.y, o.z += f * p.z, o.w += f * p.w;
-  };
+  // Also where f is 0: a part without a key that the row sees has zeros, and an
+  // infinite or NaN value that the row does see must not get lost, however small
+  // its weight (nothing else in the call drops it).
+  const auto add = [](float4& o, float f, float4 p) { o.x += f * p.x, o.y += f * p.y, o.z += f * p.z, o.w += f * p.w; };
   // outputs of parts x .. x+kAhead-1, their loads in flight together; past the last part, it again
   float4 p[kAhead];
   const auto load = [&](uint32_t x) {
@@ -1175,7 +1175,7 @@ __global__ void __launch_bounds__(256) join_kernel(AttentionArgs a) {
 #pragma unroll
       for (uint32_t j = 0; j < kAhead; ++j) {
         const float f = __shfl(fi, (i + j) % L, L);
-        add(o, i + j < some ? f : 0.0f, p[j]);
+        if (i + j < some) add(o, f, p[j]);
       }
     }
   }
