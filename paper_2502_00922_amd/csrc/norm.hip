@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(1024) norm_kernel(NormArgs a) {
     for (int i = 0; i < W; ++i) sq = fmaf(t[v][i], t[v][i], sq);
   }
   const float inv = 1.0f / sqrtf(over_row<false>(sq, a.waves, s_sum) / (float)a.hidden + a.eps);
-  t1 *= inv * g1;
+  t1 = t1 * inv * g1;  // in this order: inv * weight may leave the range where out does not
   float most = odd ? fabsf(t1) : 0.0f;
   if (odd && a.ot != HL_E4M3) store_one(t1, a.out, a.ot, last);
 #pragma unroll
@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(1024) norm_kernel(NormArgs a) {
       values(f, g[v], a.wt);
 #pragma unroll
       for (int i = 0; i < W; ++i) {
-        t[v][i] *= inv * f[i];
+        t[v][i] = t[v][i] * inv * f[i];
         most = fmaxf(most, fabsf(t[v][i]));
       }
       if (a.ot != HL_E4M3) store(t[v], a.out, a.ot, row + at);
