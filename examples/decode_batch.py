@@ -135,6 +135,10 @@ def main():
                         ("batch", 16), ("prompt", 2048), ("steps", 64), ("cache", 256), ("keep", 128), ("recent", 32)):
         p.add_argument("--" + name, type=int, default=value)
     a = p.parse_args()
+    if a.steps < 1 or a.prompt < 1 or a.cache < 1:
+        p.error("steps, prompt and cache must be at least 1")
+    if a.steps > a.cache and (a.keep < 1 or not 0 <= a.recent <= a.keep < a.cache):
+        p.error("an eviction has to leave room: 0 <= recent <= keep < cache, and keep at least 1")
     d = Decoder(a.layers, a.hidden, a.inter, a.heads, a.kv_heads, a.dim)
     g = torch.Generator(device="cuda").manual_seed(0)
     embed = lambda n: torch.randn((n, a.hidden), generator=g, device="cuda").bfloat16()  # noqa: E731
