@@ -413,9 +413,10 @@ hl_status hl_gemv_bf16(const uint16_t* w_dev, uint64_t rows, uint64_t cols,
  * out_dtype: float32, bf16, float16, or HL_E4M3 with float32 scales: the
  * columns of a group share scale = max|out| / 448 (1 where that is below the
  * least normal float32, as for a group of zeros), and out holds out / scale
- * (the float32 quotient) rounded to nearest, ties to even. group: 32, 64 or 128 columns (dividing
- * hidden; scale_dev [tokens][hidden/group]), or 0 for the whole row (scale_dev
- * [tokens][1]). For other out types group must be 0 and scale_dev is ignored.
+ * (the float32 quotient) rounded to nearest, ties to even. group: 32, 64 or 128
+ * columns (dividing hidden; scale_dev [tokens][hidden/group]), or 0 for the whole
+ * row (scale_dev [tokens][1]). For other out types group must be 0 and scale_dev
+ * is ignored.
  * A NaN in a row makes the row's out NaN.
  * Pointers are aligned to their elements, with a group to 16 bytes; hidden may
  * be any number. Errors: HL_EINVAL (also for a misaligned pointer),

@@ -37,9 +37,10 @@
 // Bounds and times (16 bits, 128 columns, 8 key heads, both kernels). Memory
 // bounds a decode step: 16 sequences of 32 heads on 4096 own keys each take 58
 // us (268 MB, 4.6 TB/s), on 131072 shared keys 111 us (537 MB, 4.8 TB/s), of 64
-// heads 122. The softmax bounds many new tokens: 4 x 256 of them on 4096 shared
-// and 512 own keys take 119 us (75 GFLOP, 630 TFLOP/s), and the matrix units are
-// busy 38 % of the first kernel's time, the vector units 45 %. Short calls are
+// heads 122. Many new tokens are bound by the order within a step (scores, then
+// softmax, then values): 4 x 256 of them on 4096 shared and 512 own keys take 119
+// us (75 GFLOP, 630 TFLOP/s), and the matrix units are busy 38 % of the first
+// kernel's time, the vector units 45 %. Short calls are
 // bound by their launches and by a few waits for memory in a row: 16 sequences
 // on 8192 shared keys take 18 us, three times what reading the keys takes.
 #include <algorithm>

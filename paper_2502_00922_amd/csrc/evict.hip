@@ -317,7 +317,8 @@ extern "C" hl_status hl_cache_evict(const hl_kv* from, const hl_kv* to, uint32_t
   const dim3 items(kv_heads, batch), threads(kThreads);
   // A block that finds few rows moves them itself, which saves a kernel: 256 rows
   // of 128 columns of 8 caches take 9.0 us so and 10.1 with a kernel more, 512
-  // 11.6 and 10.4 (but the host has one launch for two), 1024 16.9 and 11.5.
+  // 11.6 and 10.4 (but the host has one launch for two, which a captured graph
+  // does not gain), 1024 16.9 and 11.5.
   if (from->tokens <= kRow && keep * dim <= kFewMoved) return enqueue(select_kernel<1, true>, items, threads, s, a);
   // As few rows of weights a thread as hold a cache: selecting with 16 takes 13 us
   // longer for 16 x 8 caches of 1024 tokens and of 4096.
