@@ -502,6 +502,110 @@ hl_status hl_cache_evict(const hl_kv* from, const hl_kv* to, uint32_t batch, uin
                          const float* weight_dev, const int32_t* lens_dev, uint64_t keep, uint64_t recent,
                          float* weight_out_dev, int32_t* slots_dev, int32_t* lens_out_dev, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * A cache in 4 bits, and what else a decode step takes in 4 bits or ends in.
+ * ------------------------------------------------------------------------- */
+
+/* Bytes of a row of a 4-bit cache: `dim` columns of one token and key head, in
+ * G = dim / 32 groups of neighbouring columns that share a scale and a base,
+ *   value = base + scale * (code - 8),  code 0 .. 15:
+ *   16 * G bytes of codes: byte n * G + g has the codes of columns 32g + 2n (its
+ *   low half) and 32g + 2n + 1, n = 0 .. 15;
+ *   G pairs (scale, base), each bf16, the scale first;
+ *   zeros up to a multiple of 16 bytes.
+ * 0 where dim is not a multiple of 32, or above HL_ATTENTION_MAX_DIM. */
+size_t hl_cache4_row_bytes(uint32_t dim);
+
+/* Caches of such rows are hl_kv like those in 16 bits, with strides in units of
+ * 16 bits (multiples of 8), so hl_cache_evict moves them too (as rows of
+ * hl_cache4_row_bytes(dim) / 2 columns). */
+
+/* Rounds new tokens' keys and values to 4-bit rows. from: [sequence][token][key
+ * head][column] of bf16 or float16, from->tokens new ones a sequence. They go to
+ * the slots that end at the sequence's length, lens[b] - from->tokens + i for
+ * token i (lens_dev NULL: to slots 0 .. from->tokens - 1); those without a slot in
+ * the cache are left out, and other slots are not written.
+ * Of 32 columns from lo to hi:
+ *   base = (7 lo + 8 hi) / 15, scale = max((hi - base) / 7, (base - lo) / 8),
+ * computed in float32 (a rounding each operation) and rounded to bf16, and code - 8
+ * is the whole number of -8 .. 7 nearest to (x - base) / scale, ties to even (0
+ * where scale is 0). Columns among which one is an infinity or a NaN, or whose base
+ * or scale would not be finite, become NaN, all 32. Errors: HL_EINVAL,
+ * HL_EUNSUPPORTED for dim above HL_ATTENTION_MAX_DIM and sizes past 32-bit counts. */
+hl_status hl_cache_write4(const hl_kv* from, hl_dtype dtype, const hl_kv* cache, uint32_t batch, uint32_t kv_heads,
+                          uint32_t dim, const int32_t* lens_dev, void* stream);
+
+/* The values that 4-bit rows stand for, to out [batch][tokens][heads][dim] of
+ * float32, bf16 or float16: base + scale * (code - 8) in float32, rounded once
+ * more for 16 bits. Strides in bytes, multiples of 16; both pointers 16-byte
+ * aligned. Errors as hl_cache_write4. */
+hl_status hl_cache_read4(const void* rows_dev, uint64_t seq_stride, uint64_t token_stride, uint64_t head_stride,
+                         uint32_t batch, uint64_t tokens, uint32_t heads, uint32_t dim, void* out_dev, hl_dtype dtype,
+                         void* stream);
+
+/* hl_prefix_attention over a prefix and own caches of 4-bit rows; its workspace.
+ * `dtype` is q's and out's; dim is a multiple of 32. The values enter the sums as
+ * the rows have them, unrounded; p * scale is rounded to bf16 for the second
+ * product, to two bf16 pieces where out is float16. A column group of a token that
+ * a row sees is NaN in out where its scale or base is; of tokens that it does not
+ * see, rows may hold anything. Everything else, weights and errors among it, as
+ * hl_prefix_attention. */
+size_t hl_attention4_workspace_bytes(const hl_attention* attention, int with_weights);
+hl_status hl_prefix_attention4(const hl_attention* attention, const void* q_dev, const int32_t* lens_dev,
+                               void* out_dev, float* lse_dev, const float* weight_in_dev, float* weight_out_dev,
+                               void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* The product of a layer whose weights are kept in 4 bits,
+ *   y[b][r] = sum_k x[b][k] * (base + scale * (code[r][k] - 8)),
+ * for b < batch, batch in [1, HL_MAX_BATCH]. codes_dev: [rows][cols / 2], the
+ * code of an even column in the low half of a byte, of the next one in the high
+ * half. scales_dev, bases_dev: bf16 or float16 [rows][cols / group], one for each
+ * `group` neighbouring columns: 32, 64 or 128, dividing cols; bases_dev NULL: all 0.
+ * x_dev: [batch][cols] bf16 or float16; y_dev: [batch][rows] float32 (fully
+ * written). The codes multiply x exactly and sums are float32, in a fixed order;
+ * scales and bases multiply a group's sums in float32. A row with an infinite or
+ * NaN scale or base has no finite y. codes_dev and x_dev are 16-byte aligned, the
+ * others to their elements. Errors: HL_EINVAL (also for a misaligned pointer),
+ * HL_EUNSUPPORTED for sizes past 32-bit counts. */
+hl_status hl_gemv4(const uint8_t* codes_dev, const void* scales_dev, const void* bases_dev, hl_dtype scale_dtype,
+                   uint64_t rows, uint64_t cols, uint32_t group, const void* x_dev, hl_dtype x_dtype, uint32_t batch,
+                   float* y_dev, void* stream);
+
+/* How a row's token is drawn; each setting for all rows, or, where its pointer is
+ * not NULL, of each row in device memory (float32 or int32 [rows]). */
+typedef struct {
+  const float* temperature_dev;
+  const int32_t* top_k_dev;
+  const float* top_p_dev;
+  const float* min_p_dev;
+  float temperature; /* not above 0: the greatest logit's token */
+  int32_t top_k;     /* below 1, or vocab and above: all */
+  float top_p;       /* 1 and above: all */
+  float min_p;       /* 0 and below: all */
+} hl_sampling;
+
+/* A token of each row of logits: with w_i = exp((l_i - max l) / temperature) and
+ * the tokens in the order of falling logits, of equal ones the lowest index first,
+ *   of these the first top_k are kept;
+ *   of these the first ones up to that at which the sum of w reaches top_p of the
+ *   sum over all that top_k kept;
+ *   of these the ones with w >= min_p (at least the first token);
+ * the token is the lowest index i at which the sum of the kept w over 0 .. i is
+ * above u times their total, u = uniforms[row] in [0, 1) (0 for a lower one or a
+ * NaN; for 1 and above the last kept token). Tokens whose w is below 2^-40 are
+ * never drawn and count nowhere. logprobs: log of the token's w over the kept total.
+ * A logit that is NaN counts as minus infinity; where the greatest is plus infinity,
+ * those that are have w = 1 and the others 0. A row with nothing above minus
+ * infinity has token -1 and logprob minus infinity.
+ * w and its sums have 43 bits and more: the result is that of exact numbers but for
+ * u (or top_p) within about 2^-40 of where another token begins. logits_dev:
+ * [rows][vocab] float32, bf16 or float16, rows row_stride elements apart, aligned to
+ * their elements. tokens_dev int32, logprobs_dev float32 [rows]. Errors: HL_EINVAL,
+ * HL_EUNSUPPORTED for vocab of 2^20 and above. */
+hl_status hl_sample(const hl_sampling* sampling, const void* logits_dev, hl_dtype dtype, uint64_t row_stride,
+                    uint32_t rows, uint64_t vocab, const float* uniforms_dev, int32_t* tokens_dev, float* logprobs_dev,
+                    void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,7 +11,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhufflm.so")
-SOURCES = ["kernels.hip", "norm.hip", "attention.hip", "evict.hip", "host_codec.cpp"]
+SOURCES = ["kernels.hip", "norm.hip", "attention.hip", "evict.hip", "attention4.hip",
+           "cache4.hip", "gemv4.hip", "sample.hip", "host_codec.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

@@ -92,6 +92,13 @@ class AttentionShape(ctypes.Structure):
                 ("scale", ctypes.c_float), ("prefix", KeysValues), ("own", KeysValues)]
 
 
+class Sampling(ctypes.Structure):
+    """hl_sampling."""
+    _fields_ = [("temperature_dev", ctypes.c_void_p), ("top_k_dev", ctypes.c_void_p), ("top_p_dev", ctypes.c_void_p),
+                ("min_p_dev", ctypes.c_void_p), ("temperature", ctypes.c_float), ("top_k", ctypes.c_int32),
+                ("top_p", ctypes.c_float), ("min_p", ctypes.c_float)]
+
+
 _lib = None
 
 EXPORTS = ["hl_status_str", "hl_default_seg_len", "hl_default_grp_rows", "hl_build_codebook", "hl_encode",
@@ -99,7 +106,9 @@ EXPORTS = ["hl_status_str", "hl_default_seg_len", "hl_default_grp_rows", "hl_bui
            "hl_tensor_view", "hl_tensor_prepare", "hl_decode", "hl_gemv_workspace_bytes",
            "hl_decode_gemv", "hl_decode_gemv_noalloc", "hl_decode_gemv_multi", "hl_gemm_workspace_bytes",
            "hl_decode_gemm",
-           "hl_gemv_bf16", "hl_rms_norm", "hl_attention_workspace_bytes", "hl_prefix_attention", "hl_cache_evict"]
+           "hl_gemv_bf16", "hl_rms_norm", "hl_attention_workspace_bytes", "hl_prefix_attention", "hl_cache_evict",
+           "hl_cache4_row_bytes", "hl_cache_write4", "hl_cache_read4", "hl_attention4_workspace_bytes",
+           "hl_prefix_attention4", "hl_gemv4", "hl_sample"]
 
 
 def lib() -> ctypes.CDLL:
@@ -171,6 +180,25 @@ def lib() -> ctypes.CDLL:
     L.hl_cache_evict.argtypes = [c.c_void_p, c.c_void_p, c.c_uint32, c.c_uint32, c.c_uint32,
                                  c.c_void_p, c.c_void_p, c.c_uint64, c.c_uint64, c.c_void_p, c.c_void_p, c.c_void_p,
                                  c.c_void_p]
+    L.hl_cache4_row_bytes.restype = c.c_size_t
+    L.hl_cache4_row_bytes.argtypes = [c.c_uint32]
+    L.hl_cache_write4.restype = c.c_int
+    L.hl_cache_write4.argtypes = [c.c_void_p, c.c_int, c.c_void_p, c.c_uint32, c.c_uint32, c.c_uint32, c.c_void_p,
+                                  c.c_void_p]
+    L.hl_cache_read4.restype = c.c_int
+    L.hl_cache_read4.argtypes = [c.c_void_p, c.c_uint64, c.c_uint64, c.c_uint64, c.c_uint32, c.c_uint64, c.c_uint32,
+                                 c.c_uint32, c.c_void_p, c.c_int, c.c_void_p]
+    L.hl_attention4_workspace_bytes.restype = c.c_size_t
+    L.hl_attention4_workspace_bytes.argtypes = [c.c_void_p, c.c_int]
+    L.hl_prefix_attention4.restype = c.c_int
+    L.hl_prefix_attention4.argtypes = [c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p,
+                                       c.c_void_p, c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p]
+    L.hl_gemv4.restype = c.c_int
+    L.hl_gemv4.argtypes = [c.c_void_p, c.c_void_p, c.c_void_p, c.c_int, c.c_uint64, c.c_uint64, c.c_uint32,
+                           c.c_void_p, c.c_int, c.c_uint32, c.c_void_p, c.c_void_p]
+    L.hl_sample.restype = c.c_int
+    L.hl_sample.argtypes = [c.c_void_p, c.c_void_p, c.c_int, c.c_uint64, c.c_uint32, c.c_uint64, c.c_void_p,
+                            c.c_void_p, c.c_void_p, c.c_void_p]
     _lib = L
     return L
 
@@ -515,6 +543,11 @@ class EvictResult(NamedTuple):
     slots: object
 
 
+class SampleResult(NamedTuple):
+    tokens: object    # int32 [rows]
+    logprobs: object  # float32 [rows], under the kept tokens' distribution
+
+
 class _Torch:
     """What a call of the operators needs of torch and of the library, looked up once: an import statement and the
     attributes' chains cost a small call a tenth of its time."""
@@ -524,6 +557,7 @@ class _Torch:
         self.codes = {torch.float32: HL_F32, torch.bfloat16: HL_BF16, torch.float16: HL_F16,
                       torch.float8_e4m3fn: HL_E4M3}
         self.float32, self.int32, self.uint8 = torch.float32, torch.int32, torch.uint8
+        self.bfloat16 = torch.bfloat16
         self.half = {torch.bfloat16: HL_BF16, torch.float16: HL_F16}
         self.two_bytes = (torch.bfloat16, torch.float16, torch.int16)
         self.empty, self.empty_like, self.Tensor = torch.empty, torch.empty_like, torch.Tensor
@@ -688,9 +722,15 @@ def prefix_attention(q, k=None, v=None, lens=None, prefix_k=None, prefix_v=None,
     key was given by this call (``weights_out`` may be ``weights``; without ``weights``, plus zeros). ``lse``: a
     float32 [batch, queries, heads] buffer for the logarithms of the softmax sums. ``workspace``: a device buffer of
     hl_attention_workspace_bytes. Buffers that are not given are allocated (on ``stream``, where one is given)."""
+    return _attend(False, q, k, v, lens, prefix_k, prefix_v, scale, weights, out, weights_out, lse, stream, workspace)
+
+
+def _attend(four, q, k, v, lens, prefix_k, prefix_v, scale, weights, out, weights_out, lse, stream,
+            workspace) -> AttentionResult:
+    """prefix_attention, or prefix_attention4."""
     if stream is not None:
-        return _on_stream(stream, q.get_device(), prefix_attention, q, k, v, lens, prefix_k, prefix_v, scale, weights,
-                          out, weights_out, lse, None, workspace)
+        return _on_stream(stream, q.get_device(), _attend, four, q, k, v, lens, prefix_k, prefix_v, scale, weights, out,
+                          weights_out, lse, None, workspace)
     T = _torch or _lookups()
     dtype = q.dtype
     code = T.half.get(dtype)
@@ -701,20 +741,24 @@ def prefix_attention(q, k=None, v=None, lens=None, prefix_k=None, prefix_v=None,
     if dev < 0 or not q.is_contiguous():
         raise ValueError("q must be contiguous and on the GPU")
     if dev != T.current_device():
-        return _on_gpu(dev, prefix_attention, q, k, v, lens, prefix_k, prefix_v, scale, weights, out, weights_out, lse,
-                       None, workspace)
+        return _on_gpu(dev, _attend, four, q, k, v, lens, prefix_k, prefix_v, scale, weights, out, weights_out, lse, None,
+                       workspace)
+    columns = dim
+    if four:
+        columns = _row_bytes(dim)
+    rows = _rows4 if four else _keys_values
     own = prefix = _NO_KV
     kv_heads = lens_ptr = w_ptr = w_out_ptr = lse_ptr = None
     if k is not None or v is not None:
-        own = _keys_values(k, v, "k, v", 4, dtype, dev)
+        own = rows(k, v, "k, v", 4, dtype, dev)
         kv_heads = k.shape[2]
-        if k.shape[0] != batch or k.shape[3] != dim:
-            raise ValueError(f"k, v must be [{batch}, capacity, kv_heads, {dim}], got {tuple(k.shape)}")
+        if k.shape[0] != batch or k.shape[3] != columns:
+            raise ValueError(f"k, v must be [{batch}, capacity, kv_heads, {columns}], got {tuple(k.shape)}")
         lens_ptr = _small(lens, "lens", T.int32, (batch,), dev).data_ptr()
     if prefix_k is not None or prefix_v is not None:
-        prefix = _keys_values(prefix_k, prefix_v, "prefix_k, prefix_v", 3, dtype, dev)
-        if prefix_k.shape[2] != dim or (kv_heads is not None and kv_heads != prefix_k.shape[1]):
-            raise ValueError(f"prefix_k, prefix_v must be [length, kv_heads, {dim}] with the own caches' kv_heads, "
+        prefix = rows(prefix_k, prefix_v, "prefix_k, prefix_v", 3, dtype, dev)
+        if prefix_k.shape[2] != columns or (kv_heads is not None and kv_heads != prefix_k.shape[1]):
+            raise ValueError(f"prefix_k, prefix_v must be [length, kv_heads, {columns}] with the own caches' kv_heads, "
                              f"got {tuple(prefix_k.shape)}")
         kv_heads = prefix_k.shape[1]
     if not kv_heads or heads % kv_heads:
@@ -740,14 +784,16 @@ def prefix_attention(q, k=None, v=None, lens=None, prefix_k=None, prefix_v=None,
                         1.0 / math.sqrt(dim) if scale is None else scale, *prefix, *own)
     L = T.lib
     if workspace is None:
-        workspace = T.empty(L.hl_attention_workspace_bytes(a, w_out_ptr is not None), dtype=T.uint8, device=q.device)
+        size = L.hl_attention4_workspace_bytes if four else L.hl_attention_workspace_bytes
+        workspace = T.empty(size(a, w_out_ptr is not None), dtype=T.uint8, device=q.device)
     else:
         _dev_arg(workspace, "workspace")
         _on_device(q.device, workspace=workspace)
-    s = L.hl_prefix_attention(a, q.data_ptr(), lens_ptr, out.data_ptr(), lse_ptr, w_ptr, w_out_ptr,
-                              workspace.data_ptr(), workspace.nbytes, T.raw_stream(dev))
+    f = L.hl_prefix_attention4 if four else L.hl_prefix_attention
+    s = f(a, q.data_ptr(), lens_ptr, out.data_ptr(), lse_ptr, w_ptr, w_out_ptr, workspace.data_ptr(), workspace.nbytes,
+          T.raw_stream(dev))
     if s:
-        _check(s, "hl_prefix_attention")
+        _check(s, "hl_prefix_attention4" if four else "hl_prefix_attention")
     return AttentionResult(out, weights_out, lse)
 
 
@@ -788,3 +834,222 @@ def cache_evict(k, v, weights, lens, keep: int, recent: int = 0, k_out=None, v_o
     if s:
         _check(s, "hl_cache_evict")
     return EvictResult(k_out, v_out, w_out, lens_out, slots)
+
+
+_SAMPLING = struct.Struct("=4Qfiff")
+
+
+def cache4_row_bytes(dim: int) -> int:
+    """Bytes of a 4-bit cache's row, a token's ``dim`` columns of one key head (a multiple of 32, at most 256): ``dim / 2``
+    bytes of codes, byte ``n * (dim / 32) + g`` with those of columns ``32g + 2n`` (its low half) and ``32g + 2n + 1``;
+    ``dim / 32`` pairs (scale, base) of bfloat16; zeros up to a multiple of 16. Columns 32g .. 32g + 31 stand for
+    ``base + scale * (code - 8)``."""
+    n = int(lib().hl_cache4_row_bytes(dim)) if 0 < dim < 1 << 32 else 0
+    if n == 0:
+        raise ValueError("dim must be a multiple of 32, at most 256")
+    return n
+
+
+_row_sizes: dict = {}
+
+
+def _row_bytes(dim: int) -> int:
+    n = _row_sizes.get(dim)
+    if n is None:
+        n = _row_sizes[dim] = cache4_row_bytes(dim)
+    return n
+
+
+def _rows4(k, v, name: str, dims: int, dtype, device: int):
+    """The fields of hl_kv for 4-bit rows [(sequence,) token, key head, byte] with any strides but a row's bytes in a row."""
+    if k is None or v is None or k.dim() != dims or v.shape != k.shape:
+        raise ValueError(f"{name}: keys and values of one shape, {dims} dimensions")
+    if k.dtype != _torch.uint8 or v.dtype != _torch.uint8:
+        raise ValueError(f"{name}: dtype {k.dtype} and {v.dtype}, expected 4-bit rows as torch.uint8")
+    if k.get_device() != device or v.get_device() != device or device < 0:
+        raise ValueError(f"{name} must be on GPU {device}, not {k.device} and {v.device}")
+    ks, vs = k.stride(), v.stride()
+    if ks[-1] != 1 or vs[-1] != 1:
+        raise ValueError(f"{name}: the bytes of a row must lie next to each other")
+    if any(x % 16 for x in ks[:-1]) or any(x % 16 for x in vs[:-1]):
+        raise ValueError(f"{name}: strides must be multiples of 16 bytes, got {ks} and {vs}")
+    ks, vs = (tuple(x // 2 for x in t) for t in (ks, vs))
+    if dims == 3:
+        return (k.data_ptr(), v.data_ptr(), k.shape[0], 0, ks[0], ks[1], 0, vs[0], vs[1])
+    return (k.data_ptr(), v.data_ptr(), k.shape[1], *ks[:3], *vs[:3])
+
+
+def cache_write4(k, v, cache_k, cache_v, lens=None, stream=None) -> None:
+    """Rounds new tokens' keys and values to 4 bits and puts them at the ends of the sequences' caches.
+
+    k, v: [batch, tokens, kv_heads, dim] bfloat16 or float16 (any strides with columns in a row), dim a multiple of 32.
+    cache_k, cache_v: uint8 [batch, capacity, kv_heads, cache4_row_bytes(dim)] (any strides, in multiples of 16, with a
+    row's bytes in a row). Token i of sequence b goes to slot lens[b] - tokens + i (lens: int32 [batch], the lengths with
+    the new tokens; without it, to slot i); tokens whose slot is not in the cache are left out. 32 neighbouring columns
+    share a scale and a base; if one of them is an infinity or a NaN they all become NaN."""
+    if stream is not None:
+        return _on_stream(stream, k.get_device(), cache_write4, k, v, cache_k, cache_v, lens)
+    T = _torch or _lookups()
+    code = T.half.get(k.dtype)
+    if code is None or k.dim() != 4:
+        raise ValueError("k must be [batch, tokens, kv_heads, dim] bfloat16 or float16")
+    batch, tokens, heads, dim = k.shape
+    dev = k.get_device()
+    if dev >= 0 and dev != T.current_device():
+        return _on_gpu(dev, cache_write4, k, v, cache_k, cache_v, lens)
+    src = _keys_values(k, v, "k, v", 4, k.dtype, dev)
+    dst = _rows4(cache_k, cache_v, "cache_k, cache_v", 4, None, dev)
+    if cache_k.shape[0] != batch or cache_k.shape[2] != heads or cache_k.shape[3] != _row_bytes(dim):
+        raise ValueError(f"cache_k, cache_v must be [{batch}, capacity, {heads}, {_row_bytes(dim)}], "
+                         f"got {tuple(cache_k.shape)}")
+    if any(n > 1 and 0 in (x, y) for n, x, y in zip(cache_k.shape, cache_k.stride(), cache_v.stride())):
+        raise ValueError("cache_k, cache_v: every row needs memory of its own")
+    lens_ptr = None if lens is None else _small(lens, "lens", T.int32, (batch,), dev).data_ptr()
+    s = T.lib.hl_cache_write4(_KV.pack(*src), code, _KV.pack(*dst), batch, heads, dim, lens_ptr, T.raw_stream(dev))
+    if s:
+        _check(s, "hl_cache_write4")
+
+
+def cache_read4(cache, dim: int, dtype=None, out=None, stream=None):
+    """The values [..., dim] that 4-bit rows stand for.
+
+    cache: uint8 [(batch,) tokens, kv_heads, cache4_row_bytes(dim)] (any strides, in multiples of 16, with a row's bytes in
+    a row). dtype: float32, bfloat16 (the default) or float16; out (of that type) is allocated where it is not given (on
+    ``stream``, where one is given)."""
+    if stream is not None:
+        return _on_stream(stream, cache.get_device(), cache_read4, cache, dim, dtype, out)
+    T = _torch or _lookups()
+    dev = cache.get_device()
+    if dev >= 0 and dev != T.current_device():
+        return _on_gpu(dev, cache_read4, cache, dim, dtype, out)
+    if cache.dim() not in (3, 4):
+        raise ValueError("cache must be [(batch,) tokens, kv_heads, bytes of a row]")
+    rows = _rows4(cache, cache, "cache", cache.dim(), None, dev)
+    shape = cache.shape
+    if shape[-1] != _row_bytes(dim) or 0 in shape:
+        raise ValueError(f"cache must be [(batch,) tokens, kv_heads, {_row_bytes(dim)}], got {tuple(shape)}")
+    if out is None:
+        out = T.empty((*shape[:-1], dim), dtype=T.bfloat16 if dtype is None else dtype, device=cache.device)
+    else:
+        _small(out, "out", out.dtype if dtype is None else dtype, (*shape[:-1], dim), dev)
+    code = T.codes.get(out.dtype)
+    if code is None or code == HL_E4M3:
+        raise ValueError("dtype must be float32, bfloat16 or float16")
+    s = T.lib.hl_cache_read4(rows[0], 2 * rows[3], 2 * rows[4], 2 * rows[5], shape[0] if len(shape) == 4 else 1, rows[2],
+                             shape[-2], dim, out.data_ptr(), code, T.raw_stream(dev))
+    if s:
+        _check(s, "hl_cache_read4")
+    return out
+
+
+def prefix_attention4(q, k=None, v=None, lens=None, prefix_k=None, prefix_v=None, scale: Optional[float] = None,
+                      weights=None, out=None, weights_out=None, lse=None, stream=None, workspace=None) -> AttentionResult:
+    """prefix_attention over a prefix and own caches held in 4 bits.
+
+    k, v: uint8 [batch, capacity, kv_heads, cache4_row_bytes(dim)], prefix_k, prefix_v: uint8 [length, kv_heads,
+    cache4_row_bytes(dim)] (any strides, in multiples of 16, with a row's bytes in a row), as cache_write4 leaves them
+    (a prefix is a cache's only sequence, ``cache_k[0, :n]``). q's dim is a multiple of 32. The rest, and the result, are
+    prefix_attention's; ``workspace``: a device buffer of hl_attention4_workspace_bytes."""
+    return _attend(True, q, k, v, lens, prefix_k, prefix_v, scale, weights, out, weights_out, lse, stream, workspace)
+
+
+def gemv4(codes, scales, x, bases=None, y=None, stream=None):
+    """y [batch, rows] float32 = x times the rows of a matrix of 4-bit codes, base + scale * (code - 8).
+
+    codes: uint8 [rows, cols / 2], an even column's code in a byte's low half, the next one's in its high half; scales, bases
+    (or None: all 0): bfloat16 or float16 [rows, cols / group], group 32, 64 or 128; x: [batch <= 16, cols] (or [cols])
+    bfloat16 or float16. All contiguous. y is allocated where it is not given (on ``stream``, where one is given)."""
+    if stream is not None:
+        return _on_stream(stream, codes.get_device(), gemv4, codes, scales, x, bases, y)
+    T = _torch or _lookups()
+    dev = codes.get_device()
+    if dev >= 0 and dev != T.current_device():
+        return _on_gpu(dev, gemv4, codes, scales, x, bases, y)
+    if codes.dim() != 2 or codes.dtype != T.uint8 or scales.dim() != 2 or codes.numel() == 0:
+        raise ValueError("codes must be uint8 [rows, cols / 2] and scales [rows, cols / group]")
+    rows, cols, groups = codes.shape[0], 2 * codes.shape[1], scales.shape[1]
+    if scales.shape[0] != rows or groups == 0 or cols % groups or cols // groups not in (32, 64, 128):
+        raise ValueError(f"scales must be [{rows}, {cols} / group] with groups of 32, 64 or 128 columns, "
+                         f"got {tuple(scales.shape)}")
+    if x.dim() == 1:
+        x = x.unsqueeze(0)
+    if x.dim() != 2 or x.shape[1] != cols or not 1 <= x.shape[0] <= MAX_BATCH:
+        raise ValueError(f"x must be [batch <= {MAX_BATCH}, {cols}], got {tuple(x.shape)}")
+    xt, st = T.half.get(x.dtype), T.half.get(scales.dtype)
+    if xt is None or st is None:
+        raise ValueError("x and scales must be bfloat16 or float16")
+    if bases is not None and (bases.dtype != scales.dtype or bases.shape != scales.shape):
+        raise ValueError("bases must have the type and shape of scales")
+    need = (x.shape[0], rows)
+    if y is None:
+        y = T.empty(need, dtype=T.float32, device=codes.device)
+    else:
+        _small(y, "y", T.float32, need, dev)
+    if dev < 0 or not (codes.is_contiguous() and scales.is_contiguous() and x.is_contiguous()) \
+            or scales.get_device() != dev or x.get_device() != dev \
+            or (bases is not None and (bases.get_device() != dev or not bases.is_contiguous())):
+        _plain(dev, {"codes": codes, "scales": scales, "bases": bases, "x": x})
+    s = T.lib.hl_gemv4(codes.data_ptr(), scales.data_ptr(), None if bases is None else bases.data_ptr(), st, rows, cols,
+                       cols // groups, x.data_ptr(), xt, x.shape[0], y.data_ptr(), T.raw_stream(dev))
+    if s:
+        _check(s, "hl_gemv4")
+    return y
+
+
+def sample(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tokens=None, logprobs=None,
+           stream=None) -> SampleResult:
+    """A token of each row of logits [rows, vocab] (or [vocab]; float32, bfloat16 or float16, rows at any distance).
+
+    The settings are numbers, or tensors [rows] on the GPU (float32; top_k int32). With w = exp((logit - max) /
+    temperature) and the tokens in the order of falling logits, lowest index first: the first top_k (0: all) are kept; of
+    these those up to that at which the sum of w reaches top_p of all of theirs (1: all); of these those with w >= min_p.
+    The token is the first by index at which the kept tokens' running sum of w is above uniforms (float32 [rows], in
+    [0, 1)) times their total. temperature 0: the greatest logit's token. Tokens of w below 2^-40 are never drawn.
+
+    Gives the tokens (int32 [rows]; -1 where no logit is above minus infinity) and the logarithms of their shares of the
+    kept tokens' total (float32 [rows]), allocated where they are not given (on ``stream``, where one is given)."""
+    if stream is not None:
+        return _on_stream(stream, logits.get_device(), sample, logits, uniforms, temperature, top_k, top_p, min_p, tokens,
+                          logprobs)
+    T = _torch or _lookups()
+    dev = logits.get_device()
+    if dev >= 0 and dev != T.current_device():
+        return _on_gpu(dev, sample, logits, uniforms, temperature, top_k, top_p, min_p, tokens, logprobs)
+    if logits.dim() == 1:
+        logits = logits.unsqueeze(0)
+    code = T.codes.get(logits.dtype)
+    if logits.dim() != 2 or logits.numel() == 0 or code is None or code == HL_E4M3:
+        raise ValueError("logits must be [rows, vocab] float32, bfloat16 or float16")
+    rows, vocab = logits.shape
+    strides = logits.stride()
+    if dev < 0 or (strides[1] != 1 and vocab > 1):
+        raise ValueError("logits must be on the GPU, with the logits of a row next to each other")
+    if rows > 1 and strides[0] < vocab:
+        raise ValueError("logits: every row needs memory of its own")
+    need = (rows,)
+    _small(uniforms, "uniforms", T.float32, need, dev)
+    pointers, numbers = [], []
+    for value, name, dtype, most in ((temperature, "temperature", T.float32, math.inf), (top_k, "top_k", T.int32, math.inf),
+                                     (top_p, "top_p", T.float32, math.inf), (min_p, "min_p", T.float32, 1.0)):
+        if isinstance(value, T.Tensor):
+            pointers.append(_small(value, name, dtype, need, dev).data_ptr())
+            numbers.append(0)
+        elif 0 <= value <= most:
+            pointers.append(0)
+            numbers.append(value)
+        else:
+            raise ValueError(f"{name} must be at least 0{'' if most == math.inf else ' and at most 1'}, got {value}")
+    if tokens is None:
+        tokens = T.empty(need, dtype=T.int32, device=logits.device)
+    else:
+        _small(tokens, "tokens", T.int32, need, dev)
+    if logprobs is None:
+        logprobs = T.empty(need, dtype=T.float32, device=logits.device)
+    else:
+        _small(logprobs, "logprobs", T.float32, need, dev)
+    settings = _SAMPLING.pack(*pointers, numbers[0], min(int(numbers[1]), 0x7FFFFFFF), numbers[2], numbers[3])
+    s = T.lib.hl_sample(settings, logits.data_ptr(), code, strides[0], rows, vocab, uniforms.data_ptr(),
+                        tokens.data_ptr(), logprobs.data_ptr(), T.raw_stream(dev))
+    if s:
+        _check(s, "hl_sample")
+    return SampleResult(tokens, logprobs)

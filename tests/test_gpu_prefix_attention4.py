@@ -1,0 +1,264 @@
+"""prefix_attention4 against the definition in 64 bits on what the rows stand for (MI355X).
+
+Bounds of an output: one rounding to its type (u: 2^-8 for bf16, 2^-11 for float16); w = p * scale is rounded to bf16
+(r: 2^-8 of it; for a float16 output to two pieces, 2^-16), and meets code - 8: of sum |p scale (code - 8)|. A score is a
+float32 sum of products with 16 + code, less 24 times q's sum: it is off by at most e = (dim + 40) * 2^-24 * max sum |q|
+(40 scale + |base|) * the scores' scale, which moves a weight and the sum under it by at most a factor exp(e) each. The
+sums of weights times 16 + code (up to 31, less 24) and of the parts add at most 64 * 2^-24 of sum p (55 scale + |base|)."""
+import math
+
+import pytest
+import torch
+
+import paper_2502_00922_amd as hl
+from rows4 import parts, random_rows, row_bytes
+
+pytestmark = pytest.mark.gpu
+U = {torch.bfloat16: 2.0**-8, torch.float16: 2.0**-11}
+R = {torch.bfloat16: 2.0**-8, torch.float16: 2.0**-16}
+TYPES = [torch.bfloat16, torch.float16]
+
+
+def make(dtype, batch, queries, heads, kv_heads, dim, prefix, own, lens=None, size=1.5, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    c = {"q": (size * torch.randn((batch, queries, heads, dim), generator=g, device="cuda")).to(dtype)}
+    if own:
+        c["k"], c["v"] = (random_rows((batch, own, kv_heads), dim, g) for _ in range(2))
+        if lens is None:
+            lens = [own - (own - min(queries, own)) * i // max(batch, 1) for i in range(batch)]
+        c["lens"] = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    if prefix:
+        c["prefix_k"], c["prefix_v"] = (random_rows((prefix, kv_heads), dim, g) for _ in range(2))
+    return c
+
+
+def reference(c, scale=None):
+    """out, lse, own weights, and of the bounds above: sum |p scale (code - 8)|, sum p (55 scale + |base|) and e's size."""
+    q = c["q"].double().cpu()
+    batch, queries, heads, dim = q.shape
+    scale = 1 / math.sqrt(dim) if scale is None else scale
+    some = c["k"] if "k" in c else c["prefix_k"]
+    kv_heads, share = some.shape[-2], heads // some.shape[-2]
+    cap = c["k"].shape[1] if "k" in c else 0
+    held = {x: parts(c[x], dim) for x in ("k", "v", "prefix_k", "prefix_v") if x in c}
+    out, steps, sums = (torch.zeros_like(q) for _ in range(3))
+    lse = torch.full((batch, queries, heads), -math.inf, dtype=torch.float64)
+    weights = torch.zeros((batch, kv_heads, cap), dtype=torch.float64)
+    none = (torch.zeros((0, dim), dtype=torch.float64),) * 3
+    most = 0.0
+    for b in range(batch):
+        n = min(max(int(c["lens"][b]), 0), cap) if cap else 0
+        for h in range(kv_heads):
+            pk, pv = (tuple(t[:, h] for t in held[x]) if x in held else none for x in ("prefix_k", "prefix_v"))
+            ok, ov = (tuple(t[b, :n, h] for t in held[x]) if x in held else none for x in ("k", "v"))
+            for i in range(queries):
+                seen = max(0, n - (queries - 1 - i))
+                (kc, ks, kb), (vc, vs, vb) = (tuple(torch.cat([x, y[:seen]]) for x, y in zip(pre, own))
+                                              for pre, own in ((pk, ok), (pv, ov)))
+                if not len(kc):
+                    continue
+                at = slice(h * share, (h + 1) * share)
+                rows = q[b, i, at]
+                s = rows @ (kb + ks * (kc - 8)).T * scale
+                most = max(most, float((rows.abs() @ (40 * ks + kb.abs()).T).max()) * abs(scale))
+                p = torch.softmax(s, 1)
+                out[b, i, at] = p @ (vb + vs * (vc - 8))
+                steps[b, i, at] = p @ (vs * (vc - 8)).abs()
+                sums[b, i, at] = p @ (55 * vs + vb.abs())
+                lse[b, i, at] = torch.logsumexp(s, 1)
+                weights[b, h, :seen] += p[:, len(pk[0]):].sum(0)
+    return out, lse, weights, steps, sums, most
+
+
+def check(c, scale=None, **more):
+    q = c["q"]
+    batch, queries, heads, dim = q.shape
+    lse = torch.full((batch, queries, heads), 77.0, device="cuda")
+    start = None
+    if "k" in c:
+        start = torch.rand((batch, c["k"].shape[2], c["k"].shape[1]), device="cuda")
+        more = {**more, "weights": start.clone()}
+    r = hl.prefix_attention4(**c, scale=scale, lse=lse, **more)
+    out, want_lse, weights, steps, sums, most = reference(c, scale)
+    e = (dim + 40) * 2.0**-24 * most
+    u = U[q.dtype]
+    bound = u * out.abs() + (1 + u) * (R[q.dtype] * steps + (2 * e + 64 * 2.0**-24) * sums) + 2.0**-25
+    got = r.out.double().cpu()
+    assert ((got - out).abs() <= bound).all(), float(((got - out).abs() / bound).max())
+    empty = want_lse == -math.inf
+    assert (got[empty] == 0).all() and (r.lse.double().cpu()[empty] == -math.inf).all()
+    d = (r.lse.double().cpu() - want_lse)[~empty].abs()
+    assert (d <= e + 64 * 2.0**-24 + 4 * 2.0**-24 * want_lse[~empty].abs()).all()
+    if start is not None:
+        w = start.double().cpu() + weights
+        err = (r.weights.double().cpu() - w).abs()
+        assert (err <= (2 * e + 80 * 2.0**-24) * weights + 2.0**-23 * w + 1e-12).all()
+    return r
+
+
+SHAPES = [  # batch, queries, heads, kv_heads, dim, prefix, own
+    (1, 1, 1, 1, 64, 0, 1), (1, 1, 1, 1, 64, 1, 0), (1, 1, 4, 4, 32, 5, 3), (2, 1, 4, 2, 96, 31, 33),
+    (1, 1, 32, 8, 128, 512, 300), (16, 1, 32, 8, 128, 129, 65), (3, 1, 64, 8, 128, 127, 128), (5, 3, 8, 8, 128, 177, 77),
+    (4, 2, 24, 8, 160, 33, 200), (2, 5, 12, 2, 96, 100, 131), (7, 1, 16, 2, 256, 70, 45), (2, 9, 4, 1, 192, 50, 40),
+    (5, 9, 16, 4, 128, 300, 64), (2, 40, 8, 2, 128, 90, 111), (3, 33, 8, 1, 64, 65, 33), (70, 1, 4, 2, 64, 40, 19),
+    (130, 1, 2, 1, 128, 17, 9), (2, 70, 4, 2, 256, 40, 90), (1, 1, 8, 8, 128, 3001, 0), (1, 1, 8, 8, 128, 0, 3001),
+    (2, 7, 6, 3, 224, 260, 7), (1, 200, 4, 1, 128, 0, 200), (2, 1, 8, 2, 32, 1500, 700), (3, 2, 6, 2, 96, 1300, 400),
+    (2, 1, 8, 4, 160, 1200, 90), (2, 1, 8, 4, 192, 1200, 90), (2, 1, 8, 4, 224, 1200, 90), (2, 1, 8, 4, 256, 1200, 90),
+    (1, 30, 4, 2, 32, 200, 100), (1, 30, 4, 2, 160, 200, 100), (1, 30, 4, 2, 192, 200, 100), (1, 30, 4, 2, 224, 200, 100)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", SHAPES)
+def test_shapes(dtype, shape):
+    check(make(dtype, *shape))
+
+
+@pytest.mark.parametrize("queries,lens", [(1, [0, 1, 2, 64, 63, 65]), (4, [0, 1, 2, 3, 4, 5]), (3, [-5, 1000, 96, 31, 32, 33])])
+@pytest.mark.parametrize("prefix", [0, 37])
+def test_lengths(queries, lens, prefix):
+    # among them sequences without a key, and tokens that see none
+    check(make(torch.bfloat16, 6, queries, 8, 2, 64, prefix, 96, lens=lens))
+
+
+@pytest.mark.parametrize("queries,lens", [(1, [0, 1500, 1, 7]), (6, [3, 1500, 0, 1400]), (20, [3, 1500, 0, 1400])])
+def test_lengths_in_parts(queries, lens):
+    check(make(torch.float16, 4, queries, 8, 2, 128, 0, 1500, lens=lens))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("size", [0.0, 10.0, 40.0])
+def test_flat_and_steep(dtype, size):
+    check(make(dtype, 2, 2, 8, 2, 128, 500, 300, size=size))
+
+
+@pytest.mark.parametrize("scale", [-0.3, 0.0, 2.0])
+def test_scale(scale):
+    check(make(torch.float16, 2, 2, 4, 2, 64, 100, 90), scale=scale)
+
+
+def test_maximum_grows_along_the_keys():
+    # every step's scores pass the ones before by more than the slack
+    c = make(torch.bfloat16, 2, 1, 8, 2, 128, 900, 600)
+    c["q"][...] = 1
+    for x, first in (("prefix_k", 0), ("k", 900)):
+        n = c[x].shape[-3]
+        base = ((first + torch.arange(n, device="cuda")) / 300).bfloat16().view(n, 1, 1)
+        pairs = c[x][..., 64:80].contiguous().view(torch.bfloat16).unflatten(-1, (4, 2))
+        pairs[..., 1] = base
+        c[x][..., 64:80] = pairs.flatten(-2).view(torch.uint8)
+    check(c)
+
+
+def test_strides():
+    c = make(torch.bfloat16, 3, 2, 8, 2, 128, 300, 150)
+    a = check(c)
+    by_head = {x: c[x].transpose(-3, -2).contiguous().transpose(-3, -2) for x in ("k", "v", "prefix_k", "prefix_v")}
+    wide = torch.zeros((3, 150, 2, 3 * 80), dtype=torch.uint8, device="cuda")
+    wide[..., 80:160] = c["v"]
+    wide[..., 160:] = 0xFF
+    wide[..., :80] = 0xFF
+    for other in (by_head, {**by_head, "v": wide[..., 80:160]}):
+        b = hl.prefix_attention4(**{**c, **other})
+        assert torch.equal(a.out, b.out)
+
+
+def nan_rows(t):
+    t[...] = 0xFF  # codes 15, scales and bases NaN
+
+
+@pytest.mark.parametrize("queries", [1, 3, 20])
+@pytest.mark.parametrize("own", [90, 1300])
+@pytest.mark.parametrize("dim", [96, 128, 256])
+def test_unseen_rows_may_hold_anything(queries, own, dim):
+    lens = [own - 1, own // 2, queries, 0]
+    c = make(torch.bfloat16, 4, queries, 8, 2, dim, 40, own, lens=lens)
+    clean = check(c)
+    for b, n in enumerate(lens):
+        nan_rows(c["k"][b, n:]), nan_rows(c["v"][b, n:])
+    dirty = hl.prefix_attention4(**c)
+    assert torch.equal(clean.out, dirty.out)
+
+
+@pytest.mark.parametrize("queries", [4, 20])
+def test_new_tokens_of_nan_reach_only_those_that_see_them(queries):
+    lens = [70, 64, queries]
+    c = make(torch.bfloat16, 3, queries, 4, 2, 128, 30, 70, lens=lens)
+    clean = hl.prefix_attention4(**c).out
+    for b, n in enumerate(lens):
+        nan_rows(c["v"][b, n - 2:n])
+    got = hl.prefix_attention4(**c).out
+    assert torch.equal(got[:, :-2], clean[:, :-2]) and got[:, -2:].isnan().all()
+    for b, n in enumerate(lens):
+        nan_rows(c["k"][b, n - 1:n])
+    got = hl.prefix_attention4(**c).out
+    assert torch.equal(got[:, :-2], clean[:, :-2]) and got[:, -2:].isnan().all()
+
+
+def test_one_group_of_nan():
+    # other columns are as they were
+    c = make(torch.float16, 2, 1, 4, 2, 128, 50, 60)
+    clean = hl.prefix_attention4(**c).out
+    c["prefix_v"][7, 1, 64 + 4:64 + 8] = 0xFF
+    got = hl.prefix_attention4(**c).out
+    assert got[:, :, 2:, 32:64].isnan().all()
+    got[:, :, 2:, 32:64] = clean[:, :, 2:, 32:64]
+    assert torch.equal(got, clean)
+
+
+def test_bytes_past_the_pairs_do_not_matter():
+    for dim in (32, 64, 96, 160, 224):
+        c = make(torch.bfloat16, 2, 2, 4, 2, dim, 40, 50)
+        clean = hl.prefix_attention4(**c).out
+        for x in ("k", "v", "prefix_k", "prefix_v"):
+            c[x][..., dim // 2 + dim // 8:] = 0xFF
+        assert torch.equal(hl.prefix_attention4(**c).out, clean)
+
+
+def test_repeats_are_equal():
+    c = make(torch.bfloat16, 5, 1, 32, 8, 128, 3000, 900)
+    a, b = (hl.prefix_attention4(**c) for _ in range(2))
+    assert torch.equal(a.out, b.out)
+
+
+def test_captured():
+    # replays go by the lengths then
+    c = make(torch.bfloat16, 3, 1, 8, 2, 128, 1000, 500, lens=[0, 1, 2])
+    w = torch.zeros((3, 2, 500), device="cuda")
+    run = lambda: hl.prefix_attention4(**c, weights=w)  # noqa: E731
+    run()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c["lens"] += 70
+        held = run()
+    for _ in range(4):
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = run()
+        assert torch.equal(held.out, eager.out) and torch.equal(held.weights, eager.weights)
+
+
+def test_two_streams_at_once():
+    c = [make(torch.bfloat16, 4, 1, 32, 8, 128, 4000, 300, seed=i) for i in range(2)]
+    want = [hl.prefix_attention4(**x).out for x in c]
+    streams = [torch.cuda.Stream() for _ in c]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        got = [hl.prefix_attention4(**x, stream=s).out for x, s in zip(c, streams)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("queries", [1, 20])
+def test_far_tokens(queries):
+    # tokens so far apart that offsets pass 32 bits
+    stride, tokens, n = 1 << 24, 300, row_bytes(128)
+    big = torch.empty(tokens * stride + n, dtype=torch.uint8, device="cuda")
+    far = big.as_strided((1, tokens, 1, n), (0, stride, n, 1))
+    c = make(torch.bfloat16, 1, queries, 4, 1, 128, 0, tokens)
+    want = hl.prefix_attention4(**c).out
+    for name in ("k", "v"):
+        far.copy_(c[name])
+        assert torch.equal(hl.prefix_attention4(**{**c, name: far}).out, want)
+        assert torch.equal(hl.prefix_attention4(c["q"], prefix_k=c["k"][0], prefix_v=c["v"][0]).out,
+                           hl.prefix_attention4(c["q"], prefix_k=(far if name == "k" else c["k"])[0],
+                                                prefix_v=(far if name == "v" else c["v"])[0]).out)
