@@ -600,11 +600,15 @@ typedef struct {
  * w and its sums have 43 bits and more: the result is that of exact numbers but for
  * u (or top_p) within about 2^-40 of where another token begins. logits_dev:
  * [rows][vocab] float32, bf16 or float16, rows row_stride elements apart, aligned to
- * their elements. tokens_dev int32, logprobs_dev float32 [rows]. Errors: HL_EINVAL,
- * HL_EUNSUPPORTED for vocab of 2^20 and above. */
+ * their elements. tokens_dev int32, logprobs_dev float32 [rows]. workspace_dev:
+ * hl_sample_workspace_bytes (16-byte aligned, no initial contents needed; 0 on bad
+ * arguments); calls that may run concurrently need separate ones. Errors: HL_EINVAL
+ * (also for a missing or short workspace), HL_EUNSUPPORTED for vocab of 2^20 and
+ * above and more than 65535 rows. */
+size_t hl_sample_workspace_bytes(uint32_t rows, uint64_t vocab);
 hl_status hl_sample(const hl_sampling* sampling, const void* logits_dev, hl_dtype dtype, uint64_t row_stride,
                     uint32_t rows, uint64_t vocab, const float* uniforms_dev, int32_t* tokens_dev, float* logprobs_dev,
-                    void* stream);
+                    void* workspace_dev, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

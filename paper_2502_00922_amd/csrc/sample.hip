@@ -5,9 +5,19 @@
 // numbers of 2^-43 of the greatest: sums of them are exact, so they do not depend
 // on the order of additions, and equal logits have equal weights. Tokens below 2^-40
 // of the greatest weigh nothing. The tokens that top-k and top-p keep are the first
-// ones by (logit, lowest index); where they end is found from histograms, first of
-// 2048 steps of the distance to the greatest logit, then, within one step, of the
-// digits of the logits as ordered integers.
+// ones by (logit, lowest index); where they end is found in two steps: a histogram
+// of the distances to the greatest logit says in which of kSteps steps, and the few
+// logits of that step, put on a list in the order of their indexes, say where in it.
+//
+// Rows are cut into slices, so that few rows use the whole GPU too. top_kernel finds
+// each slice's greatest logit; step_kernel counts (or weighs) the steps, for the row
+// and for its slice, and its last block of a row finds the border's step;
+// finish_kernel lists that step's logits, and the last of a row's blocks to arrive
+// ends the row: it has every slice's weight below the step and the list, and looks
+// again only at the slice that the token is in. With top_k of kFew or less all that
+// is kept is on the list, and nothing else is weighed. Where a list would be too long
+// (more than kList logits in a step), the block takes the whole row's logits again
+// for each digit of the border (slow_row).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -16,14 +26,39 @@
 
 namespace hl {
 
-constexpr uint32_t kSampleThreads = 1024, kSampleWaves = kSampleThreads / 64, kSteps = 2048;
+constexpr uint32_t kSteps = 1024, kSlices = 64, kList = 2048, kFew = 1024;
+constexpr uint32_t kThreads = 256, kWaves = kThreads / 64;
+constexpr uint32_t kPairs = 256;  // logits on a list, at most, that are compared each with each
 constexpr double kSpan = 40.0;  // powers of two below the greatest weight that a token may have
+constexpr double kLn2 = 0.6931471805599453;
 constexpr double kOne = 0x1p43;
+
+typedef unsigned long long u64;
+
+// A row's part of the workspace; then its slices', one after the other.
+struct RowWork {
+  u64 mass[kSteps];
+  uint32_t count[kSteps];
+  u64 sum[kSlices];  // of the slice's weights that are kept whatever the list says
+  float most[kSlices], lowest[kSlices];
+  uint32_t first[kSlices], listed[kSlices];  // first: index of most
+  // The border. Steps below lo are kept as far as top_k and top_p go, above hi not;
+  // those between, and step `other`, go on the list. by_count, by_mass: whether
+  // top_k and top_p end there. From step `from` on, top_k's border is on the list.
+  uint32_t lo, hi, other, from, by_count, by_mass;
+  uint32_t arrived[2];
+  u64 count_from, mass_from, mass_lo;  // of the steps below `from` and lo
+  u64 unused[5];
+};
+struct SliceWork {
+  u64 mass[kSteps];
+  u64 list[kList];  // logit's bits, and its index above them
+};
 
 struct SampleArgs {
   const void* logits;
   uint64_t stride;
-  uint32_t vocab;
+  uint32_t vocab, slice, slices;  // slice: logits of one
   const float* uniforms;
   const float *temperatures, *top_ps, *min_ps;  // null: the numbers below, for all rows
   const int32_t* top_ks;
@@ -31,6 +66,14 @@ struct SampleArgs {
   int32_t top_k;
   int32_t* tokens;
   float* logprobs;
+  uint8_t* work;
+
+  __device__ RowWork& of_row(uint32_t row) const {
+    return *reinterpret_cast<RowWork*>(work + row * (sizeof(RowWork) + (uint64_t)slices * sizeof(SliceWork)));
+  }
+  __device__ SliceWork& of_slice(uint32_t row, uint32_t i) const {
+    return reinterpret_cast<SliceWork*>(&of_row(row) + 1)[i];
+  }
 };
 
 // A logit as an integer, the greater the logit the smaller; -0 is 0.
@@ -49,332 +92,731 @@ __device__ inline X scan_wave(X v) {
   return v;
 }
 
-// The row's block. Every wave has a stretch of neighbouring logits, VEC of a lane
-// next to each other. NV: logits a thread keeps in registers; 0: they are read
-// again each time.
-template <class T, int NV>
-struct RowOf {
-  static constexpr uint32_t VEC = 16 / sizeof(T), KEPT = NV ? NV : VEC;
-  const T* row;
-  uint32_t vocab, begin, end;  // this wave's stretch
-  float v[KEPT];
+template <class X>
+__device__ inline X add_wave(X v) {
+#pragma unroll
+  for (uint32_t d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
 
-  // VEC logits from `at` on; past the vocabulary and for NaN, -infinity
-  __device__ static void read(const T* row, uint32_t vocab, uint32_t at, float* to) {
+__device__ inline float most_wave(float v) {
+#pragma unroll
+  for (uint32_t d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+
+// A value that another block of the kernel stores or loads: performed at the
+// memory that all XCDs share.
+template <class X>
+__device__ inline void give(X* p, X v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <class X>
+__device__ inline X take(const X* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// Logits at .. at+VEC-1 of a row as float32; NaN, and past `end`, -infinity.
+template <class T>
+struct Logits {
+  static constexpr uint32_t VEC = 16 / sizeof(T);
+  __device__ static void read(const T* row, uint32_t end, uint32_t at, float (&to)[VEC]) {
     typedef T Vec __attribute__((ext_vector_type(VEC)));
     struct __attribute__((packed, aligned(sizeof(T)))) Loose { Vec x; };  // a row may begin anywhere
     Vec x;
-    if (at + VEC <= vocab) {
+    if (at + VEC <= end) {
       x = reinterpret_cast<const Loose*>(row + at)->x;
     } else {
 #pragma unroll
-      for (uint32_t j = 0; j < VEC; ++j) x[j] = at + j < vocab ? row[at + j] : (T)-INFINITY;
+      for (uint32_t j = 0; j < VEC; ++j) x[j] = at + j < end ? row[at + j] : (T)-INFINITY;
     }
 #pragma unroll
     for (uint32_t j = 0; j < VEC; ++j) to[j] = x[j] == x[j] ? (float)x[j] : -INFINITY;
   }
-
-  __device__ void open(const T* r, uint32_t n) {
-    row = r, vocab = n;
-    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
-    const uint32_t each = NV ? NV * 64 : (n + kSampleWaves * 64 * VEC - 1) / (kSampleWaves * 64 * VEC) * (64 * VEC);
-    begin = wave * each < n ? wave * each : n, end = begin + each < n ? begin + each : n;
-    if constexpr (NV) {
-#pragma unroll
-      for (uint32_t i = 0; i < NV / VEC; ++i) read(row, vocab, begin + (i * 64 + lane) * VEC, v + i * VEC);
-    }
-  }
-
-  // f(logit, index) for this lane's logits, in the order of their indexes
-  template <class F>
-  __device__ __attribute__((always_inline)) void each(F f) {
-    const uint32_t lane = threadIdx.x % 64;
-    if constexpr (NV) {
-#pragma unroll
-      for (uint32_t i = 0; i < NV / VEC; ++i)
-#pragma unroll
-        for (uint32_t j = 0; j < VEC; ++j) f(v[i * VEC + j], begin + (i * 64 + lane) * VEC + j);
-    } else {
-      for (uint32_t at = begin; at < end; at += 64 * VEC) {
-        read(row, vocab, at + lane * VEC, v);
-#pragma unroll
-        for (uint32_t j = 0; j < VEC; ++j) f(v[j], at + lane * VEC + j);
-      }
-    }
-  }
-
-  // The first index at which the running sum of weigh(logit, index) over the
-  // wave's stretch is above `target`. Whole wave.
-  template <class F>
-  __device__ __attribute__((always_inline)) uint32_t pick(uint64_t target, F weigh) {
-    const uint32_t lane = threadIdx.x % 64;
-    uint64_t before = 0;
-    uint32_t found = ~0u;
-    const auto look = [&](const float* l, uint32_t at) __attribute__((always_inline)) {
-      uint64_t w[VEC], sum = 0;
-#pragma unroll
-      for (uint32_t j = 0; j < VEC; ++j) w[j] = weigh(l[j], at + lane * VEC + j), sum += w[j];
-      const uint64_t upto = before + scan_wave(sum);
-      const uint64_t past = __ballot(upto > target);
-      if (past) {
-        uint64_t run = upto - sum;
-        uint32_t mine = 0;
-        bool there = false;
-#pragma unroll
-        for (uint32_t j = 0; j < VEC; ++j) {
-          run += w[j];
-          if (!there && run > target) mine = at + lane * VEC + j, there = true;
-        }
-        found = __builtin_amdgcn_readlane(mine, __builtin_ctzll(past));
-      }
-      before = __shfl(upto, 63);
-      return past != 0;
-    };
-    if constexpr (NV) {
-#pragma unroll
-      for (uint32_t i = 0; i < NV / VEC; ++i)
-        if (found == ~0u) look(v + i * VEC, begin + i * 64 * VEC);
-    } else {
-      for (uint32_t at = begin; at < end; at += 64 * VEC) {
-        read(row, vocab, at + lane * VEC, v);
-        if (look(v, at)) break;
-      }
-    }
-    return found;
-  }
 };
 
-struct SampleLds {
-  uint64_t mass[kSteps];
-  uint32_t count[kSteps];
-  double powers[64];  // 2^(i / 64)
-  uint64_t wave[kSampleWaves];
-  uint64_t before, in;
-  uint32_t step, pick;
-  float most;
-};
+// What a row's draw asks, and how its logits are weighed. `most`: the greatest.
+struct Draw {
+  float temperature, top_p, most, per;
+  uint32_t k;                // 0: all
+  double rate, floor_w;      // floor_w: least weight kept, of 1
+  bool greedy, few, border;  // few: all that is kept goes on the list; border: a step has to be found
 
-// Sum over the block; s.wave has the waves'.
-__device__ inline uint64_t add_block(SampleLds& s, uint64_t v) {
-#pragma unroll
-  for (uint32_t d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-  __syncthreads();
-  if (threadIdx.x % 64 == 0) s.wave[threadIdx.x / 64] = v;
-  __syncthreads();
-  uint64_t sum = 0;
-  for (uint32_t w = 0; w < kSampleWaves; ++w) sum += s.wave[w];
-  return sum;
-}
-
-// The first index at which the running sum of weigh over the row is above
-// `target`, which is below its sum; s.wave has the waves' sums.
-template <class R, class F>
-__device__ inline uint32_t pick_block(SampleLds& s, R& r, uint64_t target, F weigh) {
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  uint64_t before = 0;
-  for (uint32_t w = 0; w < wave; ++w) before += s.wave[w];
-  if (threadIdx.x == 0) s.pick = 0;
-  __syncthreads();
-  if (before <= target && target < before + s.wave[wave]) {
-    const uint32_t i = r.pick(target - before, weigh);
-    if (threadIdx.x % 64 == 0) s.pick = i;
+  __device__ Draw(const SampleArgs& a, uint32_t row, float m, float lowest) {
+    temperature = a.temperatures ? a.temperatures[row] : a.temperature;
+    top_p = a.top_ps ? a.top_ps[row] : a.top_p;
+    const float p = a.min_ps ? a.min_ps[row] : a.min_p;
+    const int32_t asked = a.top_ks ? a.top_ks[row] : a.top_k;
+    k = asked <= 0 || (uint32_t)asked >= a.vocab ? 0 : (uint32_t)asked;
+    greedy = !(temperature > 0.0f) || k == 1;
+    most = m;
+    rate = 1.0 / kLn2 / (double)temperature;
+    floor_w = p > 0.0f ? (double)fminf(p, 1.0f) : 0.0;
+    few = k && k <= kFew;
+    border = k || top_p < 1.0f;
+    const double far = fmin((double)most - (double)lowest, kSpan / rate);
+    per = far > 0.0 ? (float)((double)kSteps / far) : 0.0f;
   }
-  __syncthreads();
-  const uint32_t i = s.pick;
-  __syncthreads();
-  return i;
-}
-
-// The step of a histogram at which its running sum reaches a goal; s.before is the
-// sum before it, s.in what it has.
-template <class H, class Reached>
-__device__ inline uint32_t find_step(SampleLds& s, const H* hist, Reached reached) {
-  const uint32_t at = 2 * threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const uint64_t x = hist[at], y = hist[at + 1], upto = scan_wave(x + y);
-  if (threadIdx.x % 64 == 63) s.wave[wave] = upto;
-  __syncthreads();
-  uint64_t before = upto - x - y;
-  for (uint32_t w = 0; w < wave; ++w) before += s.wave[w];
-  if (!reached(before) && reached(before + x)) s.step = at, s.before = before, s.in = x;
-  if (!reached(before + x) && reached(before + x + y)) s.step = at + 1, s.before = before + x, s.in = y;
-  __syncthreads();
-  return s.step;
-}
-
-template <class T, int NV>
-__global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleArgs a) {
-  __shared__ SampleLds s;
-  const uint32_t row = blockIdx.x, tid = threadIdx.x;
-  RowOf<T, NV> r;
-  r.open(static_cast<const T*>(a.logits) + row * a.stride, a.vocab);
-  if (tid < 64) s.powers[tid] = exp2((double)tid / 64.0);
-  float top = -INFINITY;
-  r.each([&](float l, uint32_t) { top = fmaxf(top, l); });
-#pragma unroll
-  for (uint32_t d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  __shared__ float s_top[kSampleWaves];
-  if (tid % 64 == 0) s_top[tid / 64] = top;
-  __syncthreads();
-  float most = s_top[0];
-  for (uint32_t w = 1; w < kSampleWaves; ++w) most = fmaxf(most, s_top[w]);
-  if (most == -INFINITY) {  // nothing to draw
-    if (tid == 0) a.tokens[row] = -1, a.logprobs[row] = -INFINITY;
-    return;
-  }
-  const float temperature = a.temperatures ? a.temperatures[row] : a.temperature;
-  const int32_t asked = a.top_ks ? a.top_ks[row] : a.top_k;
-  const bool greedy = !(temperature > 0.0f);
-  const uint32_t k = greedy ? 1 : asked <= 0 || (uint32_t)asked >= a.vocab ? 0 : (uint32_t)asked;  // 0: all
-  if (k == 1) {
-    const auto is_top = [&](float l, uint32_t) __attribute__((always_inline)) { return (uint64_t)(l == most); };
-    uint64_t n = 0;
-    r.each([&](float l, uint32_t i) { n += is_top(l, i); });
-    add_block(s, n);
-    const uint32_t i = pick_block(s, r, 0, is_top);
-    if (tid == 0) a.tokens[row] = (int32_t)i, a.logprobs[row] = 0.0f;
-    return;
-  }
-  const float top_p = a.top_ps ? a.top_ps[row] : a.top_p;
-  const float least = a.min_ps ? a.min_ps[row] : a.min_p;
-  const double rate = 1.4426950408889634 / (double)temperature;
-  const double floor_w = least > 0.0f ? (double)fminf(least, 1.0f) : 0.0;
-  const auto power = [&](float l) __attribute__((always_inline)) { return l == most ? 0.0 : ((double)l - (double)most) * rate; };
-  const auto exact = [&](double y) __attribute__((always_inline)) {  // 2^y in units of kOne, y from -kSpan to 0
-    const double z = floor(y * 64.0), x = (y * 64.0 - z) * (0.6931471805599453 / 64.0);
-    const int n = (int)z;
-    const double e = fma(x, fma(x, fma(x, fma(x, 1.0 / 120, 1.0 / 24), 1.0 / 6), 0.5), 1.0) * x;
-    const double p = s.powers[n & 63];
-    return ldexp(fma(p, e, p), n >> 6) * kOne;
-  };
-  const auto whole = [](double w) __attribute__((always_inline)) {  // to the nearest whole number
-    return __builtin_bit_cast(uint64_t, w + 0x1p52) - 0x4330000000000000ull;
-  };
-  const float per = (float)((double)kSteps / kSpan * rate);
-  const auto step_of = [&](float l) __attribute__((always_inline)) {  // the farther from the greatest, the later
+  // log2 of the weight; below -kSpan it is out
+  __device__ double power(float l) const { return l == most ? 0.0 : ((double)l - (double)most) * rate; }
+  __device__ bool weighs(float l) const { return power(l) >= -kSpan; }
+  // the farther from the greatest, the later
+  __device__ uint32_t step(float l) const {
     const float x = (most - l) * per;
     return l == most ? 0u : x < (float)(kSteps - 1) ? (uint32_t)x : kSteps - 1;
-  };
-  // Kept so far: the logits of rank below `last`, and those of it up to index `cut`.
-  uint32_t last = ~0u, cut = ~0u;
-  const auto in = [&](float l, uint32_t i) __attribute__((always_inline)) {
-    const uint32_t x = rank_of(l);
-    return power(l) >= -kSpan && (x < last || (x == last && i <= cut));
-  };
-  const auto zero = [&] {
-    __syncthreads();
-    for (uint32_t i = tid; i < kSteps; i += kSampleThreads) s.mass[i] = 0;
-    for (uint32_t i = tid; i < kSteps; i += kSampleThreads) s.count[i] = 0;
-    __syncthreads();
-  };
-  // Ends the kept ones where the running sum of weigh, in the order of the logits,
-  // reaches a goal. reached(sum); weigh is the same for equal logits.
-  const auto shorten = [&](auto* hist, auto weigh, auto reached) __attribute__((always_inline)) {
-    typedef typename std::remove_reference<decltype(*hist)>::type H;
-    zero();
-    r.each([&](float l, uint32_t i) {
-      if (in(l, i)) atomicAdd(&hist[step_of(l)], (H)weigh(l));
-    });
-    __syncthreads();
-    const uint32_t step = find_step(s, hist, reached);
-    uint64_t before = s.before;
-    uint32_t prefix = 0, shift = 32;
-    for (int pass = 0; pass < 3; ++pass) {
-      const uint32_t width = pass < 2 ? 11 : 10;
-      zero();
-      r.each([&](float l, uint32_t i) {
-        const uint32_t x = rank_of(l);
-        if (in(l, i) && step_of(l) == step && (pass == 0 || x >> shift == prefix))
-          atomicAdd(&hist[x >> (shift - width) & ((1u << width) - 1)], (H)weigh(l));
-      });
-      __syncthreads();
-      const uint32_t digit = find_step(s, hist, [&](uint64_t sum) { return reached(before + sum); });
-      prefix = prefix << width | digit;
-      shift -= width;
-      before += s.before;
+  }
+  // 2^y in whole numbers of 1 / kOne, for y from -kSpan to 0; powers: 2^(i / 64), i = 0 .. 63
+  __device__ static u64 whole(double y, const double* powers) {
+    const double z = y * 64.0, t = z + 0x1.8p52;  // t's last bits are z rounded to a whole number
+    const int n = (int)(uint32_t)__builtin_bit_cast(u64, t);
+    const double x = (z - (t - 0x1.8p52)) * (kLn2 / 64.0);
+    const double e = fma(x, fma(x, fma(x, fma(x, 1.0 / 24, 1.0 / 6), 0.5), 1.0), 1.0);
+    const double w = ldexp(powers[n & 63] * e, (n >> 6) + 43);
+    return __builtin_bit_cast(u64, w + 0x1p52) - 0x4330000000000000ull;
+  }
+  // whether min_p keeps a logit
+  __device__ bool heavy(float l) const { return floor_w == 0.0 || l == most || exp2(power(l)) >= floor_w; }
+};
+
+// The slice's greatest and least logits. Bound by HBM: this is the pass that brings
+// the logits into the caches.
+template <class T>
+__global__ void __launch_bounds__(kThreads) top_kernel(SampleArgs a) {
+  constexpr uint32_t VEC = Logits<T>::VEC, WAVES = kThreads / 64;
+  __shared__ float s_most[WAVES], s_lowest[WAVES];
+  __shared__ uint32_t s_first[WAVES];
+  const uint32_t slice = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
+  RowWork& w = a.of_row(row);
+  if (slice == 0) {
+    for (uint32_t i = tid; i < kSteps; i += kThreads) w.mass[i] = 0, w.count[i] = 0;
+    if (tid < 2) w.arrived[tid] = 0;
+  }
+  const T* logits = static_cast<const T*>(a.logits) + row * a.stride;
+  const uint32_t begin = slice * a.slice, end = min(begin + a.slice, a.vocab);
+  float most = -INFINITY, lowest = INFINITY;
+  uint32_t first = begin;
+  for (uint32_t at = begin + tid * VEC; at < end; at += kThreads * VEC) {
+    float v[VEC];
+    Logits<T>::read(logits, end, at, v);
+#pragma unroll
+    for (uint32_t j = 0; j < VEC; ++j) {
+      if (v[j] > most) most = v[j], first = at + j;
+      lowest = fminf(lowest, v[j] > -INFINITY ? v[j] : INFINITY);
     }
-    // of the equal logits, as few of the lowest indexes as reach it
-    const auto same = [&](float l, uint32_t i) __attribute__((always_inline)) { return (uint64_t)(rank_of(l) == prefix && in(l, i)); };
-    uint64_t n = 0;
-    r.each([&](float l, uint32_t i) { n += same(l, i); });
-    const uint64_t all = add_block(s, n), each = s.in / all;
-    uint64_t low = 1, high = all;
-    while (low < high) {
-      const uint64_t mid = (low + high) / 2;
-      if (reached(before + mid * each)) high = mid;
-      else low = mid + 1;
-    }
-    cut = pick_block(s, r, low - 1, same);
-    last = prefix;
-  };
-  if (k) {
-    uint64_t n = 0;
-    r.each([&](float l, uint32_t i) { n += in(l, i); });
-    if (add_block(s, n) > k)
-      shorten(s.count, [](float) { return 1u; }, [&](uint64_t sum) { return sum >= k; });
   }
-  const auto mass = [&](float l) __attribute__((always_inline)) { return whole(exact(power(l))); };
-  if (top_p < 1.0f) {
-    uint64_t n = 0;
-    r.each([&](float l, uint32_t i) { n += in(l, i) ? mass(l) : 0; });
-    const double goal = fmax((double)top_p * (double)add_block(s, n), 1.0);
-    shorten(reinterpret_cast<unsigned long long*>(s.mass), [&](float l) { return (unsigned long long)mass(l); },
-            [&](uint64_t sum) { return (double)sum >= goal; });
+#pragma unroll
+  for (uint32_t d = 32; d; d >>= 1) {
+    const float m = __shfl_xor(most, d);
+    const uint32_t f = __shfl_xor(first, d);
+    if (m > most || (m == most && f < first)) most = m, first = f;
+    lowest = fminf(lowest, __shfl_xor(lowest, d));
   }
-  const auto weigh = [&](float l, uint32_t i) __attribute__((always_inline)) -> uint64_t {
-    if (!in(l, i)) return 0;
-    const double w = exact(power(l));
-    return w >= floor_w * kOne || l == most ? whole(w) : 0;
-  };
-  uint64_t n = 0;
-  r.each([&](float l, uint32_t i) { n += weigh(l, i); });
-  const uint64_t total = add_block(s, n);
-  const float u = a.uniforms[row];
-  const double at = u > 0.0f ? floor((double)fminf(u, 1.0f) * (double)total) : 0.0;
-  const uint64_t target = at < (double)(total - 1) ? (uint64_t)at : total - 1;
-  const uint32_t token = pick_block(s, r, target, weigh);
-  if (tid == 0) {
-    const float l = (float)r.row[token];
-    a.tokens[row] = (int32_t)token;
-    a.logprobs[row] = (float)(power(l) * 0.6931471805599453 - log((double)total / kOne));
+  if (tid % 64 == 0) s_most[tid / 64] = most, s_lowest[tid / 64] = lowest, s_first[tid / 64] = first;
+  __syncthreads();
+  if (tid != 0) return;
+  for (uint32_t i = 1; i < WAVES; ++i) {
+    if (s_most[i] > most || (s_most[i] == most && s_first[i] < first)) most = s_most[i], first = s_first[i];
+    lowest = fminf(lowest, s_lowest[i]);
   }
+  w.most[slice] = most, w.lowest[slice] = lowest, w.first[slice] = first;
 }
 
-template <class T, int NV>
-static hl_status run_sample(const SampleArgs& a, uint32_t rows, hipStream_t s) {
-  return enqueue(sample_kernel<T, NV>, dim3(rows), dim3(kSampleThreads), s, a);
+// The row's greatest and least logits. Whole wave.
+__device__ inline void ends_of(const SampleArgs& a, const RowWork& w, float& most, float& lowest) {
+  const uint32_t lane = threadIdx.x % 64;
+  most = most_wave(lane < a.slices ? w.most[lane] : -INFINITY);
+  lowest = -most_wave(lane < a.slices ? -w.lowest[lane] : -INFINITY);
+}
+
+// Whether this is the last of a row's blocks to come here, which sees what the others
+// gave before they came.
+__device__ inline bool last_of_row(const SampleArgs& a, uint32_t& arrived) {
+  __shared__ uint32_t s_arrived;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) s_arrived = __hip_atomic_fetch_add(&arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  asm volatile("" ::: "memory");
+  return s_arrived == a.slices - 1;
+}
+
+// The sum of v over the block's threads before this one; `all`: over all of them.
+__device__ inline u64 scan_block(u64 v, u64& all) {
+  __shared__ u64 s_wave[kWaves];
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const u64 upto = scan_wave(v);
+  if (threadIdx.x % 64 == 63) s_wave[wave] = upto;
+  __syncthreads();
+  u64 before = upto - v;
+  all = 0;
+#pragma unroll
+  for (uint32_t i = 0; i < kWaves; ++i) {
+    if (i < wave) before += s_wave[i];
+    all += s_wave[i];
+  }
+  __syncthreads();
+  return before;
+}
+
+__device__ inline u64 add_block(u64 v) {
+  u64 all;
+  scan_block(v, all);
+  return all;
+}
+
+// The first of N numbers a thread, one thread's after the other's, at which the
+// running sum reaches a goal that the sum of all reaches; `before`: the sum before it.
+template <uint32_t N, class Reached>
+__device__ inline uint32_t find_first(const u64 (&v)[N], Reached reached, u64& before) {
+  __shared__ u64 s_before;
+  __shared__ uint32_t s_at;
+  u64 sum = 0, all;
+#pragma unroll
+  for (uint32_t i = 0; i < N; ++i) sum += v[i];
+  u64 run = scan_block(sum, all);
+#pragma unroll
+  for (uint32_t i = 0; i < N; ++i) {
+    if (!reached(run) && reached(run + v[i])) s_at = N * threadIdx.x + i, s_before = run;
+    run += v[i];
+  }
+  __syncthreads();
+  before = s_before;
+  const uint32_t at = s_at;
+  __syncthreads();
+  return at;
+}
+
+// The steps between which a row's border is, from its histogram.
+__device__ inline void place_border(const Draw& d, RowWork& w) {
+  constexpr uint32_t N = kSteps / kThreads;
+  const uint32_t tid = threadIdx.x;
+  u64 mass[N], count[N], c = 0, m = 0;
+#pragma unroll
+  for (uint32_t i = 0; i < N; ++i) {
+    mass[i] = d.few ? 0 : take(&w.mass[N * tid + i]), count[i] = d.k ? take(&w.count[N * tid + i]) : 0;
+    c += count[i], m += mass[i];
+  }
+  const auto below = [&](const u64 (&v)[N], uint32_t step) {
+    u64 sum = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i) sum += N * tid + i < step ? v[i] : 0;
+    return add_block(sum);
+  };
+  c = add_block(c), m = add_block(m);
+  uint32_t lo = kSteps, hi = kSteps, at_k = kSteps;
+  bool by_count = d.k && c > d.k, by_mass = d.top_p < 1.0f;
+  u64 least = m, most = m, before;  // that what top_k keeps weighs
+  if (by_count) {
+    lo = hi = at_k = find_first(count, [&](u64 sum) { return sum >= d.k; }, before);
+    least = below(mass, at_k), most = below(mass, at_k + 1);
+  }
+  if (d.few) {
+    lo = 0;
+    if (!by_count) hi = kSteps - 1;
+  } else {
+    if (by_mass) {
+      const double first = fmax((double)d.top_p * (double)least, 1.0), second = fmax((double)d.top_p * (double)most, 1.0);
+      lo = find_first(mass, [&](u64 sum) { return (double)sum >= first; }, before);
+      hi = find_first(mass, [&](u64 sum) { return (double)sum >= second; }, before);
+    }
+    if (d.floor_w > 0.0) {
+      // the step of the least weight that min_p keeps, or either of two
+      const double x = -log2(d.floor_w) / d.rate * (double)d.per;
+      const uint32_t near = (uint32_t)fmin(fmax(x - 0.01, 0.0), kSteps - 1.0);
+      const uint32_t far = (uint32_t)fmin(x + 0.01, kSteps - 1.0);
+      if (far < lo) lo = near, hi = far, by_count = by_mass = false;
+      else lo = min(lo, near);
+    }
+  }
+  const bool apart = by_count && at_k > hi;  // top_k's step is not between lo and hi
+  // (without a border of top_k's, all steps weigh what top_p goes by)
+  const uint32_t from = apart ? at_k : by_count || d.few ? lo : kSteps;
+  const u64 count_from = by_count ? below(count, from) : 0, mass_from = below(mass, from), mass_lo = below(mass, lo);
+  if (tid != 0) return;
+  w.lo = lo, w.hi = hi, w.other = apart ? at_k : lo, w.from = from, w.by_count = by_count, w.by_mass = by_mass;
+  w.count_from = count_from, w.mass_from = mass_from, w.mass_lo = mass_lo;
+}
+
+// The slice's histogram, added to the row's. Bound by the weights' arithmetic, some
+// twenty instructions in float64 each, and by LDS atomics.
+template <class T>
+__global__ void __launch_bounds__(kThreads) step_kernel(SampleArgs a) {
+  constexpr uint32_t VEC = Logits<T>::VEC;
+  __shared__ u64 s_mass[kSteps];
+  __shared__ uint32_t s_count[kSteps];
+  __shared__ double s_powers[64];
+  const uint32_t slice = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
+  RowWork& w = a.of_row(row);
+  float most, lowest;
+  ends_of(a, w, most, lowest);
+  if (most == -INFINITY) return;
+  const Draw d(a, row, most, lowest);
+  if (d.greedy) return;
+  if (tid < 64) s_powers[tid] = exp2((double)tid / 64.0);
+  for (uint32_t i = tid; i < kSteps; i += kThreads) s_mass[i] = 0, s_count[i] = 0;
+  __syncthreads();
+  const T* logits = static_cast<const T*>(a.logits) + row * a.stride;
+  const uint32_t begin = slice * a.slice, end = min(begin + a.slice, a.vocab);
+  const auto each = [&](auto f) __attribute__((always_inline)) {
+    for (uint32_t at = begin + tid * VEC; at < end; at += kThreads * VEC) {
+      float v[VEC];
+      Logits<T>::read(logits, end, at, v);
+#pragma unroll
+      for (uint32_t j = 0; j < VEC; ++j) {
+        const double y = d.power(v[j]);
+        if (y >= -kSpan) f(v[j], y);
+      }
+    }
+  };
+  if (d.few) {
+    each([&](float l, double) { atomicAdd(&s_count[d.step(l)], 1u); });
+  } else if (d.border) {
+    each([&](float l, double y) {
+      const uint32_t i = d.step(l);
+      atomicAdd(&s_mass[i], Draw::whole(y, s_powers));
+      if (d.k) atomicAdd(&s_count[i], 1u);
+    });
+  } else {
+    u64 sum = 0;
+    each([&](float l, double y) { sum += d.heavy(l) ? Draw::whole(y, s_powers) : 0; });
+    sum = add_wave(sum);
+    if (tid % 64 == 0) atomicAdd(&s_mass[0], sum);
+    __syncthreads();
+    if (tid == 0) w.sum[slice] = s_mass[0];
+    return;
+  }
+  __syncthreads();
+  for (uint32_t i = tid; i < kSteps; i += kThreads) {
+    if (!d.few) {
+      a.of_slice(row, slice).mass[i] = s_mass[i];
+      if (s_mass[i]) atomicAdd(&w.mass[i], s_mass[i]);
+    }
+    if (s_count[i]) atomicAdd(&w.count[i], s_count[i]);
+  }
+  if (last_of_row(a, w.arrived[0])) place_border(d, w);
+}
+
+struct EndLds {
+  u64 bin[kThreads], weight[kList];
+  float logit[kList];
+  uint32_t index[kList];
+  double powers[64];
+  u64 wave[kWaves], total[kSlices], limit;
+  uint32_t start[kSlices + 1], pick;
+};
+
+// Where the running sum of weigh(logit), in the order of the logits, reaches a goal:
+// the rank of the last logit kept and how many of that rank are. `each` goes through
+// logits whose ranks have all bits from `top` on equal; `before` is the sum of those
+// ahead of them.
+struct Border {
+  uint32_t rank;
+  u64 need;
+};
+template <class Each, class Weigh, class Reached>
+__device__ inline Border find_border(EndLds& s, Each each, uint32_t top, uint32_t prefix, u64 before, Weigh weigh,
+                                     Reached reached) {
+  for (uint32_t shift = top; shift;) {
+    const uint32_t width = min(shift, 8u);
+    s.bin[threadIdx.x] = 0;
+    __syncthreads();
+    each([&](float l, auto i) __attribute__((always_inline)) {
+      const uint32_t x = rank_of(l);
+      if (shift == 32 || x >> shift == prefix) atomicAdd(&s.bin[x >> (shift - width) & ((1u << width) - 1)], weigh(l, i));
+    });
+    __syncthreads();
+    const u64 bin[1] = {s.bin[threadIdx.x]};
+    u64 ahead;
+    const uint32_t digit = find_first(bin, [&](u64 sum) { return reached(before + sum); }, ahead);
+    before += ahead, shift -= width;
+    prefix = prefix << width | digit;
+  }
+  u64 same = 0, sum = 0;
+  each([&](float l, auto i) __attribute__((always_inline)) {
+    if (rank_of(l) == prefix) ++same, sum += weigh(l, i);
+  });
+  same = add_block(same), sum = add_block(sum);
+  u64 low = 1, high = same;  // of equal ones, which weigh the same, as few as reach it
+  while (low < high) {
+    const u64 mid = (low + high) / 2;
+    if (reached(before + mid * (sum / same))) high = mid;
+    else low = mid + 1;
+  }
+  return {prefix, low};
+}
+
+// A stretch of a row by the whole block; each wave has a part of neighbours.
+template <class T>
+struct Stretch {
+  static constexpr uint32_t VEC = Logits<T>::VEC;
+  const T* row;
+  uint32_t begin, end;  // this wave's
+
+  __device__ Stretch(const T* r, uint32_t from, uint32_t to) : row(r) {
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t part = (to - from + kThreads * VEC - 1) / (kThreads * VEC) * (64 * VEC);
+    begin = min(from + wave * part, to), end = min(begin + part, to);
+  }
+  // f(logit, index) for this lane's logits
+  template <class F>
+  __device__ __attribute__((always_inline)) void each(F f) const {
+    for (uint32_t at = begin + threadIdx.x % 64 * VEC; at < end; at += 64 * VEC) {
+      float v[VEC];
+      Logits<T>::read(row, end, at, v);
+#pragma unroll
+      for (uint32_t j = 0; j < VEC; ++j) f(v[j], at + j);
+    }
+  }
+  // The first index at which the running sum of weigh(logit, index) over the stretch
+  // is above `target`, which is below its sum.
+  template <class F>
+  __device__ __attribute__((always_inline)) uint32_t pick(EndLds& s, u64 target, F weigh) const {
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+    u64 sum = 0;
+    each([&](float l, uint32_t i) __attribute__((always_inline)) { sum += weigh(l, i); });
+    sum = add_wave(sum);
+    if (lane == 0) s.wave[wave] = sum;
+    if (threadIdx.x == 0) s.pick = 0;
+    __syncthreads();
+    u64 before = 0;
+    for (uint32_t i = 0; i < wave; ++i) before += s.wave[i];
+    if (before <= target && target < before + sum) {
+      for (uint32_t at0 = begin; at0 < end; at0 += 64 * VEC) {
+        const uint32_t at = at0 + lane * VEC;
+        float v[VEC];
+        u64 w[VEC], mine = 0;
+        Logits<T>::read(row, end, at, v);
+#pragma unroll
+        for (uint32_t j = 0; j < VEC; ++j) w[j] = weigh(v[j], at + j), mine += w[j];
+        const u64 upto = before + scan_wave(mine), past = __ballot(upto > target);
+        if (past) {
+          u64 run = upto - mine;
+          uint32_t found = 0;
+          bool there = false;
+#pragma unroll
+          for (uint32_t j = 0; j < VEC; ++j) {
+            run += w[j];
+            if (!there && run > target) found = at + j, there = true;
+          }
+          if (lane == (uint32_t)__builtin_ctzll(past)) s.pick = found;
+          break;
+        }
+        before = __shfl(upto, 63);
+      }
+    }
+    __syncthreads();
+    const uint32_t i = s.pick;
+    __syncthreads();
+    return i;
+  }
+};
+
+// The whole number that a running sum must pass for the token of u.
+__device__ inline u64 target_of(float u, u64 total) {
+  const double at = u > 0.0f ? floor((double)fminf(u, 1.0f) * (double)total) : 0.0;
+  return at < (double)(total - 1) ? (u64)at : total - 1;
 }
 
 template <class T>
-static hl_status run_logits(const SampleArgs& a, uint32_t rows, hipStream_t s) {
-  if (a.vocab <= 8 * kSampleThreads) return run_sample<T, 8>(a, rows, s);
-  return run_sample<T, 0>(a, rows, s);
+__device__ inline void end_row(const SampleArgs& a, const Draw& d, uint32_t row, const T* logits, uint32_t token,
+                               u64 total) {
+  if (threadIdx.x != 0) return;
+  const float l = (float)logits[token];
+  a.tokens[row] = (int32_t)token;
+  a.logprobs[row] = (float)(d.power(l) * kLn2 - log((double)total / kOne));
+}
+
+// A logit's place in the order: falling logits, of equal ones the lowest index first.
+__device__ inline u64 place_of(float l, uint32_t i) { return (u64)rank_of(l) << 32 | i; }
+
+// A row by one block, from its logits alone.
+template <class T>
+__device__ inline void slow_row(const SampleArgs& a, const Draw& d, uint32_t row, const T* logits, EndLds& s) {
+  const Stretch<T> all(logits, 0, a.vocab);
+  u64 limit = ~0ull;  // the last place kept
+  const auto in = [&](float l, uint32_t i) __attribute__((always_inline)) { return d.weighs(l) && place_of(l, i) <= limit; };
+  const auto mass = [&](float l) __attribute__((always_inline)) { return Draw::whole(d.power(l), s.powers); };
+  for (int stage = 0; stage < 2; ++stage) {  // top_k, top_p
+    if (stage == 0 ? d.k == 0 : !(d.top_p < 1.0f)) continue;
+    const auto weigh = [&](float l, uint32_t) __attribute__((always_inline)) { return stage == 0 ? 1ull : mass(l); };
+    u64 n = 0;
+    all.each([&](float l, uint32_t i) __attribute__((always_inline)) { n += in(l, i) ? weigh(l, i) : 0; });
+    n = add_block(n);
+    if (stage == 0 && n <= d.k) continue;
+    const double goal = stage == 0 ? (double)d.k : fmax((double)d.top_p * (double)n, 1.0);
+    const auto each = [&](auto f) __attribute__((always_inline)) {
+      all.each([&](float l, uint32_t i) __attribute__((always_inline)) {
+        if (in(l, i)) f(l, i);
+      });
+    };
+    const Border b = find_border(s, each, 32, 0, 0, weigh, [&](u64 sum) { return (double)sum >= goal; });
+    const uint32_t i = all.pick(s, b.need - 1, [&](float l, uint32_t j) __attribute__((always_inline)) {
+      return (u64)(rank_of(l) == b.rank && in(l, j));
+    });
+    limit = (u64)b.rank << 32 | i;
+  }
+  const auto weigh = [&](float l, uint32_t i) __attribute__((always_inline)) -> u64 {
+    return in(l, i) && d.heavy(l) ? mass(l) : 0;
+  };
+  u64 n = 0;
+  all.each([&](float l, uint32_t i) __attribute__((always_inline)) { n += weigh(l, i); });
+  const u64 total = add_block(n);
+  end_row(a, d, row, logits, all.pick(s, target_of(a.uniforms[row], total), weigh), total);
+}
+
+// Lists the logits of the border's step, and ends the row in its last block. Bound by
+// launch and waits for rows of a few slices, else by reading the logits again for the
+// list.
+template <class T>
+__global__ void __launch_bounds__(kThreads) finish_kernel(SampleArgs a) {
+  constexpr uint32_t VEC = Logits<T>::VEC, EACH = kList / kThreads;
+  __shared__ EndLds s;
+  const uint32_t slice = blockIdx.x, row = blockIdx.y, tid = threadIdx.x, lane = tid % 64;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  RowWork& w = a.of_row(row);
+  const T* logits = static_cast<const T*>(a.logits) + row * a.stride;
+  float most, lowest;
+  ends_of(a, w, most, lowest);
+  if (most == -INFINITY) {  // nothing to draw
+    if (slice == 0 && tid == 0) a.tokens[row] = -1, a.logprobs[row] = -INFINITY;
+    return;
+  }
+  const Draw d(a, row, most, lowest);
+  if (d.greedy) {
+    const uint64_t at = __ballot(lane < a.slices && w.most[lane < a.slices ? lane : 0] == most);
+    if (slice == 0 && tid == 0) a.tokens[row] = (int32_t)w.first[__builtin_ctzll(at)], a.logprobs[row] = 0.0f;
+    return;
+  }
+  if (!d.border && slice != 0) return;  // nothing is listed
+  const uint32_t lo = d.border ? w.lo : kSteps, hi = d.border ? w.hi : kSteps, other = d.border ? w.other : kSteps;
+  SliceWork& own = a.of_slice(row, slice);
+  if (d.border && !d.few) {
+    u64 base = 0;
+    for (uint32_t i = tid; i < lo; i += kThreads) base += own.mass[i];
+    base = add_block(base);
+    if (tid == 0) give(&w.sum[slice], base);
+  }
+  if (lo < kSteps) {
+    const uint32_t begin = slice * a.slice, end = min(begin + a.slice, a.vocab);
+    u64 listed = 0;
+    for (uint32_t at0 = begin; at0 < end; at0 += kThreads * VEC) {
+      const uint32_t at = at0 + tid * VEC;
+      float v[VEC];
+      if (at < end) Logits<T>::read(logits, end, at, v);
+      uint32_t mine = 0;
+#pragma unroll
+      for (uint32_t j = 0; j < VEC; ++j) {
+        const uint32_t x = at < end && d.weighs(v[j]) ? d.step(v[j]) : kSteps;
+        mine |= (uint32_t)((x >= lo && x <= hi) || x == other) << j;
+      }
+      u64 all;
+      u64 to = listed + scan_block(__popc(mine), all);
+#pragma unroll
+      for (uint32_t j = 0; j < VEC; ++j)
+        if (mine >> j & 1) {
+          if (to < kList) give(&own.list[to], (u64)(at + j) << 32 | __builtin_bit_cast(uint32_t, v[j]));
+          ++to;
+        }
+      listed += all;
+    }
+    if (tid == 0) give(&w.listed[slice], (uint32_t)listed);
+  }
+  if (d.border && !last_of_row(a, w.arrived[1])) return;
+  if (tid < 64) s.powers[tid] = exp2((double)tid / 64.0);
+  uint32_t n = 0;
+  if (lo < kSteps) {
+    const uint32_t mine = lane < a.slices ? take(&w.listed[lane]) : 0, upto = scan_wave(mine);
+    if (wave == 0) s.start[lane + 1] = upto;
+    if (tid == 0) s.start[0] = 0;
+  }
+  __syncthreads();
+  if (lo < kSteps) {
+    n = s.start[kSlices];
+    if (n > kList) {
+      slow_row<T>(a, d, row, logits, s);
+      return;
+    }
+  }
+  // Logits each*tid .. of the list are this thread's: as few as take the whole list,
+  // so that a short one is one logit a thread. `kept` has a bit for each.
+  const uint32_t most_each = n <= kThreads ? 1 : EACH, first = most_each * tid;
+  uint32_t kept = 0;
+  for (uint32_t j = 0; j < most_each; ++j) {
+    const uint32_t i = first + j;
+    if (i >= n) break;
+    uint32_t from = 0;  // the slice that it is in
+#pragma unroll
+    for (uint32_t h = kSlices / 2; h; h >>= 1)
+      if (s.start[from + h] <= i) from += h;
+    const u64 x = take(&a.of_slice(row, from).list[i - s.start[from]]);
+    const float l = __builtin_bit_cast(float, (uint32_t)x);
+    s.logit[i] = l, s.index[i] = (uint32_t)(x >> 32);
+    s.weight[i] = Draw::whole(d.power(l), s.powers);
+    kept |= 1u << j;
+  }
+  if (tid == 0) s.limit = 0;
+  __syncthreads();
+  // f(place on the list) for this thread's that are kept still; those of which f is
+  // false no longer are
+  const auto each = [&](auto f) __attribute__((always_inline)) {
+    for (uint32_t j = 0; j < most_each; ++j)
+      if (kept >> j & 1) f(first + j);
+  };
+  const auto narrow = [&](auto f) __attribute__((always_inline)) {
+    uint32_t still = 0;
+    each([&](uint32_t i) {
+      if (f(i)) still |= 1u << (i - first);
+    });
+    kept = still;
+  };
+  const auto weight_kept = [&] {
+    u64 sum = 0;
+    each([&](uint32_t i) { sum += s.weight[i]; });
+    return sum;
+  };
+  const bool by_count = d.border && w.by_count, by_mass = d.border && w.by_mass;
+  const uint32_t from = d.border ? w.from : kSteps;
+  u64 limit = ~0ull;  // the last place kept, for the logits of listed steps
+  if (n && n <= kPairs) {
+    // each logit's predecessors, among those that its sum is over
+    u64 count = by_count ? w.count_from : 0, mass = d.border ? w.mass_lo : 0;
+    const u64 mine = tid < n ? place_of(s.logit[tid], s.index[tid]) : 0;
+    const uint32_t step = tid < n ? d.step(s.logit[tid]) : 0;
+    for (uint32_t i = 0; i < n; ++i) {
+      const float l = s.logit[i];
+      const uint32_t x = d.step(l);
+      const bool ahead = place_of(l, s.index[i]) < mine;
+      count += ahead && x >= from, mass += ahead && x <= hi ? s.weight[i] : 0;
+    }
+    if (by_count) narrow([&](uint32_t) { return step < from || count < d.k; });
+    if (by_mass) {
+      u64 sum = 0;
+      each([&](uint32_t i) { sum += step >= from ? s.weight[i] : 0; });
+      const double goal = fmax((double)d.top_p * (double)(w.mass_from + add_block(sum)), 1.0);
+      narrow([&](uint32_t) { return step <= hi && (double)mass < goal; });
+    }
+    each([&](uint32_t) { atomicMax(&s.limit, mine); });
+    __syncthreads();
+    limit = s.limit;
+  } else if (n) {
+    // bits in which the list's ranks differ
+    uint32_t low = ~0u, high = 0;
+    each([&](uint32_t i) { low = min(low, rank_of(s.logit[i])), high = max(high, rank_of(s.logit[i])); });
+#pragma unroll
+    for (uint32_t x = 32; x; x >>= 1) low = min(low, __shfl_xor(low, x)), high = max(high, __shfl_xor(high, x));
+    if (lane == 0) s.wave[wave] = (u64)high << 32 | low;
+    __syncthreads();
+#pragma unroll
+    for (uint32_t i = 0; i < kWaves; ++i)
+      low = min(low, (uint32_t)s.wave[i]), high = max(high, (uint32_t)(s.wave[i] >> 32));
+    const uint32_t top = low == high ? 0 : 32 - __builtin_clz(low ^ high);
+    // Ends the listed logits of which `of` is true where the sum of `weigh` reaches `to`.
+    const auto shorten = [&](auto of, auto weigh, u64 before, double to) __attribute__((always_inline)) {
+      const auto some = [&](auto f) __attribute__((always_inline)) {
+        each([&](uint32_t i) {
+          if (of(i)) f(s.logit[i], i);
+        });
+      };
+      const Border b = find_border(s, some, top, top == 32 ? 0 : low >> top, before, weigh,
+                                   [&](u64 sum) { return (double)sum >= to; });
+      u64 same = 0, all;
+      some([&](float l, uint32_t) { same += rank_of(l) == b.rank; });
+      u64 nth = scan_block(same, all);
+      some([&](float l, uint32_t i) {
+        if (rank_of(l) == b.rank && ++nth == b.need) s.limit = place_of(l, s.index[i]);
+      });
+      __syncthreads();
+      limit = s.limit;
+      narrow([&](uint32_t i) { return place_of(s.logit[i], s.index[i]) <= limit; });
+    };
+    if (by_count)
+      shorten([&](uint32_t i) { return d.step(s.logit[i]) >= from; }, [](float, uint32_t) { return 1ull; }, w.count_from,
+              (double)d.k);
+    if (by_mass) {
+      u64 sum = 0;
+      each([&](uint32_t i) { sum += d.step(s.logit[i]) >= from ? s.weight[i] : 0; });
+      const double goal = fmax((double)d.top_p * (double)(w.mass_from + add_block(sum)), 1.0);
+      shorten([&](uint32_t i) { return d.step(s.logit[i]) <= hi; }, [&](float, uint32_t i) { return s.weight[i]; }, w.mass_lo,
+              goal);
+    }
+  }
+  if (d.floor_w > 0.0) narrow([&](uint32_t i) { return d.heavy(s.logit[i]); });
+  const float u = a.uniforms[row];
+  if (d.few) {  // the list is in the order of the indexes, and has all
+    u64 total;
+    u64 run = scan_block(weight_kept(), total);
+    const u64 target = target_of(u, total);
+    each([&](uint32_t i) {
+      if (run <= target && run + s.weight[i] > target) s.pick = s.index[i];
+      run += s.weight[i];
+    });
+    __syncthreads();
+    end_row(a, d, row, logits, s.pick, total);
+    return;
+  }
+  if (tid < kSlices) s.total[tid] = tid < a.slices ? (d.border ? take(&w.sum[tid]) : w.sum[tid]) : 0;
+  __syncthreads();
+  each([&](uint32_t i) { atomicAdd(&s.total[s.index[i] / a.slice], s.weight[i]); });
+  __syncthreads();
+  const u64 mine = s.total[lane], upto = scan_wave(mine), total = __shfl(upto, 63), target = target_of(u, total);
+  const uint32_t in = (uint32_t)__builtin_ctzll(__ballot(upto > target));
+  const u64 before = __shfl(upto - mine, in);
+  const Stretch<T> there(logits, in * a.slice, min((in + 1) * a.slice, a.vocab));
+  const uint32_t token = there.pick(s, target - before, [&](float l, uint32_t i) __attribute__((always_inline)) -> u64 {
+    if (!d.weighs(l)) return 0;
+    const uint32_t step = d.step(l);
+    const bool is = step < lo || (step <= hi && place_of(l, i) <= limit);
+    return is && d.heavy(l) ? Draw::whole(d.power(l), s.powers) : 0;
+  });
+  end_row(a, d, row, logits, token, total);
+}
+
+// Logits of a slice: as few as give every compute unit blocks, at least 2048, and
+// no more slices than kSlices.
+static uint32_t slice_of(uint64_t rows, uint64_t vocab) {
+  const uint64_t blocks = 4 * (uint64_t)device_cus(), most = std::max<uint64_t>(1, blocks / rows);
+  const uint64_t each = (vocab + most - 1) / most, least = std::max<uint64_t>(2048, (vocab + kSlices - 1) / kSlices);
+  return (uint32_t)((std::min<uint64_t>(std::max(each, least), std::max<uint64_t>(least, 16384)) + 2047) / 2048 * 2048);
+}
+
+template <class T>
+static hl_status run_sample(const SampleArgs& a, uint32_t rows, hipStream_t s) {
+  const dim3 grid(a.slices, rows);
+  hl_status st = enqueue(top_kernel<T>, grid, dim3(kThreads), s, a);
+  if (st == HL_OK) st = enqueue(step_kernel<T>, grid, dim3(kThreads), s, a);
+  return st == HL_OK ? enqueue(finish_kernel<T>, grid, dim3(kThreads), s, a) : st;
 }
 
 }  // namespace hl
 
 using namespace hl;
 
+extern "C" size_t hl_sample_workspace_bytes(uint32_t rows, uint64_t vocab) {
+  if (rows == 0 || rows > 65535 || vocab == 0 || vocab >= (1u << 20)) return 0;
+  const uint64_t slice = slice_of(rows, vocab);
+  return rows * (sizeof(RowWork) + (vocab + slice - 1) / slice * sizeof(SliceWork));
+}
+
 extern "C" hl_status hl_sample(const hl_sampling* sampling, const void* logits_dev, hl_dtype dtype, uint64_t row_stride,
                                uint32_t rows, uint64_t vocab, const float* uniforms_dev, int32_t* tokens_dev,
-                               float* logprobs_dev, void* stream) {
-  if (!sampling || !logits_dev || !uniforms_dev || !tokens_dev || !logprobs_dev || rows == 0 || vocab == 0 ||
-      (rows > 1 && row_stride < vocab))
+                               float* logprobs_dev, void* workspace_dev, size_t workspace_bytes, void* stream) {
+  if (!sampling || !logits_dev || !uniforms_dev || !tokens_dev || !logprobs_dev || !workspace_dev || rows == 0 ||
+      vocab == 0 || (rows > 1 && row_stride < vocab))
     return HL_EINVAL;
   const uintptr_t size = dtype == HL_F32 ? 4 : 2;
-  if ((dtype != HL_F32 && dtype != HL_BF16 && dtype != HL_F16) || !aligned(logits_dev, size)) return HL_EINVAL;
+  if ((dtype != HL_F32 && dtype != HL_BF16 && dtype != HL_F16) || !aligned(logits_dev, size) || !aligned(workspace_dev, 16))
+    return HL_EINVAL;
   for (const void* p : {(const void*)uniforms_dev, (const void*)tokens_dev, (const void*)logprobs_dev,
                         (const void*)sampling->temperature_dev, (const void*)sampling->top_k_dev,
                         (const void*)sampling->top_p_dev, (const void*)sampling->min_p_dev})
     if (!aligned(p, 4)) return HL_EINVAL;
-  if (vocab >= (1u << 20) || row_stride >= (1ull << 40) || !grid_fits(rows, kSampleThreads)) return HL_EUNSUPPORTED;
+  if (vocab >= (1u << 20) || row_stride >= (1ull << 40) || rows > 65535) return HL_EUNSUPPORTED;
+  if (workspace_bytes < hl_sample_workspace_bytes(rows, vocab)) return HL_EINVAL;
   SampleArgs a = {};
   a.logits = logits_dev, a.stride = row_stride, a.vocab = (uint32_t)vocab, a.uniforms = uniforms_dev;
+  a.slice = slice_of(rows, vocab), a.slices = (uint32_t)((vocab + a.slice - 1) / a.slice);
   a.temperatures = sampling->temperature_dev, a.top_ks = sampling->top_k_dev;
   a.top_ps = sampling->top_p_dev, a.min_ps = sampling->min_p_dev;
   a.temperature = sampling->temperature, a.top_k = sampling->top_k, a.top_p = sampling->top_p, a.min_p = sampling->min_p;
-  a.tokens = tokens_dev, a.logprobs = logprobs_dev;
+  a.tokens = tokens_dev, a.logprobs = logprobs_dev, a.work = static_cast<uint8_t*>(workspace_dev);
   const hipStream_t s = (hipStream_t)stream;
-  return dtype == HL_F32    ? run_logits<float>(a, rows, s)
-         : dtype == HL_BF16 ? run_logits<__bf16>(a, rows, s)
-                            : run_logits<_Float16>(a, rows, s);
+  return dtype == HL_F32    ? run_sample<float>(a, rows, s)
+         : dtype == HL_BF16 ? run_sample<__bf16>(a, rows, s)
+                            : run_sample<_Float16>(a, rows, s);
 }

@@ -108,7 +108,7 @@ EXPORTS = ["hl_status_str", "hl_default_seg_len", "hl_default_grp_rows", "hl_bui
            "hl_decode_gemm",
            "hl_gemv_bf16", "hl_rms_norm", "hl_attention_workspace_bytes", "hl_prefix_attention", "hl_cache_evict",
            "hl_cache4_row_bytes", "hl_cache_write4", "hl_cache_read4", "hl_attention4_workspace_bytes",
-           "hl_prefix_attention4", "hl_gemv4", "hl_sample"]
+           "hl_prefix_attention4", "hl_gemv4", "hl_sample_workspace_bytes", "hl_sample"]
 
 
 def lib() -> ctypes.CDLL:
@@ -198,7 +198,9 @@ def lib() -> ctypes.CDLL:
                            c.c_void_p, c.c_int, c.c_uint32, c.c_void_p, c.c_void_p]
     L.hl_sample.restype = c.c_int
     L.hl_sample.argtypes = [c.c_void_p, c.c_void_p, c.c_int, c.c_uint64, c.c_uint32, c.c_uint64, c.c_void_p,
-                            c.c_void_p, c.c_void_p, c.c_void_p]
+                            c.c_void_p, c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p]
+    L.hl_sample_workspace_bytes.restype = c.c_size_t
+    L.hl_sample_workspace_bytes.argtypes = [c.c_uint32, c.c_uint64]
     _lib = L
     return L
 
@@ -996,8 +998,8 @@ def gemv4(codes, scales, x, bases=None, y=None, stream=None):
     return y
 
 
-def sample(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tokens=None, logprobs=None,
-           stream=None) -> SampleResult:
+def sample(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tokens=None, logprobs=None, stream=None,
+           workspace=None) -> SampleResult:
     """A token of each row of logits [rows, vocab] (or [vocab]; float32, bfloat16 or float16, rows at any distance).
 
     The settings are numbers, or tensors [rows] on the GPU (float32; top_k int32). With w = exp((logit - max) /
@@ -1007,14 +1009,15 @@ def sample(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tok
     [0, 1)) times their total. temperature 0: the greatest logit's token. Tokens of w below 2^-40 are never drawn.
 
     Gives the tokens (int32 [rows]; -1 where no logit is above minus infinity) and the logarithms of their shares of the
-    kept tokens' total (float32 [rows]), allocated where they are not given (on ``stream``, where one is given)."""
+    kept tokens' total (float32 [rows]). ``workspace``: a device buffer of hl_sample_workspace_bytes. Buffers that are not
+    given are allocated (on ``stream``, where one is given)."""
     if stream is not None:
         return _on_stream(stream, logits.get_device(), sample, logits, uniforms, temperature, top_k, top_p, min_p, tokens,
-                          logprobs)
+                          logprobs, None, workspace)
     T = _torch or _lookups()
     dev = logits.get_device()
     if dev >= 0 and dev != T.current_device():
-        return _on_gpu(dev, sample, logits, uniforms, temperature, top_k, top_p, min_p, tokens, logprobs)
+        return _on_gpu(dev, sample, logits, uniforms, temperature, top_k, top_p, min_p, tokens, logprobs, None, workspace)
     if logits.dim() == 1:
         logits = logits.unsqueeze(0)
     code = T.codes.get(logits.dtype)
@@ -1048,8 +1051,13 @@ def sample(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tok
     else:
         _small(logprobs, "logprobs", T.float32, need, dev)
     settings = _SAMPLING.pack(*pointers, numbers[0], min(int(numbers[1]), 0x7FFFFFFF), numbers[2], numbers[3])
+    if workspace is None:
+        workspace = T.empty(T.lib.hl_sample_workspace_bytes(rows, vocab), dtype=T.uint8, device=logits.device)
+    else:
+        _dev_arg(workspace, "workspace")
+        _on_device(logits.device, workspace=workspace)
     s = T.lib.hl_sample(settings, logits.data_ptr(), code, strides[0], rows, vocab, uniforms.data_ptr(),
-                        tokens.data_ptr(), logprobs.data_ptr(), T.raw_stream(dev))
+                        tokens.data_ptr(), logprobs.data_ptr(), workspace.data_ptr(), workspace.nbytes, T.raw_stream(dev))
     if s:
         _check(s, "hl_sample")
     return SampleResult(tokens, logprobs)

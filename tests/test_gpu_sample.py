@@ -72,6 +72,22 @@ def test_settings(dtype, vocab, settings):
     check(*make(4, vocab, dtype, seed=vocab), **settings)
 
 
+# borders in steps of their own, and in one: top_k above what a list holds, top_p near and far from it, min_p between
+@pytest.mark.parametrize("settings", [
+    dict(top_k=3000), dict(top_k=3000, top_p=0.8), dict(top_k=3000, top_p=0.999), dict(top_k=3000, top_p=1.0 - 2.0**-24),
+    dict(top_k=2000, top_p=0.8, min_p=0.05), dict(top_k=2000, min_p=0.001), dict(top_p=0.9, min_p=0.001),
+    dict(top_p=0.5, min_p=0.001), dict(top_p=0.999, min_p=0.001), dict(top_k=1025, top_p=0.95), dict(top_k=1024, top_p=0.95)])
+@pytest.mark.parametrize("size", [0.3, 2.0, 5.0])
+@pytest.mark.parametrize("vocab,dtype", [(9000, torch.float32), (150000, torch.float32), (40000, torch.bfloat16)])
+def test_borders(settings, size, vocab, dtype):
+    check(*make(3, vocab, dtype, size=size, seed=7), **settings)
+
+
+def test_many_rows():
+    x, u = make(700, 3000)
+    check(x, u, top_p=0.9)
+
+
 def test_settings_of_each_row():
     rows = 64
     x, u = make(rows, 5000, torch.bfloat16)

@@ -117,11 +117,12 @@ def test_gemv(L, bad, status):
     (dict(vocab=0), hl.HL_EINVAL), (dict(u=None), hl.HL_EINVAL), (dict(u=A + 2), hl.HL_EINVAL), (dict(tokens=None), hl.HL_EINVAL),
     (dict(tokens=A + 1), hl.HL_EINVAL), (dict(logprobs=None), hl.HL_EINVAL), (dict(logprobs=A + 1), hl.HL_EINVAL),
     (dict(vocab=1 << 20, stride=1 << 20), hl.HL_EUNSUPPORTED), (dict(stride=1 << 40), hl.HL_EUNSUPPORTED),
-    (dict(rows=1 << 30), hl.HL_EUNSUPPORTED)])
+    (dict(rows=65536), hl.HL_EUNSUPPORTED), (dict(ws=None), hl.HL_EINVAL), (dict(ws=A + 8), hl.HL_EINVAL),
+    (dict(n=100), hl.HL_EINVAL)])
 def test_sample(L, bad, status):
     settings = hl.Sampling(None, None, None, None, 1.0, 0, 1.0, 0.0)
     good = dict(settings=ctypes.byref(settings), logits=A, dtype=hl.HL_F32, stride=100, rows=2, vocab=100, u=A, tokens=A,
-                logprobs=A)
+                logprobs=A, ws=A, n=1 << 40)
     assert L.hl_sample(*{**good, **bad}.values(), None) == status
 
 
@@ -129,7 +130,12 @@ def test_sample(L, bad, status):
 def test_sample_settings_misaligned(L, field):
     settings = hl.Sampling(A, A, A, A, 1.0, 0, 1.0, 0.0)
     setattr(settings, field, A + 2)
-    assert L.hl_sample(ctypes.byref(settings), A, hl.HL_F32, 100, 2, 100, A, A, A, None) == hl.HL_EINVAL
+    assert L.hl_sample(ctypes.byref(settings), A, hl.HL_F32, 100, 2, 100, A, A, A, A, 1 << 40, None) == hl.HL_EINVAL
+
+
+def test_sample_workspace(L):
+    assert 0 < L.hl_sample_workspace_bytes(1, 1) < L.hl_sample_workspace_bytes(1, 100000) < L.hl_sample_workspace_bytes(9, 100000)
+    assert L.hl_sample_workspace_bytes(0, 9) == L.hl_sample_workspace_bytes(9, 0) == L.hl_sample_workspace_bytes(1, 1 << 20) == 0
 
 
 def test_packed_settings():
@@ -210,7 +216,7 @@ RUNS = [(lambda **m: hl.cache_write4(**{**write_args(), **m}), ["hl_cache_write4
         (lambda **m: hl.prefix_attention4(**{**attention_args(), **m}),
          ["hl_attention4_workspace_bytes", "hl_prefix_attention4"]),
         (lambda **m: hl.gemv4(**{**gemv_args(), **m}), ["hl_gemv4"]),
-        (lambda **m: hl.sample(**{**sample_args(), **m}), ["hl_sample"])]
+        (lambda **m: hl.sample(**{**sample_args(), **m}), ["hl_sample_workspace_bytes", "hl_sample"])]
 WRITE, READ, ATTENTION, GEMV, SAMPLE = range(5)
 
 

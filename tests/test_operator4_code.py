@@ -8,7 +8,8 @@ import pytest
 
 from test_operator_code import LIB, LLVM, VECTOR, span
 
-KERNELS = ("parts4_kernel", "solo4_kernel", "gemv4_kernel", "write4_kernel", "read4_kernel", "sample")
+KERNELS = ("parts4_kernel", "solo4_kernel", "gemv4_kernel", "write4_kernel", "read4_kernel", "top_kernel", "step_kernel",
+           "finish_kernel")
 
 
 @pytest.fixture(scope="module")
