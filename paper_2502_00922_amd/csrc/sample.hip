@@ -12,9 +12,9 @@
 // Rows are cut into slices, so that few rows use the whole GPU too. top_kernel finds
 // each slice's greatest logit; step_kernel counts (or weighs) the steps, for the row
 // and for its slice, and its last block of a row finds the border's step;
-// finish_kernel lists that step's logits, and the last of a row's blocks to arrive
-// ends the row: it has every slice's weight below the step and the list, and looks
-// again only at the slice that the token is in. With top_k of kFew or less all that
+// list_kernel lists that step's logits; end_kernel, one block a row, has every slice's
+// weight below the step and the list, and looks again only at the slice that the
+// token is in. With top_k of kFew or less all that
 // is kept is on the list, and nothing else is weighed. Where a list would be too long
 // (more than kList logits in a step), the block takes the whole row's logits again
 // for each digit of the border (slow_row).
@@ -27,7 +27,9 @@
 namespace hl {
 
 constexpr uint32_t kSteps = 1024, kSlices = 64, kList = 2048, kFew = 1024;
-constexpr uint32_t kThreads = 256, kWaves = kThreads / 64;
+constexpr uint32_t kThreads = 256, kWaves = kThreads / 64;  // of a slice's blocks
+constexpr uint32_t kEnd = 512, kEndWaves = kEnd / 64;       // of a row's last block
+constexpr uint32_t kAhead = 4;    // loads of a lane in flight
 constexpr uint32_t kPairs = 256;  // logits on a list, at most, that are compared each with each
 constexpr double kSpan = 40.0;  // powers of two below the greatest weight that a token may have
 constexpr double kLn2 = 0.6931471805599453;
@@ -41,18 +43,18 @@ struct RowWork {
   uint32_t count[kSteps];
   u64 sum[kSlices];  // of the slice's weights that are kept whatever the list says
   float most[kSlices], lowest[kSlices];
-  uint32_t first[kSlices], listed[kSlices];  // first: index of most
+  uint32_t first[kSlices], listed[kSlices * kWaves];  // first: index of most; listed: by each of a slice's waves
   // The border. Steps below lo are kept as far as top_k and top_p go, above hi not;
   // those between, and step `other`, go on the list. by_count, by_mass: whether
   // top_k and top_p end there. From step `from` on, top_k's border is on the list.
   uint32_t lo, hi, other, from, by_count, by_mass;
-  uint32_t arrived[2];
+  uint32_t arrived, unused0;
   u64 count_from, mass_from, mass_lo;  // of the steps below `from` and lo
   u64 unused[5];
 };
 struct SliceWork {
   u64 mass[kSteps];
-  u64 list[kList];  // logit's bits, and its index above them
+  u64 list[kWaves][kList];  // of a wave: a logit's bits, and its index above them
 };
 
 struct SampleArgs {
@@ -82,33 +84,59 @@ __device__ inline uint32_t rank_of(float l) {
   return b & 0x80000000u ? b : b ^ 0x7FFFFFFFu;
 }
 
+// v of another lane, by the row shifts and row broadcasts of scan_wave; `none` where
+// there is no such lane.
+template <int CTRL, int ROWS, class X>
+__device__ inline X moved(X v, X none) {
+  if constexpr (sizeof(X) == 8) {
+    const u64 x = __builtin_bit_cast(u64, v), o = __builtin_bit_cast(u64, none);
+    const uint32_t low = __builtin_amdgcn_update_dpp((uint32_t)o, (uint32_t)x, CTRL, ROWS, 0xF, false);
+    const uint32_t high = __builtin_amdgcn_update_dpp((uint32_t)(o >> 32), (uint32_t)(x >> 32), CTRL, ROWS, 0xF, false);
+    return __builtin_bit_cast(X, (u64)high << 32 | low);
+  } else {
+    const uint32_t x = __builtin_bit_cast(uint32_t, v), o = __builtin_bit_cast(uint32_t, none);
+    return __builtin_bit_cast(X, (uint32_t)__builtin_amdgcn_update_dpp(o, x, CTRL, ROWS, 0xF, false));
+  }
+}
+
+// f over the lanes up to this one. Whole wave; a few cycles a step, where a shuffle
+// through LDS takes a hundred.
+template <class X, class F>
+__device__ inline X over_lanes(X v, X none, F f) {
+  v = f(v, moved<0x111, 0xF>(v, none));  // lane - 1 of a row of 16
+  v = f(v, moved<0x112, 0xF>(v, none));  // lane - 2
+  v = f(v, moved<0x114, 0xF>(v, none));  // lane - 4
+  v = f(v, moved<0x118, 0xF>(v, none));  // lane - 8
+  v = f(v, moved<0x142, 0xA>(v, none));  // row 0's last to row 1, row 2's to row 3
+  return f(v, moved<0x143, 0xC>(v, none));  // lane 31 to rows 2 and 3
+}
+
 template <class X>
 __device__ inline X scan_wave(X v) {
-#pragma unroll
-  for (uint32_t d = 1; d < 64; d <<= 1) {
-    const X o = __shfl_up(v, d);
-    if (threadIdx.x % 64 >= d) v += o;
+  return over_lanes(v, (X)0, [](X x, X y) { return x + y; });
+}
+
+// v of a lane that is the same in the whole wave.
+template <class X>
+__device__ inline X lane_of(X v, uint32_t lane) {
+  if constexpr (sizeof(X) == 8) {
+    const u64 x = __builtin_bit_cast(u64, v);
+    const uint32_t low = __builtin_amdgcn_readlane((uint32_t)x, lane), high = __builtin_amdgcn_readlane((uint32_t)(x >> 32), lane);
+    return __builtin_bit_cast(X, (u64)high << 32 | low);
+  } else {
+    return __builtin_bit_cast(X, (uint32_t)__builtin_amdgcn_readlane(__builtin_bit_cast(uint32_t, v), lane));
   }
-  return v;
 }
 
 template <class X>
-__device__ inline X add_wave(X v) {
-#pragma unroll
-  for (uint32_t d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-  return v;
-}
+__device__ inline X add_wave(X v) { return lane_of(scan_wave(v), 63); }
 
 __device__ inline float most_wave(float v) {
-#pragma unroll
-  for (uint32_t d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
+  return lane_of(over_lanes(v, -INFINITY, [](float x, float y) { return fmaxf(x, y); }), 63);
 }
 
-// A value that another block of the kernel stores or loads: performed at the
-// memory that all XCDs share.
-template <class X>
-__device__ inline void give(X* p, X v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// A value that other blocks of the kernel have added to: from the memory that all
+// XCDs share.
 template <class X>
 __device__ inline X take(const X* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
@@ -130,6 +158,29 @@ struct Logits {
     for (uint32_t j = 0; j < VEC; ++j) to[j] = x[j] == x[j] ? (float)x[j] : -INFINITY;
   }
 };
+
+// f(logits, index of the first) for the vectors at begin + first, and again every
+// STRIDE, kAhead loads at a time; ends where f is true, and then is. Whole wave.
+template <class T, uint32_t STRIDE, class F>
+__device__ __attribute__((always_inline)) inline bool for_vectors(const T* row, uint32_t begin, uint32_t end,
+                                                                  uint32_t first, F f) {
+  constexpr uint32_t VEC = Logits<T>::VEC;
+  uint32_t at = begin;
+  for (; at + kAhead * STRIDE <= end; at += kAhead * STRIDE) {
+    float v[kAhead][VEC];
+#pragma unroll
+    for (uint32_t i = 0; i < kAhead; ++i) Logits<T>::read(row, ~0u, at + i * STRIDE + first, v[i]);
+#pragma unroll
+    for (uint32_t i = 0; i < kAhead; ++i)
+      if (f(v[i], at + i * STRIDE + first)) return true;
+  }
+  for (; at < end; at += STRIDE) {
+    float v[VEC];
+    Logits<T>::read(row, end, at + first, v);
+    if (f(v, at + first)) return true;
+  }
+  return false;
+}
 
 // What a row's draw asks, and how its logits are weighed. `most`: the greatest.
 struct Draw {
@@ -185,21 +236,20 @@ __global__ void __launch_bounds__(kThreads) top_kernel(SampleArgs a) {
   RowWork& w = a.of_row(row);
   if (slice == 0) {
     for (uint32_t i = tid; i < kSteps; i += kThreads) w.mass[i] = 0, w.count[i] = 0;
-    if (tid < 2) w.arrived[tid] = 0;
+    if (tid == 0) w.arrived = 0;
   }
   const T* logits = static_cast<const T*>(a.logits) + row * a.stride;
   const uint32_t begin = slice * a.slice, end = min(begin + a.slice, a.vocab);
   float most = -INFINITY, lowest = INFINITY;
   uint32_t first = begin;
-  for (uint32_t at = begin + tid * VEC; at < end; at += kThreads * VEC) {
-    float v[VEC];
-    Logits<T>::read(logits, end, at, v);
+  for_vectors<T, kThreads * VEC>(logits, begin, end, tid * VEC, [&](const float (&v)[VEC], uint32_t at) {
 #pragma unroll
     for (uint32_t j = 0; j < VEC; ++j) {
       if (v[j] > most) most = v[j], first = at + j;
       lowest = fminf(lowest, v[j] > -INFINITY ? v[j] : INFINITY);
     }
-  }
+    return false;
+  });
 #pragma unroll
   for (uint32_t d = 32; d; d >>= 1) {
     const float m = __shfl_xor(most, d);
@@ -224,8 +274,8 @@ __device__ inline void ends_of(const SampleArgs& a, const RowWork& w, float& mos
   lowest = -most_wave(lane < a.slices ? -w.lowest[lane] : -INFINITY);
 }
 
-// Whether this is the last of a row's blocks to come here, which sees what the others
-// gave before they came.
+// Whether this is the last of a row's blocks to come here. The others' atomics have
+// been performed by then.
 __device__ inline bool last_of_row(const SampleArgs& a, uint32_t& arrived) {
   __shared__ uint32_t s_arrived;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -237,8 +287,9 @@ __device__ inline bool last_of_row(const SampleArgs& a, uint32_t& arrived) {
 }
 
 // The sum of v over the block's threads before this one; `all`: over all of them.
+template <uint32_t WAVES>
 __device__ inline u64 scan_block(u64 v, u64& all) {
-  __shared__ u64 s_wave[kWaves];
+  __shared__ u64 s_wave[WAVES];
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const u64 upto = scan_wave(v);
   if (threadIdx.x % 64 == 63) s_wave[wave] = upto;
@@ -246,7 +297,7 @@ __device__ inline u64 scan_block(u64 v, u64& all) {
   u64 before = upto - v;
   all = 0;
 #pragma unroll
-  for (uint32_t i = 0; i < kWaves; ++i) {
+  for (uint32_t i = 0; i < WAVES; ++i) {
     if (i < wave) before += s_wave[i];
     all += s_wave[i];
   }
@@ -254,22 +305,23 @@ __device__ inline u64 scan_block(u64 v, u64& all) {
   return before;
 }
 
+template <uint32_t WAVES>
 __device__ inline u64 add_block(u64 v) {
   u64 all;
-  scan_block(v, all);
+  scan_block<WAVES>(v, all);
   return all;
 }
 
 // The first of N numbers a thread, one thread's after the other's, at which the
 // running sum reaches a goal that the sum of all reaches; `before`: the sum before it.
-template <uint32_t N, class Reached>
+template <uint32_t WAVES, uint32_t N, class Reached>
 __device__ inline uint32_t find_first(const u64 (&v)[N], Reached reached, u64& before) {
   __shared__ u64 s_before;
   __shared__ uint32_t s_at;
   u64 sum = 0, all;
 #pragma unroll
   for (uint32_t i = 0; i < N; ++i) sum += v[i];
-  u64 run = scan_block(sum, all);
+  u64 run = scan_block<WAVES>(sum, all);
 #pragma unroll
   for (uint32_t i = 0; i < N; ++i) {
     if (!reached(run) && reached(run + v[i])) s_at = N * threadIdx.x + i, s_before = run;
@@ -296,14 +348,14 @@ __device__ inline void place_border(const Draw& d, RowWork& w) {
     u64 sum = 0;
 #pragma unroll
     for (uint32_t i = 0; i < N; ++i) sum += N * tid + i < step ? v[i] : 0;
-    return add_block(sum);
+    return add_block<kWaves>(sum);
   };
-  c = add_block(c), m = add_block(m);
+  c = add_block<kWaves>(c), m = add_block<kWaves>(m);
   uint32_t lo = kSteps, hi = kSteps, at_k = kSteps;
   bool by_count = d.k && c > d.k, by_mass = d.top_p < 1.0f;
   u64 least = m, most = m, before;  // that what top_k keeps weighs
   if (by_count) {
-    lo = hi = at_k = find_first(count, [&](u64 sum) { return sum >= d.k; }, before);
+    lo = hi = at_k = find_first<kWaves>(count, [&](u64 sum) { return sum >= d.k; }, before);
     least = below(mass, at_k), most = below(mass, at_k + 1);
   }
   if (d.few) {
@@ -312,8 +364,8 @@ __device__ inline void place_border(const Draw& d, RowWork& w) {
   } else {
     if (by_mass) {
       const double first = fmax((double)d.top_p * (double)least, 1.0), second = fmax((double)d.top_p * (double)most, 1.0);
-      lo = find_first(mass, [&](u64 sum) { return (double)sum >= first; }, before);
-      hi = find_first(mass, [&](u64 sum) { return (double)sum >= second; }, before);
+      lo = find_first<kWaves>(mass, [&](u64 sum) { return (double)sum >= first; }, before);
+      hi = find_first<kWaves>(mass, [&](u64 sum) { return (double)sum >= second; }, before);
     }
     if (d.floor_w > 0.0) {
       // the step of the least weight that min_p keeps, or either of two
@@ -354,15 +406,15 @@ __global__ void __launch_bounds__(kThreads) step_kernel(SampleArgs a) {
   const T* logits = static_cast<const T*>(a.logits) + row * a.stride;
   const uint32_t begin = slice * a.slice, end = min(begin + a.slice, a.vocab);
   const auto each = [&](auto f) __attribute__((always_inline)) {
-    for (uint32_t at = begin + tid * VEC; at < end; at += kThreads * VEC) {
-      float v[VEC];
-      Logits<T>::read(logits, end, at, v);
+    for_vectors<T, kThreads * VEC>(logits, begin, end, tid * VEC,
+                                   [&](const float (&v)[VEC], uint32_t) __attribute__((always_inline)) {
 #pragma unroll
       for (uint32_t j = 0; j < VEC; ++j) {
         const double y = d.power(v[j]);
         if (y >= -kSpan) f(v[j], y);
       }
-    }
+      return false;
+    });
   };
   if (d.few) {
     each([&](float l, double) { atomicAdd(&s_count[d.step(l)], 1u); });
@@ -389,16 +441,17 @@ __global__ void __launch_bounds__(kThreads) step_kernel(SampleArgs a) {
     }
     if (s_count[i]) atomicAdd(&w.count[i], s_count[i]);
   }
-  if (last_of_row(a, w.arrived[0])) place_border(d, w);
+  if (last_of_row(a, w.arrived)) place_border(d, w);
 }
 
 struct EndLds {
-  u64 bin[kThreads], weight[kList];
+  u64 bin[kEnd], weight[kList];
   float logit[kList];
   uint32_t index[kList];
   double powers[64];
-  u64 wave[kWaves], total[kSlices], limit;
-  uint32_t start[kSlices + 1], pick;
+  u64 wave[kEndWaves], total[kSlices], limit;
+  ulonglong2 pair[kPairs];  // a logit's place, and its weight if its step is not past hi
+  uint32_t start[kSlices * kWaves], pick;
 };
 
 // Where the running sum of weigh(logit), in the order of the logits, reaches a goal:
@@ -423,7 +476,7 @@ __device__ inline Border find_border(EndLds& s, Each each, uint32_t top, uint32_
     __syncthreads();
     const u64 bin[1] = {s.bin[threadIdx.x]};
     u64 ahead;
-    const uint32_t digit = find_first(bin, [&](u64 sum) { return reached(before + sum); }, ahead);
+    const uint32_t digit = find_first<kEndWaves>(bin, [&](u64 sum) { return reached(before + sum); }, ahead);
     before += ahead, shift -= width;
     prefix = prefix << width | digit;
   }
@@ -431,7 +484,7 @@ __device__ inline Border find_border(EndLds& s, Each each, uint32_t top, uint32_
   each([&](float l, auto i) __attribute__((always_inline)) {
     if (rank_of(l) == prefix) ++same, sum += weigh(l, i);
   });
-  same = add_block(same), sum = add_block(sum);
+  same = add_block<kEndWaves>(same), sum = add_block<kEndWaves>(sum);
   u64 low = 1, high = same;  // of equal ones, which weigh the same, as few as reach it
   while (low < high) {
     const u64 mid = (low + high) / 2;
@@ -450,18 +503,18 @@ struct Stretch {
 
   __device__ Stretch(const T* r, uint32_t from, uint32_t to) : row(r) {
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const uint32_t part = (to - from + kThreads * VEC - 1) / (kThreads * VEC) * (64 * VEC);
+    const uint32_t part = (to - from + kEnd * VEC - 1) / (kEnd * VEC) * (64 * VEC);
     begin = min(from + wave * part, to), end = min(begin + part, to);
   }
   // f(logit, index) for this lane's logits
   template <class F>
   __device__ __attribute__((always_inline)) void each(F f) const {
-    for (uint32_t at = begin + threadIdx.x % 64 * VEC; at < end; at += 64 * VEC) {
-      float v[VEC];
-      Logits<T>::read(row, end, at, v);
+    for_vectors<T, 64 * VEC>(row, begin, end, threadIdx.x % 64 * VEC,
+                             [&](const float (&v)[VEC], uint32_t at) __attribute__((always_inline)) {
 #pragma unroll
       for (uint32_t j = 0; j < VEC; ++j) f(v[j], at + j);
-    }
+      return false;
+    });
   }
   // The first index at which the running sum of weigh(logit, index) over the stretch
   // is above `target`, which is below its sum.
@@ -477,11 +530,9 @@ struct Stretch {
     u64 before = 0;
     for (uint32_t i = 0; i < wave; ++i) before += s.wave[i];
     if (before <= target && target < before + sum) {
-      for (uint32_t at0 = begin; at0 < end; at0 += 64 * VEC) {
-        const uint32_t at = at0 + lane * VEC;
-        float v[VEC];
+      for_vectors<T, 64 * VEC>(row, begin, end, lane * VEC,
+                               [&](const float (&v)[VEC], uint32_t at) __attribute__((always_inline)) {
         u64 w[VEC], mine = 0;
-        Logits<T>::read(row, end, at, v);
 #pragma unroll
         for (uint32_t j = 0; j < VEC; ++j) w[j] = weigh(v[j], at + j), mine += w[j];
         const u64 upto = before + scan_wave(mine), past = __ballot(upto > target);
@@ -495,10 +546,10 @@ struct Stretch {
             if (!there && run > target) found = at + j, there = true;
           }
           if (lane == (uint32_t)__builtin_ctzll(past)) s.pick = found;
-          break;
         }
-        before = __shfl(upto, 63);
-      }
+        before = lane_of(upto, 63);
+        return past != 0;
+      });
     }
     __syncthreads();
     const uint32_t i = s.pick;
@@ -537,7 +588,7 @@ __device__ inline void slow_row(const SampleArgs& a, const Draw& d, uint32_t row
     const auto weigh = [&](float l, uint32_t) __attribute__((always_inline)) { return stage == 0 ? 1ull : mass(l); };
     u64 n = 0;
     all.each([&](float l, uint32_t i) __attribute__((always_inline)) { n += in(l, i) ? weigh(l, i) : 0; });
-    n = add_block(n);
+    n = add_block<kEndWaves>(n);
     if (stage == 0 && n <= d.k) continue;
     const double goal = stage == 0 ? (double)d.k : fmax((double)d.top_p * (double)n, 1.0);
     const auto each = [&](auto f) __attribute__((always_inline)) {
@@ -556,95 +607,110 @@ __device__ inline void slow_row(const SampleArgs& a, const Draw& d, uint32_t row
   };
   u64 n = 0;
   all.each([&](float l, uint32_t i) __attribute__((always_inline)) { n += weigh(l, i); });
-  const u64 total = add_block(n);
+  const u64 total = add_block<kEndWaves>(n);
   end_row(a, d, row, logits, all.pick(s, target_of(a.uniforms[row], total), weigh), total);
 }
 
-// Lists the logits of the border's step, and ends the row in its last block. Bound by
-// launch and waits for rows of a few slices, else by reading the logits again for the
-// list.
+// Lists the logits of the border's steps, and adds up what the slice has below them.
+// Bound by reading the logits again.
 template <class T>
-__global__ void __launch_bounds__(kThreads) finish_kernel(SampleArgs a) {
-  constexpr uint32_t VEC = Logits<T>::VEC, EACH = kList / kThreads;
-  __shared__ EndLds s;
+__global__ void __launch_bounds__(kThreads) list_kernel(SampleArgs a) {
+  constexpr uint32_t VEC = Logits<T>::VEC;
   const uint32_t slice = blockIdx.x, row = blockIdx.y, tid = threadIdx.x, lane = tid % 64;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  RowWork& w = a.of_row(row);
+  float most, lowest;
+  ends_of(a, w, most, lowest);
+  if (most == -INFINITY) return;
+  const Draw d(a, row, most, lowest);
+  if (d.greedy || !d.border) return;
+  const uint32_t lo = w.lo, hi = w.hi, other = w.other;
+  SliceWork& own = a.of_slice(row, slice);
+  if (!d.few) {
+    u64 base = 0;
+    for (uint32_t i = tid; i < lo; i += kThreads) base += own.mass[i];
+    base = add_block<kWaves>(base);
+    if (tid == 0) w.sum[slice] = base;
+  }
+  // every wave has its part of the slice and a list of its own
+  const T* logits = static_cast<const T*>(a.logits) + row * a.stride;
+  const uint32_t part = a.slice / kWaves, begin = min(slice * a.slice + wave * part, a.vocab);
+  uint32_t listed = 0;
+  for_vectors<T, 64 * VEC>(logits, begin, min(begin + part, a.vocab), lane * VEC,
+                           [&](const float (&v)[VEC], uint32_t at) __attribute__((always_inline)) {
+    uint32_t mine = 0;
+#pragma unroll
+    for (uint32_t j = 0; j < VEC; ++j) {
+      const uint32_t x = d.step(v[j]);
+      mine |= (uint32_t)((x >= lo && x <= hi) || x == other) << j;
+    }
+    if (!__any(mine != 0)) return false;
+#pragma unroll
+    for (uint32_t j = 0; j < VEC; ++j) mine &= ~((uint32_t)!d.weighs(v[j]) << j);
+    const uint32_t upto = scan_wave((uint32_t)__popc(mine));
+    uint32_t to = listed + upto - __popc(mine);
+#pragma unroll
+    for (uint32_t j = 0; j < VEC; ++j)
+      if (mine >> j & 1) {
+        if (to < kList) own.list[wave][to] = (u64)(at + j) << 32 | __builtin_bit_cast(uint32_t, v[j]);
+        ++to;
+      }
+    listed += lane_of(upto, 63);
+    return false;
+  });
+  if (lane == 0) w.listed[slice * kWaves + wave] = listed;
+}
+
+// Ends a row from its list and the slices' sums. Bound by its barriers and waits, one
+// after the other.
+template <class T>
+__global__ void __launch_bounds__(kEnd) end_kernel(SampleArgs a) {
+  constexpr uint32_t EACH = kList / kEnd;
+  __shared__ EndLds s;
+  const uint32_t row = blockIdx.x, tid = threadIdx.x, lane = tid % 64;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(tid / 64);
   RowWork& w = a.of_row(row);
   const T* logits = static_cast<const T*>(a.logits) + row * a.stride;
   float most, lowest;
   ends_of(a, w, most, lowest);
   if (most == -INFINITY) {  // nothing to draw
-    if (slice == 0 && tid == 0) a.tokens[row] = -1, a.logprobs[row] = -INFINITY;
+    if (tid == 0) a.tokens[row] = -1, a.logprobs[row] = -INFINITY;
     return;
   }
   const Draw d(a, row, most, lowest);
   if (d.greedy) {
     const uint64_t at = __ballot(lane < a.slices && w.most[lane < a.slices ? lane : 0] == most);
-    if (slice == 0 && tid == 0) a.tokens[row] = (int32_t)w.first[__builtin_ctzll(at)], a.logprobs[row] = 0.0f;
+    if (tid == 0) a.tokens[row] = (int32_t)w.first[__builtin_ctzll(at)], a.logprobs[row] = 0.0f;
     return;
   }
-  if (!d.border && slice != 0) return;  // nothing is listed
-  const uint32_t lo = d.border ? w.lo : kSteps, hi = d.border ? w.hi : kSteps, other = d.border ? w.other : kSteps;
-  SliceWork& own = a.of_slice(row, slice);
-  if (d.border && !d.few) {
-    u64 base = 0;
-    for (uint32_t i = tid; i < lo; i += kThreads) base += own.mass[i];
-    base = add_block(base);
-    if (tid == 0) give(&w.sum[slice], base);
-  }
-  if (lo < kSteps) {
-    const uint32_t begin = slice * a.slice, end = min(begin + a.slice, a.vocab);
-    u64 listed = 0;
-    for (uint32_t at0 = begin; at0 < end; at0 += kThreads * VEC) {
-      const uint32_t at = at0 + tid * VEC;
-      float v[VEC];
-      if (at < end) Logits<T>::read(logits, end, at, v);
-      uint32_t mine = 0;
-#pragma unroll
-      for (uint32_t j = 0; j < VEC; ++j) {
-        const uint32_t x = at < end && d.weighs(v[j]) ? d.step(v[j]) : kSteps;
-        mine |= (uint32_t)((x >= lo && x <= hi) || x == other) << j;
-      }
-      u64 all;
-      u64 to = listed + scan_block(__popc(mine), all);
-#pragma unroll
-      for (uint32_t j = 0; j < VEC; ++j)
-        if (mine >> j & 1) {
-          if (to < kList) give(&own.list[to], (u64)(at + j) << 32 | __builtin_bit_cast(uint32_t, v[j]));
-          ++to;
-        }
-      listed += all;
-    }
-    if (tid == 0) give(&w.listed[slice], (uint32_t)listed);
-  }
-  if (d.border && !last_of_row(a, w.arrived[1])) return;
+  const uint32_t lo = d.border ? w.lo : kSteps, hi = d.border ? w.hi : kSteps;
   if (tid < 64) s.powers[tid] = exp2((double)tid / 64.0);
   uint32_t n = 0;
   if (lo < kSteps) {
-    const uint32_t mine = lane < a.slices ? take(&w.listed[lane]) : 0, upto = scan_wave(mine);
-    if (wave == 0) s.start[lane + 1] = upto;
-    if (tid == 0) s.start[0] = 0;
+    static_assert(kSlices * kWaves <= kEnd, "a thread has a wave's list");
+    const uint32_t mine = tid < a.slices * kWaves ? w.listed[tid] : 0;
+    u64 all;
+    const uint32_t start = (uint32_t)scan_block<kEndWaves>(mine, all);
+    if (tid < kSlices * kWaves) s.start[tid] = start;
+    n = (uint32_t)all;
   }
   __syncthreads();
-  if (lo < kSteps) {
-    n = s.start[kSlices];
-    if (n > kList) {
-      slow_row<T>(a, d, row, logits, s);
-      return;
-    }
+  if (n > kList) {
+    slow_row<T>(a, d, row, logits, s);
+    return;
   }
   // Logits each*tid .. of the list are this thread's: as few as take the whole list,
   // so that a short one is one logit a thread. `kept` has a bit for each.
-  const uint32_t most_each = n <= kThreads ? 1 : EACH, first = most_each * tid;
+  const uint32_t most_each = n <= kEnd ? 1 : EACH, first = most_each * tid;
   uint32_t kept = 0;
   for (uint32_t j = 0; j < most_each; ++j) {
     const uint32_t i = first + j;
     if (i >= n) break;
-    uint32_t from = 0;  // the slice that it is in
+    uint32_t from = 0;  // the list that it is on
 #pragma unroll
-    for (uint32_t h = kSlices / 2; h; h >>= 1)
+    for (uint32_t h = kSlices * kWaves / 2; h; h >>= 1)
       if (s.start[from + h] <= i) from += h;
-    const u64 x = take(&a.of_slice(row, from).list[i - s.start[from]]);
+    const u64 x = a.of_slice(row, from / kWaves).list[from % kWaves][i - s.start[from]];
     const float l = __builtin_bit_cast(float, (uint32_t)x);
     s.logit[i] = l, s.index[i] = (uint32_t)(x >> 32);
     s.weight[i] = Draw::whole(d.power(l), s.powers);
@@ -674,21 +740,26 @@ __global__ void __launch_bounds__(kThreads) finish_kernel(SampleArgs a) {
   const uint32_t from = d.border ? w.from : kSteps;
   u64 limit = ~0ull;  // the last place kept, for the logits of listed steps
   if (n && n <= kPairs) {
-    // each logit's predecessors, among those that its sum is over
-    u64 count = by_count ? w.count_from : 0, mass = d.border ? w.mass_lo : 0;
-    const u64 mine = tid < n ? place_of(s.logit[tid], s.index[tid]) : 0;
-    const uint32_t step = tid < n ? d.step(s.logit[tid]) : 0;
-    for (uint32_t i = 0; i < n; ++i) {
-      const float l = s.logit[i];
-      const uint32_t x = d.step(l);
-      const bool ahead = place_of(l, s.index[i]) < mine;
-      count += ahead && x >= from, mass += ahead && x <= hi ? s.weight[i] : 0;
+    // each logit's predecessors
+    const float l = tid < n ? s.logit[tid] : 0.0f;
+    const u64 mine = tid < n ? place_of(l, s.index[tid]) : 0;
+    const uint32_t step = tid < n ? d.step(l) : 0;
+    if (tid < kPairs) s.pair[tid] = {tid < n ? mine : ~0ull, tid < n && step <= hi ? s.weight[tid] : 0};
+    u64 count = by_count ? w.count_from - add_block<kEndWaves>(tid < n && step < from) : 0, mass = d.border ? w.mass_lo : 0;
+    __syncthreads();
+    if (by_count || by_mass) {
+#pragma unroll 8
+      for (uint32_t i = 0; i < (n + 7) / 8 * 8; ++i) {
+        const ulonglong2 x = s.pair[i];
+        const bool ahead = x.x < mine;
+        count += ahead, mass += ahead ? x.y : 0;
+      }
     }
     if (by_count) narrow([&](uint32_t) { return step < from || count < d.k; });
     if (by_mass) {
       u64 sum = 0;
       each([&](uint32_t i) { sum += step >= from ? s.weight[i] : 0; });
-      const double goal = fmax((double)d.top_p * (double)(w.mass_from + add_block(sum)), 1.0);
+      const double goal = fmax((double)d.top_p * (double)(w.mass_from + add_block<kEndWaves>(sum)), 1.0);
       narrow([&](uint32_t) { return step <= hi && (double)mass < goal; });
     }
     each([&](uint32_t) { atomicMax(&s.limit, mine); });
@@ -703,7 +774,7 @@ __global__ void __launch_bounds__(kThreads) finish_kernel(SampleArgs a) {
     if (lane == 0) s.wave[wave] = (u64)high << 32 | low;
     __syncthreads();
 #pragma unroll
-    for (uint32_t i = 0; i < kWaves; ++i)
+    for (uint32_t i = 0; i < kEndWaves; ++i)
       low = min(low, (uint32_t)s.wave[i]), high = max(high, (uint32_t)(s.wave[i] >> 32));
     const uint32_t top = low == high ? 0 : 32 - __builtin_clz(low ^ high);
     // Ends the listed logits of which `of` is true where the sum of `weigh` reaches `to`.
@@ -717,7 +788,7 @@ __global__ void __launch_bounds__(kThreads) finish_kernel(SampleArgs a) {
                                    [&](u64 sum) { return (double)sum >= to; });
       u64 same = 0, all;
       some([&](float l, uint32_t) { same += rank_of(l) == b.rank; });
-      u64 nth = scan_block(same, all);
+      u64 nth = scan_block<kEndWaves>(same, all);
       some([&](float l, uint32_t i) {
         if (rank_of(l) == b.rank && ++nth == b.need) s.limit = place_of(l, s.index[i]);
       });
@@ -731,7 +802,7 @@ __global__ void __launch_bounds__(kThreads) finish_kernel(SampleArgs a) {
     if (by_mass) {
       u64 sum = 0;
       each([&](uint32_t i) { sum += d.step(s.logit[i]) >= from ? s.weight[i] : 0; });
-      const double goal = fmax((double)d.top_p * (double)(w.mass_from + add_block(sum)), 1.0);
+      const double goal = fmax((double)d.top_p * (double)(w.mass_from + add_block<kEndWaves>(sum)), 1.0);
       shorten([&](uint32_t i) { return d.step(s.logit[i]) <= hi; }, [&](float, uint32_t i) { return s.weight[i]; }, w.mass_lo,
               goal);
     }
@@ -740,7 +811,7 @@ __global__ void __launch_bounds__(kThreads) finish_kernel(SampleArgs a) {
   const float u = a.uniforms[row];
   if (d.few) {  // the list is in the order of the indexes, and has all
     u64 total;
-    u64 run = scan_block(weight_kept(), total);
+    u64 run = scan_block<kEndWaves>(weight_kept(), total);
     const u64 target = target_of(u, total);
     each([&](uint32_t i) {
       if (run <= target && run + s.weight[i] > target) s.pick = s.index[i];
@@ -750,13 +821,13 @@ __global__ void __launch_bounds__(kThreads) finish_kernel(SampleArgs a) {
     end_row(a, d, row, logits, s.pick, total);
     return;
   }
-  if (tid < kSlices) s.total[tid] = tid < a.slices ? (d.border ? take(&w.sum[tid]) : w.sum[tid]) : 0;
+  if (tid < kSlices) s.total[tid] = tid < a.slices ? w.sum[tid] : 0;
   __syncthreads();
   each([&](uint32_t i) { atomicAdd(&s.total[s.index[i] / a.slice], s.weight[i]); });
   __syncthreads();
-  const u64 mine = s.total[lane], upto = scan_wave(mine), total = __shfl(upto, 63), target = target_of(u, total);
+  const u64 mine = s.total[lane], upto = scan_wave(mine), total = lane_of(upto, 63), target = target_of(u, total);
   const uint32_t in = (uint32_t)__builtin_ctzll(__ballot(upto > target));
-  const u64 before = __shfl(upto - mine, in);
+  const u64 before = lane_of(upto - mine, in);
   const Stretch<T> there(logits, in * a.slice, min((in + 1) * a.slice, a.vocab));
   const uint32_t token = there.pick(s, target - before, [&](float l, uint32_t i) __attribute__((always_inline)) -> u64 {
     if (!d.weighs(l)) return 0;
@@ -780,7 +851,8 @@ static hl_status run_sample(const SampleArgs& a, uint32_t rows, hipStream_t s) {
   const dim3 grid(a.slices, rows);
   hl_status st = enqueue(top_kernel<T>, grid, dim3(kThreads), s, a);
   if (st == HL_OK) st = enqueue(step_kernel<T>, grid, dim3(kThreads), s, a);
-  return st == HL_OK ? enqueue(finish_kernel<T>, grid, dim3(kThreads), s, a) : st;
+  if (st == HL_OK) st = enqueue(list_kernel<T>, grid, dim3(kThreads), s, a);
+  return st == HL_OK ? enqueue(end_kernel<T>, dim3(rows), dim3(kEnd), s, a) : st;
 }
 
 }  // namespace hl

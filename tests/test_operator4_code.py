@@ -9,7 +9,7 @@ import pytest
 from test_operator_code import LIB, LLVM, VECTOR, span
 
 KERNELS = ("parts4_kernel", "solo4_kernel", "gemv4_kernel", "write4_kernel", "read4_kernel", "top_kernel", "step_kernel",
-           "finish_kernel")
+           "list_kernel", "end_kernel")
 
 
 @pytest.fixture(scope="module")
