@@ -54,7 +54,7 @@ struct RowWork {
 };
 struct SliceWork {
   u64 mass[kSteps];
-  u64 list[kWaves][kList];  // of a wave: a logit's bits, and its index above them
+  u64 list[kWaves][kList];  // of a wave: a level's bits, and its index above them
 };
 
 struct SampleArgs {
@@ -140,7 +140,7 @@ __device__ inline float most_wave(float v) {
 template <class X>
 __device__ inline X take(const X* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-// Logits at .. at+VEC-1 of a row as float32; NaN, and past `end`, -infinity.
+// Logits at .. at+VEC-1 of a row as float32; past `end`, -infinity.
 template <class T>
 struct Logits {
   static constexpr uint32_t VEC = 16 / sizeof(T);
@@ -155,7 +155,7 @@ struct Logits {
       for (uint32_t j = 0; j < VEC; ++j) x[j] = at + j < end ? row[at + j] : (T)-INFINITY;
     }
 #pragma unroll
-    for (uint32_t j = 0; j < VEC; ++j) to[j] = x[j] == x[j] ? (float)x[j] : -INFINITY;
+    for (uint32_t j = 0; j < VEC; ++j) to[j] = (float)x[j];
   }
 };
 
@@ -186,8 +186,9 @@ __device__ __attribute__((always_inline)) inline bool for_vectors(const T* row, 
 struct Draw {
   float temperature, top_p, most, per;
   uint32_t k;                // 0: all
-  double rate, floor_w;      // floor_w: least weight kept, of 1
+  double rate, rate64, top, floor_w;  // of a logit's distance: powers of two; floor_w: least weight kept, of 1
   bool greedy, few, border;  // few: all that is kept goes on the list; border: a step has to be found
+  bool endless;              // the greatest logit is infinite
 
   __device__ Draw(const SampleArgs& a, uint32_t row, float m, float lowest) {
     temperature = a.temperatures ? a.temperatures[row] : a.temperature;
@@ -201,29 +202,45 @@ struct Draw {
     floor_w = p > 0.0f ? (double)fminf(p, 1.0f) : 0.0;
     few = k && k <= kFew;
     border = k || top_p < 1.0f;
+    endless = most == INFINITY;
+    if (endless) most = 0.0f, lowest = 0.0f;
     const double far = fmin((double)most - (double)lowest, kSpan / rate);
-    per = far > 0.0 ? (float)((double)kSteps / far) : 0.0f;
+    per = far > 0.0 ? (float)fmin((double)kSteps / far, 0x1p120) : 0.0f;
+    top = (double)most, rate64 = rate * 64.0;
   }
-  // log2 of the weight; below -kSpan it is out
-  __device__ double power(float l) const { return l == most ? 0.0 : ((double)l - (double)most) * rate; }
-  __device__ bool weighs(float l) const { return power(l) >= -kSpan; }
+  // A logit; where the greatest is infinite, 0 for those that are, and -infinity.
+  __device__ float level(float l) const { return __builtin_expect(endless, 0) ? l == INFINITY ? 0.0f : -INFINITY : l; }
+  template <uint32_t VEC>
+  __device__ void levels(float (&v)[VEC]) const {
+    if (__builtin_amdgcn_readfirstlane(endless))
+#pragma unroll
+      for (uint32_t j = 0; j < VEC; ++j) v[j] = level(v[j]);
+  }
+  // 64 log2 of the weight of a level; below -64 kSpan (or NaN) it is out
+  __device__ double power(float x) const { return ((double)x - top) * rate64; }
+  __device__ static bool weighs(double z) { return z >= -64.0 * kSpan; }
   // the farther from the greatest, the later
-  __device__ uint32_t step(float l) const {
-    const float x = (most - l) * per;
-    return l == most ? 0u : x < (float)(kSteps - 1) ? (uint32_t)x : kSteps - 1;
+  __device__ uint32_t step(float x) const { return (uint32_t)fminf((most - x) * per, (float)(kSteps - 1)); }
+  // 2^(z / 64) in whole numbers of 1 / kOne, for z from -64 kSpan to 0; powers: kOne *
+  // 2^(i / 64), i = 0 .. 63
+  __device__ static u64 whole(double z, const double* powers) {
+    constexpr double c = kLn2 / 64.0;
+    const double t = z + 0x1.8p52;  // its last bits are z rounded to a whole number
+    const uint32_t n = (uint32_t)__builtin_bit_cast(u64, t);
+    const double x = z - (t - 0x1.8p52);
+    const double e = fma(x, fma(x, fma(x, fma(x, c * c * c * c / 24, c * c * c / 6), c * c / 2), c), 1.0);
+    const u64 power = __builtin_bit_cast(u64, powers[n & 63]) + ((u64)((n & ~63u) << 14) << 32);  // times 2^(n >> 6)
+    const double w = fma(__builtin_bit_cast(double, power), e, 0x1p52);
+    return __builtin_bit_cast(u64, w) - 0x4330000000000000ull;
   }
-  // 2^y in whole numbers of 1 / kOne, for y from -kSpan to 0; powers: 2^(i / 64), i = 0 .. 63
-  __device__ static u64 whole(double y, const double* powers) {
-    const double z = y * 64.0, t = z + 0x1.8p52;  // t's last bits are z rounded to a whole number
-    const int n = (int)(uint32_t)__builtin_bit_cast(u64, t);
-    const double x = (z - (t - 0x1.8p52)) * (kLn2 / 64.0);
-    const double e = fma(x, fma(x, fma(x, fma(x, 1.0 / 24, 1.0 / 6), 0.5), 1.0), 1.0);
-    const double w = ldexp(powers[n & 63] * e, (n >> 6) + 43);
-    return __builtin_bit_cast(u64, w + 0x1p52) - 0x4330000000000000ull;
-  }
-  // whether min_p keeps a logit
-  __device__ bool heavy(float l) const { return floor_w == 0.0 || l == most || exp2(power(l)) >= floor_w; }
+  // whether min_p keeps a weight
+  __device__ bool heavy(double z) const { return floor_w == 0.0 || z == 0.0 || exp2(z / 64.0) >= floor_w; }
 };
+
+// The table of whole(), by a block of 64 threads or more.
+__device__ inline void fill_powers(double* powers) {
+  if (threadIdx.x < 64) powers[threadIdx.x] = kOne * exp2((double)threadIdx.x / 64.0);
+}
 
 // The slice's greatest and least logits. Bound by HBM: this is the pass that brings
 // the logits into the caches.
@@ -246,7 +263,7 @@ __global__ void __launch_bounds__(kThreads) top_kernel(SampleArgs a) {
 #pragma unroll
     for (uint32_t j = 0; j < VEC; ++j) {
       if (v[j] > most) most = v[j], first = at + j;
-      lowest = fminf(lowest, v[j] > -INFINITY ? v[j] : INFINITY);
+      lowest = fminf(lowest, v[j] > -INFINITY ? v[j] : INFINITY);  // NaN is neither
     }
     return false;
   });
@@ -334,38 +351,59 @@ __device__ inline uint32_t find_first(const u64 (&v)[N], Reached reached, u64& b
   return at;
 }
 
-// The steps between which a row's border is, from its histogram.
-__device__ inline void place_border(const Draw& d, RowWork& w) {
+// The steps between which a row's border is, from its histogram. below: LDS for the
+// sums of the steps before each, of weights and of logits.
+__device__ inline void place_border(const Draw& d, RowWork& w, u64 (&below)[2][kSteps + 1]) {
   constexpr uint32_t N = kSteps / kThreads;
-  const uint32_t tid = threadIdx.x;
-  u64 mass[N], count[N], c = 0, m = 0;
+  __shared__ u64 s_wave[2][kWaves];
+  __shared__ uint32_t s_at[3];
+  const uint32_t tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  u64 v[2][N], sum[2] = {0, 0};
 #pragma unroll
   for (uint32_t i = 0; i < N; ++i) {
-    mass[i] = d.few ? 0 : take(&w.mass[N * tid + i]), count[i] = d.k ? take(&w.count[N * tid + i]) : 0;
-    c += count[i], m += mass[i];
+    v[0][i] = d.few ? 0 : take(&w.mass[N * tid + i]), v[1][i] = d.k ? take(&w.count[N * tid + i]) : 0;
+    sum[0] += v[0][i], sum[1] += v[1][i];
   }
-  const auto below = [&](const u64 (&v)[N], uint32_t step) {
-    u64 sum = 0;
 #pragma unroll
-    for (uint32_t i = 0; i < N; ++i) sum += N * tid + i < step ? v[i] : 0;
-    return add_block<kWaves>(sum);
+  for (uint32_t x = 0; x < 2; ++x) {
+    const u64 upto = scan_wave(sum[x]);
+    if (tid % 64 == 63) s_wave[x][wave] = upto;
+    sum[x] = upto - sum[x];
+  }
+  __syncthreads();
+#pragma unroll
+  for (uint32_t x = 0; x < 2; ++x) {
+    for (uint32_t i = 0; i < wave; ++i) sum[x] += s_wave[x][i];
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i) below[x][N * tid + i] = sum[x], sum[x] += v[x][i];
+    if (tid == kThreads - 1) below[x][kSteps] = sum[x];
+  }
+  __syncthreads();
+  // the first step at which the running sum reaches a goal that the whole sum reaches
+  const auto find = [&](uint32_t x, uint32_t to, auto reached) {
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i)
+      if (!reached(below[x][N * tid + i]) && reached(below[x][N * tid + i + 1])) s_at[to] = N * tid + i;
   };
-  c = add_block<kWaves>(c), m = add_block<kWaves>(m);
-  uint32_t lo = kSteps, hi = kSteps, at_k = kSteps;
-  bool by_count = d.k && c > d.k, by_mass = d.top_p < 1.0f;
-  u64 least = m, most = m, before;  // that what top_k keeps weighs
+  bool by_count = d.k && below[1][kSteps] > d.k, by_mass = d.top_p < 1.0f;
+  uint32_t at_k = kSteps, lo = kSteps, hi = kSteps;
   if (by_count) {
-    lo = hi = at_k = find_first<kWaves>(count, [&](u64 sum) { return sum >= d.k; }, before);
-    least = below(mass, at_k), most = below(mass, at_k + 1);
+    find(1, 0, [&](u64 n) { return n >= d.k; });
+    __syncthreads();
+    lo = hi = at_k = s_at[0];
   }
   if (d.few) {
     lo = 0;
     if (!by_count) hi = kSteps - 1;
   } else {
     if (by_mass) {
+      // what top_k keeps weighs this at least, and at most
+      const u64 least = below[0][at_k], most = below[0][min(at_k + 1, kSteps)];
       const double first = fmax((double)d.top_p * (double)least, 1.0), second = fmax((double)d.top_p * (double)most, 1.0);
-      lo = find_first<kWaves>(mass, [&](u64 sum) { return (double)sum >= first; }, before);
-      hi = find_first<kWaves>(mass, [&](u64 sum) { return (double)sum >= second; }, before);
+      find(0, 1, [&](u64 m) { return (double)m >= first; });
+      find(0, 2, [&](u64 m) { return (double)m >= second; });
+      __syncthreads();
+      lo = s_at[1], hi = s_at[2];
     }
     if (d.floor_w > 0.0) {
       // the step of the least weight that min_p keeps, or either of two
@@ -376,13 +414,12 @@ __device__ inline void place_border(const Draw& d, RowWork& w) {
       else lo = min(lo, near);
     }
   }
+  if (tid != 0) return;
   const bool apart = by_count && at_k > hi;  // top_k's step is not between lo and hi
   // (without a border of top_k's, all steps weigh what top_p goes by)
   const uint32_t from = apart ? at_k : by_count || d.few ? lo : kSteps;
-  const u64 count_from = by_count ? below(count, from) : 0, mass_from = below(mass, from), mass_lo = below(mass, lo);
-  if (tid != 0) return;
   w.lo = lo, w.hi = hi, w.other = apart ? at_k : lo, w.from = from, w.by_count = by_count, w.by_mass = by_mass;
-  w.count_from = count_from, w.mass_from = mass_from, w.mass_lo = mass_lo;
+  w.count_from = below[1][from], w.mass_from = below[0][from], w.mass_lo = below[0][lo];
 }
 
 // The slice's histogram, added to the row's. Bound by the weights' arithmetic, some
@@ -390,9 +427,10 @@ __device__ inline void place_border(const Draw& d, RowWork& w) {
 template <class T>
 __global__ void __launch_bounds__(kThreads) step_kernel(SampleArgs a) {
   constexpr uint32_t VEC = Logits<T>::VEC;
-  __shared__ u64 s_mass[kSteps];
+  __shared__ u64 s_below[2][kSteps + 1];
   __shared__ uint32_t s_count[kSteps];
   __shared__ double s_powers[64];
+  u64* s_mass = s_below[0];
   const uint32_t slice = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
   RowWork& w = a.of_row(row);
   float most, lowest;
@@ -400,33 +438,34 @@ __global__ void __launch_bounds__(kThreads) step_kernel(SampleArgs a) {
   if (most == -INFINITY) return;
   const Draw d(a, row, most, lowest);
   if (d.greedy) return;
-  if (tid < 64) s_powers[tid] = exp2((double)tid / 64.0);
+  fill_powers(s_powers);
   for (uint32_t i = tid; i < kSteps; i += kThreads) s_mass[i] = 0, s_count[i] = 0;
   __syncthreads();
   const T* logits = static_cast<const T*>(a.logits) + row * a.stride;
   const uint32_t begin = slice * a.slice, end = min(begin + a.slice, a.vocab);
   const auto each = [&](auto f) __attribute__((always_inline)) {
     for_vectors<T, kThreads * VEC>(logits, begin, end, tid * VEC,
-                                   [&](const float (&v)[VEC], uint32_t) __attribute__((always_inline)) {
+                                   [&](float (&v)[VEC], uint32_t) __attribute__((always_inline)) {
+      d.levels(v);
 #pragma unroll
       for (uint32_t j = 0; j < VEC; ++j) {
-        const double y = d.power(v[j]);
-        if (y >= -kSpan) f(v[j], y);
+        const double z = d.power(v[j]);
+        if (Draw::weighs(z)) f(v[j], z);
       }
       return false;
     });
   };
   if (d.few) {
-    each([&](float l, double) { atomicAdd(&s_count[d.step(l)], 1u); });
+    each([&](float x, double) { atomicAdd(&s_count[d.step(x)], 1u); });
   } else if (d.border) {
-    each([&](float l, double y) {
-      const uint32_t i = d.step(l);
-      atomicAdd(&s_mass[i], Draw::whole(y, s_powers));
+    each([&](float x, double z) {
+      const uint32_t i = d.step(x);
+      atomicAdd(&s_mass[i], Draw::whole(z, s_powers));
       if (d.k) atomicAdd(&s_count[i], 1u);
     });
   } else {
     u64 sum = 0;
-    each([&](float l, double y) { sum += d.heavy(l) ? Draw::whole(y, s_powers) : 0; });
+    each([&](float, double z) { sum += d.heavy(z) ? Draw::whole(z, s_powers) : 0; });
     sum = add_wave(sum);
     if (tid % 64 == 0) atomicAdd(&s_mass[0], sum);
     __syncthreads();
@@ -441,7 +480,7 @@ __global__ void __launch_bounds__(kThreads) step_kernel(SampleArgs a) {
     }
     if (s_count[i]) atomicAdd(&w.count[i], s_count[i]);
   }
-  if (last_of_row(a, w.arrived)) place_border(d, w);
+  if (last_of_row(a, w.arrived)) place_border(d, w, s_below);
 }
 
 struct EndLds {
@@ -451,27 +490,49 @@ struct EndLds {
   double powers[64];
   u64 wave[kEndWaves], total[kSlices], limit;
   ulonglong2 pair[kPairs];  // a logit's place, and its weight if its step is not past hi
-  uint32_t start[kSlices * kWaves], pick;
+  uint32_t start[kSlices * kWaves], pick, members;
 };
 
-// Where the running sum of weigh(logit), in the order of the logits, reaches a goal:
-// the rank of the last logit kept and how many of that rank are. `each` goes through
-// logits whose ranks have all bits from `top` on equal; `before` is the sum of those
-// ahead of them.
-struct Border {
-  uint32_t rank;
-  u64 need;
-};
-template <class Each, class Weigh, class Reached>
-__device__ inline Border find_border(EndLds& s, Each each, uint32_t top, uint32_t prefix, u64 before, Weigh weigh,
-                                     Reached reached) {
-  for (uint32_t shift = top; shift;) {
-    const uint32_t width = min(shift, 8u);
+// A logit's place in the order: falling logits, of equal ones the lowest index first.
+__device__ inline u64 place_of(float x, uint32_t i) { return (u64)rank_of(x) << 32 | i; }
+
+// The place of the last logit at which the running sum of weights, in the order of the
+// logits, does not reach a goal yet without it. `each` goes through logits whose ranks
+// have all bits from `top` on equal, f(level, index, weight); `before` is the sum of
+// those ahead of them. nth(rank, n): the index of the n-th logit of a rank.
+template <class Each, class Reached, class Nth>
+__device__ inline u64 find_border(EndLds& s, Each each, uint32_t top, uint32_t prefix, u64 before, Reached reached,
+                                  Nth nth) {
+  uint32_t shift = top;
+  while (true) {
+    // few enough of the prefix's logits are compared each with each
+    if (threadIdx.x == 0) s.members = 0;
+    __syncthreads();
+    each([&](float x, uint32_t i, u64 weight) __attribute__((always_inline)) {
+      if (shift < 32 && rank_of(x) >> shift != prefix) return;
+      const uint32_t at = atomicAdd(&s.members, 1u);
+      if (at < kPairs) s.pair[at] = {place_of(x, i), weight};
+    });
+    __syncthreads();
+    const uint32_t members = s.members;
+    if (members <= kPairs) {
+      if (threadIdx.x < members) {
+        const ulonglong2 mine = s.pair[threadIdx.x];
+        u64 ahead = before;
+        for (uint32_t i = 0; i < members; ++i) ahead += s.pair[i].x < mine.x ? s.pair[i].y : 0;
+        if (!reached(ahead) && reached(ahead + mine.y)) s.limit = mine.x;
+      }
+      __syncthreads();
+      return s.limit;
+    }
+    if (shift == 0) break;
+    const uint32_t width = min(shift, 9u);
+    static_assert(kEnd == 512, "a thread has a digit of 9 bits");
     s.bin[threadIdx.x] = 0;
     __syncthreads();
-    each([&](float l, auto i) __attribute__((always_inline)) {
-      const uint32_t x = rank_of(l);
-      if (shift == 32 || x >> shift == prefix) atomicAdd(&s.bin[x >> (shift - width) & ((1u << width) - 1)], weigh(l, i));
+    each([&](float x, uint32_t, u64 weight) __attribute__((always_inline)) {
+      const uint32_t r = rank_of(x);
+      if (shift == 32 || r >> shift == prefix) atomicAdd(&s.bin[r >> (shift - width) & ((1u << width) - 1)], weight);
     });
     __syncthreads();
     const u64 bin[1] = {s.bin[threadIdx.x]};
@@ -480,18 +541,19 @@ __device__ inline Border find_border(EndLds& s, Each each, uint32_t top, uint32_
     before += ahead, shift -= width;
     prefix = prefix << width | digit;
   }
-  u64 same = 0, sum = 0;
-  each([&](float l, auto i) __attribute__((always_inline)) {
-    if (rank_of(l) == prefix) ++same, sum += weigh(l, i);
+  // of equal ones, which weigh the same, as few as reach it
+  u64 sum = 0;
+  each([&](float x, uint32_t, u64 weight) __attribute__((always_inline)) {
+    if (rank_of(x) == prefix) sum += weight;
   });
-  same = add_block<kEndWaves>(same), sum = add_block<kEndWaves>(sum);
-  u64 low = 1, high = same;  // of equal ones, which weigh the same, as few as reach it
+  const u64 same = s.members, one = add_block<kEndWaves>(sum) / same;
+  u64 low = 1, high = same;
   while (low < high) {
     const u64 mid = (low + high) / 2;
-    if (reached(before + mid * (sum / same))) high = mid;
+    if (reached(before + mid * one)) high = mid;
     else low = mid + 1;
   }
-  return {prefix, low};
+  return (u64)prefix << 32 | nth(prefix, low);
 }
 
 // A stretch of a row by the whole block; each wave has a part of neighbours.
@@ -570,40 +632,41 @@ __device__ inline void end_row(const SampleArgs& a, const Draw& d, uint32_t row,
   if (threadIdx.x != 0) return;
   const float l = (float)logits[token];
   a.tokens[row] = (int32_t)token;
-  a.logprobs[row] = (float)(d.power(l) * kLn2 - log((double)total / kOne));
+  a.logprobs[row] = (float)(d.power(d.level(l)) * (kLn2 / 64.0) - log((double)total / kOne));
 }
-
-// A logit's place in the order: falling logits, of equal ones the lowest index first.
-__device__ inline u64 place_of(float l, uint32_t i) { return (u64)rank_of(l) << 32 | i; }
 
 // A row by one block, from its logits alone.
 template <class T>
 __device__ inline void slow_row(const SampleArgs& a, const Draw& d, uint32_t row, const T* logits, EndLds& s) {
   const Stretch<T> all(logits, 0, a.vocab);
   u64 limit = ~0ull;  // the last place kept
-  const auto in = [&](float l, uint32_t i) __attribute__((always_inline)) { return d.weighs(l) && place_of(l, i) <= limit; };
-  const auto mass = [&](float l) __attribute__((always_inline)) { return Draw::whole(d.power(l), s.powers); };
+  const auto mass = [&](float l, uint32_t i) __attribute__((always_inline)) -> u64 {
+    const float x = d.level(l);
+    const double z = d.power(x);
+    return Draw::weighs(z) && place_of(x, i) <= limit ? Draw::whole(z, s.powers) : 0;
+  };
   for (int stage = 0; stage < 2; ++stage) {  // top_k, top_p
     if (stage == 0 ? d.k == 0 : !(d.top_p < 1.0f)) continue;
-    const auto weigh = [&](float l, uint32_t) __attribute__((always_inline)) { return stage == 0 ? 1ull : mass(l); };
+    const auto each = [&](auto f) __attribute__((always_inline)) {
+      all.each([&](float l, uint32_t i) __attribute__((always_inline)) {
+        const u64 w = mass(l, i);
+        if (w) f(d.level(l), i, stage == 0 ? 1 : w);
+      });
+    };
     u64 n = 0;
-    all.each([&](float l, uint32_t i) __attribute__((always_inline)) { n += in(l, i) ? weigh(l, i) : 0; });
+    each([&](float, uint32_t, u64 w) __attribute__((always_inline)) { n += w; });
     n = add_block<kEndWaves>(n);
     if (stage == 0 && n <= d.k) continue;
     const double goal = stage == 0 ? (double)d.k : fmax((double)d.top_p * (double)n, 1.0);
-    const auto each = [&](auto f) __attribute__((always_inline)) {
-      all.each([&](float l, uint32_t i) __attribute__((always_inline)) {
-        if (in(l, i)) f(l, i);
+    limit = find_border(s, each, 32, 0, 0, [&](u64 sum) { return (double)sum >= goal; }, [&](uint32_t rank, u64 nth) {
+      return all.pick(s, nth - 1, [&](float l, uint32_t i) __attribute__((always_inline)) {
+        return (u64)(mass(l, i) && rank_of(d.level(l)) == rank);
       });
-    };
-    const Border b = find_border(s, each, 32, 0, 0, weigh, [&](u64 sum) { return (double)sum >= goal; });
-    const uint32_t i = all.pick(s, b.need - 1, [&](float l, uint32_t j) __attribute__((always_inline)) {
-      return (u64)(rank_of(l) == b.rank && in(l, j));
     });
-    limit = (u64)b.rank << 32 | i;
   }
   const auto weigh = [&](float l, uint32_t i) __attribute__((always_inline)) -> u64 {
-    return in(l, i) && d.heavy(l) ? mass(l) : 0;
+    const u64 w = mass(l, i);
+    return w && d.heavy(d.power(d.level(l))) ? w : 0;
   };
   u64 n = 0;
   all.each([&](float l, uint32_t i) __attribute__((always_inline)) { n += weigh(l, i); });
@@ -637,16 +700,17 @@ __global__ void __launch_bounds__(kThreads) list_kernel(SampleArgs a) {
   const uint32_t part = a.slice / kWaves, begin = min(slice * a.slice + wave * part, a.vocab);
   uint32_t listed = 0;
   for_vectors<T, 64 * VEC>(logits, begin, min(begin + part, a.vocab), lane * VEC,
-                           [&](const float (&v)[VEC], uint32_t at) __attribute__((always_inline)) {
+                           [&](float (&v)[VEC], uint32_t at) __attribute__((always_inline)) {
     uint32_t mine = 0;
+    d.levels(v);
 #pragma unroll
     for (uint32_t j = 0; j < VEC; ++j) {
-      const uint32_t x = d.step(v[j]);
-      mine |= (uint32_t)((x >= lo && x <= hi) || x == other) << j;
+      const uint32_t step = d.step(v[j]);
+      mine |= (uint32_t)((step >= lo && step <= hi) || step == other) << j;
     }
     if (!__any(mine != 0)) return false;
 #pragma unroll
-    for (uint32_t j = 0; j < VEC; ++j) mine &= ~((uint32_t)!d.weighs(v[j]) << j);
+    for (uint32_t j = 0; j < VEC; ++j) mine &= ~((uint32_t)!Draw::weighs(d.power(v[j])) << j);
     const uint32_t upto = scan_wave((uint32_t)__popc(mine));
     uint32_t to = listed + upto - __popc(mine);
 #pragma unroll
@@ -684,7 +748,7 @@ __global__ void __launch_bounds__(kEnd) end_kernel(SampleArgs a) {
     return;
   }
   const uint32_t lo = d.border ? w.lo : kSteps, hi = d.border ? w.hi : kSteps;
-  if (tid < 64) s.powers[tid] = exp2((double)tid / 64.0);
+  fill_powers(s.powers);
   uint32_t n = 0;
   if (lo < kSteps) {
     static_assert(kSlices * kWaves <= kEnd, "a thread has a wave's list");
@@ -781,33 +845,33 @@ __global__ void __launch_bounds__(kEnd) end_kernel(SampleArgs a) {
     const auto shorten = [&](auto of, auto weigh, u64 before, double to) __attribute__((always_inline)) {
       const auto some = [&](auto f) __attribute__((always_inline)) {
         each([&](uint32_t i) {
-          if (of(i)) f(s.logit[i], i);
+          if (of(i)) f(s.logit[i], s.index[i], weigh(i));
         });
       };
-      const Border b = find_border(s, some, top, top == 32 ? 0 : low >> top, before, weigh,
-                                   [&](u64 sum) { return (double)sum >= to; });
-      u64 same = 0, all;
-      some([&](float l, uint32_t) { same += rank_of(l) == b.rank; });
-      u64 nth = scan_block<kEndWaves>(same, all);
-      some([&](float l, uint32_t i) {
-        if (rank_of(l) == b.rank && ++nth == b.need) s.limit = place_of(l, s.index[i]);
-      });
-      __syncthreads();
-      limit = s.limit;
+      const auto nth = [&](uint32_t rank, u64 which) {
+        u64 same = 0, all;
+        some([&](float x, uint32_t, u64) { same += rank_of(x) == rank; });
+        u64 at = scan_block<kEndWaves>(same, all);
+        some([&](float x, uint32_t i, u64) {
+          if (rank_of(x) == rank && ++at == which) s.pick = i;
+        });
+        __syncthreads();
+        return s.pick;
+      };
+      limit = find_border(s, some, top, top == 32 ? 0 : low >> top, before, [&](u64 sum) { return (double)sum >= to; }, nth);
       narrow([&](uint32_t i) { return place_of(s.logit[i], s.index[i]) <= limit; });
+      __syncthreads();
     };
     if (by_count)
-      shorten([&](uint32_t i) { return d.step(s.logit[i]) >= from; }, [](float, uint32_t) { return 1ull; }, w.count_from,
-              (double)d.k);
+      shorten([&](uint32_t i) { return d.step(s.logit[i]) >= from; }, [](uint32_t) { return 1ull; }, w.count_from, (double)d.k);
     if (by_mass) {
       u64 sum = 0;
       each([&](uint32_t i) { sum += d.step(s.logit[i]) >= from ? s.weight[i] : 0; });
       const double goal = fmax((double)d.top_p * (double)(w.mass_from + add_block<kEndWaves>(sum)), 1.0);
-      shorten([&](uint32_t i) { return d.step(s.logit[i]) <= hi; }, [&](float, uint32_t i) { return s.weight[i]; }, w.mass_lo,
-              goal);
+      shorten([&](uint32_t i) { return d.step(s.logit[i]) <= hi; }, [&](uint32_t i) { return s.weight[i]; }, w.mass_lo, goal);
     }
   }
-  if (d.floor_w > 0.0) narrow([&](uint32_t i) { return d.heavy(s.logit[i]); });
+  if (d.floor_w > 0.0) narrow([&](uint32_t i) { return d.heavy(d.power(s.logit[i])); });
   const float u = a.uniforms[row];
   if (d.few) {  // the list is in the order of the indexes, and has all
     u64 total;
@@ -830,10 +894,12 @@ __global__ void __launch_bounds__(kEnd) end_kernel(SampleArgs a) {
   const u64 before = lane_of(upto - mine, in);
   const Stretch<T> there(logits, in * a.slice, min((in + 1) * a.slice, a.vocab));
   const uint32_t token = there.pick(s, target - before, [&](float l, uint32_t i) __attribute__((always_inline)) -> u64 {
-    if (!d.weighs(l)) return 0;
-    const uint32_t step = d.step(l);
-    const bool is = step < lo || (step <= hi && place_of(l, i) <= limit);
-    return is && d.heavy(l) ? Draw::whole(d.power(l), s.powers) : 0;
+    const float x = d.level(l);
+    const double z = d.power(x);
+    if (!Draw::weighs(z)) return 0;
+    const uint32_t step = d.step(x);
+    const bool is = step < lo || (step <= hi && place_of(x, i) <= limit);
+    return is && d.heavy(z) ? Draw::whole(z, s.powers) : 0;
   });
   end_row(a, d, row, logits, token, total);
 }
