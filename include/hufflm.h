@@ -565,8 +565,8 @@ hl_status hl_prefix_attention4(const hl_attention* attention, const void* q_dev,
  * written). The codes multiply x exactly and sums are float32, in a fixed order;
  * scales and bases multiply a group's sums in float32. A row with an infinite or
  * NaN scale or base has no finite y. codes_dev and x_dev are 16-byte aligned, the
- * others to their elements. Errors: HL_EINVAL (also for a misaligned pointer),
- * HL_EUNSUPPORTED for sizes past 32-bit counts. */
+ * others 4-byte. Errors: HL_EINVAL (also for a misaligned pointer),
+ * HL_EUNSUPPORTED for cols of 2^24 and above and rows past 32-bit counts. */
 hl_status hl_gemv4(const uint8_t* codes_dev, const void* scales_dev, const void* bases_dev, hl_dtype scale_dtype,
                    uint64_t rows, uint64_t cols, uint32_t group, const void* x_dev, hl_dtype x_dtype, uint32_t batch,
                    float* y_dev, void* stream);

@@ -100,12 +100,12 @@ def test_attention_buffers(L):
 
 @pytest.mark.parametrize("bad,status", [
     (dict(codes=None), hl.HL_EINVAL), (dict(codes=A + 8), hl.HL_EINVAL), (dict(scales=None), hl.HL_EINVAL),
-    (dict(scales=A + 1), hl.HL_EINVAL), (dict(bases=A + 1), hl.HL_EINVAL), (dict(st=hl.HL_F32), hl.HL_EINVAL),
+    (dict(scales=A + 2), hl.HL_EINVAL), (dict(bases=A + 2), hl.HL_EINVAL), (dict(st=hl.HL_F32), hl.HL_EINVAL),
     (dict(rows=0), hl.HL_EINVAL), (dict(cols=0), hl.HL_EINVAL), (dict(cols=320), hl.HL_EINVAL), (dict(group=16), hl.HL_EINVAL),
     (dict(group=0), hl.HL_EINVAL), (dict(group=256, cols=512), hl.HL_EINVAL), (dict(x=None), hl.HL_EINVAL),
     (dict(x=A + 2), hl.HL_EINVAL), (dict(xt=hl.HL_F32), hl.HL_EINVAL), (dict(batch=0), hl.HL_EINVAL),
     (dict(batch=17), hl.HL_EINVAL), (dict(y=None), hl.HL_EINVAL), (dict(y=A + 2), hl.HL_EINVAL),
-    (dict(rows=1 << 31), hl.HL_EUNSUPPORTED), (dict(cols=1 << 31), hl.HL_EUNSUPPORTED)])
+    (dict(rows=1 << 31), hl.HL_EUNSUPPORTED), (dict(cols=1 << 24), hl.HL_EUNSUPPORTED)])
 def test_gemv(L, bad, status):
     good = dict(codes=A, scales=A, bases=A, st=hl.HL_BF16, rows=64, cols=384, group=128, x=A, xt=hl.HL_F16, batch=2, y=A)
     assert L.hl_gemv4(*{**good, **bad}.values(), None) == status
