@@ -96,22 +96,25 @@ __global__ void __launch_bounds__(kRowThreads) write4_kernel(WriteArgs a) {
 }
 
 struct ReadArgs {
-  const uint8_t* from;
-  void* out;
-  uint64_t seq, token, head;  // of the rows, in bytes
+  const uint8_t* from[2];
+  void* out[2];
+  uint64_t seq[2], token[2], head[2];  // of the rows, in bytes
+  const int32_t* lens;                 // null: all tokens are read
   uint32_t tokens, heads;
   uint64_t rows;
 };
 
-// Four lanes a group, 8 columns each. Bound by HBM.
+// Four lanes a group, 8 columns each; blockIdx.y: of one set of rows or the other.
+// Bound by HBM.
 template <class T, uint32_t G>
 __global__ void __launch_bounds__(kRowThreads) read4_kernel(ReadArgs a) {
   constexpr uint32_t LANES = 4 * G, ROWS = kRowThreads / LANES;
-  const uint32_t lane = threadIdx.x % LANES, nth = threadIdx.x / LANES;
+  const uint32_t lane = threadIdx.x % LANES, nth = threadIdx.x / LANES, set = blockIdx.y;
   const uint64_t row = (uint64_t)blockIdx.x * ROWS + nth;
   if (nth >= ROWS || row >= a.rows) return;
   const uint64_t token = row / a.heads, b = token / a.tokens, t = token % a.tokens;
-  const uint8_t* p = a.from + b * a.seq + t * a.token + row % a.heads * a.head;
+  if (a.lens && (int64_t)t >= (int64_t)a.lens[b]) return;
+  const uint8_t* p = a.from[set] + b * a.seq[set] + t * a.token[set] + row % a.heads * a.head[set];
   const uint32_t g = lane / 4, c = lane % 4;
   const uint32_t pair = reinterpret_cast<const uint32_t*>(p + 16 * G)[g];
   const float scale = __builtin_bit_cast(float, pair << 16), base = __builtin_bit_cast(float, pair & 0xFFFF0000u);
@@ -123,7 +126,7 @@ __global__ void __launch_bounds__(kRowThreads) read4_kernel(ReadArgs a) {
     x[2 * j] = (T)fmaf(scale, (float)(int)(codes & 15) - 8.0f, base);
     x[2 * j + 1] = (T)fmaf(scale, (float)(int)(codes >> 4) - 8.0f, base);
   }
-  *reinterpret_cast<T8*>(static_cast<T*>(a.out) + row * (32 * G) + 8 * lane) = x;
+  *reinterpret_cast<T8*>(static_cast<T*>(a.out[set]) + row * (32 * G) + 8 * lane) = x;
 }
 
 template <class F>
@@ -138,6 +141,31 @@ static hl_status with_groups(uint32_t groups, F f) {
     case 7: return f(std::integral_constant<uint32_t, 7>());
     default: return f(std::integral_constant<uint32_t, 8>());
   }
+}
+
+// The first `sets` sets of a.
+static hl_status read_rows(const ReadArgs& a, uint32_t sets, uint32_t dim, hl_dtype dtype, hipStream_t s) {
+  return with_groups(dim / 32, [&](auto g) {
+    constexpr uint32_t G = decltype(g)::value, rows = kRowThreads / (4 * G);
+    const dim3 grid((uint32_t)((a.rows + rows - 1) / rows), sets), block(kRowThreads);
+    return dtype == HL_F32    ? enqueue(read4_kernel<float, G>, grid, block, s, a)
+           : dtype == HL_BF16 ? enqueue(read4_kernel<__bf16, G>, grid, block, s, a)
+                              : enqueue(read4_kernel<_Float16, G>, grid, block, s, a);
+  });
+}
+
+hl_status read_cache4(const hl_kv& cache, uint32_t batch, uint32_t heads, uint32_t dim, const int32_t* lens_dev,
+                      void* k_out, void* v_out, hl_dtype dtype, hipStream_t s) {
+  ReadArgs a = {};
+  a.from[0] = static_cast<const uint8_t*>(cache.k_dev), a.from[1] = static_cast<const uint8_t*>(cache.v_dev);
+  a.out[0] = k_out, a.out[1] = v_out;
+  a.seq[0] = 2 * cache.k_seq, a.token[0] = 2 * cache.k_token, a.head[0] = 2 * cache.k_head;
+  a.seq[1] = 2 * cache.v_seq, a.token[1] = 2 * cache.v_token, a.head[1] = 2 * cache.v_head;
+  a.lens = lens_dev, a.tokens = (uint32_t)cache.tokens, a.heads = heads;
+  a.rows = (uint64_t)batch * cache.tokens * heads;
+  const uint64_t rows = kRowThreads / (dim / 8);
+  if (!grid_fits((a.rows + rows - 1) / rows, kRowThreads)) return HL_EUNSUPPORTED;
+  return read_rows(a, 2, dim, dtype, s);
 }
 
 }  // namespace hl
@@ -203,14 +231,8 @@ extern "C" hl_status hl_cache_read4(const void* rows_dev, uint64_t seq_stride, u
   const hl_status st = check_rows(batch, tokens, heads, dim);
   if (st != HL_OK) return st;
   ReadArgs a = {};
-  a.from = static_cast<const uint8_t*>(rows_dev), a.out = out_dev;
-  a.seq = seq_stride, a.token = token_stride, a.head = head_stride;
+  a.from[0] = static_cast<const uint8_t*>(rows_dev), a.out[0] = out_dev;
+  a.seq[0] = seq_stride, a.token[0] = token_stride, a.head[0] = head_stride;
   a.tokens = (uint32_t)tokens, a.heads = heads, a.rows = (uint64_t)batch * tokens * heads;
-  return with_groups(dim / 32, [&](auto g) {
-    constexpr uint32_t G = decltype(g)::value, rows = kRowThreads / (4 * G);
-    const dim3 grid((uint32_t)((a.rows + rows - 1) / rows)), block(kRowThreads);
-    return dtype == HL_F32    ? enqueue(read4_kernel<float, G>, grid, block, (hipStream_t)stream, a)
-           : dtype == HL_BF16 ? enqueue(read4_kernel<__bf16, G>, grid, block, (hipStream_t)stream, a)
-                              : enqueue(read4_kernel<_Float16, G>, grid, block, (hipStream_t)stream, a);
-  });
+  return read_rows(a, 1, dim, dtype, (hipStream_t)stream);
 }

@@ -4,7 +4,11 @@ Bounds of an output: one rounding to its type (u: 2^-8 for bf16, 2^-11 for float
 (r: 2^-8 of it; for a float16 output to two pieces, 2^-16), and meets code - 8: of sum |p scale (code - 8)|. A score is a
 float32 sum of products with 16 + code, less 24 times q's sum: it is off by at most e = (dim + 40) * 2^-24 * max sum |q|
 (40 scale + |base|) * the scores' scale, which moves a weight and the sum under it by at most a factor exp(e) each. The
-sums of weights times 16 + code (up to 31, less 24) and of the parts add at most 64 * 2^-24 of sum p (55 scale + |base|)."""
+sums of weights times 16 + code (up to 31, less 24) and of the parts add at most 64 * 2^-24 of sum p (55 scale + |base|).
+
+Calls of 512 rows and more a key head give keys and values back in q's type first: each is off by u of it, which moves a
+score by u * sum |q k| and an output by u * sum p |v|, and p itself is rounded to that type (u * sum p |v|; float16 weights
+below 2^-14 are spaced 2^-24, half of that for each key)."""
 import math
 
 import pytest
@@ -41,11 +45,11 @@ def reference(c, scale=None):
     kv_heads, share = some.shape[-2], heads // some.shape[-2]
     cap = c["k"].shape[1] if "k" in c else 0
     held = {x: parts(c[x], dim) for x in ("k", "v", "prefix_k", "prefix_v") if x in c}
-    out, steps, sums = (torch.zeros_like(q) for _ in range(3))
+    out, steps, sums, sizes = (torch.zeros_like(q) for _ in range(4))
     lse = torch.full((batch, queries, heads), -math.inf, dtype=torch.float64)
     weights = torch.zeros((batch, kv_heads, cap), dtype=torch.float64)
     none = (torch.zeros((0, dim), dtype=torch.float64),) * 3
-    most = 0.0
+    most = most_qk = 0.0
     for b in range(batch):
         n = min(max(int(c["lens"][b]), 0), cap) if cap else 0
         for h in range(kv_heads):
@@ -61,13 +65,15 @@ def reference(c, scale=None):
                 rows = q[b, i, at]
                 s = rows @ (kb + ks * (kc - 8)).T * scale
                 most = max(most, float((rows.abs() @ (40 * ks + kb.abs()).T).max()) * abs(scale))
+                most_qk = max(most_qk, float((rows.abs() @ (kb + ks * (kc - 8)).abs().T).max()) * abs(scale))
                 p = torch.softmax(s, 1)
+                sizes[b, i, at] = p @ (vb + vs * (vc - 8)).abs()
                 out[b, i, at] = p @ (vb + vs * (vc - 8))
                 steps[b, i, at] = p @ (vs * (vc - 8)).abs()
                 sums[b, i, at] = p @ (55 * vs + vb.abs())
                 lse[b, i, at] = torch.logsumexp(s, 1)
                 weights[b, h, :seen] += p[:, len(pk[0]):].sum(0)
-    return out, lse, weights, steps, sums, most
+    return out, lse, weights, steps, sums, most, sizes, most_qk
 
 
 def check(c, scale=None, **more):
@@ -79,9 +85,15 @@ def check(c, scale=None, **more):
         start = torch.rand((batch, c["k"].shape[2], c["k"].shape[1]), device="cuda")
         more = {**more, "weights": start.clone()}
     r = hl.prefix_attention4(**c, scale=scale, lse=lse, **more)
-    out, want_lse, weights, steps, sums, most = reference(c, scale)
+    out, want_lse, weights, steps, sums, most, sizes, most_qk = reference(c, scale)
     e = (dim + 40) * 2.0**-24 * most
     u = U[q.dtype]
+    share = heads // (c["k"] if "k" in c else c["prefix_k"]).shape[-2]
+    if queries * share >= 512 or ("prefix_k" in c and batch * queries * share >= 512):
+        e += u * most_qk
+        keys = (c["k"].shape[1] if "k" in c else 0) + (len(c["prefix_k"]) if "prefix_k" in c else 0)
+        steps = 2 * u / R[q.dtype] * sizes + (keys * 2.0**-25 * sizes.max() / R[q.dtype] if q.dtype == torch.float16 else 0.0)
+        sums = sums + 2 * sizes
     bound = u * out.abs() + (1 + u) * (R[q.dtype] * steps + (2 * e + 64 * 2.0**-24) * sums) + 2.0**-25
     got = r.out.double().cpu()
     assert ((got - out).abs() <= bound).all(), float(((got - out).abs() / bound).max())
@@ -104,6 +116,7 @@ SHAPES = [  # batch, queries, heads, kv_heads, dim, prefix, own
     (130, 1, 2, 1, 128, 17, 9), (2, 70, 4, 2, 256, 40, 90), (1, 1, 8, 8, 128, 3001, 0), (1, 1, 8, 8, 128, 0, 3001),
     (2, 7, 6, 3, 224, 260, 7), (1, 200, 4, 1, 128, 0, 200), (2, 1, 8, 2, 32, 1500, 700), (3, 2, 6, 2, 96, 1300, 400),
     (2, 1, 8, 4, 160, 1200, 90), (2, 1, 8, 4, 192, 1200, 90), (2, 1, 8, 4, 224, 1200, 90), (2, 1, 8, 4, 256, 1200, 90),
+    (3, 180, 3, 1, 64, 77, 200), (16, 16, 8, 2, 96, 130, 50), (2, 300, 2, 1, 256, 0, 350), (1, 600, 2, 2, 32, 50, 600),
     (1, 30, 4, 2, 32, 200, 100), (1, 30, 4, 2, 160, 200, 100), (1, 30, 4, 2, 192, 200, 100), (1, 30, 4, 2, 224, 200, 100)]
 
 
@@ -166,8 +179,8 @@ def nan_rows(t):
     t[...] = 0xFF  # codes 15, scales and bases NaN
 
 
-@pytest.mark.parametrize("queries", [1, 3, 20])
-@pytest.mark.parametrize("own", [90, 1300])
+@pytest.mark.parametrize("queries", [1, 3, 20, 130])
+@pytest.mark.parametrize("own", [140, 1300])
 @pytest.mark.parametrize("dim", [96, 128, 256])
 def test_unseen_rows_may_hold_anything(queries, own, dim):
     lens = [own - 1, own // 2, queries, 0]
@@ -179,10 +192,10 @@ def test_unseen_rows_may_hold_anything(queries, own, dim):
     assert torch.equal(clean.out, dirty.out)
 
 
-@pytest.mark.parametrize("queries", [4, 20])
+@pytest.mark.parametrize("queries", [4, 20, 256])
 def test_new_tokens_of_nan_reach_only_those_that_see_them(queries):
-    lens = [70, 64, queries]
-    c = make(torch.bfloat16, 3, queries, 4, 2, 128, 30, 70, lens=lens)
+    lens = [queries + 50, queries + 44, queries]
+    c = make(torch.bfloat16, 3, queries, 4, 2, 128, 30, queries + 50, lens=lens)
     clean = hl.prefix_attention4(**c).out
     for b, n in enumerate(lens):
         nan_rows(c["v"][b, n - 2:n])
