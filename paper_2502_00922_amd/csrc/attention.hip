@@ -978,7 +978,8 @@ static Kv kv_of(const hl_kv& s) {
   return k;
 }
 
-hl_status attention_plan(const hl_attention* h, bool weights, uint32_t most_tiles, AttentionPlan* pl) {
+hl_status attention_plan(const hl_attention* h, bool weights, bool four_bits, AttentionPlan* pl) {
+  const uint32_t most_tiles = four_bits ? 1 : 2;
   if (!h || h->batch == 0 || h->queries == 0 || h->heads == 0 || h->kv_heads == 0 || h->heads % h->kv_heads ||
       h->dim == 0 || h->dim % 8 || !(h->scale == h->scale) || (h->dtype != HL_BF16 && h->dtype != HL_F16))
     return HL_EINVAL;
@@ -995,6 +996,9 @@ hl_status attention_plan(const hl_attention* h, bool weights, uint32_t most_tile
   a.prefix = kv_of(h->prefix), a.own = kv_of(h->own);
   a.batch = h->batch, a.queries = h->queries, a.heads = h->heads, a.kv_heads = h->kv_heads, a.dim = h->dim;
   a.share = h->heads / h->kv_heads;
+  // (where memory bounds both, a unit is a unit; else the waves of a wide item have
+  // all of its keys each, and those of a narrow one share them)
+  a.wide_cost = four_bits ? kWaves : 1;
   a.scale2 = h->scale == 0.0f ? 1.0f : fabsf(h->scale) * kLog2e;
   a.q_and = h->scale == 0.0f ? 0 : ~0u, a.q_xor = h->scale < 0.0f ? 0x80008000u : 0;
   const uint64_t shared_rows = (uint64_t)h->batch * h->queries * a.share, own_rows = (uint64_t)h->queries * a.share;
@@ -1109,19 +1113,19 @@ using namespace hl;
 
 extern "C" size_t hl_attention_workspace_bytes(const hl_attention* attention, int with_weights) {
   AttentionPlan pl;
-  return attention_plan(attention, with_weights != 0, 2, &pl) == HL_OK ? pl.bytes : 0;
+  return attention_plan(attention, with_weights != 0, false, &pl) == HL_OK ? pl.bytes : 0;
 }
 
 hl_status hl::attention_setup(const hl_attention* attention, const void* q_dev, const int32_t* lens_dev, void* out_dev,
                               float* lse_dev, const float* weight_in_dev, float* weight_out_dev, void* workspace_dev,
-                              size_t workspace_bytes, uint32_t most_tiles, AttentionPlan* plan) {
+                              size_t workspace_bytes, bool four_bits, AttentionPlan* plan) {
   if (!attention || !q_dev || !out_dev || !workspace_dev || (weight_in_dev && !weight_out_dev)) return HL_EINVAL;
   if (attention->own.tokens && !lens_dev) return HL_EINVAL;
   if (!aligned(q_dev, 16) || !aligned(out_dev, 16) || !aligned(workspace_dev, 16) || !aligned(lens_dev, 4) ||
       !aligned(lse_dev, 4) || !aligned(weight_in_dev, 4) || !aligned(weight_out_dev, 4))
     return HL_EINVAL;
   AttentionPlan& pl = *plan;
-  const hl_status st = attention_plan(attention, weight_out_dev != nullptr, most_tiles, &pl);
+  const hl_status st = attention_plan(attention, weight_out_dev != nullptr, four_bits, &pl);
   if (st != HL_OK) return st;
   if (workspace_bytes < pl.bytes) return HL_EINVAL;
   AttentionArgs& a = pl.a;
@@ -1143,7 +1147,7 @@ extern "C" hl_status hl_prefix_attention(const hl_attention* attention, const vo
                                          void* stream) {
   AttentionPlan pl;
   const hl_status st = attention_setup(attention, q_dev, lens_dev, out_dev, lse_dev, weight_in_dev, weight_out_dev,
-                                       workspace_dev, workspace_bytes, 2, &pl);
+                                       workspace_dev, workspace_bytes, false, &pl);
   if (st != HL_OK) return st;
   return attention->dtype == HL_BF16 ? run_type<__bf16>(pl, (hipStream_t)stream)
                                      : run_type<_Float16>(pl, (hipStream_t)stream);

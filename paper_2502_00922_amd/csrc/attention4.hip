@@ -3,17 +3,18 @@
 // multiplies the codes themselves.
 //
 // A value is base + scale * (code - 8), with a pair (scale, base) for each 32
-// columns of a row. The matrix instruction's operand is 16 + code, which is exact
-// in bf16 and in f16 and takes one and-or of a nibble in place; what is 24 too
-// much of it is taken off again by sums of the other operand:
-//   q.k  = sum_g scale_g * (q.(16 + code) - 24 Q_g) + base_g * Q_g,  Q_g the sum of q's group
-//   o_d  = sum_j w_j (16 + code_jd) - 24 sum_j w_j + sum_j p_j base_jg,  w_j = p_j * scale_jg
-// with w rounded to 16 bits once and that same rounded w in both sums, so that its
-// error meets a centred code alone. For q.k the rows' pairs are a left operand as
-// they lie in memory: times (-24 Q_g, Q_g), split into three bf16 pieces that hold
-// every bit of the float32, they give the last two terms. Where the products leave
-// a key's scores, lane n of 16 has element n of the key's pairs, and an instruction
-// takes the one it needs from that lane.
+// columns of a row. The matrix instruction's operand is 16 + code (or 128, or 64),
+// which is exact in bf16 and in f16 and takes one and-or of a nibble in place; what is
+// too much of it, 8 as well, is taken off by products with constants:
+//   q.k = sum_g scale_g * (q.(16 + code) - 24 Q_g) + base_g * Q_g,  Q_g the sum of q's group
+//   o_d = sum_j w_j (16 + code_jd) - 24 w_j + p_j base_jg,          w_j = p_j * scale_jg
+// with w rounded to 16 bits once and the same w in both products, so that its error
+// meets a centred code alone. For q.k the rows' pairs are a left operand as they lie in
+// memory: times (-24 Q_g, Q_g), split into three bf16 pieces that hold every bit of the
+// float32, they give the last two terms, and times a one they put each key's scale
+// where the products leave its scores. For o, lane n of 16 has element n of a key's
+// pairs: an instruction takes the scale that it needs from that lane, and the eight
+// keys of a lane are a left operand whose rows are the elements, for the last term.
 #include "attention_core.h"
 #include "cache4.h"
 
@@ -24,39 +25,45 @@ constexpr int held4() { return G <= 2 ? 64 : G <= 4 ? 128 : 256; }  // columns o
 
 // A step's keys and values: lane n = lane % 16 of group c = lane / 16 has the
 // codes of 8 columns of each group of keys n and 16 + n and their pairs (of 8
-// groups, half of them), and of 8 more keys and their values (key_of) element n of
-// their pairs and the codes of 2 of the values' columns of each group.
+// groups, half of them), and of 8 values (key_of) element n of the pairs and the codes
+// of 2 columns of each group.
 template <int G>
 struct Tile4 {
   static constexpr int VW = (G + 3) / 4;
   uint32_t k[2][G];
   u32x4 kr[2];
   uint32_t v[8][VW];
-  uint16_t ke[8], ve[8];
+  uint32_t ve[8];
 };
 
 template <int G, int R>
 struct State4 {
   static constexpr int E = G > 4 ? 2 : 1;
-  u32x4 q[R][G], e[R][E];  // e: pieces of (-24 Q_g, Q_g)
-  f32x4 o[R][2 * G];       // of the products: o[2g + i][r] is column 32g + 8c + 2r + i
-  f32x4 s[R][G];           // sum of w, in every element
-  float mean[R][G];        // this lane's part of the sum of p * base
+  u32x4 q[R][G], e[R][E];  // e: pieces of (minus what is too much of q's sums, Q_g)
+  f32x4 o[R][2 * G];       // o[2g + i][r] is column 32g + 8c + 2r + i
+  f32x4 base[R];           // sums of p times the pairs' element 4c + r
+  float mean[R][G];        // this lane's part of the sum of p * base, of steps with hidden keys
   float m[R], l[R], limit[R];
   uint32_t seen[R];
 };
 
+// Codes as operands, from the low bytes of two halves: even columns' in a byte's low
+// half, odd ones' in the high one. bf16: 128 + code, 16 + code; f16: 16 and 64. The
+// masks are in scalar registers and the exponents in vector ones, so that one
+// instruction takes both.
 template <class T>
-__device__ inline uint32_t low4(uint32_t pair) {
-  if constexpr (std::is_same<T, __bf16>::value) return ((pair << 3) & 0x00780078u) | 0x41804180u;
-  return ((pair << 6) & 0x03C003C0u) | 0x4C004C00u;
-}
-
-template <class T>
-__device__ inline uint32_t high4(uint32_t pair) {
-  if constexpr (std::is_same<T, __bf16>::value) return ((pair >> 1) & 0x00780078u) | 0x41804180u;
-  return ((pair << 2) & 0x03C003C0u) | 0x4C004C00u;
-}
+struct Codes4 {
+  static constexpr bool BF = std::is_same<T, __bf16>::value;
+  static constexpr float LOW = BF ? 136.0f : 24.0f, HIGH = BF ? 24.0f : 72.0f;  // with 8 too much
+  uint32_t low_mask, high_mask, low_one, high_one;
+  __device__ Codes4() {
+    low_mask = BF ? 0x000F000Fu : 0x03C003C0u, high_mask = BF ? 0x00780078u : 0x00F000F0u;
+    low_one = BF ? 0x43004300u : 0x4C004C00u, high_one = BF ? 0x41804180u : 0x54005400u;
+    asm volatile("" : "+s"(low_mask), "+s"(high_mask), "+v"(low_one), "+v"(high_one));
+  }
+  __device__ uint32_t low(uint32_t pair) const { return ((BF ? pair : pair << 6) & low_mask) | low_one; }
+  __device__ uint32_t high(uint32_t pair) const { return ((BF ? pair >> 1 : pair) & high_mask) | high_one; }
+};
 
 // Bytes i and j (counted from the first word's) of words w as the low bytes of
 // two halves.
@@ -94,8 +101,7 @@ __device__ inline void load4(Tile4<G>& t, const Item& it, uint32_t key) {
   for (int e = 0; e < 8; ++e) {
     const uint32_t nth = LAST ? min(key_of(c, e), left) : key_of(c, e), at = 16 * G + min(n, 2 * G - 1) * 2;
     fetch<4 * Tile4<G>::VW, G % 8 == 0 ? 8 : G % 4 == 0 ? 4 : G % 2 == 0 ? 2 : 1>(t.v[e], vp + (nth * vb + G * n));
-    fetch<2, 2>(&t.ve[e], vp + (nth * vb + at));
-    fetch<2, 2>(&t.ke[e], kp + (nth * kb + at));
+    t.ve[e] = *reinterpret_cast<const uint16_t*>(vp + (nth * vb + at));
   }
 }
 
@@ -105,8 +111,20 @@ __device__ inline float high_of(uint32_t pair) { return __builtin_bit_cast(float
 // x of lane N of each 16.
 template <int N>
 __device__ inline float from_lane(float x) {
-  const int i = __builtin_bit_cast(int, x);
-  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(i, i, 0x150 + N, 0xF, 0xF, true));
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x150 + N, 0xF, 0xF, true));
+}
+
+// p[e] times s[e] of lane N of each 16, in one instruction each: two wait states after
+// s and p have been written are what reading another lane takes.
+template <int N>
+__device__ inline void times_lane(float (&x)[8], const float (&s)[8], const float (&p)[8]) {
+#define HL_TIMES(o, i, j) "v_mul_f32_dpp %" o ", %" i ", %" j " row_newbcast:%24 row_mask:0xf bank_mask:0xf\n\t"
+  asm("s_nop 1\n\t" HL_TIMES("0", "8", "16") HL_TIMES("1", "9", "17") HL_TIMES("2", "10", "18") HL_TIMES("3", "11", "19")
+          HL_TIMES("4", "12", "20") HL_TIMES("5", "13", "21") HL_TIMES("6", "14", "22") HL_TIMES("7", "15", "23")
+      : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
+      : "v"(s[0]), "v"(s[1]), "v"(s[2]), "v"(s[3]), "v"(s[4]), "v"(s[5]), "v"(s[6]), "v"(s[7]), "v"(p[0]), "v"(p[1]),
+        "v"(p[2]), "v"(p[3]), "v"(p[4]), "v"(p[5]), "v"(p[6]), "v"(p[7]), "n"(N));
+#undef HL_TIMES
 }
 
 // f(0) .. f(N - 1), with the number known to the compiler.
@@ -128,8 +146,8 @@ __device__ inline void keep(const u32x4 (&v)[N]) {
 // One step: scores of 32 keys, their weights, and the weighted values. EDGE:
 // some query may not see some of the keys, whatever their rows hold.
 template <class T, int G, int R, bool EDGE>
-__device__ inline void step4(State4<G, R>& st, const Tile4<G>& t, const AttentionArgs& a, const Item& it, uint32_t key,
-                             uint32_t wave_row) {
+__device__ inline void step4(State4<G, R>& st, const Tile4<G>& t, const Codes4<T>& kf, const Codes4<__bf16>& vf,
+                             const AttentionArgs& a, const Item& it, uint32_t key, uint32_t wave_row) {
   using S = State4<G, R>;
   const uint32_t lane = lane_id(), n = lane % 16, c = lane / 16;
   const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -140,21 +158,24 @@ __device__ inline void step4(State4<G, R>& st, const Tile4<G>& t, const Attentio
     u32x4 pairs[1] = {t.kr[h]};
 #pragma unroll
     for (int g0 = 0; g0 < G; g0 += KSET) {
-      constexpr int most = KSET;
-      u32x4 codes[most];
+      u32x4 codes[KSET], one[KSET];
 #pragma unroll
-      for (int i = 0; i < most; ++i) {
+      for (int i = 0; i < KSET; ++i) {
         const int g = g0 + i < G ? g0 + i : G - 1;
         const uint32_t p01 = bytes(t.k[h], g, G + g), p23 = bytes(t.k[h], 2 * G + g, 3 * G + g);
-        codes[i] = u32x4{low4<T>(p01), high4<T>(p01), low4<T>(p23), high4<T>(p23)};
+        codes[i] = u32x4{kf.low(p01), kf.high(p01), kf.low(p23), kf.high(p23)};
+        one[i] = u32x4{0, 0, 0, 0};
+        one[i][g % 4] = c == (uint32_t)(g / 4) ? 0x3F80u : 0;
         asm volatile("" : "+v"(codes[i]));
       }
       __builtin_amdgcn_sched_barrier(0);
-      f32x4 part[R][most];
+      f32x4 part[R][KSET], scale[KSET];
 #pragma unroll
-      for (int i = 0; i < most; ++i)
+      for (int i = 0; i < KSET; ++i) {
+        scale[i] = mfma<__bf16>(pairs[0], one[i], zero);
 #pragma unroll
         for (int rt = 0; rt < R; ++rt) part[rt][i] = mfma<T>(codes[i], st.q[rt][g0 + i < G ? g0 + i : G - 1], zero);
+      }
       if (g0 == 0) {
 #pragma unroll
         for (int rt = 0; rt < R; ++rt) {
@@ -163,17 +184,15 @@ __device__ inline void step4(State4<G, R>& st, const Tile4<G>& t, const Attentio
         }
       }
       products_end();
-      keep(codes), keep(pairs);
-      each<G>([&](auto g) {
-        constexpr int N = decltype(g)::value;
-        if (N < g0 || N >= g0 + most) return;
+      keep(codes), keep(one), keep(pairs);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float scale = from_lane<2 * N>(low_of(t.ke[4 * h + r]));
+      for (int i = 0; i < KSET; ++i)
+        if (g0 + i < G) {
 #pragma unroll
-          for (int rt = 0; rt < R; ++rt) s[rt][h][r] = fmaf(scale, part[rt][N - g0 < most ? N - g0 : 0][r], s[rt][h][r]);
+          for (int rt = 0; rt < R; ++rt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[rt][h][r] = fmaf(scale[i][r], part[rt][i][r], s[rt][h][r]);
         }
-      });
     }
   }
   float p[R][8];
@@ -210,8 +229,9 @@ __device__ inline void step4(State4<G, R>& st, const Tile4<G>& t, const Attentio
         st.l[rt] *= f;
 #pragma unroll
         for (int i = 0; i < 2 * G; ++i) st.o[rt][i] *= f;
+        st.base[rt] *= f;
 #pragma unroll
-        for (int g = 0; g < G; ++g) st.s[rt][g] *= f, st.mean[rt][g] *= f;
+        for (int g = 0; g < G; ++g) st.mean[rt][g] *= f;
       }
     }
 #pragma unroll
@@ -223,9 +243,34 @@ __device__ inline void step4(State4<G, R>& st, const Tile4<G>& t, const Attentio
   // w is rounded to bf16, whose range holds any scale. Where the output has 11
   // bits, what the rounding leaves is a second operand.
   constexpr int PIECES = std::is_same<T, __bf16>::value ? 1 : 2;
-  constexpr int SET = G % 2 || G > 4 ? 1 : 2;  // groups whose products follow each other
-  u32x4 ones[1] = {u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u}};
-  asm volatile("" : "+v"(ones[0]));
+  constexpr int SET = G % 2 || G > 3 ? 1 : 2;  // groups whose products follow each other
+  float scales[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) scales[e] = low_of(t.ve[e]);
+  // rounds eight numbers to operands
+  const auto round = [](u32x4* to, const float (&x)[8]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      to[0][j] = pack<__bf16>(x[2 * j], x[2 * j + 1]);
+      if constexpr (PIECES == 2) to[1][j] = pack<__bf16>(x[2 * j] - low_of(to[0][j]), x[2 * j + 1] - high_of(to[0][j]));
+    }
+#pragma unroll
+    for (int y = 0; y < PIECES; ++y) asm volatile("" : "+v"(to[y]));
+  };
+  // what is too much of the codes (136, 24), for even and odd columns
+  u32x4 less[2] = {u32x4{0xC308C308u, 0xC308C308u, 0xC308C308u, 0xC308C308u},
+                   u32x4{0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u}};
+  asm volatile("" : "+v"(less[0]), "+v"(less[1]));
+  // rows whose keys all queries see: p times the pairs' elements, for the bases
+  constexpr int BASES = EDGE ? 0 : 1;
+  u32x4 pairs[1], pw[R * PIECES];
+  if constexpr (!EDGE) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) pairs[0][j] = t.ve[2 * j] | t.ve[2 * j + 1] << 16;
+    asm volatile("" : "+v"(pairs[0]));
+#pragma unroll
+    for (int rt = 0; rt < R; ++rt) round(&pw[rt * PIECES], p[rt]);
+  }
   each<G / SET>([&](auto nth) {
     constexpr int g0 = decltype(nth)::value * SET;
     u32x4 codes[2 * SET], w[R * SET * PIECES];
@@ -235,30 +280,24 @@ __device__ inline void step4(State4<G, R>& st, const Tile4<G>& t, const Attentio
       for (int j = 0; j < 4; ++j) {
         const uint32_t both = __builtin_amdgcn_perm(t.v[2 * j + 1][g / 4], t.v[2 * j][g / 4],
                                                     0x0C000C00u | (uint32_t)(4 + g % 4) << 16 | (uint32_t)(g % 4));
-        codes[2 * i][j] = low4<__bf16>(both), codes[2 * i + 1][j] = high4<__bf16>(both);
+        codes[2 * i][j] = vf.low(both), codes[2 * i + 1][j] = vf.high(both);
       }
       asm volatile("" : "+v"(codes[2 * i]), "+v"(codes[2 * i + 1]));
 #pragma unroll
       for (int rt = 0; rt < R; ++rt) {
         float x[8];
+        times_lane<2 * g>(x, scales, p[rt]);
+        if constexpr (EDGE) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          // a row that the query does not see may hold anything
-          const bool sees = !EDGE || key + key_of(c, e) < st.seen[rt];
-          x[e] = p[rt][e] * from_lane<2 * g>(low_of(t.ve[e]));
-          const float b = fmaf(p[rt][e], from_lane<2 * g + 1>(low_of(t.ve[e])), st.mean[rt][g]);
-          if (EDGE) x[e] = sees ? x[e] : 0.0f;
-          st.mean[rt][g] = sees ? b : st.mean[rt][g];
+          for (int e = 0; e < 8; ++e) {
+            // a row that the query does not see may hold anything
+            const bool sees = key + key_of(c, e) < st.seen[rt];
+            const float b = fmaf(p[rt][e], from_lane<2 * g + 1>(scales[e]), st.mean[rt][g]);
+            x[e] = sees ? x[e] : 0.0f;
+            st.mean[rt][g] = sees ? b : st.mean[rt][g];
+          }
         }
-        u32x4* to = &w[(i * R + rt) * PIECES];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          to[0][j] = pack<__bf16>(x[2 * j], x[2 * j + 1]);
-          if constexpr (PIECES == 2)
-            to[1][j] = pack<__bf16>(x[2 * j] - low_of(to[0][j]), x[2 * j + 1] - high_of(to[0][j]));
-        }
-#pragma unroll
-        for (int y = 0; y < PIECES; ++y) asm volatile("" : "+v"(to[y]));
+        round(&w[(i * R + rt) * PIECES], x);
       }
     });
     __builtin_amdgcn_sched_barrier(0);
@@ -269,13 +308,19 @@ __device__ inline void step4(State4<G, R>& st, const Tile4<G>& t, const Attentio
 #pragma unroll
         for (int y = 0; y < PIECES; ++y) {
           const u32x4 x = w[(i * R + rt) * PIECES + y];
-          const int g = g0 + i;
-          st.o[rt][2 * g] = mfma<__bf16>(codes[2 * i], x, st.o[rt][2 * g]);
-          st.o[rt][2 * g + 1] = mfma<__bf16>(codes[2 * i + 1], x, st.o[rt][2 * g + 1]);
-          st.s[rt][g] = mfma<__bf16>(ones[0], x, st.s[rt][g]);
+          f32x4 &even = st.o[rt][2 * (g0 + i)], &odd = st.o[rt][2 * (g0 + i) + 1];
+          even = mfma<__bf16>(codes[2 * i], x, even), odd = mfma<__bf16>(codes[2 * i + 1], x, odd);
+          even = mfma<__bf16>(less[0], x, even), odd = mfma<__bf16>(less[1], x, odd);
         }
+    if constexpr (g0 == 0 && BASES) {
+#pragma unroll
+      for (int rt = 0; rt < R; ++rt)
+#pragma unroll
+        for (int y = 0; y < PIECES; ++y) st.base[rt] = mfma<__bf16>(pairs[0], pw[rt * PIECES + y], st.base[rt]);
+    }
     products_end();
-    keep(codes), keep(w), keep(ones);
+    keep(codes), keep(w), keep(less);
+    if constexpr (g0 == 0 && BASES) keep(pairs), keep(pw);
   });
 }
 
@@ -291,20 +336,22 @@ __device__ inline void begin4(State4<G, R>& st, const AttentionArgs& a, const It
     const uint32_t row = min(wave_row + 16 * rt + n, it.rows - 1), tok = row / a.share;
     st.seen[rt] = seen_by(a, it, row);
     const uint16_t* q = it.q + ((uint64_t)tok * a.heads + row % a.share) * (32 * G);
-    float sum[G];
+    float sum[G], less[G];
+    st.base[rt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      st.o[rt][2 * g] = st.o[rt][2 * g + 1] = st.s[rt][g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      st.o[rt][2 * g] = st.o[rt][2 * g + 1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
       st.mean[rt][g] = 0.0f;
       const u32x4 x = (*reinterpret_cast<const u32x4*>(q + 32 * g + 8 * c) & a.q_and) ^ a.q_xor;
-      float part = 0.0f;
+      float even = 0.0f, odd = 0.0f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const uint32_t two = x[j];  // an element itself is not what a bit cast takes
         const pair y = __builtin_bit_cast(pair, two);
-        part += (float)y[0] + (float)y[1];
+        even += (float)y[0], odd += (float)y[1];
       }
-      sum[g] = over_lanes(part);
+      even = over_lanes(even), odd = over_lanes(odd);
+      sum[g] = even + odd, less[g] = -fmaf(Codes4<T>::LOW, even, Codes4<T>::HIGH * odd);
       // the order in which a pair of bytes gives its codes
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -320,59 +367,71 @@ __device__ inline void begin4(State4<G, R>& st, const AttentionArgs& a, const It
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const uint32_t part = S::E == 1 ? c : 2 * e + c / 2;
-        float x = j < G ? sum[j < G ? j : 0] : 0.0f;
-        if constexpr (S::E == 2) {
-          float y = 4 + j < G ? sum[4 + j < G ? 4 + j : 0] : 0.0f;
-          asm volatile("" : "+v"(x), "+v"(y));  // two registers, no array in memory
-          x = c % 2 ? y : x;
-        }
-        st.e[rt][e][j] = pack<__bf16>(piece(-24.0f * x, part), piece(x, part));
+        const auto of = [&](const float (&v)[G]) {
+          float x = j < G ? v[j < G ? j : 0] : 0.0f;
+          if constexpr (S::E == 2) {
+            float y = 4 + j < G ? v[4 + j < G ? 4 + j : 0] : 0.0f;
+            asm volatile("" : "+v"(x), "+v"(y));  // two registers, no array in memory
+            x = c % 2 ? y : x;
+          }
+          return piece(x, part);
+        };
+        st.e[rt][e][j] = pack<__bf16>(of(less), of(sum));
       }
   }
 }
 
 // A wave's share of an item's keys [.., k1) for its rows: 32 from `key` on, and
-// again every `stride`.
+// again every `stride`. Loads are a step ahead, and there are always as many of them
+// (at the end, of the last step again): waits count them.
 template <class T, int G, int R>
 __device__ inline void keys4(State4<G, R>& st, const AttentionArgs& a, const Item& it, uint32_t wave_row, uint32_t key,
                              uint32_t k1, uint32_t stride) {
+  const Codes4<T> kf;
+  const Codes4<__bf16> vf;
   const uint32_t all = seen_by(a, it, wave_row), most = seen_by(a, it, wave_row + 16 * R - 1), end = min(k1, most);
   const uint32_t whole = min(end, all);  // steps that end here or before hide no key
-  if constexpr (G > 4) {  // two steps' rows do not fit the registers
+  const auto run = [&](const Tile4<G>& t) __attribute__((always_inline)) {
+    step4<T, G, R, false>(st, t, kf, vf, a, it, key, wave_row);
+    key += stride;
+  };
+  if (key + kStep <= whole) {
+    const uint32_t last = key + (whole - kStep - key) / stride * stride;
+    if constexpr (G > 4) {  // several steps' rows do not fit the registers
 #pragma unroll 1
-    for (; key + kStep <= whole; key += stride) {
-      Tile4<G> t;
-      load4<G, false>(t, it, key);
-      step4<T, G, R, false>(st, t, a, it, key, wave_row);
-    }
-  } else if (key + kStep <= whole) {
-    Tile4<G> t;
-    load4<G, false>(t, it, key);
-    while (true) {
-      const bool more = key + stride + kStep <= whole;
-      Tile4<G> next;
-      if (more) load4<G, false>(next, it, key + stride);
-      step4<T, G, R, false>(st, t, a, it, key, wave_row);
-      key += stride;
-      if (!more) break;
-      t = next;
+      while (key <= last) {
+        Tile4<G> t;
+        load4<G, false>(t, it, key);
+        run(t);
+      }
+    } else {
+      Tile4<G> t0, t1;
+      load4<G, false>(t0, it, key);
+      while (true) {
+        load4<G, false>(t1, it, min(key + stride, last));
+        run(t0);
+        if (key > last) break;
+        load4<G, false>(t0, it, min(key + stride, last));
+        run(t1);
+        if (key > last) break;
+      }
     }
   }
 #pragma unroll 1
   for (; key < end; key += stride) {
     Tile4<G> t;
     load4<G, true>(t, it, key);
-    step4<T, G, R, true>(st, t, a, it, key, wave_row);
+    step4<T, G, R, true>(st, t, kf, vf, a, it, key, wave_row);
   }
 }
 
 // Columns 32g + 8c .. of a wave's query n, eight for each group: out(first column, four of them).
 template <int G, int R, class Out>
 __device__ inline void columns4(const State4<G, R>& st, int rt, Out out) {
-  const uint32_t c = lane_id() / 16;
+  const uint32_t n = lane_id() % 16, c = lane_id() / 16;
 #pragma unroll
   for (int g = 0; g < G; ++g) {
-    const float shift = fmaf(-24.0f, st.s[rt][g][0], over_lanes(st.mean[rt][g]));
+    const float shift = over_lanes(st.mean[rt][g]) + __shfl(st.base[rt][(2 * g + 1) % 4], (2 * g + 1) / 4 * 16 + n);
     const f32x4 x = st.o[rt][2 * g], y = st.o[rt][2 * g + 1];
     out(32 * g + 8 * c, f32x4{x[0] + shift, y[0] + shift, x[1] + shift, y[1] + shift});
     out(32 * g + 8 * c + 4, f32x4{x[2] + shift, y[2] + shift, x[3] + shift, y[3] + shift});
@@ -584,7 +643,7 @@ static hl_status wide_plan(const hl_attention& h, bool weights, uint64_t least, 
   w->shape = h;
   w->shape.prefix = whole(h.prefix), w->shape.own = whole(h.own);
   AttentionPlan pl;
-  const hl_status st = attention_plan(&w->shape, weights, 2, &pl);
+  const hl_status st = attention_plan(&w->shape, weights, false, &pl);
   if (st != HL_OK) return st;
   w->bytes = (pl.bytes + 255) / 256 * 256;
   uint64_t n = w->bytes;
@@ -605,7 +664,7 @@ extern "C" size_t hl_attention4_workspace_bytes(const hl_attention* attention, i
   AttentionPlan pl;
   Wide4 w;
   if (!attention || attention->dim % 32) return 0;
-  if (attention_plan(attention, with_weights != 0, 1, &pl) != HL_OK) return 0;
+  if (attention_plan(attention, with_weights != 0, true, &pl) != HL_OK) return 0;
   if (!many_rows(*attention)) return pl.bytes;
   return wide_plan(*attention, with_weights != 0, pl.bytes, &w) == HL_OK ? w.all : 0;
 }
@@ -618,7 +677,7 @@ extern "C" hl_status hl_prefix_attention4(const hl_attention* attention, const v
   const hipStream_t s = (hipStream_t)stream;
   AttentionPlan pl;
   hl_status st = attention_setup(attention, q_dev, lens_dev, out_dev, lse_dev, weight_in_dev, weight_out_dev,
-                                 workspace_dev, workspace_bytes, 1, &pl);
+                                 workspace_dev, workspace_bytes, true, &pl);
   if (st != HL_OK) return st;
   if (!many_rows(*attention))
     return attention->dtype == HL_BF16 ? run_groups4<__bf16>(pl, HL_BF16, s) : run_groups4<_Float16>(pl, HL_F16, s);

@@ -59,6 +59,7 @@ struct AttentionArgs {
   float *wide_o, *wide_ml, *narrow_o, *narrow_ml, *row_ml, *scores;  // workspace
   uint32_t batch, queries, heads, kv_heads, dim, share;  // share: query heads of a key head
   uint32_t blocks, wide_rows, narrow_rows, score_stride;  // rows: of a part's place in the workspace
+  uint32_t wide_cost;  // of a wide unit, in narrow ones
   Tiling tp, to;
   float scale2;  // |scale| * log2(e), or 1: scores are kept in powers of two
   uint32_t q_and, q_xor;  // on pairs of q: its sign is the scale's, and it is 0 where the scale is
@@ -155,7 +156,8 @@ __host__ __device__ inline Lines lines_of(const AttentionArgs& a, uint32_t own_u
   uint32_t w = 0;
   if (l.wide.total) {
     w = a.blocks;
-    if (l.narrow.total) w = (uint32_t)((uint64_t)a.blocks * l.wide.total / (l.wide.total + l.narrow.total));
+    const uint64_t cost = (uint64_t)l.wide.total * a.wide_cost;
+    if (l.narrow.total) w = (uint32_t)(a.blocks * cost / (cost + l.narrow.total));
     w = std::min(w, (l.wide.total + kLeastWide - 1) / kLeastWide);
     w = std::min((w + 7) / 8 * 8, a.blocks - (l.narrow.total ? 8 : 0));
     w = std::max(w, 8u);
@@ -306,15 +308,15 @@ struct AttentionPlan {
   uint64_t join_blocks;
 };
 
-// Checks a call's shape and plans it. most_tiles: 16-row tiles that a wave of a
-// wide item may have (1 or 2).
-hl_status attention_plan(const hl_attention* attention, bool weights, uint32_t most_tiles, AttentionPlan* plan);
+// Checks a call's shape and plans it, for keys and values in 16 or in 4 bits (whose
+// wide items have one 16-row tile a wave).
+hl_status attention_plan(const hl_attention* attention, bool weights, bool four_bits, AttentionPlan* plan);
 
 // Checks a call's arguments and plans it; fills the plan's arguments with the
 // buffers and the workspace's parts.
 hl_status attention_setup(const hl_attention* attention, const void* q_dev, const int32_t* lens_dev, void* out_dev,
                           float* lse_dev, const float* weight_in_dev, float* weight_out_dev, void* workspace_dev,
-                          size_t workspace_bytes, uint32_t most_tiles, AttentionPlan* plan);
+                          size_t workspace_bytes, bool four_bits, AttentionPlan* plan);
 
 // Adds the parts that a call's blocks have left, and then the keys' weights.
 hl_status attention_join(const AttentionPlan& plan, hl_dtype dtype, hipStream_t s);
