@@ -1,8 +1,8 @@
 """gemv4 against the product in 64 bits (MI355X).
 
-Bound: a group's sums of x (16 + code) and of x are float32, of up to 128 terms (134 roundings with those of the groups'
-scaling), and the groups and waves add one rounding each: (134 + groups + 8) * 2^-24 of sum |x| (40 |scale| + |base|),
-which bounds every partial sum (codes up to 31, less 24)."""
+Bound: a group's sums of x (16, 64 or 128 + code) and of x are float32, of up to 128 terms (134 roundings with those of
+the groups' scaling), and the groups and waves add one rounding each: (134 + groups + 8) * 2^-24 of sum |x| (279 |scale| +
+|base|), which bounds every partial sum (128 + code, up to 143, less 136; 64 + code less 72; 16 + code less 24)."""
 import pytest
 import torch
 
@@ -30,7 +30,7 @@ def reference(c):
     scale = wide(c["scales"])
     base = wide(c["bases"]) if c["bases"] is not None else torch.zeros_like(scale)
     x = c["x"].cpu().double()
-    return x @ (base + scale * (codes - 8)).T, x.abs() @ (40 * scale.abs() + base.abs()).T
+    return x @ (base + scale * (codes - 8)).T, x.abs() @ (279 * scale.abs() + base.abs()).T
 
 
 def check(c, **more):

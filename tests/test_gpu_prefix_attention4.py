@@ -1,10 +1,15 @@
 """prefix_attention4 against the definition in 64 bits on what the rows stand for (MI355X).
 
-Bounds of an output: one rounding to its type (u: 2^-8 for bf16, 2^-11 for float16); w = p * scale is rounded to bf16
-(r: 2^-8 of it; for a float16 output to two pieces, 2^-16), and meets code - 8: of sum |p scale (code - 8)|. A score is a
-float32 sum of products with 16 + code, less 24 times q's sum: it is off by at most e = (dim + 40) * 2^-24 * max sum |q|
-(40 scale + |base|) * the scores' scale, which moves a weight and the sum under it by at most a factor exp(e) each. The
-sums of weights times 16 + code (up to 31, less 24) and of the parts add at most 64 * 2^-24 of sum p (55 scale + |base|).
+Bounds of an output: one rounding to its type (u: 2^-8 for bf16, 2^-11 for float16); w = p * scale and p are rounded to
+bf16 (r: 2^-8 of them; for a float16 output to two pieces, 2^-16), and meet code - 8 and base: r of sum p (|scale (code -
+8)| + |base|). A score's products are with 16, 64 or 128 + code, less 24, 72 or 136 times q: a group's terms are at most
+|q| 279 scale, an instruction adds its 32 products with at most 32 roundings and what it adds them to with one, and the
+groups, the bases and the scores' scale take dim / 32 + 6 more. So a score is off by at most e = (39 + dim / 32) * 2^-24 *
+max sum |q| (279 scale + |base|) * the scores' scale, which moves a weight and the sum under it, and with them the value
+(8 scale + |base| at most), by a factor exp(e) each. The sums of w times 16 or 128 + code, less 24 or 136: those of a step
+meet 34 roundings of 279 w and later ones of what is left of them, 8 w at most, two a step of 24 steps a wave at most
+(the shapes below) and 8 of waves and parts: (34 * 279 + 56 * 8) w < 96 * 104 w. A base meets 33 + 24 + 8 < 96, and the
+sum of p as well.
 
 Calls of 512 rows and more a key head give keys and values back in q's type first: each is off by u of it, which moves a
 score by u * sum |q k| and an output by u * sum p |v|, and p itself is rounded to that type (u * sum p |v|; float16 weights
@@ -37,7 +42,8 @@ def make(dtype, batch, queries, heads, kv_heads, dim, prefix, own, lens=None, si
 
 
 def reference(c, scale=None):
-    """out, lse, own weights, and of the bounds above: sum |p scale (code - 8)|, sum p (55 scale + |base|) and e's size."""
+    """out, lse, own weights, and of the bounds above: sum p (|scale (code - 8)| + |base|), sum p (104 scale + |base|), e's
+    size, sum |p v|, the largest sum |q k| and sum p (8 scale + |base|)."""
     q = c["q"].double().cpu()
     batch, queries, heads, dim = q.shape
     scale = 1 / math.sqrt(dim) if scale is None else scale
@@ -45,7 +51,7 @@ def reference(c, scale=None):
     kv_heads, share = some.shape[-2], heads // some.shape[-2]
     cap = c["k"].shape[1] if "k" in c else 0
     held = {x: parts(c[x], dim) for x in ("k", "v", "prefix_k", "prefix_v") if x in c}
-    out, steps, sums, sizes = (torch.zeros_like(q) for _ in range(4))
+    out, steps, sums, sizes, near = (torch.zeros_like(q) for _ in range(5))
     lse = torch.full((batch, queries, heads), -math.inf, dtype=torch.float64)
     weights = torch.zeros((batch, kv_heads, cap), dtype=torch.float64)
     none = (torch.zeros((0, dim), dtype=torch.float64),) * 3
@@ -64,16 +70,17 @@ def reference(c, scale=None):
                 at = slice(h * share, (h + 1) * share)
                 rows = q[b, i, at]
                 s = rows @ (kb + ks * (kc - 8)).T * scale
-                most = max(most, float((rows.abs() @ (40 * ks + kb.abs()).T).max()) * abs(scale))
+                most = max(most, float((rows.abs() @ (279 * ks + kb.abs()).T).max()) * abs(scale))
                 most_qk = max(most_qk, float((rows.abs() @ (kb + ks * (kc - 8)).abs().T).max()) * abs(scale))
                 p = torch.softmax(s, 1)
                 sizes[b, i, at] = p @ (vb + vs * (vc - 8)).abs()
                 out[b, i, at] = p @ (vb + vs * (vc - 8))
-                steps[b, i, at] = p @ (vs * (vc - 8)).abs()
-                sums[b, i, at] = p @ (55 * vs + vb.abs())
+                steps[b, i, at] = p @ ((vs * (vc - 8)).abs() + vb.abs())
+                sums[b, i, at] = p @ (104 * vs + vb.abs())
+                near[b, i, at] = p @ (8 * vs + vb.abs())
                 lse[b, i, at] = torch.logsumexp(s, 1)
                 weights[b, h, :seen] += p[:, len(pk[0]):].sum(0)
-    return out, lse, weights, steps, sums, most, sizes, most_qk
+    return out, lse, weights, steps, sums, most, sizes, most_qk, near
 
 
 def check(c, scale=None, **more):
@@ -85,26 +92,26 @@ def check(c, scale=None, **more):
         start = torch.rand((batch, c["k"].shape[2], c["k"].shape[1]), device="cuda")
         more = {**more, "weights": start.clone()}
     r = hl.prefix_attention4(**c, scale=scale, lse=lse, **more)
-    out, want_lse, weights, steps, sums, most, sizes, most_qk = reference(c, scale)
-    e = (dim + 40) * 2.0**-24 * most
+    out, want_lse, weights, steps, sums, most, sizes, most_qk, near = reference(c, scale)
+    e = (39 + dim // 32) * 2.0**-24 * most
     u = U[q.dtype]
     share = heads // (c["k"] if "k" in c else c["prefix_k"]).shape[-2]
     if queries * share >= 512 or ("prefix_k" in c and batch * queries * share >= 512):
         e += u * most_qk
         keys = (c["k"].shape[1] if "k" in c else 0) + (len(c["prefix_k"]) if "prefix_k" in c else 0)
         steps = 2 * u / R[q.dtype] * sizes + (keys * 2.0**-25 * sizes.max() / R[q.dtype] if q.dtype == torch.float16 else 0.0)
-        sums = sums + 2 * sizes
-    bound = u * out.abs() + (1 + u) * (R[q.dtype] * steps + (2 * e + 64 * 2.0**-24) * sums) + 2.0**-25
+        near = near + sizes
+    bound = u * out.abs() + (1 + u) * (R[q.dtype] * steps + 2 * e * near + 96 * 2.0**-24 * sums) + 2.0**-25
     got = r.out.double().cpu()
     assert ((got - out).abs() <= bound).all(), float(((got - out).abs() / bound).max())
     empty = want_lse == -math.inf
     assert (got[empty] == 0).all() and (r.lse.double().cpu()[empty] == -math.inf).all()
     d = (r.lse.double().cpu() - want_lse)[~empty].abs()
-    assert (d <= e + 64 * 2.0**-24 + 4 * 2.0**-24 * want_lse[~empty].abs()).all()
+    assert (d <= e + 96 * 2.0**-24 + 4 * 2.0**-24 * want_lse[~empty].abs()).all()
     if start is not None:
         w = start.double().cpu() + weights
         err = (r.weights.double().cpu() - w).abs()
-        assert (err <= (2 * e + 80 * 2.0**-24) * weights + 2.0**-23 * w + 1e-12).all()
+        assert (err <= (2 * e + 96 * 2.0**-24) * weights + 2.0**-23 * w + 1e-12).all()
     return r
 
 
