@@ -996,8 +996,9 @@ hl_status attention_plan(const hl_attention* h, bool weights, bool four_bits, At
   a.prefix = kv_of(h->prefix), a.own = kv_of(h->own);
   a.batch = h->batch, a.queries = h->queries, a.heads = h->heads, a.kv_heads = h->kv_heads, a.dim = h->dim;
   a.share = h->heads / h->kv_heads;
-  // (where memory bounds both, a unit is a unit; else the waves of a wide item have
-  // all of its keys each, and those of a narrow one share them)
+  // (where memory bounds both, a unit is a unit; else the waves of a wide item have all of
+  // its keys each, and those of a narrow one share them: 16 sequences' tokens of 32 heads on
+  // 2048 shared and up to 16384 own keys 148 us with 1, 107 with 4)
   a.wide_cost = four_bits ? kWaves : 1;
   a.scale2 = h->scale == 0.0f ? 1.0f : fabsf(h->scale) * kLog2e;
   a.q_and = h->scale == 0.0f ? 0 : ~0u, a.q_xor = h->scale < 0.0f ? 0x80008000u : 0;
@@ -1021,6 +1022,9 @@ hl_status attention_plan(const hl_attention* h, bool weights, bool four_bits, At
   }
   const uint64_t narrow_units = prefix_units + own_units - wide_units;
   if (prefix_units + own_units >= (1ull << 31)) return HL_EUNSUPPORTED;
+  // (the queries, sums and part of a narrow item take as long as four units of 4 bits: 64
+  // sequences' tokens of 32 heads on 16384 shared and 64 own keys 167 us without, 77 with)
+  a.item_cost = four_bits ? 4 * (uint32_t)((a.tp.r ? 0 : prefix_items) + (a.to.r ? 0 : own_items)) : 0;
   const uint64_t asked = wide_units / kLeastWide + narrow_units + 15;
   a.blocks = (uint32_t)std::min<uint64_t>(most, std::max<uint64_t>(16, asked / 8 * 8));
   a.wide_rows = std::max(a.tp.r ? a.tp.rows() : 0, a.to.r ? a.to.rows() : 0);

@@ -613,12 +613,17 @@ static hl_status run_groups4(const AttentionPlan& pl, hl_dtype dtype, hipStream_
   }
 }
 
-// Rows of a key head, of the batch over the prefix or of a sequence over its own
-// cache, from which on the call's keys and values are first given back in 16 bits, in
-// the workspace. The 16-bit kernel takes a third of the time for a row and key, and
-// the way through memory costs as much as 400 rows save. 4 x 256 new tokens of 32
-// heads on 8 (4096 rows) on 4096 shared and 512 own keys: 125 us so, 355 without.
-constexpr uint64_t kManyRows = 512;
+// Rows that a key meets in the mean, from which on a call's keys and values are first
+// given back in 16 bits, in the workspace, and attended by the 16-bit kernels. The
+// prefix's keys meet the batch's rows of a key head, those of the own caches a
+// sequence's. The 16-bit kernel takes a third of the time for a row and key; the way
+// through memory costs what that saves on 200 to 250 rows. With 8 key heads of 128
+// columns, here and (in 16 bits): 192 rows on 4096, 16384 and 65536 keys 33, 60 and 185 us
+// (34, 64, 195); 256 rows 35, 80 and 230 (35, 67, 205); 512 rows 45, 133 and 426 (39, 83,
+// 266); 4 x 256 tokens of 32 heads on 4096 shared and 512 own keys 290 (139). 128
+// sequences' tokens of 32 heads, 512 rows on 8192 shared keys but 4 on 256 own ones each:
+// 90 (109).
+constexpr uint64_t kManyRows = 256;
 
 // A call by the 16-bit kernels: the same with the values' places in the workspace,
 // behind `bytes` of it that these kernels take.
@@ -628,8 +633,9 @@ struct Wide4 {
 };
 
 static bool many_rows(const hl_attention& h) {
-  const uint64_t own = (uint64_t)h.queries * (h.heads / h.kv_heads);
-  return (h.prefix.tokens && own * h.batch >= kManyRows) || (h.own.tokens && own >= kManyRows);
+  const double own = (double)h.queries * (h.heads / h.kv_heads), prefix_keys = (double)h.prefix.tokens;
+  const double own_keys = (double)h.own.tokens * h.batch;
+  return prefix_keys * own * h.batch + own_keys * own >= kManyRows * (prefix_keys + own_keys);
 }
 
 // least: bytes of workspace that the call has in any case.

@@ -11,9 +11,9 @@ meet 34 roundings of 279 w and later ones of what is left of them, 8 w at most, 
 (the shapes below) and 8 of waves and parts: (34 * 279 + 56 * 8) w < 96 * 104 w. A base meets 33 + 24 + 8 < 96, and the
 sum of p as well.
 
-Calls of 512 rows and more a key head give keys and values back in q's type first: each is off by u of it, which moves a
-score by u * sum |q k| and an output by u * sum p |v|, and p itself is rounded to that type (u * sum p |v|; float16 weights
-below 2^-14 are spaced 2^-24, half of that for each key)."""
+Calls whose keys meet 256 rows and more in the mean give keys and values back in q's type first: each is off by u of it,
+which moves a score by u * sum |q k| and an output by u * sum p |v|, and p itself is rounded to that type (u * sum p |v|;
+float16 weights below 2^-14 are spaced 2^-24, half of that for each key)."""
 import math
 
 import pytest
@@ -96,9 +96,10 @@ def check(c, scale=None, **more):
     e = (39 + dim // 32) * 2.0**-24 * most
     u = U[q.dtype]
     share = heads // (c["k"] if "k" in c else c["prefix_k"]).shape[-2]
-    if queries * share >= 512 or ("prefix_k" in c and batch * queries * share >= 512):
+    own, prefix = c["k"].shape[1] if "k" in c else 0, len(c["prefix_k"]) if "prefix_k" in c else 0
+    if queries * share * (prefix + own) * batch >= 256 * (prefix + own * batch):
         e += u * most_qk
-        keys = (c["k"].shape[1] if "k" in c else 0) + (len(c["prefix_k"]) if "prefix_k" in c else 0)
+        keys = own + prefix
         steps = 2 * u / R[q.dtype] * sizes + (keys * 2.0**-25 * sizes.max() / R[q.dtype] if q.dtype == torch.float16 else 0.0)
         near = near + sizes
     bound = u * out.abs() + (1 + u) * (R[q.dtype] * steps + 2 * e * near + 96 * 2.0**-24 * sums) + 2.0**-25
@@ -124,7 +125,8 @@ SHAPES = [  # batch, queries, heads, kv_heads, dim, prefix, own
     (2, 7, 6, 3, 224, 260, 7), (1, 200, 4, 1, 128, 0, 200), (2, 1, 8, 2, 32, 1500, 700), (3, 2, 6, 2, 96, 1300, 400),
     (2, 1, 8, 4, 160, 1200, 90), (2, 1, 8, 4, 192, 1200, 90), (2, 1, 8, 4, 224, 1200, 90), (2, 1, 8, 4, 256, 1200, 90),
     (3, 180, 3, 1, 64, 77, 200), (16, 16, 8, 2, 96, 130, 50), (2, 300, 2, 1, 256, 0, 350), (1, 600, 2, 2, 32, 50, 600),
-    (1, 30, 4, 2, 32, 200, 100), (1, 30, 4, 2, 160, 200, 100), (1, 30, 4, 2, 192, 200, 100), (1, 30, 4, 2, 224, 200, 100)]
+    (1, 30, 4, 2, 32, 200, 100), (1, 30, 4, 2, 160, 200, 100), (1, 30, 4, 2, 192, 200, 100), (1, 30, 4, 2, 224, 200, 100),
+    (300, 1, 4, 2, 64, 100, 19), (40, 4, 4, 1, 128, 500, 30), (1, 256, 1, 1, 64, 0, 256), (1, 255, 1, 1, 64, 0, 255)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
