@@ -1024,7 +1024,7 @@ hl_status attention_plan(const hl_attention* h, bool weights, bool four_bits, At
   if (prefix_units + own_units >= (1ull << 31)) return HL_EUNSUPPORTED;
   // (the queries, sums and part of a narrow item take as long as four units of 4 bits: 64
   // sequences' tokens of 32 heads on 16384 shared and 64 own keys 167 us without, 77 with)
-  a.item_cost = four_bits ? 4 * (uint32_t)((a.tp.r ? 0 : prefix_items) + (a.to.r ? 0 : own_items)) : 0;
+  a.item_cost = four_bits ? 4 : 0, a.narrow_items = (uint32_t)((a.tp.r ? 0 : prefix_items) + (a.to.r ? 0 : own_items));
   const uint64_t asked = wide_units / kLeastWide + narrow_units + 15;
   a.blocks = (uint32_t)std::min<uint64_t>(most, std::max<uint64_t>(16, asked / 8 * 8));
   a.wide_rows = std::max(a.tp.r ? a.tp.rows() : 0, a.to.r ? a.to.rows() : 0);

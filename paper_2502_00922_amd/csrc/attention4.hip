@@ -635,7 +635,8 @@ struct Wide4 {
 static bool many_rows(const hl_attention& h) {
   const double own = (double)h.queries * (h.heads / h.kv_heads), prefix_keys = (double)h.prefix.tokens;
   const double own_keys = (double)h.own.tokens * h.batch;
-  return prefix_keys * own * h.batch + own_keys * own >= kManyRows * (prefix_keys + own_keys);
+  const double keys = prefix_keys + own_keys;
+  return keys > 0 && prefix_keys * own * h.batch + own_keys * own >= kManyRows * keys;
 }
 
 // least: bytes of workspace that the call has in any case.

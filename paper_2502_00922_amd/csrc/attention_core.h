@@ -59,7 +59,8 @@ struct AttentionArgs {
   float *wide_o, *wide_ml, *narrow_o, *narrow_ml, *row_ml, *scores;  // workspace
   uint32_t batch, queries, heads, kv_heads, dim, share;  // share: query heads of a key head
   uint32_t blocks, wide_rows, narrow_rows, score_stride;  // rows: of a part's place in the workspace
-  uint32_t wide_cost, item_cost;  // of a wide unit, in narrow ones; of the narrow line's items beyond their units
+  uint32_t wide_cost, item_cost;  // of a wide unit and, beyond its units, of a narrow item, in narrow units
+  uint32_t narrow_items;          // most of them
   Tiling tp, to;
   float scale2;  // |scale| * log2(e), or 1: scores are kept in powers of two
   uint32_t q_and, q_xor;  // on pairs of q: its sign is the scale's, and it is 0 where the scale is
@@ -157,7 +158,7 @@ __host__ __device__ inline Lines lines_of(const AttentionArgs& a, uint32_t own_u
   if (l.wide.total) {
     w = a.blocks;
     const uint64_t cost = (uint64_t)l.wide.total * a.wide_cost;
-    const uint64_t rest = (uint64_t)l.narrow.total + std::min(a.item_cost, 4 * l.narrow.total);
+    const uint64_t rest = (uint64_t)l.narrow.total + a.item_cost * (uint64_t)std::min(a.narrow_items, l.narrow.total);
     if (l.narrow.total) w = (uint32_t)(a.blocks * cost / (cost + rest));
     w = std::min(w, (l.wide.total + kLeastWide - 1) / kLeastWide);
     w = std::min((w + 7) / 8 * 8, a.blocks - (l.narrow.total ? 8 : 0));

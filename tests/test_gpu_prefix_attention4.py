@@ -284,3 +284,40 @@ def test_far_tokens(queries):
         assert torch.equal(hl.prefix_attention4(c["q"], prefix_k=c["k"][0], prefix_v=c["v"][0]).out,
                            hl.prefix_attention4(c["q"], prefix_k=(far if name == "k" else c["k"])[0],
                                                 prefix_v=(far if name == "v" else c["v"])[0]).out)
+
+
+@pytest.mark.parametrize("queries", [1, 20, 300])
+@pytest.mark.parametrize("sets", ["prefix", "own", "both"])
+def test_no_keys(queries, sets):
+    # caches without room, prefixes without keys, alone and beside the other set
+    own = torch.empty((2, 0, 2, 48), dtype=torch.uint8, device="cuda")
+    empty = {"k": own, "v": own, "lens": torch.zeros(2, dtype=torch.int32, device="cuda")} if sets != "prefix" else {}
+    if sets != "own":
+        empty.update(prefix_k=own[0], prefix_v=own[0])
+    c = make(torch.bfloat16, 2, queries, 8, 2, 64, 0 if sets == "prefix" else 90, 90 if sets == "prefix" else 0)
+    lse = torch.zeros((2, queries, 8), device="cuda")
+    r = hl.prefix_attention4(c["q"], **empty, lse=lse, out=torch.ones_like(c["q"]))
+    assert (r.out == 0).all() and (lse == -math.inf).all()
+    assert torch.equal(hl.prefix_attention4(**{**empty, **c}).out, hl.prefix_attention4(**c).out)
+
+
+def test_many_rows_of_other_strides_and_replays():
+    # rows that are first given back in 16 bits, from caches that are views, in a graph
+    c = make(torch.float16, 3, 128, 8, 2, 96, 200, 150, lens=[150, 128, 0])
+    want = check(c)
+    wide = {x: torch.full((*c[x].shape[:-3], c[x].shape[-2], c[x].shape[-3], 128), 0xFF, dtype=torch.uint8, device="cuda")
+            for x in ("k", "v", "prefix_k", "prefix_v")}
+    views = {x: t.transpose(-3, -2)[..., 16:80] for x, t in wide.items()}
+    for x, t in views.items():
+        t.copy_(c[x])
+    views = {**c, **views}
+    assert torch.equal(hl.prefix_attention4(**views).out, want.out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = hl.prefix_attention4(**views)
+    for n in (140, 128, 150):
+        c["lens"][0] = n
+        c["q"].copy_(c["q"].flip(0))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(held.out, hl.prefix_attention4(**c).out)
