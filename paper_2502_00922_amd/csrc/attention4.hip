@@ -86,11 +86,18 @@ __device__ inline void load4(Tile4<G>& t, const Item& it, uint32_t key) {
   const uint8_t* kp = reinterpret_cast<const uint8_t*>(it.k + (uint64_t)key * it.k_token);
   const uint8_t* vp = reinterpret_cast<const uint8_t*>(it.v + (uint64_t)key * it.v_token);
   const uint32_t kb = 2 * it.k_token, vb = 2 * it.v_token;
+  // the lanes' offsets are the same for all keys of theirs where none is past the end:
+  // what differs is in the scalar part of the address
+  const auto k_at = [&](int h, uint32_t byte) {
+    return LAST ? kp + (min(16 * h + n, left) * kb + byte) : kp + (uint64_t)(16 * h) * kb + (n * kb + byte);
+  };
+  const auto v_at = [&](int e, uint32_t byte) {
+    return LAST ? vp + (min(key_of(c, e), left) * vb + byte) : vp + (uint64_t)key_of(0, e) * vb + (key_of(c, 0) * vb + byte);
+  };
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const uint32_t at = (LAST ? min(16 * h + n, left) : 16 * h + n) * kb;
-    fetch<4 * G, G % 4 == 0 ? 16 : G % 2 == 0 ? 8 : 4>(t.k[h], kp + (at + 4 * G * c));
-    fetch<16, 16>(&t.kr[h], kp + (at + 16 * G + (G > 4 ? c % 2 * 16 : 0)));
+    fetch<4 * G, G % 4 == 0 ? 16 : G % 2 == 0 ? 8 : 4>(t.k[h], k_at(h, 4 * G * c));
+    fetch<16, 16>(&t.kr[h], k_at(h, 16 * G + (G > 4 ? c % 2 * 16 : 0)));
 #pragma unroll
     for (int d = 0; d < 4; ++d) {
       if constexpr (G < 4) t.kr[h][d] = d < G ? t.kr[h][d] : 0;
@@ -99,9 +106,8 @@ __device__ inline void load4(Tile4<G>& t, const Item& it, uint32_t key) {
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const uint32_t nth = LAST ? min(key_of(c, e), left) : key_of(c, e), at = 16 * G + min(n, 2 * G - 1) * 2;
-    fetch<4 * Tile4<G>::VW, G % 8 == 0 ? 8 : G % 4 == 0 ? 4 : G % 2 == 0 ? 2 : 1>(t.v[e], vp + (nth * vb + G * n));
-    t.ve[e] = *reinterpret_cast<const uint16_t*>(vp + (nth * vb + at));
+    fetch<4 * Tile4<G>::VW, G % 8 == 0 ? 8 : G % 4 == 0 ? 4 : G % 2 == 0 ? 2 : 1>(t.v[e], v_at(e, G * n));
+    t.ve[e] = *reinterpret_cast<const uint16_t*>(v_at(e, 16 * G + min(n, 2u * G - 1) * 2));
   }
 }
 
