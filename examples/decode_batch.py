@@ -55,8 +55,12 @@ class Cache:
     gathered."""
 
     def __init__(self, batch, capacity, kv_heads, dim, bits=16):
-        row, dtype = (dim, torch.bfloat16) if bits == 16 else (hl.cache4_row_bytes(dim), torch.uint8)
-        self.k = torch.zeros((batch, capacity, kv_heads, row), dtype=dtype, device="cuda")
+        if bits == 16:
+            self.k = torch.zeros((batch, capacity, kv_heads, dim), dtype=torch.bfloat16, device="cuda")
+        else:
+            # a key head's rows next to each other: they are shorter than a line of memory
+            row = hl.cache4_row_bytes(dim)
+            self.k = torch.zeros((batch, kv_heads, capacity, row), dtype=torch.uint8, device="cuda").transpose(1, 2)
         self.v = torch.zeros_like(self.k)
         self.weights = torch.zeros((batch, kv_heads, capacity), device="cuda")
 
@@ -119,8 +123,9 @@ class Decoder:
             if self.bits == 4:
                 cache = Cache(1, n, self.kv_heads, self.dim, bits=4)
                 hl.cache_write4(k[None], v[None], cache.k, cache.v)
-                k, v = cache.k[0], cache.v[0]
-            self.prefix.append((k.contiguous(), v))
+                self.prefix.append((cache.k[0], cache.v[0]))
+            else:
+                self.prefix.append((k.contiguous(), v))
             a, x = self.norm(layer.o.gemm(out.view(n, -1)), x, layer.norm2)
             h = torch.nn.functional.silu(layer.gate.gemm(a)) * layer.up.gemm(a)
             delta = layer.down.gemm(h.bfloat16())

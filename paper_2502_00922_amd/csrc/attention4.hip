@@ -15,6 +15,12 @@
 // where the products leave its scores. For o, lane n of 16 has element n of a key's
 // pairs: an instruction takes the scale that it needs from that lane, and the eight
 // keys of a lane are a left operand whose rows are the elements, for the last term.
+//
+// Long own caches are bound by the lines of memory that their rows lie in, not by their
+// bytes: 16 sequences' tokens of 32 heads on 8 on 16384 own keys (335 MB) take 106 us
+// where the 80-byte rows of a token's heads are neighbours, 76 (4.4 TB/s) where a head's
+// tokens are. Fewer vector instructions a step changed neither. Short ones are bound by
+// a part's start and end.
 #include "attention_core.h"
 #include "cache4.h"
 

@@ -950,8 +950,9 @@ def prefix_attention4(q, k=None, v=None, lens=None, prefix_k=None, prefix_v=None
 
     k, v: uint8 [batch, capacity, kv_heads, cache4_row_bytes(dim)], prefix_k, prefix_v: uint8 [length, kv_heads,
     cache4_row_bytes(dim)] (any strides, in multiples of 16, with a row's bytes in a row), as cache_write4 leaves them
-    (a prefix is a cache's only sequence, ``cache_k[0, :n]``). q's dim is a multiple of 32. The rest, and the result, are
-    prefix_attention's; ``workspace``: a device buffer of hl_attention4_workspace_bytes."""
+    (a prefix is a cache's only sequence, ``cache_k[0, :n]``). Long caches are read faster where the tokens of a key head
+    lie next to each other ([batch, kv_heads, capacity, bytes], transposed). q's dim is a multiple of 32. The rest, and
+    the result, are prefix_attention's; ``workspace``: a device buffer of hl_attention4_workspace_bytes."""
     return _attend(True, q, k, v, lens, prefix_k, prefix_v, scale, weights, out, weights_out, lse, stream, workspace)
 
 
