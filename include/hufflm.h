@@ -550,9 +550,8 @@ hl_status hl_cache_read4(const void* rows_dev, uint64_t seq_stride, uint64_t tok
  * mean (prefix keys meet batch * queries * heads / kv_heads, own ones queries * heads /
  * kv_heads) first give the rows back in `dtype` (as hl_cache_read4), in the workspace,
  * which is the larger by them, and go on as hl_prefix_attention: float16 has no finite
- * value above 65504 then. A column group of a token that
- * a row sees is NaN in out where its scale or base is; of tokens that it does not
- * see, rows may hold anything. Any strides are taken; rows are shorter than a line of
+ * value above 65504 then. A column group of a token that a row sees is NaN in out where
+ * its scale or base is; of tokens that it does not see, rows may hold anything. Any strides are taken; rows are shorter than a line of
  * memory, so long caches are read faster where a key head's tokens lie next to each
  * other. Everything else, weights and errors among it, as hl_prefix_attention. */
 size_t hl_attention4_workspace_bytes(const hl_attention* attention, int with_weights);

@@ -14,10 +14,13 @@
 // and for its slice, and its last block of a row finds the border's step;
 // list_kernel lists that step's logits; end_kernel, one block a row, has every slice's
 // weight below the step and the list, and looks again only at the slice that the
-// token is in. With top_k of kFew or less all that
-// is kept is on the list, and nothing else is weighed. Where a list would be too long
-// (more than kList logits in a step), the block takes the whole row's logits again
-// for each digit of the border (slow_row).
+// token is in. With top_k of kFew or less all that is kept is on the list, and nothing
+// else is weighed. Where a list would be too long (more than kList logits in a step),
+// the block takes the whole row's logits again for each digit of the border (slow_row).
+//
+// The four kernels take 31 + 45 + 27 + 33 us for 256 rows of 131072 (134 MB, 26 us at a
+// copy's rate) and 3.6 + 7.2 + 3.7 + 9.2 for one of 32000; with one block a row they took
+// 386 and 104 us in all.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
