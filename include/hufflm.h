@@ -546,14 +546,11 @@ hl_status hl_cache_read4(const void* rows_dev, uint64_t seq_stride, uint64_t tok
 /* hl_prefix_attention over a prefix and own caches of 4-bit rows; its workspace.
  * `dtype` is q's and out's; dim is a multiple of 32. What rows stand for enters the
  * sums unrounded; p and p * scale are rounded to bf16 for the second product, to two
- * bf16 pieces where out is float16. Calls whose keys meet 256 rows of q and more in the
- * mean (prefix keys meet batch * queries * heads / kv_heads, own ones queries * heads /
- * kv_heads) first give the rows back in `dtype` (as hl_cache_read4), in the workspace,
- * which is the larger by them, and go on as hl_prefix_attention: float16 has no finite
- * value above 65504 then. A column group of a token that a row sees is NaN in out where
- * its scale or base is; of tokens that it does not see, rows may hold anything. Any strides are taken; rows are shorter than a line of
- * memory, so long caches are read faster where a key head's tokens lie next to each
- * other. Everything else, weights and errors among it, as hl_prefix_attention. */
+ * bf16 pieces where out is float16. A column group of a token that a row sees is NaN
+ * in out where its scale or base is; of tokens that it does not see, rows may hold
+ * anything. Any strides are taken; rows are shorter than a line of memory, so long
+ * caches are read faster where a key head's tokens lie next to each other. Everything
+ * else, weights and errors among it, as hl_prefix_attention. */
 size_t hl_attention4_workspace_bytes(const hl_attention* attention, int with_weights);
 hl_status hl_prefix_attention4(const hl_attention* attention, const void* q_dev, const int32_t* lens_dev,
                                void* out_dev, float* lse_dev, const float* weight_in_dev, float* weight_out_dev,

@@ -625,67 +625,14 @@ static hl_status run_groups4(const AttentionPlan& pl, hl_dtype dtype, hipStream_
   }
 }
 
-// Rows that a key meets in the mean, from which on a call's keys and values are first
-// given back in 16 bits, in the workspace, and attended by the 16-bit kernels. The
-// prefix's keys meet the batch's rows of a key head, those of the own caches a
-// sequence's. The 16-bit kernel takes a third of the time for a row and key; the way
-// through memory costs what that saves on 200 to 250 rows. With 8 key heads of 128
-// columns, here and (in 16 bits): 192 rows on 4096, 16384 and 65536 keys 33, 60 and 185 us
-// (34, 64, 195); 256 rows 35, 80 and 230 (35, 67, 205); 512 rows 45, 133 and 426 (39, 83,
-// 266); 4 x 256 tokens of 32 heads on 4096 shared and 512 own keys 290 (139). 128
-// sequences' tokens of 32 heads, 512 rows on 8192 shared keys but 4 on 256 own ones each:
-// 90 (109).
-constexpr uint64_t kManyRows = 256;
-
-// A call by the 16-bit kernels: the same with the values' places in the workspace,
-// behind `bytes` of it that these kernels take.
-struct Wide4 {
-  hl_attention shape;
-  uint64_t at[4], bytes, all;
-};
-
-static bool many_rows(const hl_attention& h) {
-  const double own = (double)h.queries * (h.heads / h.kv_heads), prefix_keys = (double)h.prefix.tokens;
-  const double own_keys = (double)h.own.tokens * h.batch;
-  const double keys = prefix_keys + own_keys;
-  return keys > 0 && prefix_keys * own * h.batch + own_keys * own >= kManyRows * keys;
-}
-
-// least: bytes of workspace that the call has in any case.
-static hl_status wide_plan(const hl_attention& h, bool weights, uint64_t least, Wide4* w) {
-  const auto whole = [&](const hl_kv& from) {
-    hl_kv to = from;
-    to.k_head = to.v_head = h.dim, to.k_token = to.v_token = (uint64_t)h.kv_heads * h.dim;
-    to.k_seq = to.v_seq = from.tokens * to.k_token;
-    return to;
-  };
-  w->shape = h;
-  w->shape.prefix = whole(h.prefix), w->shape.own = whole(h.own);
-  AttentionPlan pl;
-  const hl_status st = attention_plan(&w->shape, weights, false, &pl);
-  if (st != HL_OK) return st;
-  w->bytes = (pl.bytes + 255) / 256 * 256;
-  uint64_t n = w->bytes;
-  const uint64_t sizes[4] = {h.prefix.tokens, h.prefix.tokens, h.batch * h.own.tokens, h.batch * h.own.tokens};
-  for (int i = 0; i < 4; ++i) {
-    w->at[i] = n;
-    n += (sizes[i] * h.kv_heads * h.dim * 2 + 255) / 256 * 256;
-  }
-  w->all = std::max(n, least);
-  return HL_OK;
-}
-
 }  // namespace hl
 
 using namespace hl;
 
 extern "C" size_t hl_attention4_workspace_bytes(const hl_attention* attention, int with_weights) {
   AttentionPlan pl;
-  Wide4 w;
   if (!attention || attention->dim % 32) return 0;
-  if (attention_plan(attention, with_weights != 0, true, &pl) != HL_OK) return 0;
-  if (!many_rows(*attention)) return pl.bytes;
-  return wide_plan(*attention, with_weights != 0, pl.bytes, &w) == HL_OK ? w.all : 0;
+  return attention_plan(attention, with_weights != 0, true, &pl) == HL_OK ? pl.bytes : 0;
 }
 
 extern "C" hl_status hl_prefix_attention4(const hl_attention* attention, const void* q_dev, const int32_t* lens_dev,
@@ -693,28 +640,10 @@ extern "C" hl_status hl_prefix_attention4(const hl_attention* attention, const v
                                           float* weight_out_dev, void* workspace_dev, size_t workspace_bytes,
                                           void* stream) {
   if (!attention || attention->dim % 32) return HL_EINVAL;
-  const hipStream_t s = (hipStream_t)stream;
   AttentionPlan pl;
-  hl_status st = attention_setup(attention, q_dev, lens_dev, out_dev, lse_dev, weight_in_dev, weight_out_dev,
-                                 workspace_dev, workspace_bytes, true, &pl);
+  const hl_status st = attention_setup(attention, q_dev, lens_dev, out_dev, lse_dev, weight_in_dev, weight_out_dev,
+                                       workspace_dev, workspace_bytes, true, &pl);
   if (st != HL_OK) return st;
-  if (!many_rows(*attention))
-    return attention->dtype == HL_BF16 ? run_groups4<__bf16>(pl, HL_BF16, s) : run_groups4<_Float16>(pl, HL_F16, s);
-  Wide4 w;
-  st = wide_plan(*attention, weight_out_dev != nullptr, pl.bytes, &w);
-  if (st != HL_OK) return st;
-  if (workspace_bytes < w.all || !aligned(workspace_dev, 16)) return HL_EINVAL;
-  uint8_t* ws = static_cast<uint8_t*>(workspace_dev);
-  hl_attention& h = w.shape;
-  h.prefix.k_dev = ws + w.at[0], h.prefix.v_dev = ws + w.at[1], h.own.k_dev = ws + w.at[2], h.own.v_dev = ws + w.at[3];
-  if (h.prefix.tokens) {
-    st = read_cache4(attention->prefix, 1, h.kv_heads, h.dim, nullptr, ws + w.at[0], ws + w.at[1], h.dtype, s);
-    if (st != HL_OK) return st;
-  }
-  if (h.own.tokens) {
-    st = read_cache4(attention->own, h.batch, h.kv_heads, h.dim, lens_dev, ws + w.at[2], ws + w.at[3], h.dtype, s);
-    if (st != HL_OK) return st;
-  }
-  return hl_prefix_attention(&h, q_dev, lens_dev, out_dev, lse_dev, weight_in_dev, weight_out_dev, workspace_dev, w.bytes,
-                             stream);
+  return attention->dtype == HL_BF16 ? run_groups4<__bf16>(pl, HL_BF16, (hipStream_t)stream)
+                                     : run_groups4<_Float16>(pl, HL_F16, (hipStream_t)stream);
 }

@@ -12,13 +12,6 @@
 
 namespace hl {
 
-constexpr uint32_t kMaxGroups = 8;
-
 __host__ __device__ constexpr uint32_t row4_bytes(uint32_t groups) { return (20 * groups + 15) / 16 * 16; }
-
-// The values of a cache's tokens (of sequence b, the first lens_dev[b]; null: all) to
-// k_out and v_out [batch][tokens][heads][dim]. The arguments have been checked.
-hl_status read_cache4(const hl_kv& cache, uint32_t batch, uint32_t heads, uint32_t dim, const int32_t* lens_dev,
-                      void* k_out, void* v_out, hl_dtype dtype, hipStream_t s);
 
 }  // namespace hl

@@ -129,25 +129,22 @@ __global__ void __launch_bounds__(kRowThreads) write4_kernel(WriteArgs a) {
 }
 
 struct ReadArgs {
-  const uint8_t* from[2];
-  void* out[2];
-  uint64_t seq[2], token[2], head[2];  // of the rows, in bytes
-  const int32_t* lens;                 // null: all tokens are read
+  const uint8_t* from;
+  void* out;
+  uint64_t seq, token, head;  // of the rows, in bytes
   Divider tokens, heads;
   uint32_t rows;
 };
 
-// Four lanes a group, 8 columns each; blockIdx.y: of one set of rows or the other.
-// Bound by HBM: 16384 tokens of 8 key heads of 128 columns, 44 MB, 9 us.
+// Four lanes a group, 8 columns each. Bound by HBM: 16384 tokens of 8 key heads of 128 columns, 44 MB, 9 us.
 template <class T, uint32_t G>
 __global__ void __launch_bounds__(kRowThreads) read4_kernel(ReadArgs a) {
   constexpr uint32_t LANES = 4 * G, ROWS = kRowThreads / LANES;
-  const uint32_t lane = threadIdx.x % LANES, nth = threadIdx.x / LANES, set = blockIdx.y;
+  const uint32_t lane = threadIdx.x % LANES, nth = threadIdx.x / LANES;
   const uint32_t row = blockIdx.x * ROWS + nth;
   if (nth >= ROWS || row >= a.rows) return;
   const RowPlace r(row, a.heads, a.tokens);
-  if (a.lens && (int64_t)r.t >= (int64_t)a.lens[r.b]) return;
-  const uint8_t* p = a.from[set] + r.b * a.seq[set] + r.t * a.token[set] + r.head * a.head[set];
+  const uint8_t* p = a.from + r.b * a.seq + r.t * a.token + r.head * a.head;
   const uint32_t g = lane / 4, c = lane % 4;
   const uint32_t pair = reinterpret_cast<const uint32_t*>(p + 16 * G)[g];
   const float scale = __builtin_bit_cast(float, pair << 16), base = __builtin_bit_cast(float, pair & 0xFFFF0000u);
@@ -159,7 +156,7 @@ __global__ void __launch_bounds__(kRowThreads) read4_kernel(ReadArgs a) {
     x[2 * j] = (T)fmaf(scale, (float)(int)(codes & 15) - 8.0f, base);
     x[2 * j + 1] = (T)fmaf(scale, (float)(int)(codes >> 4) - 8.0f, base);
   }
-  *reinterpret_cast<T8*>(static_cast<T*>(a.out[set]) + (uint64_t)row * (32 * G) + 8 * lane) = x;
+  *reinterpret_cast<T8*>(static_cast<T*>(a.out) + (uint64_t)row * (32 * G) + 8 * lane) = x;
 }
 
 template <class F>
@@ -174,30 +171,6 @@ static hl_status with_groups(uint32_t groups, F f) {
     case 7: return f(std::integral_constant<uint32_t, 7>());
     default: return f(std::integral_constant<uint32_t, 8>());
   }
-}
-
-// The first `sets` sets of a.
-static hl_status read_rows(const ReadArgs& a, uint32_t sets, uint32_t dim, hl_dtype dtype, hipStream_t s) {
-  return with_groups(dim / 32, [&](auto g) {
-    constexpr uint32_t G = decltype(g)::value, rows = kRowThreads / (4 * G);
-    const dim3 grid((uint32_t)(((uint64_t)a.rows + rows - 1) / rows), sets), block(kRowThreads);
-    return dtype == HL_F32    ? enqueue(read4_kernel<float, G>, grid, block, s, a)
-           : dtype == HL_BF16 ? enqueue(read4_kernel<__bf16, G>, grid, block, s, a)
-                              : enqueue(read4_kernel<_Float16, G>, grid, block, s, a);
-  });
-}
-
-hl_status read_cache4(const hl_kv& cache, uint32_t batch, uint32_t heads, uint32_t dim, const int32_t* lens_dev,
-                      void* k_out, void* v_out, hl_dtype dtype, hipStream_t s) {
-  ReadArgs a = {};
-  a.from[0] = static_cast<const uint8_t*>(cache.k_dev), a.from[1] = static_cast<const uint8_t*>(cache.v_dev);
-  a.out[0] = k_out, a.out[1] = v_out;
-  a.seq[0] = 2 * cache.k_seq, a.token[0] = 2 * cache.k_token, a.head[0] = 2 * cache.k_head;
-  a.seq[1] = 2 * cache.v_seq, a.token[1] = 2 * cache.v_token, a.head[1] = 2 * cache.v_head;
-  const uint64_t rows = (uint64_t)batch * cache.tokens * heads, each = kRowThreads / (dim / 8);
-  if (rows > kMostRows || !grid_fits((rows + each - 1) / each, kRowThreads)) return HL_EUNSUPPORTED;
-  a.lens = lens_dev, a.tokens = Divider::by((uint32_t)cache.tokens), a.heads = Divider::by(heads), a.rows = (uint32_t)rows;
-  return read_rows(a, 2, dim, dtype, s);
 }
 
 }  // namespace hl
@@ -264,8 +237,14 @@ extern "C" hl_status hl_cache_read4(const void* rows_dev, uint64_t seq_stride, u
   const hl_status st = check_rows(batch, tokens, heads, dim);
   if (st != HL_OK) return st;
   ReadArgs a = {};
-  a.from[0] = static_cast<const uint8_t*>(rows_dev), a.out[0] = out_dev;
-  a.seq[0] = seq_stride, a.token[0] = token_stride, a.head[0] = head_stride;
+  a.from = static_cast<const uint8_t*>(rows_dev), a.out = out_dev;
+  a.seq = seq_stride, a.token = token_stride, a.head = head_stride;
   a.tokens = Divider::by((uint32_t)tokens), a.heads = Divider::by(heads), a.rows = (uint32_t)(batch * tokens * heads);
-  return read_rows(a, 1, dim, dtype, (hipStream_t)stream);
+  return with_groups(dim / 32, [&](auto g) {
+    constexpr uint32_t G = decltype(g)::value, rows = kRowThreads / (4 * G);
+    const dim3 grid((uint32_t)(((uint64_t)a.rows + rows - 1) / rows)), block(kRowThreads);
+    return dtype == HL_F32    ? enqueue(read4_kernel<float, G>, grid, block, (hipStream_t)stream, a)
+           : dtype == HL_BF16 ? enqueue(read4_kernel<__bf16, G>, grid, block, (hipStream_t)stream, a)
+                              : enqueue(read4_kernel<_Float16, G>, grid, block, (hipStream_t)stream, a);
+  });
 }
