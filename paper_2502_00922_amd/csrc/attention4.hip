@@ -3,9 +3,11 @@
 // multiplies the codes themselves.
 //
 // A value is base + scale * (code - 8), with a pair (scale, base) for each 32
-// columns of a row. The matrix instruction's operand is 16 + code (or 128, or 64),
-// which is exact in bf16 and in f16 and takes one and-or of a nibble in place; what is
-// too much of it, 8 as well, is taken off by products with constants:
+// columns of a row. The matrix instruction's operand is 16 + code, which is exact in
+// bf16 and in f16 and takes a shift and an and-or of a nibble; what is too much of it, 8
+// as well, is taken off by products with constants. (128 or 64 + code, where a nibble is
+// in place for it, save a shift in four and 4 % of the time of 192 rows on 65536 keys,
+// and lose three bits of the sums and of their range.)
 //   q.k = sum_g scale_g * (q.(16 + code) - 24 Q_g) + base_g * Q_g,  Q_g the sum of q's group
 //   o_d = sum_j w_j (16 + code_jd) - 24 w_j + p_j base_jg,          w_j = p_j * scale_jg
 // with w rounded to 16 bits once and the same w in both products, so that its error
@@ -53,22 +55,20 @@ struct State4 {
   uint32_t seen[R];
 };
 
-// Codes as operands, from the low bytes of two halves: even columns' in a byte's low
-// half, odd ones' in the high one. bf16: 128 + code, 16 + code; f16: 16 and 64. The
-// masks are in scalar registers and the exponents in vector ones, so that one
-// instruction takes both.
+// 16 + code as operands, from the low bytes of two halves: even columns' codes are in
+// a byte's low half, odd ones' in the high one. The mask is in a scalar register and the
+// exponents in a vector one, so that one instruction takes both.
+constexpr float kTooMuch = 24.0f;  // with the 8 that a code has too much
 template <class T>
 struct Codes4 {
   static constexpr bool BF = std::is_same<T, __bf16>::value;
-  static constexpr float LOW = BF ? 136.0f : 24.0f, HIGH = BF ? 24.0f : 72.0f;  // with 8 too much
-  uint32_t low_mask, high_mask, low_one, high_one;
+  uint32_t mask, one;
   __device__ Codes4() {
-    low_mask = BF ? 0x000F000Fu : 0x03C003C0u, high_mask = BF ? 0x00780078u : 0x00F000F0u;
-    low_one = BF ? 0x43004300u : 0x4C004C00u, high_one = BF ? 0x41804180u : 0x54005400u;
-    asm volatile("" : "+s"(low_mask), "+s"(high_mask), "+v"(low_one), "+v"(high_one));
+    mask = BF ? 0x00780078u : 0x03C003C0u, one = BF ? 0x41804180u : 0x4C004C00u;
+    asm volatile("" : "+s"(mask), "+v"(one));
   }
-  __device__ uint32_t low(uint32_t pair) const { return ((BF ? pair : pair << 6) & low_mask) | low_one; }
-  __device__ uint32_t high(uint32_t pair) const { return ((BF ? pair >> 1 : pair) & high_mask) | high_one; }
+  __device__ uint32_t low(uint32_t pair) const { return ((BF ? pair << 3 : pair << 6) & mask) | one; }
+  __device__ uint32_t high(uint32_t pair) const { return ((BF ? pair >> 1 : pair << 2) & mask) | one; }
 };
 
 // Bytes i and j (counted from the first word's) of words w as the low bytes of
@@ -269,10 +269,8 @@ __device__ inline void step4(State4<G, R>& st, const Tile4<G>& t, const Codes4<T
 #pragma unroll
     for (int y = 0; y < PIECES; ++y) asm volatile("" : "+v"(to[y]));
   };
-  // what is too much of the codes (136, 24), for even and odd columns
-  u32x4 less[2] = {u32x4{0xC308C308u, 0xC308C308u, 0xC308C308u, 0xC308C308u},
-                   u32x4{0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u}};
-  asm volatile("" : "+v"(less[0]), "+v"(less[1]));
+  u32x4 less[1] = {u32x4{0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u}};  // minus what is too much
+  asm volatile("" : "+v"(less[0]));
   // rows whose keys all queries see: p times the pairs' elements, for the bases
   constexpr int BASES = EDGE ? 0 : 1;
   u32x4 pairs[1], pw[R * PIECES];
@@ -322,7 +320,7 @@ __device__ inline void step4(State4<G, R>& st, const Tile4<G>& t, const Codes4<T
           const u32x4 x = w[(i * R + rt) * PIECES + y];
           f32x4 &even = st.o[rt][2 * (g0 + i)], &odd = st.o[rt][2 * (g0 + i) + 1];
           even = mfma<__bf16>(codes[2 * i], x, even), odd = mfma<__bf16>(codes[2 * i + 1], x, odd);
-          even = mfma<__bf16>(less[0], x, even), odd = mfma<__bf16>(less[1], x, odd);
+          even = mfma<__bf16>(less[0], x, even), odd = mfma<__bf16>(less[0], x, odd);
         }
     if constexpr (g0 == 0 && BASES) {
 #pragma unroll
@@ -355,15 +353,14 @@ __device__ inline void begin4(State4<G, R>& st, const AttentionArgs& a, const It
       st.o[rt][2 * g] = st.o[rt][2 * g + 1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
       st.mean[rt][g] = 0.0f;
       const u32x4 x = (*reinterpret_cast<const u32x4*>(q + 32 * g + 8 * c) & a.q_and) ^ a.q_xor;
-      float even = 0.0f, odd = 0.0f;
+      float all = 0.0f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const uint32_t two = x[j];  // an element itself is not what a bit cast takes
         const pair y = __builtin_bit_cast(pair, two);
-        even += (float)y[0], odd += (float)y[1];
+        all += (float)y[0] + (float)y[1];
       }
-      even = over_lanes(even), odd = over_lanes(odd);
-      sum[g] = even + odd, less[g] = -fmaf(Codes4<T>::LOW, even, Codes4<T>::HIGH * odd);
+      sum[g] = over_lanes(all), less[g] = -kTooMuch * sum[g];
       // the order in which a pair of bytes gives its codes
 #pragma unroll
       for (int j = 0; j < 4; ++j)
