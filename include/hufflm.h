@@ -563,9 +563,11 @@ hl_status hl_prefix_attention4(const hl_attention* attention, const void* q_dev,
  * half. scales_dev, bases_dev: bf16 or float16 [rows][cols / group], one for each
  * `group` neighbouring columns: 32, 64 or 128, dividing cols; bases_dev NULL: all 0.
  * x_dev: [batch][cols] bf16 or float16; y_dev: [batch][rows] float32 (fully
- * written). The codes multiply x exactly and sums are float32, in a fixed order;
- * scales and bases multiply a group's sums in float32. A row with an infinite or
- * NaN scale or base has no finite y. codes_dev and x_dev are 16-byte aligned, the
+ * written). The codes (as 16 + code, less 24) multiply x exactly and sums are float32,
+ * in a fixed order; scales and bases multiply a group's sums in float32. A row with an
+ * infinite or NaN scale or base has no finite y, nor has a row of x with an infinity or
+ * a NaN (NaN, too, where the definition is infinite); x above 2^115 may have none,
+ * where 55 times the sum of a group's |x| is not finite. codes_dev and x_dev are 16-byte aligned, the
  * others 4-byte. Errors: HL_EINVAL (also for a misaligned pointer),
  * HL_EUNSUPPORTED for cols of 2^24 and above and rows past 32-bit counts. */
 hl_status hl_gemv4(const uint8_t* codes_dev, const void* scales_dev, const void* bases_dev, hl_dtype scale_dtype,

@@ -2,10 +2,11 @@
 //   y[b][r] = sum_k x[b][k] * (base + scale * (code[r][k] - 8)),
 // a scale (and a base, or none) for each GROUP = 32, 64 or 128 columns of a row.
 //
-// The matrix instruction's right operand is 16 + code (or another power of two and the
-// code), exact in bf16 and f16 and one and-or of a nibble in place; what is too much
-// of it is where the sums begin: a product of x with a constant operand that all rows
-// share. x is the left one: a lane's four sums are then of one row of the matrix,
+// The matrix instruction's right operand is 16 + code, exact in bf16 and f16 and a shift
+// and an and-or of a nibble; what is too much of it is where the sums begin: a product of
+// x with a constant operand that all rows share. (128 or 64 + code, where a nibble is in
+// place for it, save a shift in four and lose three bits of the sums and of their range.)
+// x is the left one: a lane's four sums are then of one row of the matrix,
 // whose scale the lane has loaded itself.
 // A wave has RT 16-row tiles and every W-th stretch of 512 columns, a block the W waves
 // of the same rows, which are added in LDS in their order. A lane loads 16 bytes of a
@@ -86,29 +87,25 @@ __device__ inline void turn4(u32x4& w) {
   w = u32x4{u[0], u[1], v[0], v[1]};
 }
 
-// The left operand of 8 columns' codes, columns 0 4 1 5 2 6 3 7 in pairs: each code
-// plus what the nibble's place makes of the exponent, which `offset` takes off again.
-// The mask is in a scalar register and the exponents in a vector one, so that an
-// instruction takes both.
+// The right operand of 8 columns' codes, columns 0 4 1 5 2 6 3 7 in pairs: 16 + code,
+// which `offset` takes off again, and 8. The mask is in a scalar register and the exponents
+// in a vector one, so that an instruction takes both.
 template <class T>
 struct Codes {
   static constexpr bool BF = std::is_same<T, __bf16>::value;
-  uint32_t mask0, mask, one0, one;
+  uint32_t mask, one;
   __device__ Codes() {
-    mask0 = BF ? 0x000F000Fu : 0x03C003C0u, mask = BF ? 0x00780078u : 0x00F000F0u;
-    one0 = BF ? 0x43004300u : 0x4C004C00u, one = BF ? 0x41804180u : 0x54005400u;
-    asm volatile("" : "+s"(mask0), "+s"(mask), "+v"(one0), "+v"(one));
+    mask = BF ? 0x00780078u : 0x03C003C0u, one = BF ? 0x41804180u : 0x4C004C00u;
+    asm volatile("" : "+s"(mask), "+v"(one));
   }
-  // bf16: 128 + code of the first pair, 16 + code of the others; float16: 16 and 64
   __device__ u32x4 operand(uint32_t w) const {
     if constexpr (BF)
-      return u32x4{(w & mask0) | one0, ((w >> 1) & mask) | one, ((w >> 5) & mask) | one, ((w >> 9) & mask) | one};
-    return u32x4{((w << 6) & mask0) | one0, (w & mask) | one, ((w >> 4) & mask) | one, ((w >> 8) & mask) | one};
+      return u32x4{((w << 3) & mask) | one, ((w >> 1) & mask) | one, ((w >> 5) & mask) | one, ((w >> 9) & mask) | one};
+    return u32x4{((w << 6) & mask) | one, ((w << 2) & mask) | one, ((w >> 2) & mask) | one, ((w >> 6) & mask) | one};
   }
-  // minus these, and minus 8
   __device__ static u32x4 offset() {
-    if constexpr (BF) return u32x4{0xC308C308u, 0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u};
-    return u32x4{0xCE00CE00u, 0xD480D480u, 0xD480D480u, 0xD480D480u};
+    constexpr uint32_t less = BF ? 0xC1C0C1C0u : 0xCE00CE00u;  // -24
+    return u32x4{less, less, less, less};
   }
 };
 
