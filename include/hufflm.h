@@ -605,7 +605,8 @@ typedef struct {
  * [rows][vocab] float32, bf16 or float16, rows row_stride elements apart, aligned to
  * their elements. tokens_dev int32, logprobs_dev float32 [rows]. workspace_dev:
  * hl_sample_workspace_bytes (16-byte aligned, no initial contents needed; 0 on bad
- * arguments); calls that may run concurrently need separate ones. Errors: HL_EINVAL
+ * arguments; 15 to 31 KB a row and 10 for each 2048 to 16384 of its logits, 174 MB at
+ * most: further rows go after each other); calls that may run concurrently need separate ones. Errors: HL_EINVAL
  * (also for a missing or short workspace), HL_EUNSUPPORTED for vocab of 2^20 and
  * above and more than 65535 rows. */
 size_t hl_sample_workspace_bytes(uint32_t rows, uint64_t vocab);

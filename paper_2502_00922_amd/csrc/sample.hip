@@ -30,6 +30,17 @@
 namespace hl {
 
 constexpr uint32_t kSteps = 1024, kSlices = 64, kList = 2048, kFew = 1024;
+constexpr uint32_t kMostSlice = 16384;  // logits of a slice: 64 for each lane of its waves
+// Places of the list that a wave has of its own. One that lists more takes so many of the
+// row's common ones, when it knows how many, and reads these logits again (with common
+// places alone 64 rows of 131072 take 47.6 us, with these 42.8).
+constexpr uint32_t kOwn = 64;
+// Slices that a call's workspace has room for, at most (or one row's): more rows go through
+// the kernels after each other. A compute unit has 16 blocks then, and the workspace is 174
+// MB or less. us for 4096 rows of 32000 bf16 and 1024 of 131072, and MB: without an end 640
+// and 463, 664 and 619; with 2048 slices 719 and 546, 54 and 29; with 4096 674 and 440, 108
+// and 58.
+constexpr uint32_t kAtOnce = 4096;
 constexpr uint32_t kThreads = 256, kWaves = kThreads / 64;  // of a slice's blocks
 constexpr uint32_t kEnd = 512, kEndWaves = kEnd / 64;       // of a row's last block
 constexpr uint32_t kAhead = 4;    // loads of a lane in flight
@@ -40,30 +51,30 @@ constexpr double kOne = 0x1p43;
 
 typedef unsigned long long u64;
 
-// A row's part of the workspace; then its slices', one after the other.
+// A row's part of the workspace; then its list, of a level's bits and its index above
+// them, and its slices' weights of each step, one after the other.
 struct RowWork {
   u64 mass[kSteps];
   uint32_t count[kSteps];
   u64 sum[kSlices];  // of the slice's weights that are kept whatever the list says
   float most[kSlices], lowest[kSlices];
-  uint32_t first[kSlices], listed[kSlices * kWaves];  // first: index of most; listed: by each of a slice's waves
+  uint32_t first[kSlices];  // index of most
+  uint32_t listed[kSlices * kWaves], at[kSlices * kWaves];  // by each of a slice's waves: how many, and from where on
   // The border. Steps below lo are kept as far as top_k and top_p go, above hi not;
   // those between, and step `other`, go on the list. by_count, by_mass: whether
   // top_k and top_p end there. From step `from` on, top_k's border is on the list.
   uint32_t lo, hi, other, from, by_count, by_mass;
-  uint32_t arrived, unused0;
+  uint32_t arrived, used;              // used: of the list's common places
   u64 count_from, mass_from, mass_lo;  // of the steps below `from` and lo
-  u64 unused[5];
+  u64 unused;
 };
-struct SliceWork {
-  u64 mass[kSteps];
-  u64 list[kWaves][kList];  // of a wave: a level's bits, and its index above them
-};
+static_assert(sizeof(RowWork) % 16 == 0, "rows and lists begin at 16 bytes");
 
 struct SampleArgs {
   const void* logits;
   uint64_t stride;
   uint32_t vocab, slice, slices;  // slice: logits of one
+  uint32_t common;                // of a row's list: kList, or all its logits
   const float* uniforms;
   const float *temperatures, *top_ps, *min_ps;  // null: the numbers below, for all rows
   const int32_t* top_ks;
@@ -73,12 +84,13 @@ struct SampleArgs {
   float* logprobs;
   uint8_t* work;
 
-  __device__ RowWork& of_row(uint32_t row) const {
-    return *reinterpret_cast<RowWork*>(work + row * (sizeof(RowWork) + (uint64_t)slices * sizeof(SliceWork)));
+  __host__ __device__ uint32_t own() const { return slices * kWaves * kOwn; }  // places before the common ones
+  __host__ __device__ uint64_t row_bytes() const {
+    return sizeof(RowWork) + (own() + common + (uint64_t)slices * kSteps) * sizeof(u64);
   }
-  __device__ SliceWork& of_slice(uint32_t row, uint32_t i) const {
-    return reinterpret_cast<SliceWork*>(&of_row(row) + 1)[i];
-  }
+  __device__ RowWork& of_row(uint32_t row) const { return *reinterpret_cast<RowWork*>(work + row * row_bytes()); }
+  __device__ u64* list_of(RowWork& w) const { return reinterpret_cast<u64*>(&w + 1); }
+  __device__ u64* mass_of(RowWork& w, uint32_t i) const { return list_of(w) + own() + common + i * kSteps; }
 };
 
 // A logit as an integer, the greater the logit the smaller; -0 is 0.
@@ -256,7 +268,7 @@ __global__ void __launch_bounds__(kThreads) top_kernel(SampleArgs a) {
   RowWork& w = a.of_row(row);
   if (slice == 0) {
     for (uint32_t i = tid; i < kSteps; i += kThreads) w.mass[i] = 0, w.count[i] = 0;
-    if (tid == 0) w.arrived = 0;
+    if (tid == 0) w.arrived = 0, w.used = 0;
   }
   const T* logits = static_cast<const T*>(a.logits) + row * a.stride;
   const uint32_t begin = slice * a.slice, end = min(begin + a.slice, a.vocab);
@@ -478,7 +490,7 @@ __global__ void __launch_bounds__(kThreads) step_kernel(SampleArgs a) {
   __syncthreads();
   for (uint32_t i = tid; i < kSteps; i += kThreads) {
     if (!d.few) {
-      a.of_slice(row, slice).mass[i] = s_mass[i];
+      a.mass_of(w, slice)[i] = s_mass[i];
       if (s_mass[i]) atomicAdd(&w.mass[i], s_mass[i]);
     }
     if (s_count[i]) atomicAdd(&w.count[i], s_count[i]);
@@ -493,7 +505,7 @@ struct EndLds {
   double powers[64];
   u64 wave[kEndWaves], total[kSlices], limit;
   ulonglong2 pair[kPairs];  // a logit's place, and its weight if its step is not past hi
-  uint32_t start[kSlices * kWaves], pick, members;
+  uint32_t start[kSlices * kWaves], at[kSlices * kWaves], pick, members;
 };
 
 // A logit's place in the order: falling logits, of equal ones the lowest index first.
@@ -677,7 +689,8 @@ __device__ inline void slow_row(const SampleArgs& a, const Draw& d, uint32_t row
   end_row(a, d, row, logits, all.pick(s, target_of(a.uniforms[row], total), weigh), total);
 }
 
-// Lists the logits of the border's steps, and adds up what the slice has below them.
+// Lists the logits of the border's steps, and adds up what the slice has below them. A
+// lane keeps a bit for each of its logits, for a wave that lists more than it has places.
 // Bound by reading the logits again.
 template <class T>
 __global__ void __launch_bounds__(kThreads) list_kernel(SampleArgs a) {
@@ -691,17 +704,28 @@ __global__ void __launch_bounds__(kThreads) list_kernel(SampleArgs a) {
   const Draw d(a, row, most, lowest);
   if (d.greedy || !d.border) return;
   const uint32_t lo = w.lo, hi = w.hi, other = w.other;
-  SliceWork& own = a.of_slice(row, slice);
   if (!d.few) {
+    const u64* mass = a.mass_of(w, slice);
     u64 base = 0;
-    for (uint32_t i = tid; i < lo; i += kThreads) base += own.mass[i];
+    for (uint32_t i = tid; i < lo; i += kThreads) base += mass[i];
     base = add_block<kWaves>(base);
     if (tid == 0) w.sum[slice] = base;
   }
-  // every wave has its part of the slice and a list of its own
+  // every wave has its part of the slice
   const T* logits = static_cast<const T*>(a.logits) + row * a.stride;
   const uint32_t part = a.slice / kWaves, begin = min(slice * a.slice + wave * part, a.vocab);
-  uint32_t listed = 0;
+  static_assert(kMostSlice / kWaves == 64 * 64, "a lane has a bit for each of its logits");
+  u64* list = a.list_of(w);
+  const uint32_t own = (slice * kWaves + wave) * kOwn;
+  u64 bits = 0;
+  uint32_t shift = 0, listed = 0;
+  // the next places of the lanes whose bits of a vector are `mine`
+  const auto places = [&](uint32_t mine) {
+    const uint32_t upto = scan_wave((uint32_t)__popc(mine)), place = listed + upto - __popc(mine);
+    listed += lane_of(upto, 63);
+    return place;
+  };
+  const auto entry = [](uint32_t at, float level) { return (u64)at << 32 | __builtin_bit_cast(uint32_t, level); };
   for_vectors<T, 64 * VEC>(logits, begin, min(begin + part, a.vocab), lane * VEC,
                            [&](float (&v)[VEC], uint32_t at) __attribute__((always_inline)) {
     uint32_t mine = 0;
@@ -711,21 +735,41 @@ __global__ void __launch_bounds__(kThreads) list_kernel(SampleArgs a) {
       const uint32_t step = d.step(v[j]);
       mine |= (uint32_t)((step >= lo && step <= hi) || step == other) << j;
     }
-    if (!__any(mine != 0)) return false;
+    if (__any(mine != 0)) {
 #pragma unroll
-    for (uint32_t j = 0; j < VEC; ++j) mine &= ~((uint32_t)!Draw::weighs(d.power(v[j])) << j);
-    const uint32_t upto = scan_wave((uint32_t)__popc(mine));
-    uint32_t to = listed + upto - __popc(mine);
+      for (uint32_t j = 0; j < VEC; ++j) mine &= ~((uint32_t)!Draw::weighs(d.power(v[j])) << j);
+      bits |= (u64)mine << shift;
+      uint32_t place = places(mine);
 #pragma unroll
-    for (uint32_t j = 0; j < VEC; ++j)
-      if (mine >> j & 1) {
-        if (to < kList) own.list[wave][to] = (u64)(at + j) << 32 | __builtin_bit_cast(uint32_t, v[j]);
-        ++to;
-      }
-    listed += lane_of(upto, 63);
+      for (uint32_t j = 0; j < VEC; ++j)
+        if (mine >> j & 1) {
+          if (place < kOwn) list[own + place] = entry(at + j, v[j]);
+          ++place;
+        }
+    }
+    shift += VEC;
     return false;
   });
-  if (lane == 0) w.listed[slice * kWaves + wave] = listed;
+  uint32_t to = own;
+  if (listed > kOwn) {
+    uint32_t used = 0;
+    if (lane == 0) used = atomicAdd(&w.used, listed);
+    used = __builtin_amdgcn_readfirstlane(used);
+    to = a.own() + used;
+    if (used + listed <= a.common) {  // else the row has more than kList, and no use for its list
+      u64* common = list + to;
+      listed = 0;
+      for (uint32_t at = begin + lane * VEC; __any(bits != 0); at += 64 * VEC, bits >>= VEC) {
+        const uint32_t mine = (uint32_t)bits & ((1u << VEC) - 1);
+        if (!__any(mine != 0)) continue;
+        uint32_t place = places(mine);
+#pragma unroll
+        for (uint32_t j = 0; j < VEC; ++j)
+          if (mine >> j & 1) common[place++] = entry(at + j, d.level((float)logits[at + j]));
+      }
+    }
+  }
+  if (lane == 0) w.listed[slice * kWaves + wave] = listed, w.at[slice * kWaves + wave] = to;
 }
 
 // Ends a row from its list and the slices' sums. Bound by its barriers and waits, one
@@ -758,7 +802,7 @@ __global__ void __launch_bounds__(kEnd) end_kernel(SampleArgs a) {
     const uint32_t mine = tid < a.slices * kWaves ? w.listed[tid] : 0;
     u64 all;
     const uint32_t start = (uint32_t)scan_block<kEndWaves>(mine, all);
-    if (tid < kSlices * kWaves) s.start[tid] = start;
+    if (tid < kSlices * kWaves) s.start[tid] = start, s.at[tid] = tid < a.slices * kWaves ? w.at[tid] : 0;
     n = (uint32_t)all;
   }
   __syncthreads();
@@ -777,7 +821,7 @@ __global__ void __launch_bounds__(kEnd) end_kernel(SampleArgs a) {
 #pragma unroll
     for (uint32_t h = kSlices * kWaves / 2; h; h >>= 1)
       if (s.start[from + h] <= i) from += h;
-    const u64 x = a.of_slice(row, from / kWaves).list[from % kWaves][i - s.start[from]];
+    const u64 x = a.list_of(w)[s.at[from] + i - s.start[from]];
     const float l = __builtin_bit_cast(float, (uint32_t)x);
     s.logit[i] = l, s.index[i] = (uint32_t)(x >> 32);
     s.weight[i] = Draw::whole(d.power(l), s.powers);
@@ -912,16 +956,34 @@ __global__ void __launch_bounds__(kEnd) end_kernel(SampleArgs a) {
 static uint32_t slice_of(uint64_t rows, uint64_t vocab) {
   const uint64_t blocks = 4 * (uint64_t)device_cus(), most = std::max<uint64_t>(1, blocks / rows);
   const uint64_t each = (vocab + most - 1) / most, least = std::max<uint64_t>(2048, (vocab + kSlices - 1) / kSlices);
-  return (uint32_t)((std::min<uint64_t>(std::max(each, least), std::max<uint64_t>(least, 16384)) + 2047) / 2048 * 2048);
+  return (uint32_t)((std::min<uint64_t>(std::max(each, least), kMostSlice) + 2047) / 2048 * 2048);
+}
+
+// Fills in how rows are cut, and gives how many go through the kernels at once.
+static uint32_t cut_rows(SampleArgs& a, uint32_t rows, uint64_t vocab) {
+  a.vocab = (uint32_t)vocab, a.slice = slice_of(rows, vocab), a.slices = (a.vocab + a.slice - 1) / a.slice;
+  a.common = std::min<uint32_t>(kList, (a.vocab + 1) / 2 * 2);
+  return std::min(rows, std::max(1u, kAtOnce / a.slices));
 }
 
 template <class T>
-static hl_status run_sample(const SampleArgs& a, uint32_t rows, hipStream_t s) {
-  const dim3 grid(a.slices, rows);
-  hl_status st = enqueue(top_kernel<T>, grid, dim3(kThreads), s, a);
-  if (st == HL_OK) st = enqueue(step_kernel<T>, grid, dim3(kThreads), s, a);
-  if (st == HL_OK) st = enqueue(list_kernel<T>, grid, dim3(kThreads), s, a);
-  return st == HL_OK ? enqueue(end_kernel<T>, dim3(rows), dim3(kEnd), s, a) : st;
+static hl_status run_sample(SampleArgs a, uint32_t rows, uint32_t each, hipStream_t s) {
+  for (uint32_t first = 0; first < rows; first += each) {
+    const uint32_t n = std::min(each, rows - first);
+    const dim3 grid(a.slices, n);
+    hl_status st = enqueue(top_kernel<T>, grid, dim3(kThreads), s, a);
+    if (st == HL_OK) st = enqueue(step_kernel<T>, grid, dim3(kThreads), s, a);
+    if (st == HL_OK) st = enqueue(list_kernel<T>, grid, dim3(kThreads), s, a);
+    if (st == HL_OK) st = enqueue(end_kernel<T>, dim3(n), dim3(kEnd), s, a);
+    if (st != HL_OK) return st;
+    a.logits = static_cast<const T*>(a.logits) + n * a.stride;
+    a.uniforms += n, a.tokens += n, a.logprobs += n;
+    if (a.temperatures) a.temperatures += n;
+    if (a.top_ks) a.top_ks += n;
+    if (a.top_ps) a.top_ps += n;
+    if (a.min_ps) a.min_ps += n;
+  }
+  return HL_OK;
 }
 
 }  // namespace hl
@@ -930,8 +992,9 @@ using namespace hl;
 
 extern "C" size_t hl_sample_workspace_bytes(uint32_t rows, uint64_t vocab) {
   if (rows == 0 || rows > 65535 || vocab == 0 || vocab >= (1u << 20)) return 0;
-  const uint64_t slice = slice_of(rows, vocab);
-  return rows * (sizeof(RowWork) + (vocab + slice - 1) / slice * sizeof(SliceWork));
+  SampleArgs a = {};
+  const uint64_t at_once = cut_rows(a, rows, vocab);
+  return at_once * a.row_bytes();
 }
 
 extern "C" hl_status hl_sample(const hl_sampling* sampling, const void* logits_dev, hl_dtype dtype, uint64_t row_stride,
@@ -948,16 +1011,16 @@ extern "C" hl_status hl_sample(const hl_sampling* sampling, const void* logits_d
                         (const void*)sampling->top_p_dev, (const void*)sampling->min_p_dev})
     if (!aligned(p, 4)) return HL_EINVAL;
   if (vocab >= (1u << 20) || row_stride >= (1ull << 40) || rows > 65535) return HL_EUNSUPPORTED;
-  if (workspace_bytes < hl_sample_workspace_bytes(rows, vocab)) return HL_EINVAL;
   SampleArgs a = {};
-  a.logits = logits_dev, a.stride = row_stride, a.vocab = (uint32_t)vocab, a.uniforms = uniforms_dev;
-  a.slice = slice_of(rows, vocab), a.slices = (uint32_t)((vocab + a.slice - 1) / a.slice);
+  const uint32_t at_once = cut_rows(a, rows, vocab);
+  if (workspace_bytes < at_once * a.row_bytes()) return HL_EINVAL;
+  a.logits = logits_dev, a.stride = row_stride, a.uniforms = uniforms_dev;
   a.temperatures = sampling->temperature_dev, a.top_ks = sampling->top_k_dev;
   a.top_ps = sampling->top_p_dev, a.min_ps = sampling->min_p_dev;
   a.temperature = sampling->temperature, a.top_k = sampling->top_k, a.top_p = sampling->top_p, a.min_p = sampling->min_p;
   a.tokens = tokens_dev, a.logprobs = logprobs_dev, a.work = static_cast<uint8_t*>(workspace_dev);
   const hipStream_t s = (hipStream_t)stream;
-  return dtype == HL_F32    ? run_sample<float>(a, rows, s)
-         : dtype == HL_BF16 ? run_sample<__bf16>(a, rows, s)
-                            : run_sample<_Float16>(a, rows, s);
+  return dtype == HL_F32    ? run_sample<float>(a, rows, at_once, s)
+         : dtype == HL_BF16 ? run_sample<__bf16>(a, rows, at_once, s)
+                            : run_sample<_Float16>(a, rows, at_once, s);
 }

@@ -26,3 +26,12 @@ def test_attention_of_many_rows_holds_no_second_cache(dtype, queries):
     tiles = queries * 4 // 64
     parts = 512 + 8 * 16 * tiles + 16 * 8 * tiles
     assert need <= parts * 64 * (128 + 2) * 4 + 4096
+
+
+@pytest.mark.parametrize("rows,vocab,most", [
+    (1, 1, 32 << 10), (1, 32000, 256 << 10), (40000, 5, 110 << 20), (65535, 131072, 64 << 20), (4096, 32000, 110 << 20),
+    (256, 131072, 32 << 20), (61, 50001, 11 << 20), (1, (1 << 20) - 1, 1 << 20), (65535, (1 << 20) - 1, 64 << 20),
+    (2048, 2048, 90 << 20), (65535, 16384, 170 << 20)])
+def test_sampling(rows, vocab, most):
+    # rows past what fills the GPU reuse their predecessors' room, and a row has one list
+    assert 0 < hl.lib().hl_sample_workspace_bytes(rows, vocab) <= most
