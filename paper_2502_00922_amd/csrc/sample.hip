@@ -3,8 +3,9 @@
 //
 // Weights are 2^((l - max) log2(e) / T), computed in float64 and held as whole
 // numbers of 2^-43 of the greatest: sums of them are exact, so they do not depend
-// on the order of additions, and equal logits have equal weights. Tokens below 2^-40
-// of the greatest weigh nothing. The tokens that top-k and top-p keep are the first
+// on the order of additions, and equal logits have equal weights. (A light weight has few
+// bits of its own, three at 2^-40: sums over n tokens are off by n * 2^-43 at most.) Tokens
+// below 2^-40 of the greatest weigh nothing. The tokens that top-k and top-p keep are the first
 // ones by (logit, lowest index); where they end is found in two steps: a histogram
 // of the distances to the greatest logit says in which of kSteps steps, and the few
 // logits of that step, put on a list in the order of their indexes, say where in it.
