@@ -44,15 +44,15 @@ struct Tile4 {
   uint32_t ve[8];
 };
 
-template <int G, int R>
+template <int G>
 struct State4 {
   static constexpr int E = G > 4 ? 2 : 1;
-  u32x4 q[R][G], e[R][E];  // e: pieces of (minus what is too much of q's sums, Q_g)
-  f32x4 o[R][2 * G];       // o[2g + i][r] is column 32g + 8c + 2r + i
-  f32x4 base[R];           // sums of p times the pairs' element 4c + r
-  float mean[R][G];        // this lane's part of the sum of p * base, of steps with hidden keys
-  float m[R], l[R], limit[R];
-  uint32_t seen[R];
+  u32x4 q[G], e[E];  // e: pieces of (minus what is too much of q's sums, Q_g)
+  f32x4 o[2 * G];    // o[2g + i][r] is column 32g + 8c + 2r + i
+  f32x4 base;        // sums of p times the pairs' element 4c + r
+  float mean[G];     // this lane's part of the sum of p * base, of steps with hidden keys
+  float m, l, limit;
+  uint32_t seen;
 };
 
 // 16 + code as operands, from the low bytes of two halves: even columns' codes are in
@@ -157,13 +157,13 @@ __device__ inline void keep(const u32x4 (&v)[N]) {
 
 // One step: scores of 32 keys, their weights, and the weighted values. EDGE:
 // some query may not see some of the keys, whatever their rows hold.
-template <class T, int G, int R, bool EDGE>
-__device__ inline void step4(State4<G, R>& st, const Tile4<G>& t, const Codes4<T>& kf, const Codes4<__bf16>& vf,
+template <class T, int G, bool EDGE>
+__device__ inline void step4(State4<G>& st, const Tile4<G>& t, const Codes4<T>& kf, const Codes4<__bf16>& vf,
                              const AttentionArgs& a, const Item& it, uint32_t key, uint32_t wave_row) {
-  using S = State4<G, R>;
+  using S = State4<G>;
   const uint32_t lane = lane_id(), n = lane % 16, c = lane / 16;
   const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-  f32x4 s[R][2];
+  f32x4 s[2];
   constexpr int KSET = G > 4 ? 2 : G;  // groups whose products follow each other
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -181,19 +181,15 @@ __device__ inline void step4(State4<G, R>& st, const Tile4<G>& t, const Codes4<T
         asm volatile("" : "+v"(codes[i]));
       }
       __builtin_amdgcn_sched_barrier(0);
-      f32x4 part[R][KSET], scale[KSET];
+      f32x4 part[KSET], scale[KSET];
 #pragma unroll
       for (int i = 0; i < KSET; ++i) {
         scale[i] = mfma<__bf16>(pairs[0], one[i], zero);
-#pragma unroll
-        for (int rt = 0; rt < R; ++rt) part[rt][i] = mfma<T>(codes[i], st.q[rt][g0 + i < G ? g0 + i : G - 1], zero);
+        part[i] = mfma<T>(codes[i], st.q[g0 + i < G ? g0 + i : G - 1], zero);
       }
       if (g0 == 0) {
-#pragma unroll
-        for (int rt = 0; rt < R; ++rt) {
-          s[rt][h] = mfma<__bf16>(pairs[0], st.e[rt][0], zero);
-          if constexpr (S::E == 2) s[rt][h] = mfma<__bf16>(pairs[0], st.e[rt][1], s[rt][h]);
-        }
+        s[h] = mfma<__bf16>(pairs[0], st.e[0], zero);
+        if constexpr (S::E == 2) s[h] = mfma<__bf16>(pairs[0], st.e[1], s[h]);
       }
       products_end();
       keep(codes), keep(one), keep(pairs);
@@ -201,56 +197,50 @@ __device__ inline void step4(State4<G, R>& st, const Tile4<G>& t, const Codes4<T
       for (int i = 0; i < KSET; ++i)
         if (g0 + i < G) {
 #pragma unroll
-          for (int rt = 0; rt < R; ++rt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) s[rt][h][r] = fmaf(scale[i][r], part[rt][i][r], s[rt][h][r]);
+          for (int r = 0; r < 4; ++r) s[h][r] = fmaf(scale[i][r], part[i][r], s[h][r]);
         }
     }
   }
-  float p[R][8];
+  float p[8];
+  if constexpr (EDGE) {
 #pragma unroll
-  for (int rt = 0; rt < R; ++rt) {
-    if constexpr (EDGE) {
+    for (int e = 0; e < 8; ++e)
+      if (key + key_of(c, e) >= st.seen) s[e / 4][e % 4] = -INFINITY;
+  }
+  if (it.scores) {
+    const uint32_t row = here(wave_row + n);  // nothing of this is formed in a call without weights
+    if (row < it.rows) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (key + key_of(c, e) >= st.seen[rt]) s[rt][e / 4][e % 4] = -INFINITY;
+      for (int h = 0; h < 2; ++h)
+        *reinterpret_cast<f32x4*>(it.scores + (uint64_t)row * a.score_stride + key + 16 * h + 4 * c) = s[h] * a.scale2;
     }
-    if (it.scores) {
-      const uint32_t row = here(wave_row + 16 * rt + n);  // nothing of this is formed in a call without weights
-      if (row < it.rows) {
+  }
+  float top = -INFINITY;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          *reinterpret_cast<f32x4*>(it.scores + (uint64_t)row * a.score_stride + key + 16 * h + 4 * c) =
-              s[rt][h] * a.scale2;
-      }
+  for (int e = 0; e < 8; ++e) top = fmaxf(top, s[e / 4][e % 4]);
+  top *= a.scale2;
+  // The maximum need only be near the true one, as for 16 bits.
+  if (__any(top > st.limit)) {
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const bool had = st.limit != -INFINITY;
+    const float was = st.m;
+    const float now = had ? fmaxf(was, top) : top;
+    if (now != -INFINITY) {
+      const float f = had ? __builtin_amdgcn_exp2f(was - now) : 0.0f;
+      st.m = now, st.limit = now + kSlack;
+      st.l *= f;
+#pragma unroll
+      for (int i = 0; i < 2 * G; ++i) st.o[i] *= f;
+      st.base *= f;
+#pragma unroll
+      for (int g = 0; g < G; ++g) st.mean[g] *= f;
     }
-    float top = -INFINITY;
+  }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) top = fmaxf(top, s[rt][e / 4][e % 4]);
-    top *= a.scale2;
-    // The maximum need only be near the true one, as for 16 bits.
-    if (__any(top > st.limit[rt])) {
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const bool had = st.limit[rt] != -INFINITY;
-      const float was = st.m[rt];
-      const float now = had ? fmaxf(was, top) : top;
-      if (now != -INFINITY) {
-        const float f = had ? __builtin_amdgcn_exp2f(was - now) : 0.0f;
-        st.m[rt] = now, st.limit[rt] = now + kSlack;
-        st.l[rt] *= f;
-#pragma unroll
-        for (int i = 0; i < 2 * G; ++i) st.o[rt][i] *= f;
-        st.base[rt] *= f;
-#pragma unroll
-        for (int g = 0; g < G; ++g) st.mean[rt][g] *= f;
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      p[rt][e] = __builtin_amdgcn_exp2f(fmaf(s[rt][e / 4][e % 4], a.scale2, -st.m[rt]));
-      st.l[rt] += p[rt][e];
-    }
+  for (int e = 0; e < 8; ++e) {
+    p[e] = __builtin_amdgcn_exp2f(fmaf(s[e / 4][e % 4], a.scale2, -st.m));
+    st.l += p[e];
   }
   // w is rounded to bf16, whose range holds any scale. Where the output has 11
   // bits, what the rounding leaves is a second operand.
@@ -273,17 +263,16 @@ __device__ inline void step4(State4<G, R>& st, const Tile4<G>& t, const Codes4<T
   asm volatile("" : "+v"(less[0]));
   // rows whose keys all queries see: p times the pairs' elements, for the bases
   constexpr int BASES = EDGE ? 0 : 1;
-  u32x4 pairs[1], pw[R * PIECES];
+  u32x4 pairs[1], pw[PIECES];
   if constexpr (!EDGE) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) pairs[0][j] = t.ve[2 * j] | t.ve[2 * j + 1] << 16;
     asm volatile("" : "+v"(pairs[0]));
-#pragma unroll
-    for (int rt = 0; rt < R; ++rt) round(&pw[rt * PIECES], p[rt]);
+    round(&pw[0], p);
   }
   each<G / SET>([&](auto nth) {
     constexpr int g0 = decltype(nth)::value * SET;
-    u32x4 codes[2 * SET], w[R * SET * PIECES];
+    u32x4 codes[2 * SET], w[SET * PIECES];
     each<SET>([&](auto mth) {
       constexpr int i = decltype(mth)::value, g = g0 + i;
 #pragma unroll
@@ -293,40 +282,33 @@ __device__ inline void step4(State4<G, R>& st, const Tile4<G>& t, const Codes4<T
         codes[2 * i][j] = vf.low(both), codes[2 * i + 1][j] = vf.high(both);
       }
       asm volatile("" : "+v"(codes[2 * i]), "+v"(codes[2 * i + 1]));
+      float x[8];
+      times_lane<2 * g>(x, scales, p);
+      if constexpr (EDGE) {
 #pragma unroll
-      for (int rt = 0; rt < R; ++rt) {
-        float x[8];
-        times_lane<2 * g>(x, scales, p[rt]);
-        if constexpr (EDGE) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            // a row that the query does not see may hold anything
-            const bool sees = key + key_of(c, e) < st.seen[rt];
-            const float b = fmaf(p[rt][e], from_lane<2 * g + 1>(scales[e]), st.mean[rt][g]);
-            x[e] = sees ? x[e] : 0.0f;
-            st.mean[rt][g] = sees ? b : st.mean[rt][g];
-          }
+        for (int e = 0; e < 8; ++e) {
+          // a row that the query does not see may hold anything
+          const bool sees = key + key_of(c, e) < st.seen;
+          const float b = fmaf(p[e], from_lane<2 * g + 1>(scales[e]), st.mean[g]);
+          x[e] = sees ? x[e] : 0.0f;
+          st.mean[g] = sees ? b : st.mean[g];
         }
-        round(&w[(i * R + rt) * PIECES], x);
       }
+      round(&w[i * PIECES], x);
     });
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < SET; ++i)
 #pragma unroll
-      for (int rt = 0; rt < R; ++rt)
-#pragma unroll
-        for (int y = 0; y < PIECES; ++y) {
-          const u32x4 x = w[(i * R + rt) * PIECES + y];
-          f32x4 &even = st.o[rt][2 * (g0 + i)], &odd = st.o[rt][2 * (g0 + i) + 1];
-          even = mfma<__bf16>(codes[2 * i], x, even), odd = mfma<__bf16>(codes[2 * i + 1], x, odd);
-          even = mfma<__bf16>(less[0], x, even), odd = mfma<__bf16>(less[0], x, odd);
-        }
+      for (int y = 0; y < PIECES; ++y) {
+        const u32x4 x = w[i * PIECES + y];
+        f32x4 &even = st.o[2 * (g0 + i)], &odd = st.o[2 * (g0 + i) + 1];
+        even = mfma<__bf16>(codes[2 * i], x, even), odd = mfma<__bf16>(codes[2 * i + 1], x, odd);
+        even = mfma<__bf16>(less[0], x, even), odd = mfma<__bf16>(less[0], x, odd);
+      }
     if constexpr (g0 == 0 && BASES) {
 #pragma unroll
-      for (int rt = 0; rt < R; ++rt)
-#pragma unroll
-        for (int y = 0; y < PIECES; ++y) st.base[rt] = mfma<__bf16>(pairs[0], pw[rt * PIECES + y], st.base[rt]);
+      for (int y = 0; y < PIECES; ++y) st.base = mfma<__bf16>(pairs[0], pw[y], st.base);
     }
     products_end();
     keep(codes), keep(w), keep(less);
@@ -335,73 +317,70 @@ __device__ inline void step4(State4<G, R>& st, const Tile4<G>& t, const Codes4<T
 }
 
 // Starts a wave's state: its queries, from row `wave_row` of the item's head.
-template <class T, int G, int R>
-__device__ inline void begin4(State4<G, R>& st, const AttentionArgs& a, const Item& it, uint32_t wave_row) {
-  using S = State4<G, R>;
+template <class T, int G>
+__device__ inline void begin4(State4<G>& st, const AttentionArgs& a, const Item& it, uint32_t wave_row) {
+  using S = State4<G>;
   typedef T pair __attribute__((ext_vector_type(2)));
   const uint32_t lane = lane_id(), n = lane % 16, c = lane / 16;
+  st.m = 0.0f, st.l = 0.0f, st.limit = -INFINITY;
+  const uint32_t row = min(wave_row + n, it.rows - 1), tok = row / a.share;
+  st.seen = seen_by(a, it, row);
+  const uint16_t* q = it.q + ((uint64_t)tok * a.heads + row % a.share) * (32 * G);
+  float sum[G], less[G];
+  st.base = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-  for (int rt = 0; rt < R; ++rt) {
-    st.m[rt] = 0.0f, st.l[rt] = 0.0f, st.limit[rt] = -INFINITY;
-    const uint32_t row = min(wave_row + 16 * rt + n, it.rows - 1), tok = row / a.share;
-    st.seen[rt] = seen_by(a, it, row);
-    const uint16_t* q = it.q + ((uint64_t)tok * a.heads + row % a.share) * (32 * G);
-    float sum[G], less[G];
-    st.base[rt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int g = 0; g < G; ++g) {
+    st.o[2 * g] = st.o[2 * g + 1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    st.mean[g] = 0.0f;
+    const u32x4 x = (*reinterpret_cast<const u32x4*>(q + 32 * g + 8 * c) & a.q_and) ^ a.q_xor;
+    float all = 0.0f;
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-      st.o[rt][2 * g] = st.o[rt][2 * g + 1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      st.mean[rt][g] = 0.0f;
-      const u32x4 x = (*reinterpret_cast<const u32x4*>(q + 32 * g + 8 * c) & a.q_and) ^ a.q_xor;
-      float all = 0.0f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t two = x[j];  // an element itself is not what a bit cast takes
-        const pair y = __builtin_bit_cast(pair, two);
-        all += (float)y[0] + (float)y[1];
-      }
-      sum[g] = over_lanes(all), less[g] = -kTooMuch * sum[g];
-      // the order in which a pair of bytes gives its codes
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        st.q[rt][g][j] = __builtin_amdgcn_perm(x[j / 2 * 2 + 1], x[j / 2 * 2], j % 2 ? 0x07060302u : 0x05040100u);
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t two = x[j];  // an element itself is not what a bit cast takes
+      const pair y = __builtin_bit_cast(pair, two);
+      all += (float)y[0] + (float)y[1];
     }
-    // pieces 0, 1 and 2 of a float32, of 8 bits each
-    const auto piece = [](float x, uint32_t i) {
-      const float p0 = (float)(__bf16)x, p1 = (float)(__bf16)(x - p0), p2 = x - p0 - p1;
-      return i == 0 ? p0 : i == 1 ? p1 : i == 2 ? p2 : 0.0f;
-    };
+    sum[g] = over_lanes(all), less[g] = -kTooMuch * sum[g];
+    // the order in which a pair of bytes gives its codes
 #pragma unroll
-    for (int e = 0; e < S::E; ++e)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t part = S::E == 1 ? c : 2 * e + c / 2;
-        const auto of = [&](const float (&v)[G]) {
-          float x = j < G ? v[j < G ? j : 0] : 0.0f;
-          if constexpr (S::E == 2) {
-            float y = 4 + j < G ? v[4 + j < G ? 4 + j : 0] : 0.0f;
-            asm volatile("" : "+v"(x), "+v"(y));  // two registers, no array in memory
-            x = c % 2 ? y : x;
-          }
-          return piece(x, part);
-        };
-        st.e[rt][e][j] = pack<__bf16>(of(less), of(sum));
-      }
+    for (int j = 0; j < 4; ++j)
+      st.q[g][j] = __builtin_amdgcn_perm(x[j / 2 * 2 + 1], x[j / 2 * 2], j % 2 ? 0x07060302u : 0x05040100u);
   }
+  // pieces 0, 1 and 2 of a float32, of 8 bits each
+  const auto piece = [](float x, uint32_t i) {
+    const float p0 = (float)(__bf16)x, p1 = (float)(__bf16)(x - p0), p2 = x - p0 - p1;
+    return i == 0 ? p0 : i == 1 ? p1 : i == 2 ? p2 : 0.0f;
+  };
+#pragma unroll
+  for (int e = 0; e < S::E; ++e)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t part = S::E == 1 ? c : 2 * e + c / 2;
+      const auto of = [&](const float (&v)[G]) {
+        float x = j < G ? v[j < G ? j : 0] : 0.0f;
+        if constexpr (S::E == 2) {
+          float y = 4 + j < G ? v[4 + j < G ? 4 + j : 0] : 0.0f;
+          asm volatile("" : "+v"(x), "+v"(y));  // two registers, no array in memory
+          x = c % 2 ? y : x;
+        }
+        return piece(x, part);
+      };
+      st.e[e][j] = pack<__bf16>(of(less), of(sum));
+    }
 }
 
 // A wave's share of an item's keys [.., k1) for its rows: 32 from `key` on, and
 // again every `stride`. Loads are a step ahead, and there are always as many of them
 // (at the end, of the last step again): waits count them.
-template <class T, int G, int R>
-__device__ inline void keys4(State4<G, R>& st, const AttentionArgs& a, const Item& it, uint32_t wave_row, uint32_t key,
+template <class T, int G>
+__device__ inline void keys4(State4<G>& st, const AttentionArgs& a, const Item& it, uint32_t wave_row, uint32_t key,
                              uint32_t k1, uint32_t stride) {
   const Codes4<T> kf;
   const Codes4<__bf16> vf;
-  const uint32_t all = seen_by(a, it, wave_row), most = seen_by(a, it, wave_row + 16 * R - 1), end = min(k1, most);
+  const uint32_t all = seen_by(a, it, wave_row), most = seen_by(a, it, wave_row + 15), end = min(k1, most);
   const uint32_t whole = min(end, all);  // steps that end here or before hide no key
   const auto run = [&](const Tile4<G>& t) __attribute__((always_inline)) {
-    step4<T, G, R, false>(st, t, kf, vf, a, it, key, wave_row);
+    step4<T, G, false>(st, t, kf, vf, a, it, key, wave_row);
     key += stride;
   };
   if (key + kStep <= whole) {
@@ -430,18 +409,18 @@ __device__ inline void keys4(State4<G, R>& st, const AttentionArgs& a, const Ite
   for (; key < end; key += stride) {
     Tile4<G> t;
     load4<G, true>(t, it, key);
-    step4<T, G, R, true>(st, t, kf, vf, a, it, key, wave_row);
+    step4<T, G, true>(st, t, kf, vf, a, it, key, wave_row);
   }
 }
 
 // Columns 32g + 8c .. of a wave's query n, eight for each group: out(first column, four of them).
-template <int G, int R, class Out>
-__device__ inline void columns4(const State4<G, R>& st, int rt, Out out) {
+template <int G, class Out>
+__device__ inline void columns4(const State4<G>& st, Out out) {
   const uint32_t n = lane_id() % 16, c = lane_id() / 16;
 #pragma unroll
   for (int g = 0; g < G; ++g) {
-    const float shift = over_lanes(st.mean[rt][g]) + __shfl(st.base[rt][(2 * g + 1) % 4], (2 * g + 1) / 4 * 16 + n);
-    const f32x4 x = st.o[rt][2 * g], y = st.o[rt][2 * g + 1];
+    const float shift = over_lanes(st.mean[g]) + __shfl(st.base[(2 * g + 1) % 4], (2 * g + 1) / 4 * 16 + n);
+    const f32x4 x = st.o[2 * g], y = st.o[2 * g + 1];
     out(32 * g + 8 * c, f32x4{x[0] + shift, y[0] + shift, x[1] + shift, y[1] + shift});
     out(32 * g + 8 * c + 4, f32x4{x[2] + shift, y[2] + shift, x[3] + shift, y[3] + shift});
   }
@@ -450,15 +429,15 @@ __device__ inline void columns4(const State4<G, R>& st, int rt, Out out) {
 // Adds the results that WAVES waves have of the same 16 rows and calls
 // out(row, d, o, m, l) for four columns from d on of each of the first `rows`.
 template <int G, int WAVES, class Out>
-__device__ inline void add_waves4(const State4<G, 1>& st, uint32_t rows, float* lds, Out out) {
+__device__ inline void add_waves4(const State4<G>& st, uint32_t rows, float* lds, Out out) {
   constexpr uint32_t D = 32 * G;
   const uint32_t lane = lane_id(), n = lane % 16, c = lane / 16;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   float* lds_ml = lds + WAVES * 16 * (D + 4);
-  const float sum = over_lanes(st.l[0]);
+  const float sum = over_lanes(st.l);
   const uint32_t at = here(wave * 16 + n);  // formed here: no register holds it through the loops
-  if (c == 0) lds_ml[2 * at] = st.limit[0] != -INFINITY || sum != sum ? st.m[0] : -INFINITY, lds_ml[2 * at + 1] = sum;
-  columns4<G, 1>(st, 0, [&](uint32_t d, f32x4 o) { *reinterpret_cast<f32x4*>(lds + (uint64_t)at * (D + 4) + d) = o; });
+  if (c == 0) lds_ml[2 * at] = st.limit != -INFINITY || sum != sum ? st.m : -INFINITY, lds_ml[2 * at + 1] = sum;
+  columns4<G>(st, [&](uint32_t d, f32x4 o) { *reinterpret_cast<f32x4*>(lds + (uint64_t)at * (D + 4) + d) = o; });
   __syncthreads();
   for (uint32_t x = here(threadIdx.x); x < rows * (D / 4); x += WAVES * 64) {
     const uint32_t row = x / (D / 4), d = x % (D / 4) * 4;
@@ -483,9 +462,9 @@ __device__ inline void narrow_part4(const AttentionArgs& a, const Item& it, uint
                                     float* lds) {
   constexpr uint32_t H = held4<G>();
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  State4<G, 1> st;
-  begin4<T, G, 1>(st, a, it, 0);
-  keys4<T, G, 1>(st, a, it, 0, k0 + kStep * wave, k1, kUnit);
+  State4<G> st;
+  begin4<T, G>(st, a, it, 0);
+  keys4<T, G>(st, a, it, 0, k0 + kStep * wave, k1, kUnit);
   float* po = a.narrow_o + (uint64_t)slot * a.narrow_rows * H;
   float* pml = a.narrow_ml + (uint64_t)slot * a.narrow_rows * 2;
   add_waves4<G, kWaves>(st, it.rows, lds, [&](uint32_t row, uint32_t d, f32x4 o, float m, float l) {
@@ -497,45 +476,43 @@ __device__ inline void narrow_part4(const AttentionArgs& a, const Item& it, uint
 
 // Keys [k0, k1) of a wide item by one block, whose waves take different rows;
 // each writes its rows of the part at `slot`.
-template <class T, int G, int R>
+template <class T, int G>
 __device__ inline void wide_part4(const AttentionArgs& a, const Item& it, uint32_t k0, uint32_t k1, uint32_t slot) {
   constexpr uint32_t H = held4<G>();
   const uint32_t n = lane_id() % 16, c = lane_id() / 16;
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wave_row = it.row0 + wave * 16 * R;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wave_row = it.row0 + wave * 16;
   if (wave_row >= it.rows) return;
-  State4<G, R> st;
-  begin4<T, G, R>(st, a, it, wave_row);
-  keys4<T, G, R>(st, a, it, wave_row, k0, k1, kStep);
+  State4<G> st;
+  begin4<T, G>(st, a, it, wave_row);
+  keys4<T, G>(st, a, it, wave_row, k0, k1, kStep);
   float* po = a.wide_o + (uint64_t)slot * a.wide_rows * H;
   float* pml = a.wide_ml + (uint64_t)slot * a.wide_rows * 2;
-#pragma unroll
-  for (int rt = 0; rt < R; ++rt) {
-    const float sum = over_lanes(st.l[rt]);
-    const uint32_t row = here(wave * 16 * R + 16 * rt + n);
-    const bool in = it.row0 + row < it.rows;
-    if (in && c == 0)
-      pml[2 * row] = st.limit[rt] != -INFINITY || sum != sum ? st.m[rt] : -INFINITY, pml[2 * row + 1] = sum;
-    columns4<G, R>(st, rt, [&](uint32_t d, f32x4 o) {
-      if (in) *reinterpret_cast<f32x4*>(po + (uint64_t)row * H + d) = o;
-    });
-  }
+  const float sum = over_lanes(st.l);
+  const uint32_t row = here(wave * 16 + n);
+  const bool in = it.row0 + row < it.rows;
+  if (in && c == 0)
+    pml[2 * row] = st.limit != -INFINITY || sum != sum ? st.m : -INFINITY, pml[2 * row + 1] = sum;
+  columns4<G>(st, [&](uint32_t d, f32x4 o) {
+    if (in) *reinterpret_cast<f32x4*>(po + (uint64_t)row * H + d) = o;
+  });
 }
 
-// RW: 16-row tiles of a wave in wide items (0: the call has none).
-template <class T, int G, int RW>
+// WIDE: whether the call has wide items. A wave has 16 rows of them: two such tiles (128
+// columns) would not fit its registers.
+template <class T, int G, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 2) parts4_kernel(AttentionArgs a) {
   __shared__ __attribute__((aligned(16))) float lds[kWaves * 16 * (32 * G + 4) + kWaves * 16 * 2];
   const OwnLine line = a.own.tokens ? own_line(a, 0) : OwnLine{0, 0, 0};
   const Lines l = lines_of(a, own_units_before(a, line, a.batch));
   const uint32_t xcd = blockIdx.x % 8, nth = blockIdx.x / 8, wide = l.wide_blocks / 8;
-  if (RW && nth < wide) {
+  if (WIDE && nth < wide) {
     const uint32_t taker = xcd * wide + nth;
     if (taker >= l.wide.takers) return;
     const uint32_t end = l.wide.first(taker + 1);
     for (uint32_t u = l.wide.first(taker); u < end;) {
       const Place p = place_of<true>(a, line, l, u);
       const uint32_t take = min(p.each - p.in, end - u);
-      wide_part4<T, G, RW ? RW : 1>(a, p.it, p.in * kUnit, (p.in + take) * kUnit, taker + p.item);
+      wide_part4<T, G>(a, p.it, p.in * kUnit, (p.in + take) * kUnit, taker + p.item);
       u += take;
     }
     return;
@@ -564,13 +541,13 @@ __global__ void __launch_bounds__(kSoloWaves * 64, 2) solo4_kernel(AttentionArgs
   if (a.own.tokens) own = own_item(a, b, head, 0);
   Item pre = prefix_item(a, head, 0);
   pre.q += (uint64_t)b * a.queries * a.heads * a.dim, pre.rows = rows;
-  State4<G, 1> st;
-  begin4<T, G, 1>(st, a, pre, 0);  // every row sees the whole prefix
-  if (pre.keys) keys4<T, G, 1>(st, a, pre, 0, kStep * wave, pre.keys, stride);
+  State4<G> st;
+  begin4<T, G>(st, a, pre, 0);  // every row sees the whole prefix
+  if (pre.keys) keys4<T, G>(st, a, pre, 0, kStep * wave, pre.keys, stride);
   if (a.own.tokens) {
-    st.seen[0] = seen_by(a, own, lane_id() % 16);
+    st.seen = seen_by(a, own, lane_id() % 16);
     // the waves that had a step of the prefix less than the others begin
-    keys4<T, G, 1>(st, a, own, 0, kStep * ((wave - (pre.keys + kStep - 1) / kStep) % kSoloWaves), own.keys, stride);
+    keys4<T, G>(st, a, own, 0, kStep * ((wave - (pre.keys + kStep - 1) / kStep) % kSoloWaves), own.keys, stride);
   }
   const uint64_t first = (uint64_t)b * a.queries * a.heads + (uint64_t)head * a.share;
   add_waves4<G, kSoloWaves>(st, rows, lds, [&](uint32_t row, uint32_t d, f32x4 o, float m, float l) {
@@ -599,12 +576,8 @@ static hl_status run4(const AttentionPlan& pl, hl_dtype dtype, hipStream_t s) {
   const AttentionArgs& a = pl.a;
   if (pl.solo) return enqueue(solo4_kernel<T, G>, dim3(a.kv_heads, a.batch), dim3(kSoloWaves * 64), s, a);
   const dim3 blocks(a.blocks), threads(kThreads);
-  hl_status st;
-  if (!pl.wide) {
-    st = enqueue(parts4_kernel<T, G, 0>, blocks, threads, s, a);
-  } else {
-    st = enqueue(parts4_kernel<T, G, 1>, blocks, threads, s, a);
-  }
+  const hl_status st = pl.wide ? enqueue(parts4_kernel<T, G, true>, blocks, threads, s, a)
+                               : enqueue(parts4_kernel<T, G, false>, blocks, threads, s, a);
   return st != HL_OK ? st : attention_join(pl, dtype, s);
 }
 

@@ -207,11 +207,11 @@ __device__ inline void load_chunk(Chunk<RT>& k, const Gemv4Args& a, const uint8_
   for (int t = 0; t < 4; ++t) k.x[t] = *reinterpret_cast<const u32x4*>(x + 2 * min(col + 32 * t, a.cols - 32) + b);
 }
 
-// The product's loop reads RING - 1 chunks ahead of the one it multiplies: everything
+// The product's loop reads a chunk ahead of the one it multiplies: everything
 // that a chunk takes is on its way before, x as well, for loads come back in order and
 // a wait for x would be one for the codes behind it.
 // W waves a block; T, S: types of x and of the scales.
-template <class T, class S, int GROUP, bool BASES, int RT, int RING, int W>
+template <class T, class S, int GROUP, bool BASES, int RT, int W>
 __global__ void __launch_bounds__(64 * W, 2) gemv4_kernel(Gemv4Args a) {
   constexpr int PARTS = 128 / GROUP, EACH = 4 / PARTS;  // groups of a chunk, instructions of a group
   constexpr int SET = RT < 2 ? RT : 2;                  // row tiles whose products follow each other
@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(64 * W, 2) gemv4_kernel(Gemv4Args a) {
     load_scales<GROUP, RT>(next_scale, a, first_scale, col / GROUP, total, scale_row);
     if constexpr (BASES) load_scales<GROUP, RT>(next_base, a, first_base, col / GROUP, total, scale_row);
   };
-  Chunk<RT> ring[RING];
+  Chunk<RT> ring[2];
   // Blocks begin at different columns: rows are often a power of two apart, and all
   // blocks at one column would keep few of the memory's channels busy.
   const uint32_t stretches = (a.cols + kStretch - 1) / kStretch, turn = blockIdx.x % stretches;
@@ -250,8 +250,7 @@ __global__ void __launch_bounds__(64 * W, 2) gemv4_kernel(Gemv4Args a) {
   uint32_t nth = wave, col = nth < stretches ? column(nth) : a.cols;
   if (nth < stretches) {
     scales_at(col);
-#pragma unroll
-    for (int i = 0; i < RING - 1; ++i) load_chunk<RT>(ring[i], a, first, row, b, col + 128 * i);
+    load_chunk<RT>(ring[0], a, first, row, b, col);
   }
   while (nth < stretches) {
     scale = next_scale;
@@ -260,11 +259,11 @@ __global__ void __launch_bounds__(64 * W, 2) gemv4_kernel(Gemv4Args a) {
     const uint32_t then = nth < stretches ? column(nth) : col;
     scales_at(then);
     every<kChunks>([&](auto chunk) {
-      constexpr int i = decltype(chunk)::value, ahead = i + RING - 1;
-      const uint32_t at = col + 128 * i, next = ahead < kChunks ? col + 128 * ahead : then + 128 * (ahead - kChunks);
-      load_chunk<RT>(ring[ahead % RING], a, first, row, b, next);
+      constexpr int i = decltype(chunk)::value;
+      const uint32_t at = col + 128 * i, next = i + 1 < kChunks ? at + 128 : then;
+      load_chunk<RT>(ring[(i + 1) % 2], a, first, row, b, next);
       if (at >= a.cols) return;
-      Chunk<RT>& k = ring[i % RING];
+      Chunk<RT>& k = ring[i % 2];
       if (at + 128 > a.cols) {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -361,8 +360,8 @@ __global__ void __launch_bounds__(64 * W, 2) gemv4_kernel(Gemv4Args a) {
 template <class T, class S, int GROUP, bool BASES>
 static hl_status run_gemv4(const Gemv4Args& a, hipStream_t s) {
   if (a.rows >= kTwoTiles)
-    return enqueue(gemv4_kernel<T, S, GROUP, BASES, 2, 2, 4>, dim3((a.rows + 31) / 32), dim3(256), s, a);
-  return enqueue(gemv4_kernel<T, S, GROUP, BASES, 1, 2, 8>, dim3((a.rows + 15) / 16), dim3(512), s, a);
+    return enqueue(gemv4_kernel<T, S, GROUP, BASES, 2, 4>, dim3((a.rows + 31) / 32), dim3(256), s, a);
+  return enqueue(gemv4_kernel<T, S, GROUP, BASES, 1, 8>, dim3((a.rows + 15) / 16), dim3(512), s, a);
 }
 
 template <class T, class S, int GROUP>
