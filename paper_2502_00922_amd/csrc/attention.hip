@@ -56,6 +56,7 @@ __device__ inline uint32_t beyond(uint32_t pair) {
   return (m - (m >> 15)) | m;
 }
 
+// D: columns held (64, 128 or 256); the head's own count may be less (FULL: it
 // is D). VE: neighbouring value columns of a lane, in HALVES groups of 16*VE.
 template <int D>
 struct Shape {

@@ -218,7 +218,6 @@ struct Item {
   uint32_t row0, rows;          // first row of the item's tile, rows of the whole head (and sequence)
 };
 
-// D: columns held (64, 128 or 256); the head's own count may be less (FULL: it
 // Key of value row e in lane group c, counted from the step's first: the order
 // in which the first product leaves its scores in a lane.
 __device__ inline uint32_t key_of(uint32_t c, int e) { return (e < 4 ? 0 : 12) + 4 * c + e; }
