@@ -839,6 +839,7 @@ def cache_evict(k, v, weights, lens, keep: int, recent: int = 0, k_out=None, v_o
 
 
 _SAMPLING = struct.Struct("=4Qfiff")
+_MOST = (2 - 2.0**-23) * 2.0**127  # of float32
 
 
 def cache4_row_bytes(dim: int) -> int:
@@ -888,7 +889,8 @@ def cache_write4(k, v, cache_k, cache_v, lens=None, stream=None) -> None:
     cache_k, cache_v: uint8 [batch, capacity, kv_heads, cache4_row_bytes(dim)] (any strides, in multiples of 16, with a
     row's bytes in a row). Token i of sequence b goes to slot lens[b] - tokens + i (lens: int32 [batch], the lengths with
     the new tokens; without it, to slot i); tokens whose slot is not in the cache are left out. 32 neighbouring columns
-    share a scale and a base; if one of them is an infinity or a NaN they all become NaN."""
+    share a scale and a base; if one of them is an infinity or a NaN they all become NaN. (cache_evict moves such caches
+    viewed as int16.)"""
     if stream is not None:
         return _on_stream(stream, k.get_device(), cache_write4, k, v, cache_k, cache_v, lens)
     T = _torch or _lookups()
@@ -1040,7 +1042,7 @@ def sample(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tok
             numbers.append(0)
         elif 0 <= value <= most:
             pointers.append(0)
-            numbers.append(value)
+            numbers.append(value if value == math.inf else min(value, _MOST))
         else:
             raise ValueError(f"{name} must be at least 0{'' if most == math.inf else ' and at most 1'}, got {value}")
     if tokens is None:
@@ -1051,7 +1053,7 @@ def sample(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tok
         logprobs = T.empty(need, dtype=T.float32, device=logits.device)
     else:
         _small(logprobs, "logprobs", T.float32, need, dev)
-    settings = _SAMPLING.pack(*pointers, numbers[0], min(int(numbers[1]), 0x7FFFFFFF), numbers[2], numbers[3])
+    settings = _SAMPLING.pack(*pointers, numbers[0], int(min(numbers[1], 0x7FFFFFFF)), numbers[2], numbers[3])
     if workspace is None:
         workspace = T.empty(T.lib.hl_sample_workspace_bytes(rows, vocab), dtype=T.uint8, device=logits.device)
     else:
