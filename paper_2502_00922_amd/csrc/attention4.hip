@@ -55,22 +55,6 @@ struct State4 {
   uint32_t seen;
 };
 
-// 16 + code as operands, from the low bytes of two halves: even columns' codes are in
-// a byte's low half, odd ones' in the high one. The mask is in a scalar register and the
-// exponents in a vector one, so that one instruction takes both.
-constexpr float kTooMuch = 24.0f;  // with the 8 that a code has too much
-template <class T>
-struct Codes4 {
-  static constexpr bool BF = std::is_same<T, __bf16>::value;
-  uint32_t mask, one;
-  __device__ Codes4() {
-    mask = BF ? 0x00780078u : 0x03C003C0u, one = BF ? 0x41804180u : 0x4C004C00u;
-    asm volatile("" : "+s"(mask), "+v"(one));
-  }
-  __device__ uint32_t low(uint32_t pair) const { return ((BF ? pair << 3 : pair << 6) & mask) | one; }
-  __device__ uint32_t high(uint32_t pair) const { return ((BF ? pair >> 1 : pair << 2) & mask) | one; }
-};
-
 // Bytes i and j (counted from the first word's) of words w as the low bytes of
 // two halves.
 template <int N>
@@ -139,15 +123,6 @@ __device__ inline void times_lane(float (&x)[8], const float (&s)[8], const floa
 #undef HL_TIMES
 }
 
-// f(0) .. f(N - 1), with the number known to the compiler.
-template <int N, class F>
-__device__ inline void each(F f) {
-  if constexpr (N > 0) {
-    each<N - 1>(f);
-    f(std::integral_constant<int, N - 1>());
-  }
-}
-
 // Keeps operands in their registers up to here, past products_end.
 template <int N>
 __device__ inline void keep(const u32x4 (&v)[N]) {
@@ -158,7 +133,7 @@ __device__ inline void keep(const u32x4 (&v)[N]) {
 // One step: scores of 32 keys, their weights, and the weighted values. EDGE:
 // some query may not see some of the keys, whatever their rows hold.
 template <class T, int G, bool EDGE>
-__device__ inline void step4(State4<G>& st, const Tile4<G>& t, const Codes4<T>& kf, const Codes4<__bf16>& vf,
+__device__ inline void step4(State4<G>& st, const Tile4<G>& t, const Codes<T>& kf, const Codes<__bf16>& vf,
                              const AttentionArgs& a, const Item& it, uint32_t key, uint32_t wave_row) {
   using S = State4<G>;
   const uint32_t lane = lane_id(), n = lane % 16, c = lane / 16;
@@ -175,7 +150,7 @@ __device__ inline void step4(State4<G>& st, const Tile4<G>& t, const Codes4<T>& 
       for (int i = 0; i < KSET; ++i) {
         const int g = g0 + i < G ? g0 + i : G - 1;
         const uint32_t p01 = bytes(t.k[h], g, G + g), p23 = bytes(t.k[h], 2 * G + g, 3 * G + g);
-        codes[i] = u32x4{kf.low(p01), kf.high(p01), kf.low(p23), kf.high(p23)};
+        codes[i] = u32x4{kf.template pair<0>(p01), kf.template pair<4>(p01), kf.template pair<0>(p23), kf.template pair<4>(p23)};
         one[i] = u32x4{0, 0, 0, 0};
         one[i][g % 4] = c == (uint32_t)(g / 4) ? 0x3F80u : 0;
         asm volatile("" : "+v"(codes[i]));
@@ -259,7 +234,8 @@ __device__ inline void step4(State4<G>& st, const Tile4<G>& t, const Codes4<T>& 
 #pragma unroll
     for (int y = 0; y < PIECES; ++y) asm volatile("" : "+v"(to[y]));
   };
-  u32x4 less[1] = {u32x4{0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u}};  // minus what is too much
+  constexpr uint32_t minus = Codes<__bf16>::LESS;
+  u32x4 less[1] = {u32x4{minus, minus, minus, minus}};
   asm volatile("" : "+v"(less[0]));
   // rows whose keys all queries see: p times the pairs' elements, for the bases
   constexpr int BASES = EDGE ? 0 : 1;
@@ -279,7 +255,7 @@ __device__ inline void step4(State4<G>& st, const Tile4<G>& t, const Codes4<T>& 
       for (int j = 0; j < 4; ++j) {
         const uint32_t both = __builtin_amdgcn_perm(t.v[2 * j + 1][g / 4], t.v[2 * j][g / 4],
                                                     0x0C000C00u | (uint32_t)(4 + g % 4) << 16 | (uint32_t)(g % 4));
-        codes[2 * i][j] = vf.low(both), codes[2 * i + 1][j] = vf.high(both);
+        codes[2 * i][j] = vf.pair<0>(both), codes[2 * i + 1][j] = vf.pair<4>(both);
       }
       asm volatile("" : "+v"(codes[2 * i]), "+v"(codes[2 * i + 1]));
       float x[8];
@@ -340,7 +316,7 @@ __device__ inline void begin4(State4<G>& st, const AttentionArgs& a, const Item&
       const pair y = __builtin_bit_cast(pair, two);
       all += (float)y[0] + (float)y[1];
     }
-    sum[g] = over_lanes(all), less[g] = -kTooMuch * sum[g];
+    sum[g] = over_lanes(all), less[g] = -24.0f * sum[g];
     // the order in which a pair of bytes gives its codes
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -375,8 +351,8 @@ __device__ inline void begin4(State4<G>& st, const AttentionArgs& a, const Item&
 template <class T, int G>
 __device__ inline void keys4(State4<G>& st, const AttentionArgs& a, const Item& it, uint32_t wave_row, uint32_t key,
                              uint32_t k1, uint32_t stride) {
-  const Codes4<T> kf;
-  const Codes4<__bf16> vf;
+  const Codes<T> kf;
+  const Codes<__bf16> vf;
   const uint32_t all = seen_by(a, it, wave_row), most = seen_by(a, it, wave_row + 15), end = min(k1, most);
   const uint32_t whole = min(end, all);  // steps that end here or before hide no key
   const auto run = [&](const Tile4<G>& t) __attribute__((always_inline)) {

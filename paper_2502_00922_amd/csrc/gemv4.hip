@@ -21,14 +21,9 @@
 #include <type_traits>
 
 #include "gpu_host.h"
+#include "matrix.h"
 
 namespace hl {
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 struct Gemv4Args {
   const uint8_t* codes;
@@ -36,26 +31,6 @@ struct Gemv4Args {
   float* y;
   uint32_t rows, cols, batch, groups;  // groups: of a row
 };
-
-template <class T>
-__device__ inline f32x4 product(u32x4 a, u32x4 b, f32x4 c) {
-  if constexpr (std::is_same<T, __bf16>::value)
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
-                                                   0, 0);
-  else
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0,
-                                                  0);
-}
-
-// Ends a row of matrix instructions: the instructions after it may write the
-// operands of those before. On gfx950 a product has come out wrong now and then
-// when the instruction right after it wrote one of its operand registers; the
-// compiler places no wait states there, and five are enough.
-__device__ inline void row_end() {
-  __builtin_amdgcn_sched_barrier(0);
-  asm volatile("s_nop 4");
-  __builtin_amdgcn_sched_barrier(0);
-}
 
 // Keeps what is made of v behind the instructions before.
 __device__ inline uint32_t after(uint32_t v) {
@@ -69,14 +44,6 @@ __device__ inline float number(uint32_t bits) {
   return (float)__builtin_bit_cast(T, (uint16_t)bits);
 }
 
-template <int N, class F>
-__device__ inline void every(F f) {
-  if constexpr (N > 0) {
-    every<N - 1>(f);
-    f(std::integral_constant<int, N - 1>());
-  }
-}
-
 // Words 0 .. 3 of four lanes, 16 apart, turned: word j of lane group c becomes word
 // c of lane group j.
 __device__ inline void turn4(u32x4& w) {
@@ -87,27 +54,11 @@ __device__ inline void turn4(u32x4& w) {
   w = u32x4{u[0], u[1], v[0], v[1]};
 }
 
-// The right operand of 8 columns' codes, columns 0 4 1 5 2 6 3 7 in pairs: 16 + code,
-// which `offset` takes off again, and 8. The mask is in a scalar register and the exponents
-// in a vector one, so that an instruction takes both.
+// The right operand of 8 columns' codes, columns 0 4 1 5 2 6 3 7 in pairs.
 template <class T>
-struct Codes {
-  static constexpr bool BF = std::is_same<T, __bf16>::value;
-  uint32_t mask, one;
-  __device__ Codes() {
-    mask = BF ? 0x00780078u : 0x03C003C0u, one = BF ? 0x41804180u : 0x4C004C00u;
-    asm volatile("" : "+s"(mask), "+v"(one));
-  }
-  __device__ u32x4 operand(uint32_t w) const {
-    if constexpr (BF)
-      return u32x4{((w << 3) & mask) | one, ((w >> 1) & mask) | one, ((w >> 5) & mask) | one, ((w >> 9) & mask) | one};
-    return u32x4{((w << 6) & mask) | one, ((w << 2) & mask) | one, ((w >> 2) & mask) | one, ((w >> 6) & mask) | one};
-  }
-  __device__ static u32x4 offset() {
-    constexpr uint32_t less = BF ? 0xC1C0C1C0u : 0xCE00CE00u;  // -24
-    return u32x4{less, less, less, less};
-  }
-};
+__device__ inline u32x4 operand(const Codes<T>& form, uint32_t w) {
+  return u32x4{form.template pair<0>(w), form.template pair<4>(w), form.template pair<8>(w), form.template pair<12>(w)};
+}
 
 // Rows from which on a wave has two row tiles, and a block four waves: x is loaded
 // for both, and there are blocks enough. us, one tile and eight waves against this:
@@ -231,7 +182,7 @@ __global__ void __launch_bounds__(64 * W, 2) gemv4_kernel(Gemv4Args a) {
   const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
   const Codes<T> form;
   constexpr uint32_t unit = std::is_same<T, __bf16>::value ? 0x3F803F80u : 0x3C003C00u;
-  u32x4 ones = {unit, unit, unit, unit}, offset = Codes<T>::offset();
+  u32x4 ones = {unit, unit, unit, unit}, offset = {Codes<T>::LESS, Codes<T>::LESS, Codes<T>::LESS, Codes<T>::LESS};
   asm volatile("" : "+v"(ones), "+v"(offset));
   f32x4 y[RT];
 #pragma unroll
@@ -258,7 +209,7 @@ __global__ void __launch_bounds__(64 * W, 2) gemv4_kernel(Gemv4Args a) {
     nth += W;
     const uint32_t then = nth < stretches ? column(nth) : col;
     scales_at(then);
-    every<kChunks>([&](auto chunk) {
+    each<kChunks>([&](auto chunk) {
       constexpr int i = decltype(chunk)::value;
       const uint32_t at = col + 128 * i, next = i + 1 < kChunks ? at + 128 : then;
       load_chunk<RT>(ring[(i + 1) % 2], a, first, row, b, next);
@@ -287,7 +238,7 @@ __global__ void __launch_bounds__(64 * W, 2) gemv4_kernel(Gemv4Args a) {
           turn4(w);
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
-            codes[rt * 4 + t] = form.operand(w[t]);
+            codes[rt * 4 + t] = operand(form, w[t]);
             asm volatile("" : "+v"(codes[rt * 4 + t]));
           }
         }
@@ -298,8 +249,8 @@ __global__ void __launch_bounds__(64 * W, 2) gemv4_kernel(Gemv4Args a) {
           if (r0 == 0) {
 #pragma unroll
             for (int t = p * EACH; t < (p + 1) * EACH; ++t) {
-              less[p] = product<T>(xs[t], offset, t == p * EACH ? zero : less[p]);
-              if constexpr (BASES) sum[p] = product<T>(xs[t], ones, t == p * EACH ? zero : sum[p]);
+              less[p] = mfma<T>(xs[t], offset, t == p * EACH ? zero : less[p]);
+              if constexpr (BASES) sum[p] = mfma<T>(xs[t], ones, t == p * EACH ? zero : sum[p]);
             }
           }
         }
@@ -309,7 +260,7 @@ __global__ void __launch_bounds__(64 * W, 2) gemv4_kernel(Gemv4Args a) {
           for (int p = 0; p < PARTS; ++p)
 #pragma unroll
             for (int rt = 0; rt < SET; ++rt)
-              part[rt][p] = product<T>(xs[p * EACH + t], codes[rt * 4 + p * EACH + t], t == 0 ? less[p] : part[rt][p]);
+              part[rt][p] = mfma<T>(xs[p * EACH + t], codes[rt * 4 + p * EACH + t], t == 0 ? less[p] : part[rt][p]);
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
           if constexpr (BASES) asm volatile("" : "+v"(sum[p]));
@@ -317,7 +268,7 @@ __global__ void __launch_bounds__(64 * W, 2) gemv4_kernel(Gemv4Args a) {
 #pragma unroll
           for (int rt = 0; rt < SET; ++rt) asm volatile("" : "+v"(part[rt][p]));
         }
-        row_end();
+        products_end();
 #pragma unroll
         for (int t = 0; t < 4; ++t) asm volatile("" ::"v"(xs[t]));
 #pragma unroll
