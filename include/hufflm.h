@@ -596,7 +596,8 @@ typedef struct {
  * the token is the lowest index i at which the sum of the kept w over 0 .. i is
  * above u times their total, u = uniforms[row] in [0, 1) (0 for a lower one or a
  * NaN; for 1 and above the last kept token). Tokens whose w is below 2^-40 are
- * never drawn and count nowhere. logprobs: log of the token's w over the kept total.
+ * never drawn and count nowhere. A row is many times slower where top_k or top_p ends
+ * among more than 2048 logits of a thousandth of the distance that weighs (equal ones). logprobs: log of the token's w over the kept total.
  * A logit that is NaN counts as minus infinity; where the greatest is plus infinity,
  * those that are have w = 1 and the others 0. A row with nothing above minus
  * infinity has token -1 and logprob minus infinity.

@@ -948,7 +948,9 @@ static Tiling tiling(uint64_t rows, uint32_t r) {
 // where there is a block for every second compute unit. One sequence on 256 own
 // keys takes 5.6 us so and 9.0 in parts, on 512 8.0 and 9.4, on 768 9.8 and 9.5
 // (but one launch for two), on 1024 13.2 and 10.1; 16 sequences on 768 17.6 and
-// 19.9, on 1024 22 and 23, on 1536 30 and 28.
+// 19.9, on 1024 22 and 23, on 1536 30 and 28. In 4 bits: one sequence on 512 8.7 and 10.5
+// (float16 queries: 9.4 and 10.6), on 768 10.2 and 10.4 (11.4 and 10.6), on 1024 11.7 and
+// 10.5; 16 on 768 13.1 and 14.4 (14.4 and 15.4), on 1024 15.3 and 14.6 (17.0 and 15.6).
 constexpr uint64_t kSoloKeys = 768, kSoloKeysMany = 1024;
 
 // A workspace's size, at least: 0 says that the arguments are bad, and

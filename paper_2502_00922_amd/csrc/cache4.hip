@@ -75,7 +75,7 @@ __device__ inline uint32_t code4(float x, float base, float scale, float inverse
 
 // Four lanes a group of 32 columns, 8 columns each; the rows are put together in
 // LDS and stored in 16-byte pieces. 16384 tokens of 8 key heads of 128 columns, keys
-// and values, 88 MB: 31 us, 0.55 of a copy's rate, bound by the vector instructions
+// and values, 88 MB: 30 us, 0.57 of a copy's rate, bound by the vector instructions
 // (some 40 a column pair; 43 us with a division each column and 64-bit quotients for
 // the places).
 template <class T, uint32_t G>

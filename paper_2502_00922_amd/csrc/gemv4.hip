@@ -6,15 +6,17 @@
 // and an and-or of a nibble; what is too much of it is where the sums begin: a product of
 // x with a constant operand that all rows share. (128 or 64 + code, where a nibble is in
 // place for it, save a shift in four and lose three bits of the sums and of their range.)
-// x is the left one: a lane's four sums are then of one row of the matrix,
-// whose scale the lane has loaded itself.
+// x is the left one: a lane's four sums are then of one row of the matrix, whose scale
+// the lane has loaded itself.
 // A wave has RT 16-row tiles and every W-th stretch of 512 columns, a block the W waves
 // of the same rows, which are added in LDS in their order. A lane loads 16 bytes of a
 // row, four lanes 64; two rounds of lane swaps turn the four words of four lanes, so
 // that each instruction's 32 columns are neighbours and of one group.
 // Bound by the loads' way to the compute units where there are few rows (4096 x 4096
-// for one row of x 5.2 us, 1.7 TB/s), by vector instructions and x, which every block
-// reads, where there are many (28672 x 8192 for 16 with bases 60 us, 2.2 TB/s). Sixteen
+// for one row of x 5.2 us, 1.7 TB/s, the waves at waits 56 % of their time). Of 28672 x
+// 8192 for 16 with bases (60 us, 2.2 TB/s) neither memory nor the vector (28 %) nor the
+// matrix units (10 %) are the bound by themselves: the 1.4 waves that a SIMD has in the mean
+// wait for their instructions' turn 53 % of their time and for loads 22 %. Sixteen
 // waves a block instead of eight for matrices of at most 2048 rows gain nothing (1024 x
 // 8192 for one 6.8 and 7.7 us).
 #include <algorithm>
