@@ -99,3 +99,22 @@ def test_long_prefix_of_many_rows():
     bound = 2.0**-8 * out.abs() + (1 + 2.0**-8) * (2.0**-8 * steps + 2 * e * near + 96 * 2.0**-24 * sums) + 2.0**-25
     assert ((got.out[some].double().cpu() - out).abs() <= bound).all()
     assert math.isfinite(float(got.out.float().abs().max()))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", [(1, 2048, 16, 4, 128, 0, 2048), (16, 300, 8, 2, 64, 5000, 900), (3, 700, 12, 4, 96, 1777, 1003),
+                                   (2, 513, 8, 8, 256, 300, 2000), (128, 1, 32, 8, 128, 16384, 40)])
+def test_large_calls_beside_16_bits(dtype, shape):
+    # values (code - 8) / 16 of both types: the 16-bit attention's, on the same numbers. Either is off by u of the output and,
+    # by its rounding of p, by u (r) of sum p |v|; scores and sums by some 2^-16 (|q k| below 40)
+    c = make(dtype, *shape)
+    dim = shape[4]
+    for name in ("k", "v", "prefix_k", "prefix_v"):
+        if name in c:
+            set_pairs(c[name], dim, scale=0.0625, base=0.0)
+    wide = {n: t if n in ("q", "lens") else hl.cache_read4(t, dim, dtype=dtype) for n, t in c.items()}
+    got, want = hl.prefix_attention4(**c).out.float(), hl.prefix_attention(**wide).out.float()
+    sizes = hl.prefix_attention(**{n: t.abs() if n.endswith("v") else t for n, t in wide.items()}).out.float()
+    u, r = U[dtype], R[dtype]
+    bound = u * (got.abs() + want.abs()) + (u + r + 2.0**-10) * sizes * (1 + 4 * u) + 2.0**-20
+    assert got.isfinite().all() and ((got - want).abs() <= bound).all(), float(((got - want).abs() / bound).max())
