@@ -593,24 +593,25 @@ typedef struct {
  *   of these the first ones up to that at which the sum of w reaches top_p of the
  *   sum over all that top_k kept;
  *   of these the ones with w >= min_p (at least the first token);
- * the token is the lowest index i at which the sum of the kept w over 0 .. i is
- * above u times their total, u = uniforms[row] in [0, 1) (0 for a lower one or a
- * NaN; for 1 and above the last kept token). Tokens whose w is below 2^-40 are
- * never drawn and count nowhere. A row is many times slower where top_k or top_p ends
- * among more than 2048 logits of a thousandth of the distance that weighs (equal ones). logprobs: log of the token's w over the kept total.
- * A logit that is NaN counts as minus infinity; where the greatest is plus infinity,
- * those that are have w = 1 and the others 0. A row with nothing above minus
- * infinity has token -1 and logprob minus infinity.
- * Each w is held to 2^-43 of the greatest (not of itself), and sums of what is held
- * are exact: a sum over n tokens is off by n * 2^-43 of the greatest at most. The token
- * is that of exact numbers but where u times the total (top_p times it) is within
- * n * 2^-42 of where another token begins. logits_dev: [rows][vocab] float32, bf16 or
- * float16, rows row_stride elements apart, aligned to their elements. tokens_dev int32, logprobs_dev float32 [rows]. workspace_dev:
- * hl_sample_workspace_bytes (16-byte aligned, no initial contents needed; 0 on bad
- * arguments; 15 to 31 KB a row and 10 for each 2048 to 16384 of its logits, 174 MB at
- * most: further rows go after each other); calls that may run concurrently need
- * separate ones. Errors: HL_EINVAL (also for a missing or short workspace),
- * HL_EUNSUPPORTED for vocab of 2^20 and above and more than 65535 rows. */
+ * the token is the lowest index i at which the sum of the kept w over 0 .. i is above
+ * u times their total, u = uniforms[row] in [0, 1) (0 for a lower one or a NaN; for 1
+ * and above the last kept token). Tokens whose w is below 2^-40 are never drawn and
+ * count nowhere. A row is many times slower where top_k or top_p ends among more than
+ * 2048 logits of a thousandth of the distance that weighs (equal ones). logprobs: log
+ * of the token's w over the kept total. A logit that is NaN counts as minus infinity;
+ * where the greatest is plus infinity, those that are have w = 1 and the others 0. A
+ * row with nothing above minus infinity has token -1 and logprob minus infinity. Each
+ * w is held to 2^-43 of the greatest (not of itself), and sums of what is held are
+ * exact: a sum over n tokens is off by n * 2^-43 of the greatest at most. The token is
+ * that of exact numbers but where u times the total (top_p times it) is within n *
+ * 2^-42 of where another token begins. logits_dev: [rows][vocab] float32, bf16 or
+ * float16, rows row_stride elements apart, aligned to their elements. tokens_dev
+ * int32, logprobs_dev float32 [rows]. workspace_dev: hl_sample_workspace_bytes
+ * (16-byte aligned, no initial contents needed; 0 on bad arguments; 15 to 31 KB a row
+ * and 10 for each 2048 to 16384 of its logits, 174 MB at most: further rows go after
+ * each other); calls that may run concurrently need separate ones. Errors: HL_EINVAL
+ * (also for a missing or short workspace), HL_EUNSUPPORTED for vocab of 2^20 and above
+ * and more than 65535 rows. */
 size_t hl_sample_workspace_bytes(uint32_t rows, uint64_t vocab);
 hl_status hl_sample(const hl_sampling* sampling, const void* logits_dev, hl_dtype dtype, uint64_t row_stride,
                     uint32_t rows, uint64_t vocab, const float* uniforms_dev, int32_t* tokens_dev, float* logprobs_dev,
